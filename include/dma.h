@@ -259,6 +259,90 @@ int dma_decode_state_init(const dma_problem_t* p, const float* delta, int64_t de
 int dma_decode_step(const dma_problem_t* p, const void* q, const void* K, const void* V, const float* delta, int64_t delta_ld,
                     void* state, void* o, float* lse, void* ws, size_t ws_bytes, void* cuda_stream);
 
+/* ---- Serving requests of different lengths: a paged cache of keys and values held in 4 bits ------------------------------
+ * (A property of the library: the paper decodes over one contiguous cache in bf16.) The cache is a pool of pages; a page
+ * holds page_size keys of every head, in three arrays of the caller's:
+ *   codes   uint8 [num_pages, Hkv, page_size, 2, d/2]       a key's K row, then its V row: channel 2i in the low half of byte
+ *                                                           i, channel 2i + 1 in the high half
+ *   scales  bf16  [num_pages, Hkv, page_size, 2, d/64, 2]   (s, z) of every 64 channels: a code n stands for z + s n
+ *   delta   fp32  [num_pages, Hq, page_size]                the keys' dynamic weights
+ * that is 4.5 bits per value. Slot = page number * page_size + place in the page. Key j of sequence r lies in the page
+ * block_table[r, j / page_size], at place j % page_size. Page numbers outside [0, num_pages) and slots outside [0, num_pages *
+ * page_size) are never followed (each call says what it does instead), so that stale or padded tables do no harm.
+ * Rows are the tokens of a step: row t belongs to sequence row_seq[t] at position row_pos[t]. Several rows may belong to
+ * one sequence (a prompt chunk, drafts).
+ * int32 arrays, A, lse, delta_new and delta_out need 4-byte alignment only; all other pointers 16 bytes. */
+typedef struct {
+    int32_t Hq, Hkv, d, w;       /* as in dma_problem_t; w: keep window of dma_cache4_decode                      */
+    int32_t dtype;               /* element type of q, K, V, o: DMA_BF16 | DMA_FP32                               */
+    int32_t page_size;           /* keys per page: 16, 32, 64, 128 or 256                                         */
+    int32_t num_pages;           /* pages of the pool; num_pages * page_size < 2^31                               */
+    int32_t max_blocks;          /* pages that a sequence may hold; max_blocks * page_size < 2^31                 */
+    int32_t nseq;                /* sequences: rows of block_table                                                */
+    int32_t rows;                /* rows (tokens) of this call, >= 1                                              */
+    int32_t flags;               /* DMA_FLAG_SIMT: dma_cache4_decode on the CUDA cores also for bf16; others refused */
+    float softmax_scale;         /* 0 -> 1/sqrt(d)                                                                */
+    int64_t table_ld;            /* entries between rows of block_table; 0 = max_blocks                           */
+    int64_t q_stride[2];         /* row and head strides of q in elements; both 0 = contiguous                    */
+    int64_t k_stride[2];         /* same for K                                                                    */
+    int64_t v_stride[2];         /* same for V                                                                    */
+    int64_t o_stride[2];         /* same for o                                                                    */
+} dma_cache_t;
+
+/* Bytes of the three arrays (any pointer may be NULL). */
+int dma_cache4_bytes(const dma_cache_t* c, size_t* codes, size_t* scales, size_t* delta);
+
+/* Pages for requests that begin, grow, shrink and end: from the sequences' lengths to block table, row and slot maps, on the
+ * GPU alone (a captured step replays with the lengths of the day). Reads page_size, num_pages, max_blocks, nseq, rows, table_ld.
+ *   lens, want [nseq]    keys that sequence r holds, and is to hold. want > lens: the positions lens .. want - 1 are this step's
+ *                        rows of r. want < lens: the tail is dropped (0: the request has ended). lens may be lens_out.
+ *   block_table          [nseq, table_ld]; the entries of new pages are written. Entries behind a sequence's last page are
+ *                        left as they are.
+ *   free_pages           [num_pages] a ring: the free pages are entries head, head + 1, ... (modulo num_pages), `free` of them.
+ *                        New pages are taken at the head in the order of sequences and positions; pages given back are written
+ *                        behind the tail in that order, and can be taken from the next call on.
+ *   pool, pool_out [4]   {head, free, -, -} before and {head, free, sequences refused, rows} after; may be the same array.
+ *   lens_out [nseq]      want, or lens where the request was refused.
+ *   cu_rows [nseq + 1]   rows of sequence r: cu_rows[r] .. cu_rows[r + 1] - 1
+ *   row_seq, row_pos, slot [rows]   of every row; -1 behind the last one.
+ * Requests are granted in order: r is refused if want or lens lies outside [0, max_blocks * page_size], if it needs pages and
+ * the pages asked for by sequences 0 .. r exceed `free`, or if it brings rows and those of the sequences 0 .. r that were not
+ * refused for pages exceed `rows`. A refused request keeps its length and pages and gets no rows. */
+int dma_page_plan(const dma_cache_t* c, const int32_t* lens, const int32_t* want, int32_t* block_table, int32_t* free_pages,
+                  const int32_t* pool, int32_t* lens_out, int32_t* pool_out, int32_t* cu_rows, int32_t* row_seq, int32_t* row_pos,
+                  int32_t* slot, void* cuda_stream);
+
+/* Writes rows into the cache. K, V: [rows, Hkv, d] (k_stride, v_stride); slot [rows]: where each goes; a row whose slot lies
+ * outside the pool is skipped. Slots of one call are distinct (of rows that share one, either's values may be left, in parts).
+ *   codes, scales: of each 64 channels, in fp32 operations rounded one by one,
+ *     z = bf16(min x),  s = max(0, bf16((max x / 2 - z / 2) / 7.5)),  n = min(15, max(0, rint((x / 2 - z / 2) / (s / 2))))
+ *   (ties to even; n = 0 where the quotient is NaN, so with s = 0 too). 64 channels that hold a NaN, an infinity or a value that bf16 rounds to one read back as NaN.
+ *   delta: of the row's V as given (not as held), the bits of dma_mask_build: W_delta [Hq, d], A [Hq]. Or, with delta_new not
+ *   NULL, delta_new[h * delta_ld + t] as it is (dma_mask_build's bias, or dma_delta_range's output for the full weights);
+ *   W_delta and A are then not read. */
+int dma_cache4_append(const dma_cache_t* c, const void* K, const void* V, const float* W_delta, const float* A, const float* delta_new,
+                      int64_t delta_ld, const int32_t* slot, void* codes, void* scales, float* delta, void* cuda_stream);
+
+/* Reads rows back: K, V [rows, Hkv, d] (k_stride, v_stride) get z + s n, formed in fp32 and rounded once; delta_out, if not NULL,
+ * gets [Hq, delta_ld >= rows] (dma_decode's and dma_mask_build's layout for one batch entry). Rows whose slot lies outside the
+ * pool are left as they are. */
+int dma_cache4_read(const dma_cache_t* c, const void* codes, const void* scales, const float* delta, const int32_t* slot, void* K,
+                    void* V, float* delta_out, int64_t delta_ld, void* cuda_stream);
+
+/* Decoding over the pages: dma_decode for every row t over the keys 0 .. row_pos[t] of sequence row_seq[t]. Every query head
+ * keeps the min(w, visible) keys with the largest delta (ties to the lower index) and
+ *   o[t, h] = softmax(q . K_sel^T scale + delta_sel) V_sel,  lse[t, h] its log-sum-exp (natural log)
+ * with the values that the cache holds. q, o: [rows, Hq, d] (q_stride, o_stride); lse [rows, Hq]. Positions beyond the table's
+ * max_blocks pages, and keys in pages whose number is outside the pool, are not visible. A row that sees no key gets
+ * o = 0, lse = -inf; a row whose row_seq is outside [0, nseq) (padding) is left as it is. Only the kept keys' codes are read (those
+ * that some head of a group keeps). Results depend on the call's rows and lengths in the last bits (where long rows are cut),
+ * and are the same bits from run to run.
+ * ws: dma_cache4_decode_workspace() bytes, a size that does not fall as rows, Hq or max_blocks grow. */
+int dma_cache4_decode_workspace(const dma_cache_t* c, size_t* bytes);
+int dma_cache4_decode(const dma_cache_t* c, const void* q, const void* codes, const void* scales, const float* delta,
+                      const int32_t* block_table, const int32_t* row_seq, const int32_t* row_pos, void* o, float* lse, void* ws,
+                      size_t ws_bytes, void* cuda_stream);
+
 /* The whole hot path on HOST buffers (all contiguous, default strides only): copies Q,K,V,(dO),W_delta,A into the
  * caller's device arena, runs dma_mask_build, dma_attn_fwd and, if `backward` != 0, dma_attn_bwd on the stream,
  * copies O, lse (and dQ,dK,dV,dM) back and synchronises the stream before returning. The copies run on two helper

@@ -21,7 +21,8 @@ ENTRY_POINTS = ("dma_query_workspace", "dma_bitmap_words", "dma_mask_build", "dm
                 "dma_read_status", "dma_launch_count", "dma_strerror", "dma_step_host_arena", "dma_step_host", "dma_mask_build_static", "dma_selftest_wait_timeout",
                 "dma_mask_bwd_workspace", "dma_mask_bwd", "dma_delta_range", "dma_decode_workspace", "dma_decode",
                 "dma_mask_build_varlen", "dma_decode_state_bytes", "dma_decode_state_init", "dma_decode_step",
-                "dma_attn_fwd_chunk", "dma_kernel_timing", "dma_kernel_timing_read")
+                "dma_attn_fwd_chunk", "dma_kernel_timing", "dma_kernel_timing_read",
+                "dma_cache4_bytes", "dma_page_plan", "dma_cache4_append", "dma_cache4_read", "dma_cache4_decode_workspace", "dma_cache4_decode")
 
 
 class DmaError(RuntimeError):
@@ -37,6 +38,15 @@ class dma_problem_t(ctypes.Structure):
                 ("softmax_scale", ctypes.c_float),
                 ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3),
                 ("v_stride", ctypes.c_int64 * 3), ("o_stride", ctypes.c_int64 * 3)]
+
+
+class dma_cache_t(ctypes.Structure):
+    _fields_ = [("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32), ("w", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("max_blocks", ctypes.c_int32), ("nseq", ctypes.c_int32), ("rows", ctypes.c_int32), ("flags", ctypes.c_int32),
+                ("softmax_scale", ctypes.c_float), ("table_ld", ctypes.c_int64),
+                ("q_stride", ctypes.c_int64 * 2), ("k_stride", ctypes.c_int64 * 2),
+                ("v_stride", ctypes.c_int64 * 2), ("o_stride", ctypes.c_int64 * 2)]
 
 
 def lib():
@@ -59,15 +69,18 @@ def dma_strerror(status):
         return "?"
 
 
+def _dtype_code(dtype):
+    if dtype in (torch.bfloat16, torch.float32):
+        return DMA_BF16 if dtype == torch.bfloat16 else DMA_FP32
+    if type(dtype) is int and dtype in (DMA_BF16, DMA_FP32):
+        return dtype
+    raise TypeError(f"element type {dtype!r}: torch.bfloat16, torch.float32, DMA_BF16 or DMA_FP32")
+
+
 def problem(B, Hq, Hkv, L, d, w, dtype=torch.bfloat16, causal=1, tile_m=0, tile_n=0, flags=0, softmax_scale=0.0):
     p = dma_problem_t()
     p.B, p.Hq, p.Hkv, p.L, p.d, p.w, p.causal = B, Hq, Hkv, L, d, w, causal
-    if dtype in (torch.bfloat16, torch.float32):
-        p.dtype = DMA_BF16 if dtype == torch.bfloat16 else DMA_FP32
-    elif type(dtype) is int and dtype in (DMA_BF16, DMA_FP32):
-        p.dtype = dtype
-    else:
-        raise TypeError(f"element type {dtype!r}: torch.bfloat16, torch.float32, DMA_BF16 or DMA_FP32")
+    p.dtype = _dtype_code(dtype)
     p.tile_m, p.tile_n, p.flags, p.softmax_scale = tile_m, tile_n, flags, softmax_scale
     return p
 
@@ -104,7 +117,8 @@ _SIGNATURES = {
     "dma_mask_bwd": "Pvvvvvvvvvzv", "dma_attn_fwd": "Pvvvvvvvvvzv", "dma_attn_fwd_chunk": "Piivvvvvvvvzv",
     "dma_attn_bwd": "Pvvvvvvvvvvvvvvzv", "dma_delta_range": "Pvvvvliiv", "dma_decode": "Pvvvvlvvvvzv",
     "dma_decode_state_init": "Pvlvvzv", "dma_decode_step": "Pvvvvlvvvvzv", "dma_step_host": "Pivvvvvvvvvvvvvzv",
-    "dma_read_status": "vv", "dma_selftest_wait_timeout": "vzv"}
+    "dma_page_plan": "vvvvvvvvvvvvv", "dma_cache4_append": "vvvvvvlvvvvv", "dma_cache4_read": "vvvvvvvvlv",
+    "dma_cache4_decode": "vvvvvvvvvvvzv", "dma_read_status": "vv", "dma_selftest_wait_timeout": "vzv"}
 _KINDS = {"P": ctypes.POINTER(dma_problem_t), "v": ctypes.c_void_p, "i": ctypes.c_int32, "l": ctypes.c_int64, "z": ctypes.c_size_t}
 _typed = {}                  # name -> function object with typed parameters
 _typed_lib = None            # a handle of its own: the function objects of lib() stay untyped
@@ -320,6 +334,169 @@ def dma_attn_bwd(p, Q, K, V, O, dO, lse, bias, expiry, bitmap, dQ=None, dK=None,
     _call("dma_attn_bwd", p, _ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(dO), _ptr(lse), _ptr(bias), _ptr(expiry), _ptr(bitmap),
           _ptr(dQ), _ptr(dK), _ptr(dV), _ptr(dM), _ptr(ws), ws.numel(), _stream())
     return dQ, dK, dV, dM
+
+
+def cache(Hq=1, Hkv=1, d=64, w=1, dtype=torch.bfloat16, rows=1, nseq=1, page_size=64, num_pages=1, max_blocks=1, flags=0, softmax_scale=0.0):
+    """Descriptor of a paged 4-bit cache and of one call's rows (contiguous q, K, V, o; strides are set on the result). dma_page_plan
+    reads the rows, sequences and pages only."""
+    c = dma_cache_t()
+    c.Hq, c.Hkv, c.d, c.w, c.dtype = Hq, Hkv, d, w, _dtype_code(dtype)
+    c.page_size, c.num_pages, c.max_blocks, c.nseq, c.rows = page_size, num_pages, max_blocks, nseq, rows
+    c.flags, c.softmax_scale = flags, softmax_scale
+    return c
+
+
+def _on_device(want, /, **tensors):
+    """Tensors of type `want` on the current device, whose stream and memory the library uses."""
+    dev = torch.cuda.current_device() if _raw_device is None else _raw_device()
+    for name, t in tensors.items():
+        if t.dtype is not want:
+            raise TypeError(f"{name}: {t.dtype} where {want} is read")
+        if t.get_device() != dev:
+            raise ValueError(f"{name} is on {t.device}, the call runs on cuda:{dev}")
+
+
+def _rows_of(c, stride, /, **tensors):
+    """[rows, heads, d] tensors of the descriptor's element type, laid out as its strides say."""
+    _on_device(torch.bfloat16 if c.dtype == DMA_BF16 else torch.float32, **tensors)
+    for name, t in tensors.items():
+        heads = c.Hq if name in ("q", "o") else c.Hkv
+        if t.dim() != 3 or t.shape[0] < c.rows or t.shape[1] != heads or t.shape[2] != c.d:
+            raise ValueError(f"{name}: shape {tuple(t.shape)} where [{c.rows}, {heads}, {c.d}] is read")
+        row, head = stride
+        want = (row, head, 1) if row or head else (heads * c.d, c.d, 1)
+        if t.stride() != want and any(n > 1 and a != b for n, a, b in zip(t.shape, t.stride(), want)):
+            raise ValueError(f"{name}: strides {t.stride()} differ from the descriptor's")
+
+
+def _at_least(n, /, **tensors):
+    for name, t in tensors.items():
+        if t.numel() < n or not t.is_contiguous():
+            raise ValueError(f"{name}: {n} contiguous entries are read or written, it is {tuple(t.shape)} with strides {t.stride()}")
+
+
+def dma_cache4_bytes(c):
+    """Bytes of (codes, scales, delta)."""
+    n = [ctypes.c_size_t() for _ in range(3)]
+    _check(lib().dma_cache4_bytes(ctypes.byref(c), *map(ctypes.byref, n)), "dma_cache4_bytes")
+    return tuple(x.value for x in n)
+
+
+def cache4(c, device):
+    """Arrays of the descriptor's pool: (codes uint8, scales bf16, delta fp32), zero-filled."""
+    return (torch.zeros(c.num_pages, c.Hkv, c.page_size, 2, c.d // 2, dtype=torch.uint8, device=device),
+            torch.zeros(c.num_pages, c.Hkv, c.page_size, 2, c.d // 64, 2, dtype=torch.bfloat16, device=device),
+            torch.zeros(c.num_pages, c.Hq, c.page_size, dtype=torch.float32, device=device))
+
+
+def _cache4_arrays(c, codes, scales, delta):
+    _on_device(torch.uint8, codes=codes)
+    _on_device(torch.bfloat16, scales=scales)
+    _on_device(torch.float32, delta=delta)
+    keys = c.num_pages * c.page_size
+    _at_least(keys * c.Hkv * c.d, codes=codes)
+    _at_least(keys * c.Hkv * (c.d // 16), scales=scales)
+    _at_least(keys * c.Hq, delta=delta)
+
+
+def dma_page_plan(c, lens, want, block_table, free_pages, pool, lens_out=None, pool_out=None, cu_rows=None, row_seq=None, row_pos=None, slot=None):
+    """Pages for the sequences' new lengths (int32 tensors; block_table and free_pages are updated in place). Returns (lens_out,
+    pool_out, cu_rows, row_seq, row_pos, slot)."""
+    def new(t, n):
+        return torch.empty(n, dtype=torch.int32, device=lens.device) if t is None else t
+    lens_out, pool_out, cu_rows = new(lens_out, c.nseq), new(pool_out, 4), new(cu_rows, c.nseq + 1)
+    row_seq, row_pos, slot = (new(t, c.rows) for t in (row_seq, row_pos, slot))
+    _on_device(torch.int32, lens=lens, want=want, block_table=block_table, free_pages=free_pages, pool=pool, lens_out=lens_out, pool_out=pool_out,
+               cu_rows=cu_rows, row_seq=row_seq, row_pos=row_pos, slot=slot)
+    _at_least(c.nseq, lens=lens, want=want, lens_out=lens_out)
+    _at_least(4, pool=pool, pool_out=pool_out)
+    _at_least(c.num_pages, free_pages=free_pages)
+    _at_least(c.nseq + 1, cu_rows=cu_rows)
+    _at_least(c.rows, row_seq=row_seq, row_pos=row_pos, slot=slot)
+    _table(c, block_table)
+    _call("dma_page_plan", ctypes.byref(c), _ptr(lens), _ptr(want), _ptr(block_table), _ptr(free_pages), _ptr(pool), _ptr(lens_out), _ptr(pool_out),
+          _ptr(cu_rows), _ptr(row_seq), _ptr(row_pos), _ptr(slot), _stream())
+    return lens_out, pool_out, cu_rows, row_seq, row_pos, slot
+
+
+def _table(c, block_table):
+    ld = c.table_ld or c.max_blocks
+    if block_table.dim() != 2 or block_table.shape[0] < c.nseq or block_table.shape[1] < c.max_blocks or (
+            block_table.stride() != (ld, 1) and any(n > 1 and a != b for n, a, b in zip(block_table.shape, block_table.stride(), (ld, 1)))):
+        raise ValueError(f"block_table: {tuple(block_table.shape)} with strides {block_table.stride()} where [{c.nseq}, {c.max_blocks}] with rows of {ld} is read")
+
+
+def dma_cache4_append(c, K, V, slot, codes, scales, delta, W_delta=None, A=None, delta_new=None):
+    """Writes the rows K, V [rows, Hkv, d] into their slots, with the dynamic weights of V (W_delta [Hq, d], A [Hq]) or those given
+    as delta_new [Hq, >= rows]."""
+    _rows_of(c, c.k_stride, K=K)
+    _rows_of(c, c.v_stride, V=V)
+    _on_device(torch.int32, slot=slot)
+    _at_least(c.rows, slot=slot)
+    _cache4_arrays(c, codes, scales, delta)
+    ld = 0
+    if delta_new is not None:
+        _on_device(torch.float32, delta_new=delta_new)
+        ld = delta_new.stride(0) if delta_new.shape[0] > 1 else max(c.rows, delta_new.shape[1])
+        if delta_new.dim() != 2 or delta_new.shape[0] < c.Hq or delta_new.shape[1] < c.rows or delta_new.stride(1) != 1:
+            raise ValueError(f"delta_new: {tuple(delta_new.shape)} where [{c.Hq}, {c.rows}] is read")
+    else:
+        if W_delta is None or A is None:
+            raise ValueError("either W_delta and A or delta_new")
+        _on_device(torch.float32, W_delta=W_delta, A=A)
+        _at_least(c.Hq * c.d, W_delta=W_delta)
+        _at_least(c.Hq, A=A)
+    _call("dma_cache4_append", ctypes.byref(c), _ptr(K), _ptr(V), _ptr(W_delta), _ptr(A), _ptr(delta_new), ld, _ptr(slot), _ptr(codes), _ptr(scales),
+          _ptr(delta), _stream())
+
+
+def dma_cache4_read(c, codes, scales, delta, slot, K=None, V=None, delta_out=None, want_delta=True):
+    """The rows in the given slots: (K, V [rows, Hkv, d], delta_out [Hq, rows] or None)."""
+    dt = torch.bfloat16 if c.dtype == DMA_BF16 else torch.float32
+    K = torch.empty(c.rows, c.Hkv, c.d, dtype=dt, device=slot.device) if K is None else K
+    V = torch.empty(c.rows, c.Hkv, c.d, dtype=dt, device=slot.device) if V is None else V
+    if delta_out is None and want_delta:
+        delta_out = torch.empty(c.Hq, c.rows, dtype=torch.float32, device=slot.device)
+    _rows_of(c, c.k_stride, K=K)
+    _rows_of(c, c.v_stride, V=V)
+    _on_device(torch.int32, slot=slot)
+    _at_least(c.rows, slot=slot)
+    _cache4_arrays(c, codes, scales, delta)
+    ld = 0
+    if delta_out is not None:
+        _on_device(torch.float32, delta_out=delta_out)
+        ld = delta_out.stride(0) if delta_out.shape[0] > 1 else max(c.rows, delta_out.shape[1])
+        if delta_out.dim() != 2 or delta_out.shape[0] < c.Hq or delta_out.shape[1] < c.rows or delta_out.stride(1) != 1:
+            raise ValueError(f"delta_out: {tuple(delta_out.shape)} where [{c.Hq}, {c.rows}] is written")
+    _call("dma_cache4_read", ctypes.byref(c), _ptr(codes), _ptr(scales), _ptr(delta), _ptr(slot), _ptr(K), _ptr(V), _ptr(delta_out), ld, _stream())
+    return K, V, delta_out
+
+
+def dma_cache4_decode_workspace(c):
+    n = ctypes.c_size_t()
+    _check(lib().dma_cache4_decode_workspace(ctypes.byref(c), ctypes.byref(n)), "dma_cache4_decode_workspace")
+    return n.value
+
+
+def dma_cache4_decode(c, q, codes, scales, delta, block_table, row_seq, row_pos, o=None, lse=None, ws=None):
+    """One step over the pages for every row; returns (o [rows, Hq, d], lse [rows, Hq])."""
+    if o is None:
+        o = torch.empty(c.rows, c.Hq, c.d, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty(c.rows, c.Hq, dtype=torch.float32, device=q.device)
+    if ws is None:
+        ws = _ws(dma_cache4_decode_workspace(c), q.device)
+    _rows_of(c, c.q_stride, q=q)
+    _rows_of(c, c.o_stride, o=o)
+    _cache4_arrays(c, codes, scales, delta)
+    _on_device(torch.int32, block_table=block_table, row_seq=row_seq, row_pos=row_pos)
+    _on_device(torch.float32, lse=lse)
+    _at_least(c.rows, row_seq=row_seq, row_pos=row_pos)
+    _at_least(c.rows * c.Hq, lse=lse)
+    _table(c, block_table)
+    _call("dma_cache4_decode", ctypes.byref(c), _ptr(q), _ptr(codes), _ptr(scales), _ptr(delta), _ptr(block_table), _ptr(row_seq), _ptr(row_pos),
+          _ptr(o), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), _stream())
+    return o, lse
 
 
 def dma_read_status(ws):
