@@ -90,22 +90,255 @@ __device__ unsigned long long radix_select(RadixShared& S, Load&& load, int n, i
     return order_key(u_lo, j_lo);
 }
 
-__global__ void __launch_bounds__(kSelectThreads) select_kernel(Rows R, int w, unsigned long long* weakest) {
-    __shared__ RadixShared S;
-    pdl_enter(R.table, R.seq, R.pos, R.delta, weakest);
-    const int t = blockIdx.x / R.Hq, h = blockIdx.x % R.Hq;
+// What every row's attention is cut by: units of keys, dealt out to the CTAs in equal shares. ustart[t]: units before row t, over all its `per_row` items.
+struct Plan { int32_t* ustart; int32_t* tickets; int per_row, unit_log; };
+
+template <int NT>
+__device__ void make_plan(const Rows& R, int rows, const Plan& P) {
+    __shared__ int part[NT / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int carry = 0;
+    for (int base = 0; base < rows; base += NT) {
+        const int t = base + tid;
+        int r, units = 0;
+        if (t < rows) {
+            const int n = R.visible(t, r);
+            // (an item's fixed cost, its queries and its end, is about that of a unit)
+            units = n < 0 ? 0 : (((n + (1 << P.unit_log) - 1) >> P.unit_log) + 1) * P.per_row;
+        }
+        int x = units;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+        }
+        if (lane == 31) part[warp] = x;
+        __syncthreads();
+        int before = 0, all = 0;
+        for (int i = 0; i < NT / 32; ++i) {
+            before += i < warp ? part[i] : 0;
+            all += part[i];
+        }
+        if (t < rows) P.ustart[t] = carry + before + x - units;
+        carry += all;
+        __syncthreads();
+    }
+    if (tid == 0) P.ustart[rows] = carry;
+    for (int i = tid; i < rows * P.per_row; i += NT) P.tickets[i] = 0;
+}
+
+__global__ void __launch_bounds__(1024) plan_kernel(Rows R, int rows, Plan P) {
+    pdl_enter(R.seq, R.pos, P.ustart, P.tickets);
+    make_plan<1024>(R, rows, P);
+}
+
+// The weakest kept key of a (row, query head). A sample brackets its delta (4.5 standard deviations of the sample's rank to either side); one sweep over the row
+// counts the keys above the bracket and notes those inside, a few per cent, each thread in slots of its own; the need-th of these is found by
+// a histogram over the bracket and a ranking of the bin's keys. Rows of up to kSample keys are their own sample: the bracket is one bin. Where
+// the bracket misses or holds too many (weights that crowd, equal weights) radix_select takes the row.
+// Many rows: 256 threads each, so that an SM works on several and their barriers and round trips hide each other; few rows: 1024.
+constexpr int kOwn = 10, kShared = 1024, kRank = 128;     // slots per thread, overflow slots, most keys ranked against each other
+template <int NT>
+struct alignas(16) SelectShared {
+    unsigned long long own[kOwn * NT], more[kShared], cand[kRank];
+    int hist[1024];
+    RadixShared radix;
+    uint32_t wmin[NT / 32], wmax[NT / 32];
+    int part[NT / 32], above[NT / 32];
+    int bin[2], need, count, ncand, nmore;
+    unsigned long long found;
+};
+
+template <int NT, int kPer>
+__global__ void __launch_bounds__(NT) select_kernel(Rows R, int rows, int w, unsigned long long* weakest, Plan P) {
+    extern __shared__ __align__(16) uint8_t select_smem[];
+    SelectShared<NT>& S = *reinterpret_cast<SelectShared<NT>*>(select_smem);
+    constexpr int kSample = NT * kPer, kWarps = NT / 32, kBins = 1024;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    for (int i = tid; i < kBins; i += NT) S.hist[i] = 0;
+    if (tid == 0) { S.ncand = S.nmore = 0; S.bin[0] = S.bin[1] = -1; }
+    pdl_enter(R.table, R.seq, R.pos, R.delta, weakest, P.ustart, P.tickets);
+    if (P.ustart && blockIdx.x == 0) {
+        make_plan<NT>(R, rows, P);
+        return;
+    }
+    const int item = blockIdx.x - (P.ustart ? 1 : 0), t = item / R.Hq, h = item % R.Hq;
     int r;
     const int n = R.visible(t, r);
-    unsigned long long k = 0ull;                                  // (every key)
-    if (n > w) {
-        const int32_t* pages = R.table + r * R.ld;
-        k = radix_select(S, [&](int j) {
-            const int page = pages[j >> R.page_log];
-            if ((unsigned)page >= (unsigned)R.num_pages) return 0u;
-            return __float_as_uint(R.delta[(((size_t)page * R.Hq + h) << R.page_log) + (j & R.mask())]) & 0x7FFFFFFFu;
-        }, n, w);
+    if (n <= w) {                                                 // every key
+        if (tid == 0) weakest[item] = 0ull;
+        return;
     }
-    if (threadIdx.x == 0) weakest[blockIdx.x] = k;
+    const int32_t* pages = R.table + r * R.ld;
+    const float* plane = R.delta + ((size_t)h << R.page_log);
+    const int stride = R.Hq << R.page_log;                        // floats between pages (checked: a page's weights are fewer than 2^31)
+    auto load = [&](int j) {
+        const int page = pages[j >> R.page_log];
+        if ((unsigned)page >= (unsigned)R.num_pages) return 0u;
+        return __float_as_uint(plane[(size_t)page * stride + (j & R.mask())]) & 0x7FFFFFFFu;
+    };
+    // the bin (descending) that holds rank `want`, and how many keys lie above it; the bins are zeroed again. Two barriers.
+    auto scan = [&](int& excl, int (&c)[kBins / NT]) {
+        int sum = 0;
+        constexpr int kB = kBins / NT;
+        const int top = kBins - 1 - tid * kB;
+#pragma unroll
+        for (int i = 0; i < kB; ++i) { c[i] = S.hist[top - i]; S.hist[top - i] = 0; sum += c[i]; }
+        int incl = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        if (lane == 31) S.part[warp] = incl;
+        __syncthreads();
+        excl = __reduce_add_sync(0xffffffffu, lane < warp && lane < kWarps ? S.part[lane] : 0) + incl - sum;
+    };
+    auto bin_of = [&](int want, int excl, const int (&c)[kBins / NT], int& bin, int& before, int& count) {
+        bool mine = false;
+#pragma unroll
+        for (int i = 0; i < kBins / NT; ++i) {
+            if (excl < want && want <= excl + c[i]) { bin = kBins - 1 - tid * (kBins / NT) - i; before = excl; count = c[i]; mine = true; }
+            excl += c[i];
+        }
+        return mine;
+    };
+    auto shift_of = [](uint32_t width) { return max(0, 22 - __clz((int)width)); };        // 1024 bins over width + 1 patterns
+    // sample
+    uint32_t lo = 0u, hi = 0x7FFFFFFFu;
+    {
+        uint32_t u[kPer], umin = 0x7FFFFFFFu, umax = 0u;
+        const bool whole = n <= kSample;
+        const uint32_t step = (uint32_t)n / kSample;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            const uint32_t i = k * NT + tid;
+            const uint32_t j = whole ? i : (uint32_t)((uint64_t)i * (uint32_t)n / kSample) + (((i * 2654435761u) >> 16) * step >> 16);
+            u[k] = j < (uint32_t)n ? load(j) : 0xFFFFFFFFu;
+        }
+#pragma unroll
+        for (int k = 0; k < kPer; ++k)
+            if (u[k] != 0xFFFFFFFFu) { umin = min(umin, u[k]); umax = max(umax, u[k]); }
+        umin = __reduce_min_sync(0xffffffffu, umin);
+        umax = __reduce_max_sync(0xffffffffu, umax);
+        if (lane == 0) { S.wmin[warp] = umin; S.wmax[warp] = umax; }
+        __syncthreads();
+        umin = __reduce_min_sync(0xffffffffu, S.wmin[lane % kWarps]);
+        umax = __reduce_max_sync(0xffffffffu, S.wmax[lane % kWarps]);
+        const int shift = shift_of(umax - umin);
+#pragma unroll
+        for (int k = 0; k < kPer; ++k)
+            if (u[k] != 0xFFFFFFFFu) atomicAdd(&S.hist[(u[k] - umin) >> shift], 1);
+        __syncthreads();
+        int excl, c[kBins / NT];
+        scan(excl, c);
+        const float q = (float)w / (float)n, mid = q * kSample, dev = 4.5f * sqrtf(mid * (1.0f - q)) + 4.0f;
+        const int r0 = whole ? w : (int)(mid - dev), r1 = whole ? w : (int)(mid + dev) + 1;
+        int bin, before, count;
+        if (bin_of(r0, excl, c, bin, before, count)) S.bin[0] = bin;
+        if (bin_of(r1, excl, c, bin, before, count)) S.bin[1] = bin;
+        __syncthreads();
+        // (a rank beyond the sample: no bracket on that side)
+        if (S.bin[0] >= 0 && r0 >= 1) hi = min(umin + ((uint32_t)(S.bin[0] + 1) << shift) - 1u, 0x7FFFFFFFu);
+        if (S.bin[1] >= 0) lo = umin + ((uint32_t)S.bin[1] << shift);
+    }
+    // sweep: four neighbouring keys of a page per thread and step
+    int above = 0, mine = 0;
+    auto take = [&](uint32_t u, int j) {
+        above += u > hi;
+        if (u - lo <= hi - lo) {
+            const unsigned long long k = order_key(u, j);
+            if (mine < kOwn) {
+                S.own[mine * NT + tid] = k;
+            } else {
+                const int at = atomicAdd(&S.nmore, 1);
+                if (at < kShared) S.more[at] = k;
+            }
+            ++mine;
+        }
+    };
+    const int chunks = (n + 3) / 4;
+    constexpr int kAhead = 4;
+    for (int i0 = 0; i0 < chunks; i0 += NT * kAhead) {
+        uint4 u[kAhead];
+        int page[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int i = i0 + k * NT + tid;
+            page[k] = i < chunks ? pages[(4 * i) >> R.page_log] : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int j = 4 * (i0 + k * NT + tid);
+            u[k] = make_uint4(0u, 0u, 0u, 0u);
+            if ((unsigned)page[k] < (unsigned)R.num_pages) u[k] = *reinterpret_cast<const uint4*>(plane + (size_t)page[k] * stride + (j & R.mask()));
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int j = 4 * (i0 + k * NT + tid);
+            if (j < n) {
+                take(u[k].x & 0x7FFFFFFFu, j);
+                if (j + 1 < n) take(u[k].y & 0x7FFFFFFFu, j + 1);
+                if (j + 2 < n) take(u[k].z & 0x7FFFFFFFu, j + 2);
+                if (j + 3 < n) take(u[k].w & 0x7FFFFFFFu, j + 3);
+            }
+        }
+    }
+    const int sum_above = __reduce_add_sync(0xffffffffu, above), sum_in = __reduce_add_sync(0xffffffffu, mine);
+    if (lane == 0) { S.above[warp] = sum_above; S.part[warp] = sum_in; }
+    __syncthreads();
+    const int inside = __reduce_add_sync(0xffffffffu, lane < kWarps ? S.part[lane] : 0);
+    int need = w - __reduce_add_sync(0xffffffffu, lane < kWarps ? S.above[lane] : 0);
+    const int nmore = S.nmore;
+    unsigned long long found;
+    if (need < 1 || need > inside || nmore > kShared) {
+        found = radix_select(S.radix, load, n, w);
+    } else {
+        // the need-th of the keys inside, from the bins of their range down
+        auto each = [&](auto&& f) {
+            for (int i = 0; i < min(mine, kOwn); ++i) f(S.own[i * NT + tid]);
+            for (int i = tid; i < nmore; i += NT) f(S.more[i]);
+        };
+        unsigned long long base = (unsigned long long)lo << 32;
+        int s = 32 + shift_of(hi - lo), nbins = kBins, count = inside;
+        while (count > kRank) {
+            __syncthreads();                                      // (part and count have been read)
+            each([&](unsigned long long x) {
+                const unsigned long long bin = (x - base) >> s;
+                if (x >= base && bin < (unsigned long long)nbins) atomicAdd(&S.hist[bin], 1);
+            });
+            __syncthreads();
+            int excl, c[kBins / NT], bin, before, in_bin;
+            scan(excl, c);
+            if (bin_of(need, excl, c, bin, before, in_bin)) { S.bin[0] = bin; S.need = need - before; S.count = in_bin; }
+            __syncthreads();
+            base += (unsigned long long)S.bin[0] << s;
+            need = S.need;
+            count = S.count;
+            const int narrower = max(0, s - 10);
+            nbins = 1 << (s - narrower);
+            s = narrower;
+        }
+        // (s: the width of the next pass's bins; the keys left are those in [base, base + nbins << s), or all of them)
+        __syncthreads();
+        const bool all = count == inside;
+        each([&](unsigned long long x) {
+            if (all || (x >= base && (x - base) >> s < (unsigned long long)nbins)) {
+                const int at = atomicAdd(&S.ncand, 1);
+                if (at < kRank) S.cand[at] = x;
+            }
+        });
+        __syncthreads();
+        for (int i = tid; i < min(count, kRank); i += NT) {
+            const unsigned long long k = S.cand[i];
+            int before = 0;
+            for (int e = 0; e < min(count, kRank); ++e) before += S.cand[e] > k;
+            if (before == need - 1) S.found = k;
+        }
+        __syncthreads();
+        found = S.found;
+    }
+    if (tid == 0) weakest[item] = found;
 }
 
 // CUDA cores, fp32 throughout. A warp looks at 32 keys at a time, a lane per key, and queues the kept ones; eight lanes take one of them, with d / 8
@@ -176,7 +409,7 @@ __global__ void __launch_bounds__(32 * kSimtWarps) simt_attn_kernel(Rows R, cons
             float s = 0.0f;
 #pragma unroll
             for (int c = 0; c < C; ++c) s = fmaf(qv[c], (float)(kw[c / 8] >> (4 * (c % 8)) & 15u), s);
-            s = fmaf(s, pair_s(kp), qsum * pair_z(kp));
+            s = odd_pair(kp) ? NAN : fmaf(s, pair_s(kp), qsum * pair_z(kp));       // (infinities of both signs, or NaN)
 #pragma unroll
             for (int x = 1; x < 8; x <<= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
             s = real ? s + sDelta[warp][i + grp] : -INFINITY;
@@ -249,13 +482,508 @@ __global__ void __launch_bounds__(D) simt_combine_kernel(Rows R, const float* pa
     if (c == 0) lse[item] = top + logf(sum);
 }
 
+// ---- bf16 on the tensor cores ------------------------------------------------------------------------------------------------------
+// A CTA has up to eight query heads of a group (one KV head) and a range of its row's keys; its four warps go through 64 keys in turn, each by itself:
+//   scan     a lane per key tests its weight against every head's weakest kept key; keys that some head keeps are queued, with the heads' biases
+//            (-inf where a head drops the key), so that a key that several heads keep is read and expanded once
+//   gather   32 queued keys at a time, codes and scales, by cp.async into one of the warp's stages while the stage before is used
+//   attend   S^T = K q^T: 16 keys x 8 heads per mma.m16n8k16, the codes 0 .. 15 as exact bf16 numbers, a group of 64 channels per chain of four, whose sum
+//            takes the group's scale and, with the query's own sum over the group, its zero in fp32: nothing of K is rounded. Softmax in
+//            registers with a running maximum per warp and head. O^T += V^T P^T with the codes less 8 as the exact operand (16 channels x 16 keys) and P s, each group's
+//            scale in the weight; P s goes in as two bf16 numbers, high and low part (2^-15 of it is lost; with one the output's error grew by 1.4),
+//            where a group has up to four heads in the operand's other four columns, free of charge. (z + 8 s) P is summed in fp32.
+// (tcgen05 needs 64 rows of A at least, of which a decoding step has the group's 1 to 8 heads or, turned around, the keys: then the expanded codes would
+// have to go through shared memory once more. mma.sync takes them from the registers that the expansion leaves them in, and its rate is not what bounds this kernel.)
+constexpr int kWarps = 4, kThreads = 32 * kWarps, kBatch = 32, kStages = 2, kRing = kStages + 1;
+template <int D, int kH>
+struct AttnShape {
+    static constexpr int kCols = kH <= 4 ? 4 : 8;                 // heads with a bias slot
+    static constexpr int NG = D / kGroup;
+    static constexpr int kPitch = D == 128 ? 160 : 96;            // a key's codes and scales; 32 modulo 128: the rows of a fragment meet every bank once
+    struct alignas(16) Warp {
+        uint8_t data[kStages][kBatch * kPitch];
+        float bias[kRing][kBatch][kCols];
+        size_t row[kRing][kBatch];
+        float delta[kH][64];
+    };
+    struct Merge { float o[kWarps][kCols][D]; };
+    static constexpr size_t kBytes = sizeof(Warp) * kWarps > sizeof(Merge) ? sizeof(Warp) * kWarps : sizeof(Merge);
+};
+constexpr int kAttnCtas = 4 * 148;
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void cp8(uint32_t dst, const void* src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t turn8x8(uint32_t a) {
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
+// two codes (bits 0 - 3 and 16 - 19 of x) as bf16 numbers less kLess: 0x4300 is 128, whose last mantissa bit counts 1
+template <int kLess>
+__device__ __forceinline__ uint32_t codes_bf16(uint32_t x) {
+    const uint32_t v = (x & 0x000f000fu) | 0x43004300u;
+    constexpr uint32_t off = kLess == 0 ? 0x43004300u : 0x43084308u;        // 128, 136
+    uint32_t d;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(v), "r"(off));
+    return d;
+}
+__device__ __forceinline__ float ex2f(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// One item's share of the work, as a CTA finds it.
+struct Piece { int t, i, k0, k1; bool whole; };
+
+// The heads' softmax state and sums of a warp, in the layout of the accumulators: this lane's columns are heads 2 (lane % 4) and the next one, of eight, or of four
+// high parts and four low parts.
+template <int D>
+struct WarpState {
+    static constexpr int NG = D / kGroup;
+    float o[NG][4][4], oz[NG][2], m[2], l[2];
+    uint32_t q[NG][4][2];
+    float qsum[NG][2];
+};
+
+// 32 keys of a stage. kOdd: some scale is not finite; a head that does not keep the key is to get nothing of it.
+template <int D, int kH, bool kOdd>
+__device__ __forceinline__ void attend(WarpState<D>& W, const uint8_t* data, const float (*bias)[AttnShape<D, kH>::kCols], float scale) {
+    using Sh = AttnShape<D, kH>;
+    constexpr int NG = D / kGroup, kPitch = Sh::kPitch;
+    const int lane = threadIdx.x & 31, r = lane >> 2, t = lane & 3, kr = r ^ (r >> 2 & 1), col = (2 * t) % Sh::kCols;
+    float x[2][4];
+    uint32_t sv[2][2][NG];                                        // V's pairs of keys r and r + 8 of both tiles
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint8_t* ka = data + (16 * i + kr) * kPitch;
+        const uint8_t* kb = ka + 8 * kPitch;
+        uint32_t pa[2 * NG], pb[2 * NG];
+        if constexpr (NG == 2) {
+            const uint4 a = *reinterpret_cast<const uint4*>(ka + D), b = *reinterpret_cast<const uint4*>(kb + D);
+            pa[0] = a.x; pa[1] = a.y; pa[2] = a.z; pa[3] = a.w;
+            pb[0] = b.x; pb[1] = b.y; pb[2] = b.z; pb[3] = b.w;
+        } else {
+            const uint2 a = *reinterpret_cast<const uint2*>(ka + D), b = *reinterpret_cast<const uint2*>(kb + D);
+            pa[0] = a.x; pa[1] = a.y;
+            pb[0] = b.x; pb[1] = b.y;
+        }
+        float dot[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            const uint2 a = *reinterpret_cast<const uint2*>(ka + g * 32 + t * 8), b = *reinterpret_cast<const uint2*>(kb + g * 32 + t * 8);
+            float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+                mma16816(c, codes_bf16<0>(a.x >> (4 * s)), codes_bf16<0>(b.x >> (4 * s)), codes_bf16<0>(a.y >> (4 * s)), codes_bf16<0>(b.y >> (4 * s)), W.q[g][s][0], W.q[g][s][1]);
+            const float sa = pair_s(pa[g]), za = pair_z(pa[g]), sb = pair_s(pb[g]), zb = pair_z(pb[g]);
+            dot[0] = fmaf(sa, c[0], fmaf(za, W.qsum[g][0], dot[0]));
+            dot[1] = fmaf(sa, c[1], fmaf(za, W.qsum[g][1], dot[1]));
+            dot[2] = fmaf(sb, c[2], fmaf(zb, W.qsum[g][0], dot[2]));
+            dot[3] = fmaf(sb, c[3], fmaf(zb, W.qsum[g][1], dot[3]));
+            sv[i][0][g] = pa[NG + g];
+            sv[i][1][g] = pb[NG + g];
+        }
+        const float2 ba = *reinterpret_cast<const float2*>(&bias[16 * i + kr][col]), bb = *reinterpret_cast<const float2*>(&bias[16 * i + 8 + kr][col]);
+        x[i][0] = fmaf(dot[0], scale, ba.x);
+        x[i][1] = fmaf(dot[1], scale, ba.y);
+        x[i][2] = fmaf(dot[2], scale, bb.x);
+        x[i][3] = fmaf(dot[3], scale, bb.y);
+        if (kOdd) {                                               // (values of a group without finite scale are NaN, or infinities of both signs)
+            bool na = false, nb = false;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) { na = na || odd_pair(pa[g]); nb = nb || odd_pair(pb[g]); }
+            x[i][0] = ba.x == -INFINITY ? -INFINITY : na ? NAN : x[i][0];
+            x[i][1] = ba.y == -INFINITY ? -INFINITY : na ? NAN : x[i][1];
+            x[i][2] = bb.x == -INFINITY ? -INFINITY : nb ? NAN : x[i][2];
+            x[i][3] = bb.y == -INFINITY ? -INFINITY : nb ? NAN : x[i][3];
+        }
+    }
+    // The maximum that the exponentials refer to moves only when it is passed by more than 5: p stays below e^5, and the sums are rescaled rarely.
+    float mx[2] = {fmaxf(fmaxf(x[0][0], x[0][2]), fmaxf(x[1][0], x[1][2])), fmaxf(fmaxf(x[0][1], x[0][3]), fmaxf(x[1][1], x[1][3]))};
+    if (__any_sync(0xffffffffu, mx[0] > W.m[0] + 5.0f || mx[1] > W.m[1] + 5.0f)) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], o));
+            const float top = fmaxf(W.m[e], mx[e]), f = ex2f((W.m[e] - top) * kLog2e);
+            W.m[e] = top;
+            W.l[e] *= f;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                W.oz[g][e] *= f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { W.o[g][j][e] *= f; W.o[g][j][e + 2] *= f; }
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] = ex2f((x[i][e] - W.m[e & 1]) * kLog2e);
+        W.l[0] += p[0] + p[2];
+        W.l[1] += p[1] + p[3];
+        const int ra = (2 * t) ^ (t >> 1);                        // the row of operand key 2t; key 2t + 1 lies in the other row of the pair
+        const uint8_t* vrow = data + (16 * i + ra) * kPitch + D / 2 + 4 * r;
+        const int other = (t >> 1) ? -kPitch : kPitch;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            const float sa = pair_s(sv[i][0][g]), za = fmaf(8.0f, sa, pair_z(sv[i][0][g])), sb = pair_s(sv[i][1][g]), zb = fmaf(8.0f, sb, pair_z(sv[i][1][g]));
+            float w[4] = {p[0] * sa, p[1] * sa, p[2] * sb, p[3] * sb};
+            if (kOdd) {
+                const bool k[4] = {x[i][0] != -INFINITY, x[i][1] != -INFINITY, x[i][2] != -INFINITY, x[i][3] != -INFINITY};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = k[e] ? w[e] : 0.0f;
+                W.oz[g][0] += (k[0] ? p[0] * za : 0.0f) + (k[2] ? p[2] * zb : 0.0f);
+                W.oz[g][1] += (k[1] ? p[1] * za : 0.0f) + (k[3] ? p[3] * zb : 0.0f);
+            } else {
+                W.oz[g][0] = fmaf(p[0], za, fmaf(p[2], zb, W.oz[g][0]));
+                W.oz[g][1] = fmaf(p[1], za, fmaf(p[3], zb, W.oz[g][1]));
+            }
+            // high parts: the upper halves as they are; low parts: what they leave
+            uint32_t hi0 = __byte_perm(__float_as_uint(w[0]), __float_as_uint(w[1]), 0x7632), hi1 = __byte_perm(__float_as_uint(w[2]), __float_as_uint(w[3]), 0x7632);
+            float lw[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) lw[e] = w[e] - __uint_as_float(__float_as_uint(w[e]) & 0xffff0000u);
+            uint32_t lo0 = __byte_perm(__float_as_uint(lw[0]), __float_as_uint(lw[1]), 0x7632), lo1 = __byte_perm(__float_as_uint(lw[2]), __float_as_uint(lw[3]), 0x7632);
+            if (kH <= 4 && t >= 2) { hi0 = lo0; hi1 = lo1; }
+            const uint32_t b0 = turn8x8(hi0), b1 = turn8x8(hi1);
+            const uint32_t wa = *reinterpret_cast<const uint32_t*>(vrow + g * 32), wb = *reinterpret_cast<const uint32_t*>(vrow + g * 32 + other);
+            const uint32_t wc = *reinterpret_cast<const uint32_t*>(vrow + g * 32 + 8 * kPitch), wd = *reinterpret_cast<const uint32_t*>(vrow + g * 32 + 8 * kPitch + other);
+            const uint32_t x0 = __byte_perm(wa, wb, 0x5410), x1 = __byte_perm(wa, wb, 0x7632), y0 = __byte_perm(wc, wd, 0x5410), y1 = __byte_perm(wc, wd, 0x7632);
+            uint32_t c0 = 0u, c1 = 0u;
+            if constexpr (kH > 4) { c0 = turn8x8(lo0); c1 = turn8x8(lo1); }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t a0 = codes_bf16<8>(x0 >> (4 * j)), a1 = codes_bf16<8>(x1 >> (4 * j)), a2 = codes_bf16<8>(y0 >> (4 * j)), a3 = codes_bf16<8>(y1 >> (4 * j));
+                mma16816(W.o[g][j], a0, a1, a2, a3, b0, b1);
+                if constexpr (kH > 4) mma16816(W.o[g][j], a0, a1, a2, a3, c0, c1);
+            }
+        }
+    }
+}
+
+struct AttnArgs {
+    Rows R;
+    const __nv_bfloat16* q;
+    const uint8_t* codes;
+    const uint8_t* scales;
+    const unsigned long long* weakest;
+    __nv_bfloat16* o;
+    float *lse, *partial;
+    Plan plan;
+    int Hkv, G, hb, hpb;                                          // heads of a group, blocks that they come in, heads per block
+    float scale;
+    int64_t qs_row, qs_head, os_row, os_head;
+    int rows;
+};
+
+// The last i in [0, n) with first[i] <= x, by a warp: 32 probes per round.
+__device__ __forceinline__ int warp_find(const int32_t* first, int n, int x) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, len = n;                                          // first[lo] <= x; the answer lies in [lo, lo + len)
+    while (len > 1) {
+        const int step = (len + 31) / 32, at = lo + lane * step;
+        const bool in = lane * step < len && first[at] <= x;
+        const int last = __popc(__ballot_sync(0xffffffffu, in)) - 1;       // (ascending: a prefix of the lanes)
+        const int end = lo + len;
+        lo += last * step;
+        len = min(step, end - lo);
+    }
+    return lo;
+}
+
+template <int D, int kH>
+__global__ void __launch_bounds__(kThreads, 4) attn_kernel(AttnArgs A) {
+    using Sh = AttnShape<D, kH>;
+    constexpr int NG = Sh::NG, kCols = Sh::kCols, kPitch = Sh::kPitch;
+    extern __shared__ __align__(16) uint8_t attn_smem[];
+    __shared__ float sM[kWarps][kCols], sL[kWarps][kCols];
+    __shared__ int sTicket;
+    auto& M = *reinterpret_cast<typename Sh::Merge*>(attn_smem);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, t4 = lane & 3;
+    auto& S = reinterpret_cast<typename Sh::Warp*>(attn_smem)[warp];
+    Rows& R = A.R;
+    pdl_enter(R.table, R.seq, R.pos, R.delta, A.q, A.codes, A.scales, A.weakest, A.o, A.lse, A.partial, A.plan.ustart, A.plan.tickets);
+    const int per_row = A.Hkv * A.hb;
+    int at = 0, until = 1, E = 1, U = 1;                          // units of this CTA; without a plan the CTA's item
+    const int cta = blockIdx.x;
+    if (A.plan.ustart) {
+        U = A.plan.ustart[A.rows];
+        E = min((int)gridDim.x, max(U / 4, 1));                   // (four units at least)
+        if (cta >= E || U == 0) return;
+        at = (int)((int64_t)cta * U / E);
+        until = (int)((int64_t)(cta + 1) * U / E);
+    }
+    const int begin = at;
+    while (at < until) {
+        int t, i, n, seq, k0 = 0, k1, u0 = 0, u1 = 1;
+        if (A.plan.ustart) {
+            t = warp_find(A.plan.ustart, A.rows, at);
+            const int first = A.plan.ustart[t], units = (A.plan.ustart[t + 1] - first) / per_row;
+            i = (at - first) / units;
+            u0 = first + i * units;
+            u1 = u0 + units;
+            n = R.visible(t, seq);
+            const int e = min(u1, until);
+            k0 = min((int64_t)n, (int64_t)(at - u0) << A.plan.unit_log);
+            k1 = min((int64_t)n, (int64_t)(e - u0) << A.plan.unit_log);
+            at = e;
+        } else {
+            t = cta / per_row;
+            i = cta % per_row;
+            n = R.visible(t, seq);
+            if (n < 0) return;
+            k1 = n;
+            at = until;
+        }
+        const int hk = i / A.hb, h0 = hk * A.G + (i % A.hb) * A.hpb, heads = min(A.hpb, (hk + 1) * A.G - h0);
+        const int32_t* pages = R.table + seq * R.ld;
+        unsigned long long least[kH];
+#pragma unroll
+        for (int h = 0; h < kH; ++h) least[h] = h >= heads ? ~0ull : A.weakest ? A.weakest[t * R.Hq + h0 + h] : 0ull;
+        // queries: column r of the operand is head r % kCols; channels in the order that the codes come in
+        WarpState<D> W;
+        {
+            const int h = r % kCols;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
+                if (h < heads) {
+                    const uint4* src = reinterpret_cast<const uint4*>(A.q + t * A.qs_row + (h0 + h) * A.qs_head + g * kGroup + t4 * 16);
+                    a = src[0];
+                    b = src[1];
+                }
+                W.q[g][0][0] = __byte_perm(a.x, a.z, 0x5410); W.q[g][1][0] = __byte_perm(a.x, a.z, 0x7632);
+                W.q[g][2][0] = __byte_perm(a.y, a.w, 0x5410); W.q[g][3][0] = __byte_perm(a.y, a.w, 0x7632);
+                W.q[g][0][1] = __byte_perm(b.x, b.z, 0x5410); W.q[g][1][1] = __byte_perm(b.x, b.z, 0x7632);
+                W.q[g][2][1] = __byte_perm(b.y, b.w, 0x5410); W.q[g][3][1] = __byte_perm(b.y, b.w, 0x7632);
+                float sum = 0.0f;
+                const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum += __uint_as_float(w[e] << 16) + __uint_as_float(w[e] & 0xffff0000u);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                W.qsum[g][0] = __shfl_sync(0xffffffffu, sum, 8 * t4);
+                W.qsum[g][1] = __shfl_sync(0xffffffffu, sum, 8 * t4 + 4);
+                W.oz[g][0] = W.oz[g][1] = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) W.o[g][j][0] = W.o[g][j][1] = W.o[g][j][2] = W.o[g][j][3] = 0.0f;
+            }
+            W.m[0] = W.m[1] = -3.4e38f;
+            W.l[0] = W.l[1] = 0.0f;
+        }
+        for (int e = lane; e < kRing * kBatch * kCols; e += 32) (&S.bias[0][0][0])[e] = -INFINITY;
+        __syncwarp();
+
+        int tail = 0, issued = 0, used = 0;                       // keys queued, batches requested, batches attended to
+        auto gather = [&](int batch) {                            // (the batch's rows and biases are in the ring)
+            const int ring = batch % kRing, count = min(kBatch, tail - batch * kBatch);
+            const uint32_t dst = (uint32_t)__cvta_generic_to_shared(S.data[batch % kStages]);
+            constexpr int kLanes = D / 16, kKeys = 32 / kLanes;   // lanes per key, keys per instruction
+#pragma unroll
+            for (int e = 0; e < kBatch; e += kKeys) {
+                const int key = e + lane / kLanes;
+                if (key < count) cp16(dst + key * kPitch + lane % kLanes * 16, A.codes + S.row[ring][key] * D + lane % kLanes * 16);
+            }
+            if (lane < count) {
+                const uint8_t* src = A.scales + S.row[ring][lane] * (D / 8);
+                if constexpr (D == 128) cp16(dst + lane * kPitch + D, src); else cp8(dst + lane * kPitch + D, src);
+            } else {                                              // places without a key: finite, and of no weight
+                uint32_t* p = reinterpret_cast<uint32_t*>(S.data[batch % kStages] + lane * kPitch + D);
+#pragma unroll
+                for (int e = 0; e < D / 32; ++e) p[e] = 0u;
+#pragma unroll
+                for (int e = 0; e < kCols; ++e) S.bias[ring][lane][e] = -INFINITY;
+            }
+            cp_commit();
+        };
+        auto use = [&](int batch) {                               // (its copies have arrived)
+            __syncwarp();
+            const uint8_t* data = S.data[batch % kStages];
+            bool odd = false;
+            const uint32_t* p = reinterpret_cast<const uint32_t*>(data + lane * kPitch + D);
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) odd |= odd_pair(p[e]);
+            if (__any_sync(0xffffffffu, odd)) attend<D, kH, true>(W, data, S.bias[batch % kRing], A.scale);
+            else attend<D, kH, false>(W, data, S.bias[batch % kRing], A.scale);
+            __syncwarp();
+        };
+        auto step = [&]() {                                       // requests the next batch, then attends to the one before
+            __syncwarp();
+            gather(issued++);
+            if (issued - used == kStages) {
+                cp_wait<kStages - 1>();
+                use(used++);
+            }
+        };
+        // 64 keys per turn: lane's pair of neighbouring keys, in every head; the next turn's weights are requested before this one's are tested
+        float2 dl[kH];
+        int page = -1, next_page = -1;
+        auto page_of = [&](int j) {
+            if (j >= k1) return -1;
+            const int p = pages[j >> R.page_log];
+            return (unsigned)p < (unsigned)R.num_pages ? p : -1;
+        };
+        auto request = [&](int j, int p) {
+#pragma unroll
+            for (int h = 0; h < kH; ++h) {
+                dl[h] = make_float2(0.0f, 0.0f);
+                if (p >= 0 && h < heads) dl[h] = *reinterpret_cast<const float2*>(R.delta + (((size_t)p * R.Hq + h0 + h) << R.page_log) + (j & R.mask()));
+            }
+        };
+        const int j0 = k0 + warp * 64;
+        next_page = page_of(j0 + 2 * lane);
+        request(j0 + 2 * lane, next_page);
+        int after = page_of(j0 + kWarps * 64 + 2 * lane);
+        for (int j = j0; j < k1; j += kWarps * 64) {
+            page = next_page;
+#pragma unroll
+            for (int h = 0; h < kH; ++h) *reinterpret_cast<float2*>(&S.delta[h][2 * lane]) = dl[h];
+            __syncwarp();
+            next_page = after;
+            request(j + kWarps * 64 + 2 * lane, next_page);
+            after = page_of(j + 2 * kWarps * 64 + 2 * lane);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int key = j + 32 * half + lane, p = __shfl_sync(0xffffffffu, page, 16 * half + lane / 2);
+                float b[kCols];
+                bool any = false;
+#pragma unroll
+                for (int h = 0; h < kCols; ++h) b[h] = -INFINITY;
+                const bool there = p >= 0 && key < k1;
+#pragma unroll
+                for (int h = 0; h < kH; ++h) {
+                    const float d = S.delta[h][32 * half + lane];
+                    const bool kept = there && order_key(__float_as_uint(d) & 0x7FFFFFFFu, key) >= least[h];
+                    b[h] = kept ? d : -INFINITY;
+                    any = any || kept;
+                }
+                const uint32_t ballot = __ballot_sync(0xffffffffu, any);
+                if (any) {
+                    const int to = tail + __popc(ballot & ((1u << lane) - 1u)), ring = to / kBatch % kRing;
+                    S.row[ring][to % kBatch] = key_row(p, hk, key & R.mask(), A.Hkv, R.page_log);
+                    float4* dst = reinterpret_cast<float4*>(S.bias[ring][to % kBatch]);
+                    dst[0] = make_float4(b[0], b[1], b[2], b[3]);
+                    if constexpr (kCols == 8) dst[1] = make_float4(b[4], b[5], b[6], b[7]);
+                }
+                tail += __popc(ballot);
+                if (tail - issued * kBatch >= kBatch) step();
+            }
+            __syncwarp();
+        }
+        if (tail > issued * kBatch) step();
+        cp_wait<0>();
+        while (used < issued) use(used++);
+
+        // the warp's sums: keys of one residue per lane row; then low parts to the high ones
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) {
+                W.l[e] += __shfl_xor_sync(0xffffffffu, W.l[e], o);
+#pragma unroll
+                for (int g = 0; g < NG; ++g) W.oz[g][e] += __shfl_xor_sync(0xffffffffu, W.oz[g][e], o);
+            }
+        }
+        __syncthreads();                                          // (stages become the merge's memory)
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float v = W.o[g][j][e];
+                    if (kH <= 4) v += __shfl_xor_sync(0xffffffffu, v, 2);
+                    const int h = 2 * t4 + (e & 1), c = g * kGroup + 8 * r + 4 * (e >> 1) + j;
+                    if (h < kCols) M.o[warp][h][c] = v + W.oz[g][e & 1];
+                }
+        if (r == 0 && 2 * t4 < kCols) {
+            sM[warp][2 * t4] = W.m[0]; sM[warp][2 * t4 + 1] = W.m[1];
+            sL[warp][2 * t4] = W.l[0]; sL[warp][2 * t4 + 1] = W.l[1];
+        }
+        __syncthreads();
+        const bool whole = !A.plan.ustart || (u0 >= begin && u1 <= until);
+        const int item = t * per_row + i;
+        float* slot = A.partial + (size_t)(2 * cta + (u0 > begin ? 1 : 0)) * kCols * (D + 2);
+        // thread: four channels of a head
+        for (int e = tid; e < heads * (D / 4); e += kThreads) {
+            const int h = e / (D / 4), c = e % (D / 4) * 4;
+            float top = sM[0][h];
+#pragma unroll
+            for (int x = 1; x < kWarps; ++x) top = fmaxf(top, sM[x][h]);
+            float sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int x = 0; x < kWarps; ++x) {
+                const float f = ex2f((sM[x][h] - top) * kLog2e);
+                const float4 a = *reinterpret_cast<const float4*>(&M.o[x][h][c]);
+                sum = fmaf(sL[x][h], f, sum);
+                v[0] = fmaf(a.x, f, v[0]); v[1] = fmaf(a.y, f, v[1]); v[2] = fmaf(a.z, f, v[2]); v[3] = fmaf(a.w, f, v[3]);
+            }
+            if (whole) {
+                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                __nv_bfloat162 lo = __floats2bfloat162_rn(v[0] * inv, v[1] * inv), hi = __floats2bfloat162_rn(v[2] * inv, v[3] * inv);
+                *reinterpret_cast<uint2*>(A.o + t * A.os_row + (h0 + h) * A.os_head + c) = make_uint2(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi));
+                if (c == 0) A.lse[t * R.Hq + h0 + h] = sum == 0.0f ? -INFINITY : top + logf(sum);
+            } else {
+                *reinterpret_cast<float4*>(slot + 2 * kCols + h * D + c) = make_float4(v[0], v[1], v[2], v[3]);
+                if (c == 0) { slot[2 * h] = top; slot[2 * h + 1] = sum; }
+            }
+        }
+        if (!whole) {
+            // the CTA that finishes the item last adds its pieces, in their order
+            const int c0 = (int)(((int64_t)(u0 + 1) * E - 1) / U), c1 = (int)(((int64_t)u1 * E - 1) / U), pieces = c1 - c0 + 1;
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) sTicket = atomicAdd(&A.plan.tickets[item], 1);
+            __syncthreads();
+            if (sTicket == pieces - 1) {
+                __threadfence();
+                auto piece = [&](int c) {
+                    const int first = (int)((int64_t)c * U / E);
+                    return A.partial + (size_t)(2 * c + (u0 > first ? 1 : 0)) * kCols * (D + 2);
+                };
+                for (int e = tid; e < heads * (D / 4); e += kThreads) {
+                    const int h = e / (D / 4), c = e % (D / 4) * 4;
+                    float top = -3.4e38f;
+                    for (int x = c0; x <= c1; ++x) top = fmaxf(top, __ldcg(piece(x) + 2 * h));
+                    float sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+                    for (int x = c0; x <= c1; ++x) {
+                        const float* s = piece(x);
+                        const float f = ex2f((__ldcg(s + 2 * h) - top) * kLog2e);
+                        const float4 a = __ldcg(reinterpret_cast<const float4*>(s + 2 * kCols + h * D + c));
+                        sum = fmaf(__ldcg(s + 2 * h + 1), f, sum);
+                        v[0] = fmaf(a.x, f, v[0]); v[1] = fmaf(a.y, f, v[1]); v[2] = fmaf(a.z, f, v[2]); v[3] = fmaf(a.w, f, v[3]);
+                    }
+                    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                    __nv_bfloat162 lo = __floats2bfloat162_rn(v[0] * inv, v[1] * inv), hi = __floats2bfloat162_rn(v[2] * inv, v[3] * inv);
+                    *reinterpret_cast<uint2*>(A.o + t * A.os_row + (h0 + h) * A.os_head + c) = make_uint2(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi));
+                    if (c == 0) A.lse[t * R.Hq + h0 + h] = sum == 0.0f ? -INFINITY : top + logf(sum);
+                }
+            }
+        }
+        __syncthreads();                                          // the merge's memory becomes stages
+    }
+}
+
 constexpr int kSimtCtas = 148 * 8;
 int simt_splits(const Cache& C) {
     const int64_t items = (int64_t)C.rows * C.Hq, keys = (int64_t)C.max_blocks << C.page_log;
     return (int)std::min<int64_t>((kSimtCtas + items - 1) / items, std::min<int64_t>(64, (keys + 255) / 256));
 }
 
-size_t weakest_bytes(const Cache& C) { return ((size_t)C.rows * C.Hq * sizeof(unsigned long long) + 255) / 256 * 256; }
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+size_t weakest_bytes(const Cache& C) { return round256((size_t)C.rows * C.Hq * sizeof(unsigned long long)); }
+// heads of a group: blocks of at most eight, of the same size
+int head_blocks(const Cache& C) { return (C.G + 7) / 8; }
+size_t plan_bytes(const Cache& C) { return round256(((size_t)C.rows + 1 + (size_t)C.rows * C.Hkv * head_blocks(C)) * sizeof(int32_t)); }
 
 template <typename T, int D>
 int simt_decode(const Cache& C, const Rows& R, const void* q, const uint8_t* codes, const __nv_bfloat16* scales, const unsigned long long* weakest, void* o, float* lse,
@@ -267,25 +995,61 @@ int simt_decode(const Cache& C, const Rows& R, const void* q, const uint8_t* cod
     return launch_overlapped(simt_combine_kernel<T, D>, dim3(items), dim3(D), 0, st, 1, R, partial, (T*)o, lse, splits, C.os[0], C.os[1]);
 }
 
+template <int D, int kH>
+int tc_decode(const AttnArgs& A, int grid, cudaStream_t st) {
+    constexpr size_t bytes = AttnShape<D, kH>::kBytes;
+    if (cudaFuncSetAttribute(attn_kernel<D, kH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return DMA_ERR_CUDA;
+    return launch_overlapped(attn_kernel<D, kH>, dim3(grid), dim3(kThreads), bytes, st, 1, A);
+}
+
+template <int NT, int kPer>
+int select(const Cache& C, const Rows& R, unsigned long long* weakest, const Plan& plan, cudaStream_t st) {
+    constexpr size_t bytes = sizeof(SelectShared<NT>);
+    if (cudaFuncSetAttribute(select_kernel<NT, kPer>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return DMA_ERR_CUDA;
+    return launch_overlapped(select_kernel<NT, kPer>, dim3(C.rows * C.Hq + (plan.ustart ? 1 : 0)), dim3(NT), bytes, st, 1, R, C.rows, C.w, weakest, plan);
+}
+
 }  // namespace
 
 size_t cache4_decode_ws_bytes(const Cache& C) {
-    return kWsHeaderBytes + weakest_bytes(C) + ((size_t)C.rows * C.Hq + kSimtCtas) * (C.d + 2) * sizeof(float);
+    const size_t simt = ((size_t)C.rows * C.Hq + kSimtCtas) * (C.d + 2), pieces = (size_t)2 * kAttnCtas * 8 * (C.d + 2);
+    return kWsHeaderBytes + weakest_bytes(C) + plan_bytes(C) + std::max(simt, pieces) * sizeof(float);
 }
 
 int launch_cache4_decode(const Cache& C, const void* q, const uint8_t* codes, const __nv_bfloat16* scales, const float* delta, const int32_t* table,
                          const int32_t* row_seq, const int32_t* row_pos, void* o, float* lse, void* ws, cudaStream_t st) {
     const Rows R{table, row_seq, row_pos, delta, C.table_ld, C.nseq, C.page_log, C.num_pages, C.max_blocks, C.Hq};
+    const int64_t capacity = (int64_t)C.max_blocks << C.page_log;      // (no row sees more keys than the table holds)
+    const bool tensor = C.dtype == DMA_BF16 && !(C.flags & DMA_FLAG_SIMT);
+    const int hb = head_blocks(C), per_row = C.Hkv * hb;
     unsigned long long* weakest = nullptr;
-    if (((int64_t)C.max_blocks << C.page_log) > C.w) {            // (no row sees more keys than the table holds)
-        weakest = reinterpret_cast<unsigned long long*>((char*)ws + kWsHeaderBytes);
-        const int rc = launch_overlapped(select_kernel, dim3(C.rows * C.Hq), dim3(kSelectThreads), 0, st, 1, R, C.w, weakest);
+    Plan plan{nullptr, nullptr, per_row, 8};
+    char* at = (char*)ws + kWsHeaderBytes;
+    if (tensor && capacity > 1024) {
+        plan.ustart = reinterpret_cast<int32_t*>(at + weakest_bytes(C));
+        plan.tickets = plan.ustart + C.rows + 1;
+        while ((int64_t)C.rows * per_row > INT32_MAX / ((capacity >> plan.unit_log) + 2)) ++plan.unit_log;
+    }
+    int rc;
+    if (capacity > C.w) {
+        weakest = reinterpret_cast<unsigned long long*>(at);
+        rc = C.rows * C.Hq >= 3 * 148 ? select<256, 8>(C, R, weakest, plan, st) : select<1024, 4>(C, R, weakest, plan, st);
+        if (rc) return rc;
+    } else if (plan.ustart) {
+        rc = launch_overlapped(plan_kernel, dim3(1), dim3(1024), 0, st, 1, R, C.rows, plan);
         if (rc) return rc;
     }
-    float* partial = reinterpret_cast<float*>((char*)ws + kWsHeaderBytes + weakest_bytes(C));
-    auto f = C.dtype == DMA_BF16 ? (C.d == 128 ? simt_decode<__nv_bfloat16, 128> : simt_decode<__nv_bfloat16, 64>)
-                                 : (C.d == 128 ? simt_decode<float, 128> : simt_decode<float, 64>);
-    return f(C, R, q, codes, scales, weakest, o, lse, partial, st);
+    float* partial = reinterpret_cast<float*>(at + weakest_bytes(C) + plan_bytes(C));
+    if (!tensor) {
+        auto f = C.dtype == DMA_BF16 ? (C.d == 128 ? simt_decode<__nv_bfloat16, 128> : simt_decode<__nv_bfloat16, 64>)
+                                     : (C.d == 128 ? simt_decode<float, 128> : simt_decode<float, 64>);
+        return f(C, R, q, codes, scales, weakest, o, lse, partial, st);
+    }
+    const int hpb = (C.G + hb - 1) / hb, grid = plan.ustart ? kAttnCtas : C.rows * per_row;
+    const AttnArgs A{R, (const __nv_bfloat16*)q, codes, (const uint8_t*)scales, weakest, (__nv_bfloat16*)o, lse, partial, plan, C.Hkv, C.G, hb, hpb, C.scale,
+                     C.qs[0], C.qs[1], C.os[0], C.os[1], C.rows};
+    if (C.d == 128) return hpb == 1 ? tc_decode<128, 1>(A, grid, st) : hpb == 2 ? tc_decode<128, 2>(A, grid, st) : hpb <= 4 ? tc_decode<128, 4>(A, grid, st) : tc_decode<128, 8>(A, grid, st);
+    return hpb == 1 ? tc_decode<64, 1>(A, grid, st) : hpb == 2 ? tc_decode<64, 2>(A, grid, st) : hpb <= 4 ? tc_decode<64, 4>(A, grid, st) : tc_decode<64, 8>(A, grid, st);
 }
 
 }  // namespace dma

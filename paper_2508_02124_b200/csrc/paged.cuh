@@ -37,4 +37,7 @@ __device__ __forceinline__ size_t key_row(int page, int head, int place, int Hkv
 __device__ __forceinline__ float pair_s(uint32_t p) { return __uint_as_float(p << 16); }
 __device__ __forceinline__ float pair_z(uint32_t p) { return __uint_as_float(p & 0xffff0000u); }
 
+// one of the two is a NaN or an infinity (all ones in the exponent carry into the sign's place)
+__device__ __forceinline__ bool odd_pair(uint32_t p) { return (((p & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0u; }
+
 }  // namespace dma

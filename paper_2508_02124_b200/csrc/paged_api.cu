@@ -35,7 +35,7 @@ int resolve_cache(const dma_cache_t* c, Cache* o) {
     const int rc = resolve_pages(c, o);
     if (rc) return rc;
     if (c->Hq < 1 || c->Hkv < 1 || c->Hq % c->Hkv || c->w < 1) return DMA_ERR_SHAPE;
-    if ((int64_t)c->rows * c->Hq > INT32_MAX / 2 || c->Hkv > 65535) return DMA_ERR_SHAPE;
+    if ((int64_t)c->rows * c->Hq > INT32_MAX / 2 || (int64_t)c->Hq * c->page_size > INT32_MAX || c->Hkv > 65535) return DMA_ERR_SHAPE;
     if (c->d != 64 && c->d != 128) return DMA_ERR_UNSUPPORTED;
     if (c->dtype != DMA_BF16 && c->dtype != DMA_FP32) return DMA_ERR_UNSUPPORTED;
     if (c->flags & ~DMA_FLAG_SIMT) return DMA_ERR_UNSUPPORTED;
