@@ -487,11 +487,14 @@ __global__ void __launch_bounds__(D) simt_combine_kernel(Rows R, const float* pa
 //   scan     a lane per key tests its weight against every head's weakest kept key; keys that some head keeps are queued, with the heads' biases
 //            (-inf where a head drops the key), so that a key that several heads keep is read and expanded once
 //   gather   32 queued keys at a time, codes and scales, by cp.async into one of the warp's stages while the stage before is used
-//   attend   S^T = K q^T: 16 keys x 8 heads per mma.m16n8k16, the codes 0 .. 15 as exact bf16 numbers, a group of 64 channels per chain of four, whose sum
-//            takes the group's scale and, with the query's own sum over the group, its zero in fp32: nothing of K is rounded. Softmax in
-//            registers with a running maximum per warp and head. O^T += V^T P^T with the codes less 8 as the exact operand (16 channels x 16 keys) and P s, each group's
-//            scale in the weight; P s goes in as two bf16 numbers, high and low part (2^-15 of it is lost; with one the output's error grew by 1.4),
-//            where a group has up to four heads in the operand's other four columns, free of charge. (z + 8 s) P is summed in fp32.
+//   attend   S^T = K q^T and O^T += V^T P^T by mma.m16n8k16 (keys, then channels, by heads). What bounds this kernel is the integer pipe that expands the codes, so they are
+//            expanded as little as possible: a code n in the lowest mantissa bits of a half is the subnormal number n 2^-24, exactly, and four bits higher 16 n 2^-24; eight
+//            codes of a word take a shift and four masks. A group of 64 channels is a chain of four products, whose sum takes the group's scale, and with the query's own sum
+//            over the group its zero, in fp32; the query goes in as halves, scaled by a power of two per head (its 8 bits survive down to 2^-27 of the head's largest
+//            channel; the products of 16 n take q / 16). Nothing of K is rounded. Softmax in registers, with a running maximum per warp and head. Of V the
+//            scale goes into the weight, P s as a half, scaled by a power of two per head and group that follows its largest (WarpState); that rounding, at most 2^-11 of a
+//            weight, is the kernel's largest after the output's (its error against 64 bits grows by a sixth). z P is summed in fp32.
+//            With up to four heads the operand's columns 4 to 7 hold the same heads again, and their lanes take the second 16 keys through the softmax.
 // (tcgen05 needs 64 rows of A at least, of which a decoding step has the group's 1 to 8 heads or, turned around, the keys: then the expanded codes would
 // have to go through shared memory once more. mma.sync takes them from the registers that the expansion leaves them in, and its rate is not what bounds this kernel.)
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kBatch = 32, kStages = 2, kRing = kStages + 1;
@@ -517,7 +520,7 @@ __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_grou
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t turn8x8(uint32_t a) {
@@ -525,76 +528,97 @@ __device__ __forceinline__ uint32_t turn8x8(uint32_t a) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
     return d;
 }
-// two codes (bits 0 - 3 and 16 - 19 of x) as bf16 numbers less kLess: 0x4300 is 128, whose last mantissa bit counts 1
-template <int kLess>
-__device__ __forceinline__ uint32_t codes_bf16(uint32_t x) {
-    const uint32_t v = (x & 0x000f000fu) | 0x43004300u;
-    constexpr uint32_t off = kLess == 0 ? 0x43004300u : 0x43084308u;        // 128, 136
+__device__ __forceinline__ uint32_t halves(float lo, float hi) {
     uint32_t d;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(v), "r"(off));
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
+}
+// a word's codes in four pairs of halves: pair s holds codes s and s + 4, times 2^-24, and 16 where s is odd
+__device__ __forceinline__ void expand_word(uint32_t x, uint32_t (&d)[4]) {
+    const uint32_t y = x >> 8;
+    d[0] = x & 0x000f000fu;
+    d[1] = x & 0x00f000f0u;
+    d[2] = y & 0x000f000fu;
+    d[3] = y & 0x00f000f0u;
 }
 __device__ __forceinline__ float ex2f(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
 
-// One item's share of the work, as a CTA finds it.
-struct Piece { int t, i, k0, k1; bool whole; };
-
-// The heads' softmax state and sums of a warp, in the layout of the accumulators: this lane's columns are heads 2 (lane % 4) and the next one, of eight, or of four
-// high parts and four low parts.
+// The heads' softmax state and sums of a warp, in the layout of the accumulators: this lane's columns are heads 2 (lane % 4) and the next one, modulo 4 where there are
+// up to four. o is in units of 2^-24 f (odd j: 16 times that); f, a power of two, brings the largest weight so far, wref, to 2^7 .. 2^8.
 template <int D>
 struct WarpState {
     static constexpr int NG = D / kGroup;
-    float o[NG][4][4], oz[NG][2], m[2], l[2];
+    float o[NG][4][4], oz[NG][2], f[NG][2], wref[NG][2], m[2], l[2];
     uint32_t q[NG][4][2];
-    float qsum[NG][2];
+    float qsum[NG][2], scale[2];
 };
 
-// 32 keys of a stage. kOdd: some scale is not finite; a head that does not keep the key is to get nothing of it.
-template <int D, int kH, bool kOdd>
-__device__ __forceinline__ void attend(WarpState<D>& W, const uint8_t* data, const float (*bias)[AttnShape<D, kH>::kCols], float scale) {
+// 32 keys of a stage. odd (of the warp): some scale is not finite; a head that does not keep the key is to get nothing of it. One instance of this code per kernel:
+// with six, warps waited for instructions two thirds of the time.
+template <int D, int kH>
+__device__ __forceinline__ void attend(WarpState<D>& W, const uint8_t* data, const float (*bias)[AttnShape<D, kH>::kCols], bool odd) {
     using Sh = AttnShape<D, kH>;
-    constexpr int NG = D / kGroup, kPitch = Sh::kPitch;
+    constexpr int NG = D / kGroup, kPitch = Sh::kPitch, kSets = kH <= 4 ? 1 : 2;       // sets of 16 keys by 8 columns that a lane takes through the softmax
     const int lane = threadIdx.x & 31, r = lane >> 2, t = lane & 3, kr = r ^ (r >> 2 & 1), col = (2 * t) % Sh::kCols;
-    float x[2][4];
-    uint32_t sv[2][2][NG];                                        // V's pairs of keys r and r + 8 of both tiles
+    float c[kSets][NG][4];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint8_t* ka = data + (16 * i + kr) * kPitch;
+    for (int g = 0; g < NG; ++g) {
+        float two[2][4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint8_t* ka = data + (16 * i + kr) * kPitch + g * 32 + t * 8;
+            const uint2 a = *reinterpret_cast<const uint2*>(ka), b = *reinterpret_cast<const uint2*>(ka + 8 * kPitch);
+            uint32_t a0[4], a1[4], a2[4], a3[4];
+            expand_word(a.x, a0);
+            expand_word(b.x, a1);
+            expand_word(a.y, a2);
+            expand_word(b.y, a3);
+            two[i][0] = two[i][1] = two[i][2] = two[i][3] = 0.0f;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) mma16816(two[i], a0[s], a1[s], a2[s], a3[s], W.q[g][s][0], W.q[g][s][1]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (kSets == 1) c[0][g][e] = t < 2 ? two[0][e] : two[1][e];
+            else { c[0][g][e] = two[0][e]; c[1][g][e] = two[1][e]; }
+        }
+    }
+    float x[kSets][4];
+    uint32_t sv[kSets][2][NG];                                    // V's pairs of the lane's keys
+#pragma unroll
+    for (int i = 0; i < kSets; ++i) {
+        const int key = 16 * (kSets == 1 ? t >> 1 : i) + kr;
+        const uint8_t* ka = data + key * kPitch + D;
         const uint8_t* kb = ka + 8 * kPitch;
         uint32_t pa[2 * NG], pb[2 * NG];
         if constexpr (NG == 2) {
-            const uint4 a = *reinterpret_cast<const uint4*>(ka + D), b = *reinterpret_cast<const uint4*>(kb + D);
+            const uint4 a = *reinterpret_cast<const uint4*>(ka), b = *reinterpret_cast<const uint4*>(kb);
             pa[0] = a.x; pa[1] = a.y; pa[2] = a.z; pa[3] = a.w;
             pb[0] = b.x; pb[1] = b.y; pb[2] = b.z; pb[3] = b.w;
         } else {
-            const uint2 a = *reinterpret_cast<const uint2*>(ka + D), b = *reinterpret_cast<const uint2*>(kb + D);
+            const uint2 a = *reinterpret_cast<const uint2*>(ka), b = *reinterpret_cast<const uint2*>(kb);
             pa[0] = a.x; pa[1] = a.y;
             pb[0] = b.x; pb[1] = b.y;
         }
         float dot[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-            const uint2 a = *reinterpret_cast<const uint2*>(ka + g * 32 + t * 8), b = *reinterpret_cast<const uint2*>(kb + g * 32 + t * 8);
-            float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int s = 0; s < 4; ++s)
-                mma16816(c, codes_bf16<0>(a.x >> (4 * s)), codes_bf16<0>(b.x >> (4 * s)), codes_bf16<0>(a.y >> (4 * s)), codes_bf16<0>(b.y >> (4 * s)), W.q[g][s][0], W.q[g][s][1]);
             const float sa = pair_s(pa[g]), za = pair_z(pa[g]), sb = pair_s(pb[g]), zb = pair_z(pb[g]);
-            dot[0] = fmaf(sa, c[0], fmaf(za, W.qsum[g][0], dot[0]));
-            dot[1] = fmaf(sa, c[1], fmaf(za, W.qsum[g][1], dot[1]));
-            dot[2] = fmaf(sb, c[2], fmaf(zb, W.qsum[g][0], dot[2]));
-            dot[3] = fmaf(sb, c[3], fmaf(zb, W.qsum[g][1], dot[3]));
+            dot[0] = fmaf(sa, c[i][g][0], fmaf(za, W.qsum[g][0], dot[0]));
+            dot[1] = fmaf(sa, c[i][g][1], fmaf(za, W.qsum[g][1], dot[1]));
+            dot[2] = fmaf(sb, c[i][g][2], fmaf(zb, W.qsum[g][0], dot[2]));
+            dot[3] = fmaf(sb, c[i][g][3], fmaf(zb, W.qsum[g][1], dot[3]));
             sv[i][0][g] = pa[NG + g];
             sv[i][1][g] = pb[NG + g];
         }
-        const float2 ba = *reinterpret_cast<const float2*>(&bias[16 * i + kr][col]), bb = *reinterpret_cast<const float2*>(&bias[16 * i + 8 + kr][col]);
-        x[i][0] = fmaf(dot[0], scale, ba.x);
-        x[i][1] = fmaf(dot[1], scale, ba.y);
-        x[i][2] = fmaf(dot[2], scale, bb.x);
-        x[i][3] = fmaf(dot[3], scale, bb.y);
-        if (kOdd) {                                               // (values of a group without finite scale are NaN, or infinities of both signs)
+        const float2 ba = *reinterpret_cast<const float2*>(&bias[key][col]), bb = *reinterpret_cast<const float2*>(&bias[key + 8][col]);
+        x[i][0] = fmaf(dot[0], W.scale[0], ba.x);
+        x[i][1] = fmaf(dot[1], W.scale[1], ba.y);
+        x[i][2] = fmaf(dot[2], W.scale[0], bb.x);
+        x[i][3] = fmaf(dot[3], W.scale[1], bb.y);
+        if (odd) {                                                // (values of a group without finite scale are NaN, or infinities of both signs)
             bool na = false, nb = false;
 #pragma unroll
             for (int g = 0; g < NG; ++g) { na = na || odd_pair(pa[g]); nb = nb || odd_pair(pb[g]); }
@@ -604,67 +628,103 @@ __device__ __forceinline__ void attend(WarpState<D>& W, const uint8_t* data, con
             x[i][3] = bb.y == -INFINITY ? -INFINITY : nb ? NAN : x[i][3];
         }
     }
-    // The maximum that the exponentials refer to moves only when it is passed by more than 5: p stays below e^5, and the sums are rescaled rarely.
-    float mx[2] = {fmaxf(fmaxf(x[0][0], x[0][2]), fmaxf(x[1][0], x[1][2])), fmaxf(fmaxf(x[0][1], x[0][3]), fmaxf(x[1][1], x[1][3]))};
-    if (__any_sync(0xffffffffu, mx[0] > W.m[0] + 5.0f || mx[1] > W.m[1] + 5.0f)) {
+    // Over the lanes that hold the same head's other keys
+    auto over_keys = [&](float v) {
+#pragma unroll
+        for (int o = kSets == 1 ? 2 : 4; o < 32; o <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+        return v;
+    };
+    // The maximum that the exponentials refer to moves only when it is passed by more than 5, and the weights' power of two when one of them would pass 2^15: the sums
+    // are rescaled rarely.
+    float mx[2] = {fmaxf(x[0][0], x[0][2]), fmaxf(x[0][1], x[0][3])};
+    if constexpr (kSets == 2) {
+        mx[0] = fmaxf(mx[0], fmaxf(x[1][0], x[1][2]));
+        mx[1] = fmaxf(mx[1], fmaxf(x[1][1], x[1][3]));
+    }
+    bool move = __any_sync(0xffffffffu, mx[0] > W.m[0] + 5.0f || mx[1] > W.m[1] + 5.0f);
+    float fade[2] = {1.0f, 1.0f};
+    if (move) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-#pragma unroll
-            for (int o = 4; o < 32; o <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], o));
-            const float top = fmaxf(W.m[e], mx[e]), f = ex2f((W.m[e] - top) * kLog2e);
+            const float top = fmaxf(W.m[e], over_keys(mx[e]));
+            fade[e] = ex2f((W.m[e] - top) * kLog2e);
             W.m[e] = top;
-            W.l[e] *= f;
+            W.l[e] *= fade[e];
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                W.oz[g][e] *= f;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) { W.o[g][j][e] *= f; W.o[g][j][e + 2] *= f; }
-            }
+            for (int g = 0; g < NG; ++g) W.oz[g][e] *= fade[e];
         }
     }
+    float w[kSets][NG][4];
+    float most = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kSets; ++i) {
         float p[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) p[e] = ex2f((x[i][e] - W.m[e & 1]) * kLog2e);
         W.l[0] += p[0] + p[2];
         W.l[1] += p[1] + p[3];
-        const int ra = (2 * t) ^ (t >> 1);                        // the row of operand key 2t; key 2t + 1 lies in the other row of the pair
-        const uint8_t* vrow = data + (16 * i + ra) * kPitch + D / 2 + 4 * r;
-        const int other = (t >> 1) ? -kPitch : kPitch;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-            const float sa = pair_s(sv[i][0][g]), za = fmaf(8.0f, sa, pair_z(sv[i][0][g])), sb = pair_s(sv[i][1][g]), zb = fmaf(8.0f, sb, pair_z(sv[i][1][g]));
-            float w[4] = {p[0] * sa, p[1] * sa, p[2] * sb, p[3] * sb};
-            if (kOdd) {
-                const bool k[4] = {x[i][0] != -INFINITY, x[i][1] != -INFINITY, x[i][2] != -INFINITY, x[i][3] != -INFINITY};
+            const float sa = pair_s(sv[i][0][g]), za = pair_z(sv[i][0][g]), sb = pair_s(sv[i][1][g]), zb = pair_z(sv[i][1][g]);
+            w[i][g][0] = p[0] * sa; w[i][g][1] = p[1] * sa; w[i][g][2] = p[2] * sb; w[i][g][3] = p[3] * sb;
+            float z[4] = {p[0] * za, p[1] * za, p[2] * zb, p[3] * zb};
+            if (odd) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w[e] = k[e] ? w[e] : 0.0f;
-                W.oz[g][0] += (k[0] ? p[0] * za : 0.0f) + (k[2] ? p[2] * zb : 0.0f);
-                W.oz[g][1] += (k[1] ? p[1] * za : 0.0f) + (k[3] ? p[3] * zb : 0.0f);
-            } else {
-                W.oz[g][0] = fmaf(p[0], za, fmaf(p[2], zb, W.oz[g][0]));
-                W.oz[g][1] = fmaf(p[1], za, fmaf(p[3], zb, W.oz[g][1]));
+                for (int e = 0; e < 4; ++e)
+                    if (x[i][e] == -INFINITY) w[i][g][e] = z[e] = 0.0f;
             }
-            // high parts: the upper halves as they are; low parts: what they leave
-            uint32_t hi0 = __byte_perm(__float_as_uint(w[0]), __float_as_uint(w[1]), 0x7632), hi1 = __byte_perm(__float_as_uint(w[2]), __float_as_uint(w[3]), 0x7632);
-            float lw[4];
+            W.oz[g][0] += z[0] + z[2];
+            W.oz[g][1] += z[1] + z[3];
+            most = fmaxf(most, fmaxf(fmaxf(w[i][g][0], w[i][g][2]) * W.f[g][0], fmaxf(w[i][g][1], w[i][g][3]) * W.f[g][1]));
+        }
+    }
+    move = move || __any_sync(0xffffffffu, most > 32768.0f);
+    if (move) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) lw[e] = w[e] - __uint_as_float(__float_as_uint(w[e]) & 0xffff0000u);
-            uint32_t lo0 = __byte_perm(__float_as_uint(lw[0]), __float_as_uint(lw[1]), 0x7632), lo1 = __byte_perm(__float_as_uint(lw[2]), __float_as_uint(lw[3]), 0x7632);
-            if (kH <= 4 && t >= 2) { hi0 = lo0; hi1 = lo1; }
-            const uint32_t b0 = turn8x8(hi0), b1 = turn8x8(hi1);
-            const uint32_t wa = *reinterpret_cast<const uint32_t*>(vrow + g * 32), wb = *reinterpret_cast<const uint32_t*>(vrow + g * 32 + other);
-            const uint32_t wc = *reinterpret_cast<const uint32_t*>(vrow + g * 32 + 8 * kPitch), wd = *reinterpret_cast<const uint32_t*>(vrow + g * 32 + 8 * kPitch + other);
-            const uint32_t x0 = __byte_perm(wa, wb, 0x5410), x1 = __byte_perm(wa, wb, 0x7632), y0 = __byte_perm(wc, wd, 0x5410), y1 = __byte_perm(wc, wd, 0x7632);
-            uint32_t c0 = 0u, c1 = 0u;
-            if constexpr (kH > 4) { c0 = turn8x8(lo0); c1 = turn8x8(lo1); }
+        for (int g = 0; g < NG; ++g)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t a0 = codes_bf16<8>(x0 >> (4 * j)), a1 = codes_bf16<8>(x1 >> (4 * j)), a2 = codes_bf16<8>(y0 >> (4 * j)), a3 = codes_bf16<8>(y1 >> (4 * j));
-                mma16816(W.o[g][j], a0, a1, a2, a3, b0, b1);
-                if constexpr (kH > 4) mma16816(W.o[g][j], a0, a1, a2, a3, c0, c1);
+            for (int e = 0; e < 2; ++e) {
+                float top = fmaxf(w[0][g][e], w[0][g][e + 2]);
+                if constexpr (kSets == 2) top = fmaxf(top, fmaxf(w[1][g][e], w[1][g][e + 2]));
+                top = fmaxf(over_keys(top), W.wref[g][e] * fade[e]);
+                W.wref[g][e] = top;
+                const int up = 7 + 127 - (int)(__float_as_uint(top) >> 23);
+                const float f = top > 0.0f ? __uint_as_float((uint32_t)(127 + max(-126, min(up, 126))) << 23) : W.f[g][e];
+                // (what fades to nothing has no factor: the ratio of the powers may be any)
+                const float by = fade[e] == 0.0f ? 0.0f : fade[e] * (f / W.f[g][e]);
+                W.f[g][e] = f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { W.o[g][j][e] *= by; W.o[g][j][e + 2] *= by; }
             }
+    }
+    const int ra = (2 * t) ^ (t >> 1), other = (t >> 1) ? -kPitch : kPitch;       // the row of operand key 2t; key 2t + 1 lies in the other row of the pair
+    const uint8_t* vrow = data + ra * kPitch + D / 2 + 4 * r;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+        uint32_t b[2][2];
+#pragma unroll
+        for (int i = 0; i < kSets; ++i) {
+            b[i][0] = turn8x8(halves(w[i][g][0] * W.f[g][0], w[i][g][1] * W.f[g][1]));
+            b[i][1] = turn8x8(halves(w[i][g][2] * W.f[g][0], w[i][g][3] * W.f[g][1]));
+        }
+        if constexpr (kSets == 1) {                               // (columns 0 to 3 hold the first 16 keys' weights, 4 to 7 the others': zeros for the other product)
+            b[1][0] = lane < 16 ? 0u : b[0][0];
+            b[1][1] = lane < 16 ? 0u : b[0][1];
+            b[0][0] = lane < 16 ? b[0][0] : 0u;
+            b[0][1] = lane < 16 ? b[0][1] : 0u;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint8_t* v = vrow + 16 * i * kPitch + g * 32;
+            const uint32_t wa = *reinterpret_cast<const uint32_t*>(v), wb = *reinterpret_cast<const uint32_t*>(v + other);
+            const uint32_t wc = *reinterpret_cast<const uint32_t*>(v + 8 * kPitch), wd = *reinterpret_cast<const uint32_t*>(v + 8 * kPitch + other);
+            uint32_t a0[4], a1[4], a2[4], a3[4];
+            expand_word(__byte_perm(wa, wb, 0x5410), a0);
+            expand_word(__byte_perm(wa, wb, 0x7632), a1);
+            expand_word(__byte_perm(wc, wd, 0x5410), a2);
+            expand_word(__byte_perm(wc, wd, 0x7632), a3);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mma16816(W.o[g][j], a0[j], a1[j], a2[j], a3[j], b[i][0], b[i][1]);
         }
     }
 }
@@ -752,30 +812,57 @@ __global__ void __launch_bounds__(kThreads, 4) attn_kernel(AttnArgs A) {
         WarpState<D> W;
         {
             const int h = r % kCols;
+            uint4 raw[NG][2];
+            uint32_t big = 0u;
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-                uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
+                raw[g][0] = raw[g][1] = make_uint4(0u, 0u, 0u, 0u);
                 if (h < heads) {
                     const uint4* src = reinterpret_cast<const uint4*>(A.q + t * A.qs_row + (h0 + h) * A.qs_head + g * kGroup + t4 * 16);
-                    a = src[0];
-                    b = src[1];
+                    raw[g][0] = src[0];
+                    raw[g][1] = src[1];
                 }
-                W.q[g][0][0] = __byte_perm(a.x, a.z, 0x5410); W.q[g][1][0] = __byte_perm(a.x, a.z, 0x7632);
-                W.q[g][2][0] = __byte_perm(a.y, a.w, 0x5410); W.q[g][3][0] = __byte_perm(a.y, a.w, 0x7632);
-                W.q[g][0][1] = __byte_perm(b.x, b.z, 0x5410); W.q[g][1][1] = __byte_perm(b.x, b.z, 0x7632);
-                W.q[g][2][1] = __byte_perm(b.y, b.w, 0x5410); W.q[g][3][1] = __byte_perm(b.y, b.w, 0x7632);
-                float sum = 0.0f;
-                const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum += __uint_as_float(w[e] << 16) + __uint_as_float(w[e] & 0xffff0000u);
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t v[4] = {raw[g][e].x, raw[g][e].y, raw[g][e].z, raw[g][e].w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) big = max(big, max(v[k] & 0x7fff0000u, v[k] << 16 & 0x7fff0000u));
+                }
+            }
+            big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
+            big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
+            // the head's power of two brings its largest channel to 2^14 .. 2^15
+            const int up = max(-113, min(100, 127 + 14 - (int)(big >> 23)));
+            const float k = __uint_as_float((uint32_t)(127 + up) << 23), even = k, odd_k = k * 0.0625f;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t v[4] = {raw[g][e].x, raw[g][e].y, raw[g][e].z, raw[g][e].w};
+                    float ch[8];
+#pragma unroll
+                    for (int n8 = 0; n8 < 4; ++n8) { ch[2 * n8] = __uint_as_float(v[n8] << 16); ch[2 * n8 + 1] = __uint_as_float(v[n8] & 0xffff0000u); }
+#pragma unroll
+                    for (int n8 = 0; n8 < 8; ++n8) sum += ch[n8];
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) W.q[g][s][e] = halves(ch[s] * (s & 1 ? odd_k : even), ch[s + 4] * (s & 1 ? odd_k : even));
+                }
                 sum += __shfl_xor_sync(0xffffffffu, sum, 1);
                 sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                // (in the products' units: codes 2^-24, queries k)
+                sum *= k * 0x1p-24f;
                 W.qsum[g][0] = __shfl_sync(0xffffffffu, sum, 8 * t4);
                 W.qsum[g][1] = __shfl_sync(0xffffffffu, sum, 8 * t4 + 4);
                 W.oz[g][0] = W.oz[g][1] = 0.0f;
+                W.f[g][0] = W.f[g][1] = 1.0f;
+                W.wref[g][0] = W.wref[g][1] = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) W.o[g][j][0] = W.o[g][j][1] = W.o[g][j][2] = W.o[g][j][3] = 0.0f;
             }
+            const float unit = A.scale / k * 0x1p24f;
+            W.scale[0] = __shfl_sync(0xffffffffu, unit, 8 * t4);
+            W.scale[1] = __shfl_sync(0xffffffffu, unit, 8 * t4 + 4);
             W.m[0] = W.m[1] = -3.4e38f;
             W.l[0] = W.l[1] = 0.0f;
         }
@@ -802,26 +889,6 @@ __global__ void __launch_bounds__(kThreads, 4) attn_kernel(AttnArgs A) {
 #pragma unroll
                 for (int e = 0; e < kCols; ++e) S.bias[ring][lane][e] = -INFINITY;
             }
-            cp_commit();
-        };
-        auto use = [&](int batch) {                               // (its copies have arrived)
-            __syncwarp();
-            const uint8_t* data = S.data[batch % kStages];
-            bool odd = false;
-            const uint32_t* p = reinterpret_cast<const uint32_t*>(data + lane * kPitch + D);
-#pragma unroll
-            for (int e = 0; e < D / 32; ++e) odd |= odd_pair(p[e]);
-            if (__any_sync(0xffffffffu, odd)) attend<D, kH, true>(W, data, S.bias[batch % kRing], A.scale);
-            else attend<D, kH, false>(W, data, S.bias[batch % kRing], A.scale);
-            __syncwarp();
-        };
-        auto step = [&]() {                                       // requests the next batch, then attends to the one before
-            __syncwarp();
-            gather(issued++);
-            if (issued - used == kStages) {
-                cp_wait<kStages - 1>();
-                use(used++);
-            }
         };
         // 64 keys per turn: lane's pair of neighbouring keys, in every head; the next turn's weights are requested before this one's are tested
         float2 dl[kH];
@@ -842,16 +909,20 @@ __global__ void __launch_bounds__(kThreads, 4) attn_kernel(AttnArgs A) {
         next_page = page_of(j0 + 2 * lane);
         request(j0 + 2 * lane, next_page);
         int after = page_of(j0 + kWarps * 64 + 2 * lane);
-        for (int j = j0; j < k1; j += kWarps * 64) {
-            page = next_page;
+        int j = j0, half = 0;
+        while (true) {
+            // keys are queued until a batch is full
+            while (j < k1 && tail - issued * kBatch < kBatch) {
+                if (half == 0) {
+                    __syncwarp();
+                    page = next_page;
 #pragma unroll
-            for (int h = 0; h < kH; ++h) *reinterpret_cast<float2*>(&S.delta[h][2 * lane]) = dl[h];
-            __syncwarp();
-            next_page = after;
-            request(j + kWarps * 64 + 2 * lane, next_page);
-            after = page_of(j + 2 * kWarps * 64 + 2 * lane);
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
+                    for (int h = 0; h < kH; ++h) *reinterpret_cast<float2*>(&S.delta[h][2 * lane]) = dl[h];
+                    __syncwarp();
+                    next_page = after;
+                    request(j + kWarps * 64 + 2 * lane, next_page);
+                    after = page_of(j + 2 * kWarps * 64 + 2 * lane);
+                }
                 const int key = j + 32 * half + lane, p = __shfl_sync(0xffffffffu, page, 16 * half + lane / 2);
                 float b[kCols];
                 bool any = false;
@@ -874,19 +945,34 @@ __global__ void __launch_bounds__(kThreads, 4) attn_kernel(AttnArgs A) {
                     if constexpr (kCols == 8) dst[1] = make_float4(b[4], b[5], b[6], b[7]);
                 }
                 tail += __popc(ballot);
-                if (tail - issued * kBatch >= kBatch) step();
+                half ^= 1;
+                if (half == 0) j += kWarps * 64;
             }
+            // the next batch is requested, the one before it is used; behind the last one an empty group keeps the count
+            const bool more = tail > issued * kBatch;
+            if (!more && used == issued) break;
             __syncwarp();
+            if (more) gather(issued++);
+            cp_commit();
+            if (issued - used == kStages || !more) {
+                cp_wait<kStages - 1>();
+                __syncwarp();
+                const uint8_t* data = S.data[used % kStages];
+                bool odd = false;
+                const uint32_t* sc = reinterpret_cast<const uint32_t*>(data + lane * kPitch + D);
+#pragma unroll
+                for (int e = 0; e < D / 32; ++e) odd |= odd_pair(sc[e]);
+                attend<D, kH>(W, data, S.bias[used % kRing], __any_sync(0xffffffffu, odd));
+                __syncwarp();
+                ++used;
+            }
         }
-        if (tail > issued * kBatch) step();
-        cp_wait<0>();
-        while (used < issued) use(used++);
 
-        // the warp's sums: keys of one residue per lane row; then low parts to the high ones
+        // the warp's sums: over the lanes that hold a head's other keys
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
 #pragma unroll
-            for (int o = 4; o < 32; o <<= 1) {
+            for (int o = kH <= 4 ? 2 : 4; o < 32; o <<= 1) {
                 W.l[e] += __shfl_xor_sync(0xffffffffu, W.l[e], o);
 #pragma unroll
                 for (int g = 0; g < NG; ++g) W.oz[g][e] += __shfl_xor_sync(0xffffffffu, W.oz[g][e], o);
@@ -896,14 +982,18 @@ __global__ void __launch_bounds__(kThreads, 4) attn_kernel(AttnArgs A) {
 #pragma unroll
         for (int g = 0; g < NG; ++g)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int e = 0; e < 4; ++e) {
+                const float unit = 0x1p24f / W.f[g][e & 1];
+                float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float v = W.o[g][j][e];
-                    if (kH <= 4) v += __shfl_xor_sync(0xffffffffu, v, 2);
-                    const int h = 2 * t4 + (e & 1), c = g * kGroup + 8 * r + 4 * (e >> 1) + j;
-                    if (h < kCols) M.o[warp][h][c] = v + W.oz[g][e & 1];
+                for (int j = 0; j < 4; ++j) {
+                    v[j] = W.o[g][j][e] * (j & 1 ? unit * 0.0625f : unit);
+                    if (kH <= 4) v[j] += __shfl_xor_sync(0xffffffffu, v[j], 2);
+                    v[j] += W.oz[g][e & 1];
                 }
+                const int h = 2 * t4 + (e & 1), c = g * kGroup + 8 * r + 4 * (e >> 1);
+                if (h < kCols) *reinterpret_cast<float4*>(&M.o[warp][h][c]) = make_float4(v[0], v[1], v[2], v[3]);
+            }
         if (r == 0 && 2 * t4 < kCols) {
             sM[warp][2 * t4] = W.m[0]; sM[warp][2 * t4 + 1] = W.m[1];
             sL[warp][2 * t4] = W.l[0]; sL[warp][2 * t4 + 1] = W.l[1];

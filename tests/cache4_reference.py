@@ -76,14 +76,14 @@ def plan(lens, want, table, ring, pool, page, max_blocks, rows):
 
 def decode(q, K, V, delta, w, scale):
     """One row over the keys that it sees: q [Hq, d], K, V [n, Hkv, d], delta [Hq, n] fp32, `there` already applied. Returns (o [Hq, d], lse [Hq], and per head
-    what its tolerances are made of: kept keys, largest |score term|, sum of p |v| per channel)."""
+    what its tolerances are made of: kept keys, largest |score term|, sums of p |v| and of p (v - the smallest value of v's group) per channel)."""
     Hq, d = q.shape
     n, G = K.shape[0], Hq // K.shape[1]
     o, lse, parts = np.zeros((Hq, d)), np.full(Hq, -np.inf), []
     for h in range(Hq):
         best = sorted(range(n), key=lambda j: (-float(delta[h, j]), j))[:w]
         if not best:
-            parts.append((0, 0.0, np.zeros(d)))
+            parts.append((0, 0.0, np.zeros(d), np.zeros(d)))
             continue
         k, v, b = K[best, h // G], V[best, h // G], delta[h, best].astype(np.float64)
         s = k @ q[h] * scale + b
@@ -92,5 +92,6 @@ def decode(q, K, V, delta, w, scale):
         lse[h] = top + np.log(p.sum())
         p /= p.sum()
         o[h] = p @ v
-        parts.append((len(best), float((np.abs(k) @ np.abs(q[h]) * scale + np.abs(b)).max()), p @ np.abs(v)))
+        low = np.repeat(v.reshape(len(best), -1, GROUP).min(-1), GROUP, -1)
+        parts.append((len(best), float((np.abs(k) @ np.abs(q[h]) * scale + np.abs(b)).max()), p @ np.abs(v), p @ (v - low)))
     return o, lse, parts

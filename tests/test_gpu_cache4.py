@@ -271,13 +271,14 @@ def filled(c, codes, scales, delta, seed, gate=0.25, ties=False, offset=0.0):
 
 def tolerances(parts, lse, dtype):
     """Per head (o [d], lse). Rounding errors, with u the fp32 half step 2^-24: a score is a sum of d products and a few more operations, at most (d + 8) u of the sum
-    of its terms' magnitudes (`big`); the running maximum's, exponentials' and sums' part is (n + 64) u of a sum of n terms; bf16 weights: p s is split into two
-    truncated bf16 numbers, at most 2^-14 of it lost. The output's own rounding is added by the caller."""
+    of its terms' magnitudes (`big`); the running maximum's, exponentials' and sums' part is (n + 64) u of a sum of n terms. The bf16 kernel multiplies codes by weights
+    p s rounded to halves: o = sum p z + sum half(p s) n, and half(x) is x within finfo(float16).eps / 2 = 2^-11 of it, so the second sum is off by at most
+    2^-11 sum p s n = 2^-11 sum p (v - z); a group's zero z is its smallest value (its smallest code is 0). The output's own rounding is added by the caller."""
     u = 2.0 ** -24
     tol = []
-    for n, big, pv in parts:
+    for n, big, pv, above in parts:
         e = (128 + 8) * u * big
-        tol.append(((2 * e + (n + 64) * u + (2.0 ** -14 if dtype == torch.bfloat16 else 0.0)) * pv, e + (n + 64) * u))
+        tol.append(((2 * e + (n + 64) * u) * pv + (torch.finfo(torch.float16).eps / 2 * above if dtype == torch.bfloat16 else 0.0), e + (n + 64) * u))
     return tol
 
 
