@@ -90,8 +90,16 @@ __device__ unsigned long long radix_select(RadixShared& S, Load&& load, int n, i
     return order_key(u_lo, j_lo);
 }
 
-// What every row's attention is cut by: units of keys, dealt out to the CTAs in equal shares. ustart[t]: units before row t, over all its `per_row` items.
-struct Plan { int32_t* ustart; int32_t* tickets; int per_row, unit_log; };
+// What every row's attention is cut by: units of about the same work, dealt out to the CTAs in equal shares. ustart[t]: units before row t, over all its
+// `per_row` items. A key costs its test, and its expansion where some head of the group keeps it; the heads' kept keys are taken to be independent.
+// (By keys alone, rows that keep all theirs took up to twice a long row's time.)
+struct Plan { int32_t* ustart; int32_t* tickets; int per_row, unit_log, heads, w; };
+__device__ __forceinline__ int row_units(const Plan& P, int n) {
+    if (n < 0) return 0;
+    const float drop = n > P.w ? 1.0f - (float)P.w / (float)n : 0.0f, all = n > P.w ? 1.0f - powf(drop, (float)P.heads) : 1.0f;
+    // (the fixed cost of an item, its queries and its end, is about that of a unit)
+    return (int)ceilf((float)n * (0.15f + 0.85f * all) / (float)(1 << P.unit_log)) + 1;
+}
 
 template <int NT>
 __device__ void make_plan(const Rows& R, int rows, const Plan& P) {
@@ -103,8 +111,7 @@ __device__ void make_plan(const Rows& R, int rows, const Plan& P) {
         int r, units = 0;
         if (t < rows) {
             const int n = R.visible(t, r);
-            // (an item's fixed cost, its queries and its end, is about that of a unit)
-            units = n < 0 ? 0 : (((n + (1 << P.unit_log) - 1) >> P.unit_log) + 1) * P.per_row;
+            units = row_units(P, n) * P.per_row;
         }
         int x = units;
 #pragma unroll
@@ -497,7 +504,8 @@ __global__ void __launch_bounds__(D) simt_combine_kernel(Rows R, const float* pa
 //            With up to four heads the operand's columns 4 to 7 hold the same heads again, and their lanes take the second 16 keys through the softmax.
 // (tcgen05 needs 64 rows of A at least, of which a decoding step has the group's 1 to 8 heads or, turned around, the keys: then the expanded codes would
 // have to go through shared memory once more. mma.sync takes them from the registers that the expansion leaves them in, and its rate is not what bounds this kernel.)
-constexpr int kWarps = 4, kThreads = 32 * kWarps, kBatch = 32, kStages = 2, kRing = kStages + 1;
+constexpr int kWarps = 4, kThreads = 32 * kWarps, kBatch = 32, kStages = 2;
+constexpr int kRing = 4 * kBatch;           // queue: a batch that is on its way, one that is full, and what a turn's 64 keys may add
 template <int D, int kH>
 struct AttnShape {
     static constexpr int kCols = kH <= 4 ? 4 : 8;                 // heads with a bias slot
@@ -505,11 +513,11 @@ struct AttnShape {
     static constexpr int kPitch = D == 128 ? 160 : 96;            // a key's codes and scales; 32 modulo 128: the rows of a fragment meet every bank once
     struct alignas(16) Warp {
         uint8_t data[kStages][kBatch * kPitch];
-        float bias[kRing][kBatch][kCols];
-        size_t row[kRing][kBatch];
-        float delta[kH][64];
+        float bias[kRing][kCols];
+        size_t off[kRing];                                        // the key's codes, in bytes from the pool's first
     };
     struct Merge { float o[kWarps][kCols][D]; };
+    using Query = uint2[NG][4][32];                               // operand fragments, the same for every warp
     static constexpr size_t kBytes = sizeof(Warp) * kWarps > sizeof(Merge) ? sizeof(Warp) * kWarps : sizeof(Merge);
 };
 constexpr int kAttnCtas = 4 * 148;
@@ -551,14 +559,13 @@ template <int D>
 struct WarpState {
     static constexpr int NG = D / kGroup;
     float o[NG][4][4], oz[NG][2], f[NG][2], wref[NG][2], m[2], l[2];
-    uint32_t q[NG][4][2];
     float qsum[NG][2], scale[2];
 };
 
 // 32 keys of a stage. odd (of the warp): some scale is not finite; a head that does not keep the key is to get nothing of it. One instance of this code per kernel:
 // with six, warps waited for instructions two thirds of the time.
 template <int D, int kH>
-__device__ __forceinline__ void attend(WarpState<D>& W, const uint8_t* data, const float (*bias)[AttnShape<D, kH>::kCols], bool odd) {
+__device__ __forceinline__ void attend(WarpState<D>& W, const typename AttnShape<D, kH>::Query& q, const uint8_t* data, const float (*bias)[AttnShape<D, kH>::kCols], bool odd) {
     using Sh = AttnShape<D, kH>;
     constexpr int NG = D / kGroup, kPitch = Sh::kPitch, kSets = kH <= 4 ? 1 : 2;       // sets of 16 keys by 8 columns that a lane takes through the softmax
     const int lane = threadIdx.x & 31, r = lane >> 2, t = lane & 3, kr = r ^ (r >> 2 & 1), col = (2 * t) % Sh::kCols;
@@ -566,6 +573,9 @@ __device__ __forceinline__ void attend(WarpState<D>& W, const uint8_t* data, con
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
         float two[2][4];
+        uint2 qf[4];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) qf[s] = q[g][s][lane];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint8_t* ka = data + (16 * i + kr) * kPitch + g * 32 + t * 8;
@@ -577,7 +587,7 @@ __device__ __forceinline__ void attend(WarpState<D>& W, const uint8_t* data, con
             expand_word(b.y, a3);
             two[i][0] = two[i][1] = two[i][2] = two[i][3] = 0.0f;
 #pragma unroll
-            for (int s = 0; s < 4; ++s) mma16816(two[i], a0[s], a1[s], a2[s], a3[s], W.q[g][s][0], W.q[g][s][1]);
+            for (int s = 0; s < 4; ++s) mma16816(two[i], a0[s], a1[s], a2[s], a3[s], qf[s].x, qf[s].y);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -667,14 +677,17 @@ __device__ __forceinline__ void attend(WarpState<D>& W, const uint8_t* data, con
         for (int g = 0; g < NG; ++g) {
             const float sa = pair_s(sv[i][0][g]), za = pair_z(sv[i][0][g]), sb = pair_s(sv[i][1][g]), zb = pair_z(sv[i][1][g]);
             w[i][g][0] = p[0] * sa; w[i][g][1] = p[1] * sa; w[i][g][2] = p[2] * sb; w[i][g][3] = p[3] * sb;
-            float z[4] = {p[0] * za, p[1] * za, p[2] * zb, p[3] * zb};
             if (odd) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (x[i][e] == -INFINITY) w[i][g][e] = z[e] = 0.0f;
+                for (int e = 0; e < 4; ++e) {
+                    const bool kept = x[i][e] != -INFINITY;
+                    w[i][g][e] = kept ? w[i][g][e] : 0.0f;
+                    W.oz[g][e & 1] += kept ? p[e] * (e < 2 ? za : zb) : 0.0f;
+                }
+            } else {
+                W.oz[g][0] = fmaf(p[0], za, fmaf(p[2], zb, W.oz[g][0]));
+                W.oz[g][1] = fmaf(p[1], za, fmaf(p[3], zb, W.oz[g][1]));
             }
-            W.oz[g][0] += z[0] + z[2];
-            W.oz[g][1] += z[1] + z[3];
             most = fmaxf(most, fmaxf(fmaxf(w[i][g][0], w[i][g][2]) * W.f[g][0], fmaxf(w[i][g][1], w[i][g][3]) * W.f[g][1]));
         }
     }
@@ -765,6 +778,7 @@ __global__ void __launch_bounds__(kThreads, 4) attn_kernel(AttnArgs A) {
     constexpr int NG = Sh::NG, kCols = Sh::kCols, kPitch = Sh::kPitch;
     extern __shared__ __align__(16) uint8_t attn_smem[];
     __shared__ float sM[kWarps][kCols], sL[kWarps][kCols];
+    __shared__ typename Sh::Query sQ;
     __shared__ int sTicket;
     auto& M = *reinterpret_cast<typename Sh::Merge*>(attn_smem);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, t4 = lane & 3;
@@ -792,8 +806,10 @@ __global__ void __launch_bounds__(kThreads, 4) attn_kernel(AttnArgs A) {
             u1 = u0 + units;
             n = R.visible(t, seq);
             const int e = min(u1, until);
-            k0 = min((int64_t)n, (int64_t)(at - u0) << A.plan.unit_log);
-            k1 = min((int64_t)n, (int64_t)(e - u0) << A.plan.unit_log);
+            // units of 64 keys or a multiple, the last one of the item without any
+            const int span = (int)((((uint32_t)n + units - 2) / max(units - 1, 1) + 63) / 64 * 64);
+            k0 = min((int64_t)n, (int64_t)(at - u0) * span);
+            k1 = min((int64_t)n, (int64_t)(e - u0) * span);
             at = e;
         } else {
             t = cta / per_row;
@@ -837,6 +853,7 @@ __global__ void __launch_bounds__(kThreads, 4) attn_kernel(AttnArgs A) {
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
                 float sum = 0.0f;
+                uint32_t frag[4][2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const uint32_t v[4] = {raw[g][e].x, raw[g][e].y, raw[g][e].z, raw[g][e].w};
@@ -846,8 +863,11 @@ __global__ void __launch_bounds__(kThreads, 4) attn_kernel(AttnArgs A) {
 #pragma unroll
                     for (int n8 = 0; n8 < 8; ++n8) sum += ch[n8];
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) W.q[g][s][e] = halves(ch[s] * (s & 1 ? odd_k : even), ch[s + 4] * (s & 1 ? odd_k : even));
+                    for (int s = 0; s < 4; ++s) frag[s][e] = halves(ch[s] * (s & 1 ? odd_k : even), ch[s + 4] * (s & 1 ? odd_k : even));
                 }
+                if (warp == 0)
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) sQ[g][s][lane] = make_uint2(frag[s][0], frag[s][1]);
                 sum += __shfl_xor_sync(0xffffffffu, sum, 1);
                 sum += __shfl_xor_sync(0xffffffffu, sum, 2);
                 // (in the products' units: codes 2^-24, queries k)
@@ -866,87 +886,98 @@ __global__ void __launch_bounds__(kThreads, 4) attn_kernel(AttnArgs A) {
             W.m[0] = W.m[1] = -3.4e38f;
             W.l[0] = W.l[1] = 0.0f;
         }
-        for (int e = lane; e < kRing * kBatch * kCols; e += 32) (&S.bias[0][0][0])[e] = -INFINITY;
-        __syncwarp();
+        __syncthreads();                                          // (the queries; the last item's have been used)
 
-        int tail = 0, issued = 0, used = 0;                       // keys queued, batches requested, batches attended to
-        auto gather = [&](int batch) {                            // (the batch's rows and biases are in the ring)
-            const int ring = batch % kRing, count = min(kBatch, tail - batch * kBatch);
-            const uint32_t dst = (uint32_t)__cvta_generic_to_shared(S.data[batch % kStages]);
-            constexpr int kLanes = D / 16, kKeys = 32 / kLanes;   // lanes per key, keys per instruction
-#pragma unroll
-            for (int e = 0; e < kBatch; e += kKeys) {
-                const int key = e + lane / kLanes;
-                if (key < count) cp16(dst + key * kPitch + lane % kLanes * 16, A.codes + S.row[ring][key] * D + lane % kLanes * 16);
-            }
-            if (lane < count) {
-                const uint8_t* src = A.scales + S.row[ring][lane] * (D / 8);
-                if constexpr (D == 128) cp16(dst + lane * kPitch + D, src); else cp8(dst + lane * kPitch + D, src);
-            } else {                                              // places without a key: finite, and of no weight
-                uint32_t* p = reinterpret_cast<uint32_t*>(S.data[batch % kStages] + lane * kPitch + D);
+        // keys queued, batches requested, batches attended to
+        int tail = 0, issued = 0, used = 0;
+        const uint32_t page_bytes = (uint32_t)(A.Hkv << R.page_log) * D, head_bytes = (uint32_t)(hk << R.page_log) * D;       // (checked: fewer than 2^32)
+        constexpr int kLanes = D / 16, kKeys = 32 / kLanes;       // lanes per key, keys per instruction of a gather
+        const uint8_t* codes = A.codes + lane % kLanes * 16;
+        auto gather = [&](int batch) {
+            const int at = batch * kBatch % kRing, count = min(kBatch, tail - batch * kBatch);
+            uint8_t* to = S.data[batch % kStages];
+            const uint32_t dst = (uint32_t)__cvta_generic_to_shared(to);
+            const uint32_t dst_codes = dst + lane / kLanes * kPitch + lane % kLanes * 16;
+            if (count < kBatch && lane >= count) {                // places without a key: finite, and of no weight
+                S.off[at + lane] = S.off[at];
+                uint32_t* p = reinterpret_cast<uint32_t*>(to + lane * kPitch + D);
 #pragma unroll
                 for (int e = 0; e < D / 32; ++e) p[e] = 0u;
 #pragma unroll
-                for (int e = 0; e < kCols; ++e) S.bias[ring][lane][e] = -INFINITY;
+                for (int e = 0; e < kCols; ++e) S.bias[at + lane][e] = -INFINITY;
+            }
+            __syncwarp();
+#pragma unroll
+            for (int e = 0; e < kBatch; e += kKeys) cp16(dst_codes + e * kPitch, codes + S.off[at + e + lane / kLanes]);
+            if (lane < count) {
+                const uint8_t* src = A.scales + (S.off[at + lane] >> 3);          // (an eighth of the codes' bytes)
+                if constexpr (D == 128) cp16(dst + lane * kPitch + D, src); else cp8(dst + lane * kPitch + D, src);
             }
         };
-        // 64 keys per turn: lane's pair of neighbouring keys, in every head; the next turn's weights are requested before this one's are tested
-        float2 dl[kH];
-        int page = -1, next_page = -1;
+        // 64 keys per turn, a lane's two neighbouring keys in every head, requested kAhead turns before they are tested
+        constexpr int kAhead = kH <= 4 ? 2 : 1;
+        float2 dl[kAhead][kH];
+        int page[kAhead];
         auto page_of = [&](int j) {
             if (j >= k1) return -1;
             const int p = pages[j >> R.page_log];
             return (unsigned)p < (unsigned)R.num_pages ? p : -1;
         };
-        auto request = [&](int j, int p) {
+        const float* plane = R.delta + ((size_t)h0 << R.page_log);
+        auto request = [&](int a, int j, int p) {
+            page[a] = p;
+            const float* src = plane + (size_t)p * ((uint32_t)R.Hq << R.page_log) + (j & R.mask());
 #pragma unroll
             for (int h = 0; h < kH; ++h) {
-                dl[h] = make_float2(0.0f, 0.0f);
-                if (p >= 0 && h < heads) dl[h] = *reinterpret_cast<const float2*>(R.delta + (((size_t)p * R.Hq + h0 + h) << R.page_log) + (j & R.mask()));
+                dl[a][h] = make_float2(0.0f, 0.0f);
+                if (p >= 0 && h < heads) dl[a][h] = *reinterpret_cast<const float2*>(src + (h << R.page_log));
             }
         };
-        const int j0 = k0 + warp * 64;
-        next_page = page_of(j0 + 2 * lane);
-        request(j0 + 2 * lane, next_page);
-        int after = page_of(j0 + kWarps * 64 + 2 * lane);
-        int j = j0, half = 0;
+        int j = k0 + warp * 64;
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) request(a, j + a * kWarps * 64 + 2 * lane, page_of(j + a * kWarps * 64 + 2 * lane));
+        int after = page_of(j + kAhead * kWarps * 64 + 2 * lane);
         while (true) {
             // keys are queued until a batch is full
             while (j < k1 && tail - issued * kBatch < kBatch) {
-                if (half == 0) {
-                    __syncwarp();
-                    page = next_page;
+                const int key = j + 2 * lane;
+                float b[2][kCols];
+                bool any[2] = {false, false};
 #pragma unroll
-                    for (int h = 0; h < kH; ++h) *reinterpret_cast<float2*>(&S.delta[h][2 * lane]) = dl[h];
-                    __syncwarp();
-                    next_page = after;
-                    request(j + kWarps * 64 + 2 * lane, next_page);
-                    after = page_of(j + 2 * kWarps * 64 + 2 * lane);
-                }
-                const int key = j + 32 * half + lane, p = __shfl_sync(0xffffffffu, page, 16 * half + lane / 2);
-                float b[kCols];
-                bool any = false;
-#pragma unroll
-                for (int h = 0; h < kCols; ++h) b[h] = -INFINITY;
-                const bool there = p >= 0 && key < k1;
+                for (int h = 0; h < kCols; ++h) b[0][h] = b[1][h] = -INFINITY;
 #pragma unroll
                 for (int h = 0; h < kH; ++h) {
-                    const float d = S.delta[h][32 * half + lane];
-                    const bool kept = there && order_key(__float_as_uint(d) & 0x7FFFFFFFu, key) >= least[h];
-                    b[h] = kept ? d : -INFINITY;
-                    any = any || kept;
+                    const bool k0h = order_key(__float_as_uint(dl[0][h].x) & 0x7FFFFFFFu, key) >= least[h], k1h = order_key(__float_as_uint(dl[0][h].y) & 0x7FFFFFFFu, key + 1) >= least[h];
+                    b[0][h] = k0h ? dl[0][h].x : -INFINITY;
+                    b[1][h] = k1h ? dl[0][h].y : -INFINITY;
+                    any[0] = any[0] || k0h;
+                    any[1] = any[1] || k1h;
                 }
-                const uint32_t ballot = __ballot_sync(0xffffffffu, any);
-                if (any) {
-                    const int to = tail + __popc(ballot & ((1u << lane) - 1u)), ring = to / kBatch % kRing;
-                    S.row[ring][to % kBatch] = key_row(p, hk, key & R.mask(), A.Hkv, R.page_log);
-                    float4* dst = reinterpret_cast<float4*>(S.bias[ring][to % kBatch]);
-                    dst[0] = make_float4(b[0], b[1], b[2], b[3]);
-                    if constexpr (kCols == 8) dst[1] = make_float4(b[4], b[5], b[6], b[7]);
+                any[0] = any[0] && page[0] >= 0 && key < k1;
+                any[1] = any[1] && page[0] >= 0 && key + 1 < k1;
+                const uint32_t ballot[2] = {__ballot_sync(0xffffffffu, any[0]), __ballot_sync(0xffffffffu, any[1])}, below = (1u << lane) - 1u;
+                const size_t off = (size_t)(uint32_t)page[0] * page_bytes + (head_bytes + (uint32_t)(key & R.mask()) * D);
+                int to = tail + __popc(ballot[0] & below);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    if (any[e]) {
+                        S.off[to % kRing] = off + e * D;
+                        float4* dst = reinterpret_cast<float4*>(S.bias[to % kRing]);
+                        dst[0] = make_float4(b[e][0], b[e][1], b[e][2], b[e][3]);
+                        if constexpr (kCols == 8) dst[1] = make_float4(b[e][4], b[e][5], b[e][6], b[e][7]);
+                    }
+                    if (e == 0) to = tail + __popc(ballot[0]) + __popc(ballot[1] & below);
                 }
-                tail += __popc(ballot);
-                half ^= 1;
-                if (half == 0) j += kWarps * 64;
+                tail += __popc(ballot[0]) + __popc(ballot[1]);
+                j += kWarps * 64;
+#pragma unroll
+                for (int a = 0; a + 1 < kAhead; ++a) {
+                    page[a] = page[a + 1];
+#pragma unroll
+                    for (int h = 0; h < kH; ++h) dl[a][h] = dl[a + 1][h];
+                }
+                request(kAhead - 1, j + (kAhead - 1) * kWarps * 64 + 2 * lane, after);
+                after = page_of(j + kAhead * kWarps * 64 + 2 * lane);
             }
             // the next batch is requested, the one before it is used; behind the last one an empty group keeps the count
             const bool more = tail > issued * kBatch;
@@ -962,7 +993,7 @@ __global__ void __launch_bounds__(kThreads, 4) attn_kernel(AttnArgs A) {
                 const uint32_t* sc = reinterpret_cast<const uint32_t*>(data + lane * kPitch + D);
 #pragma unroll
                 for (int e = 0; e < D / 32; ++e) odd |= odd_pair(sc[e]);
-                attend<D, kH>(W, data, S.bias[used % kRing], __any_sync(0xffffffffu, odd));
+                attend<D, kH>(W, sQ, data, &S.bias[used * kBatch % kRing], __any_sync(0xffffffffu, odd));
                 __syncwarp();
                 ++used;
             }
@@ -1113,7 +1144,7 @@ int launch_cache4_decode(const Cache& C, const void* q, const uint8_t* codes, co
     const bool tensor = C.dtype == DMA_BF16 && !(C.flags & DMA_FLAG_SIMT);
     const int hb = head_blocks(C), per_row = C.Hkv * hb;
     unsigned long long* weakest = nullptr;
-    Plan plan{nullptr, nullptr, per_row, 8};
+    Plan plan{nullptr, nullptr, per_row, 8, (C.G + hb - 1) / hb, C.w};
     char* at = (char*)ws + kWsHeaderBytes;
     if (tensor && capacity > 1024) {
         plan.ustart = reinterpret_cast<int32_t*>(at + weakest_bytes(C));
