@@ -5,12 +5,17 @@
 //   select_kernel        per (row, query head): the weakest kept key, as a 64-bit order key. A key is kept iff its order key is not below it
 //   simt_attn_kernel     per (row, query head, split of the keys), fp32: CUDA cores
 //   simt_combine_kernel  the splits' partials -> o, lse
+#include <cooperative_groups.h>
+
 #include <algorithm>
+#include <type_traits>
 
 #include "paged.cuh"
 
 namespace dma {
 namespace {
+
+namespace cg = cooperative_groups;
 
 // (delta descending, index ascending) as one unsigned compare; delta > 0, so its pattern orders like its value. The sign is masked, and keys in
 // pages outside the pool count as 0: behind all others.
@@ -31,63 +36,67 @@ struct Rows {
     }
 };
 
-constexpr int kSelectThreads = 256;
-
-// The weakest of the `keep` best of the row's n keys, by radix passes of eight bits over the row: four over the patterns, then as many as the
-// indices take over the keys with the threshold's pattern. Each pass reads the row again (from the L2).
+// By radix passes of eight bits over the row, each of which reads it again (from the L2).
 struct RadixShared { int hist[256]; int bin, before, count; };
-template <typename Load>
-__device__ unsigned long long radix_select(RadixShared& S, Load&& load, int n, int keep) {
+// the bin of the need-th in descending (down) or ascending order
+__device__ __forceinline__ void radix_pick(RadixShared& S, bool down, int need) {
     const int tid = threadIdx.x;
-    int need = keep;
-    uint32_t u_lo = 0u;
-    // the bin of the need-th in descending (down) or ascending order
-    auto pick = [&](bool down) {
-        __syncthreads();
-        if (tid < 32) {
-            int c[8], sum = 0;
+    __syncthreads();
+    if (tid < 32) {
+        int c[8], sum = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { c[i] = S.hist[down ? 255 - (8 * tid + i) : 8 * tid + i]; sum += c[i]; }
-            int incl = sum;
+        for (int i = 0; i < 8; ++i) { c[i] = S.hist[down ? 255 - (8 * tid + i) : 8 * tid + i]; sum += c[i]; }
+        int incl = sum;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int v = __shfl_up_sync(0xffffffffu, incl, o);
-                if (tid >= o) incl += v;
-            }
-            int before = incl - sum;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (before < need && need <= before + c[i]) { S.bin = down ? 255 - (8 * tid + i) : 8 * tid + i; S.before = before; S.count = c[i]; }
-                before += c[i];
-            }
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (tid >= o) incl += v;
         }
-        __syncthreads();
-    };
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < 256; i += blockDim.x) S.hist[i] = 0;
-        __syncthreads();
-        for (int j = tid; j < n; j += blockDim.x) {
-            const uint32_t u = load(j);
-            if (shift == 24 || (u ^ u_lo) >> (shift + 8) == 0) atomicAdd(&S.hist[u >> shift & 255u], 1);
+        int before = incl - sum;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (before < need && need <= before + c[i]) { S.bin = down ? 255 - (8 * tid + i) : 8 * tid + i; S.before = before; S.count = c[i]; }
+            before += c[i];
         }
-        pick(true);
-        u_lo |= (uint32_t)S.bin << shift;
-        need -= S.before;
-        if (S.count == need) return order_key(u_lo, INT32_MAX);              // the whole bin is kept
     }
-    // the need-th lowest index among the keys with this pattern
+    __syncthreads();
+}
+__device__ __forceinline__ void radix_clear(RadixShared& S) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < 256; i += blockDim.x) S.hist[i] = 0;
+    __syncthreads();
+}
+// the need-th lowest index among the row's keys of pattern u
+template <typename Load>
+__device__ __noinline__ int radix_index(RadixShared& S, Load load, int n, uint32_t u, int need) {
     int j_lo = 0;
     for (int shift = (31 - __clz(n)) / 8 * 8; shift >= 0; shift -= 8) {
-        __syncthreads();
-        for (int i = tid; i < 256; i += blockDim.x) S.hist[i] = 0;
-        __syncthreads();
-        for (int j = tid; j < n; j += blockDim.x)
-            if (load(j) == u_lo && (shift == 24 || (j ^ j_lo) >> (shift + 8) == 0)) atomicAdd(&S.hist[j >> shift & 255], 1);
-        pick(false);
+        radix_clear(S);
+        for (int j = threadIdx.x; j < n; j += blockDim.x)
+            if (load(j) == u && (shift == 24 || (j ^ j_lo) >> (shift + 8) == 0)) atomicAdd(&S.hist[j >> shift & 255], 1);
+        radix_pick(S, false, need);
         j_lo |= S.bin << shift;
         need -= S.before;
     }
-    return order_key(u_lo, j_lo);
+    return j_lo;
+}
+// the order key of the weakest of the row's `keep` best
+template <typename Load>
+__device__ __noinline__ unsigned long long radix_select(RadixShared& S, Load load, int n, int keep) {
+    int need = keep;
+    uint32_t u = 0u;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        radix_clear(S);
+        for (int j = threadIdx.x; j < n; j += blockDim.x) {
+            const uint32_t v = load(j);
+            if (shift == 24 || (v ^ u) >> (shift + 8) == 0) atomicAdd(&S.hist[v >> shift & 255u], 1);
+        }
+        radix_pick(S, true, need);
+        u |= (uint32_t)S.bin << shift;
+        need -= S.before;
+        if (S.count == need) return order_key(u, INT32_MAX);      // the whole bin is kept
+    }
+    return order_key(u, radix_index(S, load, n, u, need));
 }
 
 // What every row's attention is cut by: units of about the same work, dealt out to the CTAs in equal shares. ustart[t]: units before row t, over all its
@@ -143,24 +152,119 @@ __global__ void __launch_bounds__(1024) plan_kernel(Rows R, int rows, Plan P) {
 // counts the keys above the bracket and notes those inside, a few per cent, each thread in slots of its own; the need-th of these is found by
 // a histogram over the bracket and a ranking of the bin's keys. Rows of up to kSample keys are their own sample: the bracket is one bin. Where
 // the bracket misses or holds too many (weights that crowd, equal weights) radix_select takes the row.
-// Many rows: 256 threads each, so that an SM works on several and their barriers and round trips hide each other; few rows: 1024.
-constexpr int kOwn = 10, kShared = 1024, kRank = 128;     // slots per thread, overflow slots, most keys ranked against each other
+// Many rows: 256 threads each, so that an SM works on several and their barriers and round trips hide each other; fewer long ones: 512.
+constexpr int kOwn = 20, kShared = 512, kRank = 128;     // slots per thread, overflow slots, most keys ranked against each other
+constexpr int kBins = 1024;
 template <int NT>
-struct alignas(16) SelectShared {
-    unsigned long long own[kOwn * NT], more[kShared], cand[kRank];
-    int hist[1024];
+struct alignas(16) HeldShared {
+    unsigned long long cand[kRank];
+    int hist[kBins];
     RadixShared radix;
     uint32_t wmin[NT / 32], wmax[NT / 32];
     int part[NT / 32], above[NT / 32];
     int bin[2], need, count, ncand, nmore;
+    uint32_t umin, umax;
     unsigned long long found;
 };
+template <int NT>
+struct alignas(16) SelectShared : HeldShared<NT> {
+    uint2 own[kOwn * NT], more[kShared];                          // (pattern, index) of keys inside the bracket
+};
+template <int NT>
+struct alignas(16) ClusterShared : HeldShared<NT> { int sum[kBins]; };       // the whole row's bins
+__device__ __forceinline__ int shift_of(uint32_t width) { return max(0, 22 - __clz((int)width)); }       // kBins bins over width + 1 patterns
+
+// The descending running count of the bins in hist: a thread's bins are kBins - 1 - tid kBins / NT and those below it, `excl` keys lie above them. The bins are zeroed again. One barrier.
+template <int NT>
+__device__ __forceinline__ void scan_bins(HeldShared<NT>& S, int* hist, int& excl, int (&c)[kBins / NT]) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, top = kBins - 1 - tid * (kBins / NT);
+    int sum = 0;
+#pragma unroll
+    for (int i = 0; i < kBins / NT; ++i) { c[i] = hist[top - i]; hist[top - i] = 0; sum += c[i]; }
+    int incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+    }
+    if (lane == 31) S.part[warp] = incl;
+    __syncthreads();
+    excl = __reduce_add_sync(0xffffffffu, lane < warp && lane < NT / 32 ? S.part[lane] : 0) + incl - sum;
+}
+// whether one of the thread's bins holds rank `want` (from 1): which, how many keys it holds and how many lie above it
+template <int NT>
+__device__ __forceinline__ bool bin_of(int want, int excl, const int (&c)[kBins / NT], int& bin, int& before, int& count) {
+    bool mine = false;
+#pragma unroll
+    for (int i = 0; i < kBins / NT; ++i) {
+        if (excl < want && want <= excl + c[i]) { bin = kBins - 1 - threadIdx.x * (kBins / NT) - i; before = excl; count = c[i]; mine = true; }
+        excl += c[i];
+    }
+    return mine;
+}
+// the CTA's least and largest pattern; one barrier
+template <int NT>
+__device__ __forceinline__ void range_of(HeldShared<NT>& S, uint32_t& umin, uint32_t& umax) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    umin = __reduce_min_sync(0xffffffffu, umin);
+    umax = __reduce_max_sync(0xffffffffu, umax);
+    if (lane == 0) { S.wmin[warp] = umin; S.wmax[warp] = umax; }
+    __syncthreads();
+    umin = __reduce_min_sync(0xffffffffu, S.wmin[lane % (NT / 32)]);
+    umax = __reduce_max_sync(0xffffffffu, S.wmax[lane % (NT / 32)]);
+}
+// The need-th largest of the first `count` candidates. One barrier behind their last write is the caller's.
+template <int NT>
+__device__ __forceinline__ unsigned long long rank_candidates(HeldShared<NT>& S, int count, int need) {
+    const int tid = threadIdx.x;
+    for (int i = tid; i < count; i += NT) {
+        const unsigned long long k = S.cand[i];
+        int before = 0;
+        for (int e = 0; e < count; ++e) before += S.cand[e] > k;
+        if (before == need - 1) S.found = k;
+    }
+    __syncthreads();
+    return S.found;
+}
+
+// The need-th (from 1) of the order keys in [base, base + nbins << s), of which there are `count`. each(f): f(order key) for the thread's keys, others among them.
+// Called behind a barrier after the last use of part, bin, need and count.
+template <int NT, typename Each>
+__device__ __forceinline__ unsigned long long find_weakest(HeldShared<NT>& S, Each&& each, unsigned long long base, int s, int nbins, int count, int need) {
+    const int tid = threadIdx.x;
+    while (count > kRank) {
+        each([&](unsigned long long x) {
+            const unsigned long long bin = (x - base) >> s;
+            if (x >= base && bin < (unsigned long long)nbins) atomicAdd(&S.hist[bin], 1);
+        });
+        __syncthreads();
+        int excl, c[kBins / NT], bin, before, in_bin;
+        scan_bins<NT>(S, S.hist, excl, c);
+        if (bin_of<NT>(need, excl, c, bin, before, in_bin)) { S.bin[0] = bin; S.need = need - before; S.count = in_bin; }
+        __syncthreads();
+        base += (unsigned long long)S.bin[0] << s;
+        need = S.need;
+        count = S.count;
+        const int narrower = max(0, s - 10);
+        nbins = 1 << (s - narrower);
+        s = narrower;
+        __syncthreads();
+    }
+    each([&](unsigned long long x) {
+        if (x >= base && (x - base) >> s < (unsigned long long)nbins) {
+            const int at = atomicAdd(&S.ncand, 1);
+            if (at < kRank) S.cand[at] = x;
+        }
+    });
+    __syncthreads();
+    return rank_candidates<NT>(S, count, need);
+}
 
 template <int NT, int kPer>
-__global__ void __launch_bounds__(NT) select_kernel(Rows R, int rows, int w, unsigned long long* weakest, Plan P) {
+__global__ void __launch_bounds__(NT, 1024 / NT) select_kernel(Rows R, int rows, int w, unsigned long long* weakest, Plan P) {
     extern __shared__ __align__(16) uint8_t select_smem[];
     SelectShared<NT>& S = *reinterpret_cast<SelectShared<NT>*>(select_smem);
-    constexpr int kSample = NT * kPer, kWarps = NT / 32, kBins = 1024;
+    constexpr int kSample = NT * kPer, kWarps = NT / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     for (int i = tid; i < kBins; i += NT) S.hist[i] = 0;
     if (tid == 0) { S.ncand = S.nmore = 0; S.bin[0] = S.bin[1] = -1; }
@@ -184,33 +288,6 @@ __global__ void __launch_bounds__(NT) select_kernel(Rows R, int rows, int w, uns
         if ((unsigned)page >= (unsigned)R.num_pages) return 0u;
         return __float_as_uint(plane[(size_t)page * stride + (j & R.mask())]) & 0x7FFFFFFFu;
     };
-    // the bin (descending) that holds rank `want`, and how many keys lie above it; the bins are zeroed again. Two barriers.
-    auto scan = [&](int& excl, int (&c)[kBins / NT]) {
-        int sum = 0;
-        constexpr int kB = kBins / NT;
-        const int top = kBins - 1 - tid * kB;
-#pragma unroll
-        for (int i = 0; i < kB; ++i) { c[i] = S.hist[top - i]; S.hist[top - i] = 0; sum += c[i]; }
-        int incl = sum;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += v;
-        }
-        if (lane == 31) S.part[warp] = incl;
-        __syncthreads();
-        excl = __reduce_add_sync(0xffffffffu, lane < warp && lane < kWarps ? S.part[lane] : 0) + incl - sum;
-    };
-    auto bin_of = [&](int want, int excl, const int (&c)[kBins / NT], int& bin, int& before, int& count) {
-        bool mine = false;
-#pragma unroll
-        for (int i = 0; i < kBins / NT; ++i) {
-            if (excl < want && want <= excl + c[i]) { bin = kBins - 1 - tid * (kBins / NT) - i; before = excl; count = c[i]; mine = true; }
-            excl += c[i];
-        }
-        return mine;
-    };
-    auto shift_of = [](uint32_t width) { return max(0, 22 - __clz((int)width)); };        // 1024 bins over width + 1 patterns
     // sample
     uint32_t lo = 0u, hi = 0x7FFFFFFFu;
     {
@@ -226,72 +303,82 @@ __global__ void __launch_bounds__(NT) select_kernel(Rows R, int rows, int w, uns
 #pragma unroll
         for (int k = 0; k < kPer; ++k)
             if (u[k] != 0xFFFFFFFFu) { umin = min(umin, u[k]); umax = max(umax, u[k]); }
-        umin = __reduce_min_sync(0xffffffffu, umin);
-        umax = __reduce_max_sync(0xffffffffu, umax);
-        if (lane == 0) { S.wmin[warp] = umin; S.wmax[warp] = umax; }
-        __syncthreads();
-        umin = __reduce_min_sync(0xffffffffu, S.wmin[lane % kWarps]);
-        umax = __reduce_max_sync(0xffffffffu, S.wmax[lane % kWarps]);
+        range_of<NT>(S, umin, umax);
         const int shift = shift_of(umax - umin);
 #pragma unroll
         for (int k = 0; k < kPer; ++k)
             if (u[k] != 0xFFFFFFFFu) atomicAdd(&S.hist[(u[k] - umin) >> shift], 1);
         __syncthreads();
         int excl, c[kBins / NT];
-        scan(excl, c);
+        scan_bins<NT>(S, S.hist, excl, c);
         const float q = (float)w / (float)n, mid = q * kSample, dev = 4.5f * sqrtf(mid * (1.0f - q)) + 4.0f;
         const int r0 = whole ? w : (int)(mid - dev), r1 = whole ? w : (int)(mid + dev) + 1;
         int bin, before, count;
-        if (bin_of(r0, excl, c, bin, before, count)) S.bin[0] = bin;
-        if (bin_of(r1, excl, c, bin, before, count)) S.bin[1] = bin;
+        if (bin_of<NT>(r0, excl, c, bin, before, count)) S.bin[0] = bin;
+        if (bin_of<NT>(r1, excl, c, bin, before, count)) S.bin[1] = bin;
         __syncthreads();
         // (a rank beyond the sample: no bracket on that side)
         if (S.bin[0] >= 0 && r0 >= 1) hi = min(umin + ((uint32_t)(S.bin[0] + 1) << shift) - 1u, 0x7FFFFFFFu);
         if (S.bin[1] >= 0) lo = umin + ((uint32_t)S.bin[1] << shift);
     }
-    // sweep: four neighbouring keys of a page per thread and step
-    int above = 0, mine = 0;
-    auto take = [&](uint32_t u, int j) {
-        above += u > hi;
-        if (u - lo <= hi - lo) {
-            const unsigned long long k = order_key(u, j);
-            if (mine < kOwn) {
-                S.own[mine * NT + tid] = k;
-            } else {
-                const int at = atomicAdd(&S.nmore, 1);
-                if (at < kShared) S.more[at] = k;
-            }
-            ++mine;
-        }
-    };
+    // sweep: four neighbouring keys of a page per thread and step. What lies inside is noted by predicated stores, without a branch per key, and what lies below
+    // is counted by the sign of its distance (with a branch and two comparisons per key, the sweep was 50 of the 62 instructions that 32 keys took).
+    uint32_t below = 0u, seen = 0u;
+    int extra = 0;
+    uint2 *own = S.own + tid, *const own_end = own + (kOwn - 4) * NT;
+    const uint32_t width = hi - lo, beyond = lo > 0u ? 0u : 0xFFFFFFFFu;          // beyond: below the bracket, wherever that is
     const int chunks = (n + 3) / 4;
     constexpr int kAhead = 4;
-    for (int i0 = 0; i0 < chunks; i0 += NT * kAhead) {
-        uint4 u[kAhead];
-        int page[kAhead];
+    int page[kAhead];
+    auto pages_at = [&](int i0) {
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             const int i = i0 + k * NT + tid;
             page[k] = i < chunks ? pages[(4 * i) >> R.page_log] : -1;
         }
+    };
+    pages_at(0);
+    for (int i0 = 0; i0 < chunks; i0 += NT * kAhead) {
+        uint4 u[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            const int j = 4 * (i0 + k * NT + tid);
             u[k] = make_uint4(0u, 0u, 0u, 0u);
-            if ((unsigned)page[k] < (unsigned)R.num_pages) u[k] = *reinterpret_cast<const uint4*>(plane + (size_t)page[k] * stride + (j & R.mask()));
+            if ((unsigned)page[k] < (unsigned)R.num_pages) u[k] = *reinterpret_cast<const uint4*>(plane + (size_t)page[k] * stride + (4 * (i0 + k * NT + tid) & R.mask()));
         }
+        pages_at(i0 + NT * kAhead);
+        seen += 4 * kAhead;
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             const int j = 4 * (i0 + k * NT + tid);
-            if (j < n) {
-                take(u[k].x & 0x7FFFFFFFu, j);
-                if (j + 1 < n) take(u[k].y & 0x7FFFFFFFu, j + 1);
-                if (j + 2 < n) take(u[k].z & 0x7FFFFFFFu, j + 2);
-                if (j + 3 < n) take(u[k].w & 0x7FFFFFFFu, j + 3);
+            uint32_t v[4] = {u[k].x & 0x7FFFFFFFu, u[k].y & 0x7FFFFFFFu, u[k].z & 0x7FFFFFFFu, u[k].w & 0x7FFFFFFFu};
+            if (j + 4 > n) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (j + e >= n) v[e] = beyond;
+            }
+            if (own <= own_end) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t d = v[e] - lo;
+                    below += d >> 31;
+                    if (d <= width) { *own = make_uint2(v[e], (uint32_t)(j + e)); own += NT; }
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t d = v[e] - lo;
+                    below += d >> 31;
+                    if (d <= width) {
+                        const int at = atomicAdd(&S.nmore, 1);
+                        if (at < kShared) S.more[at] = make_uint2(v[e], (uint32_t)(j + e));
+                        ++extra;
+                    }
+                }
             }
         }
     }
-    const int sum_above = __reduce_add_sync(0xffffffffu, above), sum_in = __reduce_add_sync(0xffffffffu, mine);
+    const int mine = (int)(own - (S.own + tid)) / NT;
+    const int sum_above = __reduce_add_sync(0xffffffffu, (int)(seen - below) - mine - extra), sum_in = __reduce_add_sync(0xffffffffu, mine + extra);
     if (lane == 0) { S.above[warp] = sum_above; S.part[warp] = sum_in; }
     __syncthreads();
     const int inside = __reduce_add_sync(0xffffffffu, lane < kWarps ? S.part[lane] : 0);
@@ -301,49 +388,144 @@ __global__ void __launch_bounds__(NT) select_kernel(Rows R, int rows, int w, uns
     if (need < 1 || need > inside || nmore > kShared) {
         found = radix_select(S.radix, load, n, w);
     } else {
-        // the need-th of the keys inside, from the bins of their range down
-        auto each = [&](auto&& f) {
-            for (int i = 0; i < min(mine, kOwn); ++i) f(S.own[i * NT + tid]);
+        __syncthreads();                                          // (part and above have been read)
+        auto inside_keys = [&](auto&& f) {
+            for (int i = 0; i < mine; ++i) f(S.own[i * NT + tid]);
             for (int i = tid; i < nmore; i += NT) f(S.more[i]);
         };
-        unsigned long long base = (unsigned long long)lo << 32;
-        int s = 32 + shift_of(hi - lo), nbins = kBins, count = inside;
-        while (count > kRank) {
-            __syncthreads();                                      // (part and count have been read)
-            each([&](unsigned long long x) {
-                const unsigned long long bin = (x - base) >> s;
-                if (x >= base && bin < (unsigned long long)nbins) atomicAdd(&S.hist[bin], 1);
-            });
-            __syncthreads();
-            int excl, c[kBins / NT], bin, before, in_bin;
-            scan(excl, c);
-            if (bin_of(need, excl, c, bin, before, in_bin)) { S.bin[0] = bin; S.need = need - before; S.count = in_bin; }
-            __syncthreads();
-            base += (unsigned long long)S.bin[0] << s;
-            need = S.need;
-            count = S.count;
-            const int narrower = max(0, s - 10);
-            nbins = 1 << (s - narrower);
-            s = narrower;
-        }
-        // (s: the width of the next pass's bins; the keys left are those in [base, base + nbins << s), or all of them)
+        // the bin of the bracket that holds it, then the order keys of that bin
+        const int shift = shift_of(hi - lo);
+        inside_keys([&](uint2 x) { atomicAdd(&S.hist[(x.x - lo) >> shift], 1); });
         __syncthreads();
-        const bool all = count == inside;
-        each([&](unsigned long long x) {
-            if (all || (x >= base && (x - base) >> s < (unsigned long long)nbins)) {
-                const int at = atomicAdd(&S.ncand, 1);
-                if (at < kRank) S.cand[at] = x;
+        int excl, c[kBins / NT], bin, before, count;
+        scan_bins<NT>(S, S.hist, excl, c);
+        if (bin_of<NT>(need, excl, c, bin, before, count)) { S.bin[0] = bin; S.need = need - before; S.count = count; }
+        __syncthreads();
+        const uint32_t low = lo + ((uint32_t)S.bin[0] << shift);
+        need = S.need;
+        count = S.count;
+        __syncthreads();
+        found = find_weakest<NT>(S, [&](auto&& f) {
+            inside_keys([&](uint2 x) { if ((x.x - low) >> shift == 0u) f(order_key(x.x, (int)x.y)); });
+        }, (unsigned long long)low << 32, 32 + shift - 10, 1 << 10, count, need);
+    }
+    if (tid == 0) weakest[item] = found;
+}
+
+// The same for rows that the registers hold: NT threads with kKeys keys each, and where there are few rows up to eight such CTAs as a cluster. The row is read in one go, a
+// histogram of all its keys over their range finds the threshold's bin, and that bin is ranked: a third of the sample's and the sweep's instructions, and fewer
+// barriers and round trips, which is what counts for few rows.
+template <int NT, int kKeys>
+__global__ void __launch_bounds__(NT, 1024 / NT) select_held_kernel(Rows R, int rows, int w, unsigned long long* weakest, Plan P) {
+    static_assert(NT <= kBins, "a thread has a bin at least");
+    extern __shared__ __align__(16) uint8_t select_smem[];
+    ClusterShared<NT>& S = *reinterpret_cast<ClusterShared<NT>*>(select_smem);
+    cg::cluster_group cluster = cg::this_cluster();
+    const int tid = threadIdx.x, nrank = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    for (int i = tid; i < kBins; i += NT) S.hist[i] = 0;
+    if (tid == 0) S.ncand = 0;
+    pdl_enter(R.table, R.seq, R.pos, R.delta, weakest, P.ustart, P.tickets);
+    int item = blockIdx.x / nrank;
+    if (P.ustart && item-- == 0) {
+        if (rank == 0) make_plan<NT>(R, rows, P);
+        return;
+    }
+    const int t = item / R.Hq, h = item % R.Hq;
+    int r;
+    const int n = R.visible(t, r);
+    if (n <= w) {                                                 // every key
+        if (tid == 0 && rank == 0) weakest[item] = 0ull;
+        return;
+    }
+    const int32_t* pages = R.table + r * R.ld;
+    const float* plane = R.delta + ((size_t)h << R.page_log);
+    const int stride = R.Hq << R.page_log;
+    auto index = [&](int k) { return 4 * (((k >> 2) * nrank + rank) * NT + tid) + (k & 3); };
+    constexpr uint32_t kNone = 0xFFFFFFFFu;
+    constexpr int kTogether = kKeys < 16 ? kKeys : 16;            // keys of a thread on their way at a time
+    uint32_t u[kKeys], umin = 0x7FFFFFFFu, umax = 0u;
+#pragma unroll
+    for (int k0 = 0; k0 < kKeys; k0 += kTogether) {
+        int page[kTogether / 4];
+#pragma unroll
+        for (int k = 0; k < kTogether / 4; ++k) page[k] = index(k0 + 4 * k) < n ? pages[index(k0 + 4 * k) >> R.page_log] : -1;
+#pragma unroll
+        for (int k = 0; k < kTogether; k += 4) {
+            const int j = index(k0 + k), pg = page[k / 4];
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if ((unsigned)pg < (unsigned)R.num_pages) v = *reinterpret_cast<const uint4*>(plane + (size_t)pg * stride + (j & R.mask()));
+            u[k0 + k] = j < n ? v.x & 0x7FFFFFFFu : kNone;
+            u[k0 + k + 1] = j + 1 < n ? v.y & 0x7FFFFFFFu : kNone;
+            u[k0 + k + 2] = j + 2 < n ? v.z & 0x7FFFFFFFu : kNone;
+            u[k0 + k + 3] = j + 3 < n ? v.w & 0x7FFFFFFFu : kNone;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kKeys; ++k) {
+        umin = min(umin, u[k]);                                   // (kNone: no minimum, and as an int no maximum)
+        umax = (uint32_t)max((int)umax, (int)u[k]);
+    }
+    range_of<NT>(S, umin, umax);                                  // (its barrier: the histogram is zero)
+    if (nrank > 1) {
+        if (tid == 0) { S.umin = umin; S.umax = umax; }
+        cluster.sync();
+        for (int q = 0; q < nrank; ++q) {
+            umin = min(umin, *cluster.map_shared_rank(&S.umin, q));
+            umax = max(umax, *cluster.map_shared_rank(&S.umax, q));
+        }
+    }
+    // the bin that holds the need-th, then, while it holds many keys of several patterns, the bins of its own range
+    uint32_t lo = umin, nbins = kBins;
+    int shift = shift_of(umax - umin), need = w, count;
+    for (;;) {
+#pragma unroll
+        for (int k = 0; k < kKeys; ++k) {
+            const uint32_t bin = (u[k] - lo) >> shift;            // (kNone: beyond the bins, since its distance to any key is 2^31 at least)
+            if (bin < nbins) atomicAdd(&S.hist[bin], 1);
+        }
+        int excl, c[kBins / NT], bin, before, in_bin;
+        if (nrank > 1) {
+            // the bins of the whole row in `sum`, which nobody else reads; then, when all have read them, this CTA's are zeroed
+            cluster.sync();
+            for (int i = tid; i < kBins; i += NT) {
+                int all = 0;
+                for (int q = 0; q < nrank; ++q) all += cluster.map_shared_rank(S.hist, q)[i];
+                S.sum[i] = all;
             }
-        });
-        __syncthreads();
-        for (int i = tid; i < min(count, kRank); i += NT) {
-            const unsigned long long k = S.cand[i];
-            int before = 0;
-            for (int e = 0; e < min(count, kRank); ++e) before += S.cand[e] > k;
-            if (before == need - 1) S.found = k;
+            cluster.sync();
+            for (int i = tid; i < kBins; i += NT) S.hist[i] = 0;
+            scan_bins<NT>(S, S.sum, excl, c);
+        } else {
+            __syncthreads();
+            scan_bins<NT>(S, S.hist, excl, c);
         }
+        if (bin_of<NT>(need, excl, c, bin, before, in_bin)) { S.bin[0] = bin; S.need = need - before; S.count = in_bin; }
         __syncthreads();
-        found = S.found;
+        lo += (uint32_t)S.bin[0] << shift;
+        need = S.need;
+        count = S.count;
+        if (count <= kRank || shift == 0) break;
+        const int narrower = max(0, shift - 10);
+        nbins = 1u << (shift - narrower);
+        shift = narrower;
+        __syncthreads();                                          // (bin, need and count have been read)
+    }
+    unsigned long long found;
+    if (count <= kRank) {
+        ClusterShared<NT>* first = nrank > 1 ? cluster.map_shared_rank(&S, 0) : &S;
+#pragma unroll
+        for (int k = 0; k < kKeys; ++k)
+            if ((u[k] - lo) >> shift == 0u) first->cand[atomicAdd(&first->ncand, 1)] = order_key(u[k], index(k));
+        if (nrank > 1) cluster.sync(); else __syncthreads();
+        if (rank != 0) return;
+        found = rank_candidates<NT>(S, count, need);
+    } else {                                                      // equal weights: by their indices
+        if (rank != 0) return;                                    // (no CTA reads another's shared memory any more: the loop's second barrier)
+        found = order_key(lo, radix_index(S.radix, [&](int j) {
+            const int page = pages[j >> R.page_log];
+            if ((unsigned)page >= (unsigned)R.num_pages) return 0u;
+            return __float_as_uint(plane[(size_t)page * stride + (j & R.mask())]) & 0x7FFFFFFFu;
+        }, n, lo, need));
     }
     if (tid == 0) weakest[item] = found;
 }
@@ -1123,11 +1305,30 @@ int tc_decode(const AttnArgs& A, int grid, cudaStream_t st) {
     return launch_overlapped(attn_kernel<D, kH>, dim3(grid), dim3(kThreads), bytes, st, 1, A);
 }
 
-template <int NT, int kPer>
-int select(const Cache& C, const Rows& R, unsigned long long* weakest, const Plan& plan, cudaStream_t st) {
-    constexpr size_t bytes = sizeof(SelectShared<NT>);
-    if (cudaFuncSetAttribute(select_kernel<NT, kPer>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return DMA_ERR_CUDA;
-    return launch_overlapped(select_kernel<NT, kPer>, dim3(C.rows * C.Hq + (plan.ustart ? 1 : 0)), dim3(NT), bytes, st, 1, R, C.rows, C.w, weakest, plan);
+int select_launch(void (*kernel)(Rows, int, int, unsigned long long*, Plan), int threads, size_t bytes, int cluster, const Cache& C, const Rows& R,
+                  unsigned long long* weakest, const Plan& plan, cudaStream_t st) {
+    if (bytes > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return DMA_ERR_CUDA;
+    return launch_overlapped(kernel, dim3((unsigned)((C.rows * C.Hq + (plan.ustart ? 1 : 0)) * cluster)), dim3(threads), bytes, st, cluster, R, C.rows, C.w, weakest, plan);
+}
+int select(const Cache& C, const Rows& R, unsigned long long* weakest, const Plan& plan, int64_t capacity, cudaStream_t st) {
+    auto stream = [&](auto nt, auto kernel) { return select_launch(kernel, nt, sizeof(SelectShared<nt>), 1, C, R, weakest, plan, st); };
+    auto held = [&](auto nt, auto kernel, int cluster) { return select_launch(kernel, nt, sizeof(ClusterShared<nt>), cluster, C, R, weakest, plan, st); };
+    using std::integral_constant;
+    constexpr integral_constant<int, 128> t128{};
+    constexpr integral_constant<int, 256> t256{};
+    constexpr integral_constant<int, 512> t512{};
+    constexpr integral_constant<int, 1024> t1024{};
+    constexpr int K = 1024;
+    const int items = C.rows * C.Hq;
+    if (items >= 3 * 148) {
+        if (capacity <= 2 * K) return held(t256, select_held_kernel<256, 8>, 1);
+        return stream(t128, select_kernel<128, 8>);
+    }
+    if (capacity <= 4 * K) return held(t1024, select_held_kernel<1024, 4>, 1);
+    if (capacity <= 8 * K) return held(t1024, select_held_kernel<1024, 8>, 1);
+    if (capacity <= 16 * K) return held(t1024, select_held_kernel<1024, 16>, 1);
+    if (capacity <= 256 * K && items * (capacity / (32 * K)) <= 148) return held(t1024, select_held_kernel<1024, 32>, capacity <= 32 * K ? 1 : capacity <= 64 * K ? 2 : capacity <= 128 * K ? 4 : 8);
+    return stream(t512, select_kernel<512, 8>);
 }
 
 }  // namespace
@@ -1154,8 +1355,7 @@ int launch_cache4_decode(const Cache& C, const void* q, const uint8_t* codes, co
     int rc;
     if (capacity > C.w) {
         weakest = reinterpret_cast<unsigned long long*>(at);
-        rc = C.rows * C.Hq >= 3 * 148 ? select<256, 8>(C, R, weakest, plan, st) : select<1024, 4>(C, R, weakest, plan, st);
-        if (rc) return rc;
+        if ((rc = select(C, R, weakest, plan, capacity, st))) return rc;
     } else if (plan.ustart) {
         rc = launch_overlapped(plan_kernel, dim3(1), dim3(1024), 0, st, 1, R, C.rows, plan);
         if (rc) return rc;
