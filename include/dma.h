@@ -319,7 +319,7 @@ int dma_page_plan(const dma_cache_t* c, const int32_t* lens, const int32_t* want
  *   (ties to even; n = 0 where the quotient is NaN, so with s = 0 too). 64 channels that hold a NaN, an infinity or a value that bf16 rounds to one read back as NaN.
  *   delta: of the row's V as given (not as held), the bits of dma_mask_build: W_delta [Hq, d], A [Hq]. Or, with delta_new not
  *   NULL, delta_new[h * delta_ld + t] as it is (dma_mask_build's bias, or dma_delta_range's output for the full weights);
- *   W_delta and A are then not read. */
+ *   W_delta and A are then not read. Hq / Hkv at most 76 (d = 128) or 96 (d = 64); DMA_ERR_UNSUPPORTED beyond. */
 int dma_cache4_append(const dma_cache_t* c, const void* K, const void* V, const float* W_delta, const float* A, const float* delta_new,
                       int64_t delta_ld, const int32_t* slot, void* codes, void* scales, float* delta, void* cuda_stream);
 

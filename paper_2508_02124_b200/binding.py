@@ -346,33 +346,71 @@ def cache(Hq=1, Hkv=1, d=64, w=1, dtype=torch.bfloat16, rows=1, nseq=1, page_siz
     return c
 
 
-def _on_device(want, /, **tensors):
-    """Tensors of type `want` on the current device, whose stream and memory the library uses."""
-    dev = torch.cuda.current_device() if _raw_device is None else _raw_device()
-    for name, t in tensors.items():
-        if t.dtype is not want:
-            raise TypeError(f"{name}: {t.dtype} where {want} is read")
-        if t.get_device() != dev:
-            raise ValueError(f"{name} is on {t.device}, the call runs on cuda:{dev}")
+# Checks of the paged calls: a tensor that the library would misread is refused before its address is passed on. They take the host's time of every token, so each
+# tensor has one call that tests it and returns its address (0.3 us; the tests by keyword that these replace took half of a call's 14 us).
+def _here():
+    """The current device, whose stream and memory the library uses."""
+    return torch.cuda.current_device() if _raw_device is None else _raw_device()
 
 
-def _rows_of(c, stride, /, **tensors):
-    """[rows, heads, d] tensors of the descriptor's element type, laid out as its strides say."""
-    _on_device(torch.bfloat16 if c.dtype == DMA_BF16 else torch.float32, **tensors)
-    for name, t in tensors.items():
-        heads = c.Hq if name in ("q", "o") else c.Hkv
-        if t.dim() != 3 or t.shape[0] < c.rows or t.shape[1] != heads or t.shape[2] != c.d:
-            raise ValueError(f"{name}: shape {tuple(t.shape)} where [{c.rows}, {heads}, {c.d}] is read")
-        row, head = stride
-        want = (row, head, 1) if row or head else (heads * c.d, c.d, 1)
-        if t.stride() != want and any(n > 1 and a != b for n, a, b in zip(t.shape, t.stride(), want)):
-            raise ValueError(f"{name}: strides {t.stride()} differ from the descriptor's")
+def _flat(name, t, dtype, n, dev):
+    """Address of at least n contiguous entries of `dtype` on the device."""
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: {t.dtype} where {dtype} is read")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the call runs on cuda:{dev}")
+    if t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{name}: {n} contiguous entries are read or written, it is {tuple(t.shape)} with strides {t.stride()}")
+    return t.data_ptr()
 
 
-def _at_least(n, /, **tensors):
-    for name, t in tensors.items():
-        if t.numel() < n or not t.is_contiguous():
-            raise ValueError(f"{name}: {n} contiguous entries are read or written, it is {tuple(t.shape)} with strides {t.stride()}")
+def _same_layout(shape, got, want):
+    return got == want or all(n <= 1 or a == b for n, a, b in zip(shape, got, want))
+
+
+def _row_major(name, t, dtype, rows, heads, d, stride, dev):
+    """Address of [rows, heads, d] laid out as the descriptor's row and head strides say."""
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: {t.dtype} where {dtype} is read")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the call runs on cuda:{dev}")
+    shape = t.shape
+    if shape != (rows, heads, d) and (len(shape) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != d):
+        raise ValueError(f"{name}: shape {tuple(shape)} where [{rows}, {heads}, {d}] is read")
+    row = stride[0]
+    if not (t.is_contiguous() if row == 0 and stride[1] == 0 else _same_layout(shape, t.stride(), (row, stride[1], 1))):
+        raise ValueError(f"{name}: strides {t.stride()} differ from the descriptor's")
+    return t.data_ptr()
+
+
+def _table(c, t, dev):
+    if t.dtype is not torch.int32:
+        raise TypeError(f"block_table: {t.dtype} where {torch.int32} is read")
+    if t.get_device() != dev:
+        raise ValueError(f"block_table is on {t.device}, the call runs on cuda:{dev}")
+    blocks, shape = c.max_blocks, t.shape
+    ld = c.table_ld or blocks
+    if len(shape) != 2 or shape[0] < c.nseq or shape[1] < blocks or not _same_layout(shape, t.stride(), (ld, 1)):
+        raise ValueError(f"block_table: {tuple(shape)} with strides {t.stride()} where [{c.nseq}, {blocks}] with rows of {ld} is read")
+    return t.data_ptr()
+
+
+def _by_head(name, t, heads, rows, dev):
+    """Address and row stride of [heads, >= rows] fp32."""
+    if t.dtype is not torch.float32:
+        raise TypeError(f"{name}: {t.dtype} where {torch.float32} is read")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the call runs on cuda:{dev}")
+    shape, (ld, one) = t.shape, t.stride() if t.dim() == 2 else (0, 0)
+    if len(shape) != 2 or shape[0] < heads or shape[1] < rows or (one != 1 and shape[1] > 1):
+        raise ValueError(f"{name}: {tuple(shape)} with strides {t.stride()} where [{heads}, {rows}] is read")
+    return t.data_ptr(), ld if shape[0] > 1 else max(rows, shape[1])
+
+
+def _pool(c, codes, scales, delta, heads, kv_heads, d, dev):
+    keys = c.num_pages * c.page_size
+    return (_flat("codes", codes, torch.uint8, keys * kv_heads * d, dev), _flat("scales", scales, torch.bfloat16, keys * kv_heads * (d // 16), dev),
+            _flat("delta", delta, torch.float32, keys * heads, dev))
 
 
 def dma_cache4_bytes(c):
@@ -389,86 +427,47 @@ def cache4(c, device):
             torch.zeros(c.num_pages, c.Hq, c.page_size, dtype=torch.float32, device=device))
 
 
-def _cache4_arrays(c, codes, scales, delta):
-    _on_device(torch.uint8, codes=codes)
-    _on_device(torch.bfloat16, scales=scales)
-    _on_device(torch.float32, delta=delta)
-    keys = c.num_pages * c.page_size
-    _at_least(keys * c.Hkv * c.d, codes=codes)
-    _at_least(keys * c.Hkv * (c.d // 16), scales=scales)
-    _at_least(keys * c.Hq, delta=delta)
-
-
 def dma_page_plan(c, lens, want, block_table, free_pages, pool, lens_out=None, pool_out=None, cu_rows=None, row_seq=None, row_pos=None, slot=None):
     """Pages for the sequences' new lengths (int32 tensors; block_table and free_pages are updated in place). Returns (lens_out,
     pool_out, cu_rows, row_seq, row_pos, slot)."""
+    dev, i32, nseq, rows = _here(), torch.int32, c.nseq, c.rows
+
     def new(t, n):
-        return torch.empty(n, dtype=torch.int32, device=lens.device) if t is None else t
-    lens_out, pool_out, cu_rows = new(lens_out, c.nseq), new(pool_out, 4), new(cu_rows, c.nseq + 1)
-    row_seq, row_pos, slot = (new(t, c.rows) for t in (row_seq, row_pos, slot))
-    _on_device(torch.int32, lens=lens, want=want, block_table=block_table, free_pages=free_pages, pool=pool, lens_out=lens_out, pool_out=pool_out,
-               cu_rows=cu_rows, row_seq=row_seq, row_pos=row_pos, slot=slot)
-    _at_least(c.nseq, lens=lens, want=want, lens_out=lens_out)
-    _at_least(4, pool=pool, pool_out=pool_out)
-    _at_least(c.num_pages, free_pages=free_pages)
-    _at_least(c.nseq + 1, cu_rows=cu_rows)
-    _at_least(c.rows, row_seq=row_seq, row_pos=row_pos, slot=slot)
-    _table(c, block_table)
-    _call("dma_page_plan", ctypes.byref(c), _ptr(lens), _ptr(want), _ptr(block_table), _ptr(free_pages), _ptr(pool), _ptr(lens_out), _ptr(pool_out),
-          _ptr(cu_rows), _ptr(row_seq), _ptr(row_pos), _ptr(slot), _stream())
+        return torch.empty(n, dtype=i32, device=lens.device) if t is None else t
+    lens_out, pool_out, cu_rows = new(lens_out, nseq), new(pool_out, 4), new(cu_rows, nseq + 1)
+    row_seq, row_pos, slot = new(row_seq, rows), new(row_pos, rows), new(slot, rows)
+    _call("dma_page_plan", ctypes.byref(c), _flat("lens", lens, i32, nseq, dev), _flat("want", want, i32, nseq, dev), _table(c, block_table, dev),
+          _flat("free_pages", free_pages, i32, c.num_pages, dev), _flat("pool", pool, i32, 4, dev), _flat("lens_out", lens_out, i32, nseq, dev),
+          _flat("pool_out", pool_out, i32, 4, dev), _flat("cu_rows", cu_rows, i32, nseq + 1, dev), _flat("row_seq", row_seq, i32, rows, dev),
+          _flat("row_pos", row_pos, i32, rows, dev), _flat("slot", slot, i32, rows, dev), _stream())
     return lens_out, pool_out, cu_rows, row_seq, row_pos, slot
-
-
-def _table(c, block_table):
-    ld = c.table_ld or c.max_blocks
-    if block_table.dim() != 2 or block_table.shape[0] < c.nseq or block_table.shape[1] < c.max_blocks or (
-            block_table.stride() != (ld, 1) and any(n > 1 and a != b for n, a, b in zip(block_table.shape, block_table.stride(), (ld, 1)))):
-        raise ValueError(f"block_table: {tuple(block_table.shape)} with strides {block_table.stride()} where [{c.nseq}, {c.max_blocks}] with rows of {ld} is read")
 
 
 def dma_cache4_append(c, K, V, slot, codes, scales, delta, W_delta=None, A=None, delta_new=None):
     """Writes the rows K, V [rows, Hkv, d] into their slots, with the dynamic weights of V (W_delta [Hq, d], A [Hq]) or those given
     as delta_new [Hq, >= rows]."""
-    _rows_of(c, c.k_stride, K=K)
-    _rows_of(c, c.v_stride, V=V)
-    _on_device(torch.int32, slot=slot)
-    _at_least(c.rows, slot=slot)
-    _cache4_arrays(c, codes, scales, delta)
-    ld = 0
+    dev, rows, heads, kv_heads, d, dt = _here(), c.rows, c.Hq, c.Hkv, c.d, torch.bfloat16 if c.dtype == DMA_BF16 else torch.float32
+    given, ld, w, a = None, 0, None, None
     if delta_new is not None:
-        _on_device(torch.float32, delta_new=delta_new)
-        ld = delta_new.stride(0) if delta_new.shape[0] > 1 else max(c.rows, delta_new.shape[1])
-        if delta_new.dim() != 2 or delta_new.shape[0] < c.Hq or delta_new.shape[1] < c.rows or delta_new.stride(1) != 1:
-            raise ValueError(f"delta_new: {tuple(delta_new.shape)} where [{c.Hq}, {c.rows}] is read")
+        given, ld = _by_head("delta_new", delta_new, heads, rows, dev)
+    elif W_delta is None or A is None:
+        raise ValueError("either W_delta and A or delta_new")
     else:
-        if W_delta is None or A is None:
-            raise ValueError("either W_delta and A or delta_new")
-        _on_device(torch.float32, W_delta=W_delta, A=A)
-        _at_least(c.Hq * c.d, W_delta=W_delta)
-        _at_least(c.Hq, A=A)
-    _call("dma_cache4_append", ctypes.byref(c), _ptr(K), _ptr(V), _ptr(W_delta), _ptr(A), _ptr(delta_new), ld, _ptr(slot), _ptr(codes), _ptr(scales),
-          _ptr(delta), _stream())
+        w, a = _flat("W_delta", W_delta, torch.float32, heads * d, dev), _flat("A", A, torch.float32, heads, dev)
+    _call("dma_cache4_append", ctypes.byref(c), _row_major("K", K, dt, rows, kv_heads, d, c.k_stride, dev), _row_major("V", V, dt, rows, kv_heads, d, c.v_stride, dev),
+          w, a, given, ld, _flat("slot", slot, torch.int32, rows, dev), *_pool(c, codes, scales, delta, heads, kv_heads, d, dev), _stream())
 
 
 def dma_cache4_read(c, codes, scales, delta, slot, K=None, V=None, delta_out=None, want_delta=True):
     """The rows in the given slots: (K, V [rows, Hkv, d], delta_out [Hq, rows] or None)."""
-    dt = torch.bfloat16 if c.dtype == DMA_BF16 else torch.float32
-    K = torch.empty(c.rows, c.Hkv, c.d, dtype=dt, device=slot.device) if K is None else K
-    V = torch.empty(c.rows, c.Hkv, c.d, dtype=dt, device=slot.device) if V is None else V
+    dev, rows, heads, kv_heads, d, dt = _here(), c.rows, c.Hq, c.Hkv, c.d, torch.bfloat16 if c.dtype == DMA_BF16 else torch.float32
+    K = torch.empty(rows, kv_heads, d, dtype=dt, device=slot.device) if K is None else K
+    V = torch.empty(rows, kv_heads, d, dtype=dt, device=slot.device) if V is None else V
     if delta_out is None and want_delta:
-        delta_out = torch.empty(c.Hq, c.rows, dtype=torch.float32, device=slot.device)
-    _rows_of(c, c.k_stride, K=K)
-    _rows_of(c, c.v_stride, V=V)
-    _on_device(torch.int32, slot=slot)
-    _at_least(c.rows, slot=slot)
-    _cache4_arrays(c, codes, scales, delta)
-    ld = 0
-    if delta_out is not None:
-        _on_device(torch.float32, delta_out=delta_out)
-        ld = delta_out.stride(0) if delta_out.shape[0] > 1 else max(c.rows, delta_out.shape[1])
-        if delta_out.dim() != 2 or delta_out.shape[0] < c.Hq or delta_out.shape[1] < c.rows or delta_out.stride(1) != 1:
-            raise ValueError(f"delta_out: {tuple(delta_out.shape)} where [{c.Hq}, {c.rows}] is written")
-    _call("dma_cache4_read", ctypes.byref(c), _ptr(codes), _ptr(scales), _ptr(delta), _ptr(slot), _ptr(K), _ptr(V), _ptr(delta_out), ld, _stream())
+        delta_out = torch.empty(heads, rows, dtype=torch.float32, device=slot.device)
+    out, ld = (None, 0) if delta_out is None else _by_head("delta_out", delta_out, heads, rows, dev)
+    _call("dma_cache4_read", ctypes.byref(c), *_pool(c, codes, scales, delta, heads, kv_heads, d, dev), _flat("slot", slot, torch.int32, rows, dev),
+          _row_major("K", K, dt, rows, kv_heads, d, c.k_stride, dev), _row_major("V", V, dt, rows, kv_heads, d, c.v_stride, dev), out, ld, _stream())
     return K, V, delta_out
 
 
@@ -480,22 +479,16 @@ def dma_cache4_decode_workspace(c):
 
 def dma_cache4_decode(c, q, codes, scales, delta, block_table, row_seq, row_pos, o=None, lse=None, ws=None):
     """One step over the pages for every row; returns (o [rows, Hq, d], lse [rows, Hq])."""
+    dev, rows, heads, d, dt = _here(), c.rows, c.Hq, c.d, torch.bfloat16 if c.dtype == DMA_BF16 else torch.float32
     if o is None:
-        o = torch.empty(c.rows, c.Hq, c.d, dtype=q.dtype, device=q.device)
+        o = torch.empty(rows, heads, d, dtype=q.dtype, device=q.device)
     if lse is None:
-        lse = torch.empty(c.rows, c.Hq, dtype=torch.float32, device=q.device)
+        lse = torch.empty(rows, heads, dtype=torch.float32, device=q.device)
     if ws is None:
         ws = _ws(dma_cache4_decode_workspace(c), q.device)
-    _rows_of(c, c.q_stride, q=q)
-    _rows_of(c, c.o_stride, o=o)
-    _cache4_arrays(c, codes, scales, delta)
-    _on_device(torch.int32, block_table=block_table, row_seq=row_seq, row_pos=row_pos)
-    _on_device(torch.float32, lse=lse)
-    _at_least(c.rows, row_seq=row_seq, row_pos=row_pos)
-    _at_least(c.rows * c.Hq, lse=lse)
-    _table(c, block_table)
-    _call("dma_cache4_decode", ctypes.byref(c), _ptr(q), _ptr(codes), _ptr(scales), _ptr(delta), _ptr(block_table), _ptr(row_seq), _ptr(row_pos),
-          _ptr(o), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), _stream())
+    _call("dma_cache4_decode", ctypes.byref(c), _row_major("q", q, dt, rows, heads, d, c.q_stride, dev), *_pool(c, codes, scales, delta, heads, c.Hkv, d, dev),
+          _table(c, block_table, dev), _flat("row_seq", row_seq, torch.int32, rows, dev), _flat("row_pos", row_pos, torch.int32, rows, dev),
+          _row_major("o", o, dt, rows, heads, d, c.o_stride, dev), _flat("lse", lse, torch.float32, rows * heads, dev), _flat("ws", ws, torch.uint8, 0, dev), ws.numel(), _stream())
     return o, lse
 
 

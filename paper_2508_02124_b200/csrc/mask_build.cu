@@ -24,52 +24,6 @@ namespace {
 
 constexpr int kChunk = 256;   // the sort pads a head to a multiple of this many keys
 
-// eight consecutive channels of one value row, as loaded (converted to fp32 only when the chain runs)
-struct Raw8f { float4 a, b; };
-__device__ __forceinline__ Raw8f load_raw8(const float* p) { return {*reinterpret_cast<const float4*>(p), *reinterpret_cast<const float4*>(p + 4)}; }
-__device__ __forceinline__ uint4 load_raw8(const __nv_bfloat16* p) { return *reinterpret_cast<const uint4*>(p); }
-__device__ __forceinline__ void widen8(const Raw8f& r, float (&v)[8]) {
-    v[0] = r.a.x; v[1] = r.a.y; v[2] = r.a.z; v[3] = r.a.w; v[4] = r.b.x; v[5] = r.b.y; v[6] = r.b.z; v[7] = r.b.w;
-}
-__device__ __forceinline__ void widen8(const uint4& a, float (&v)[8]) {
-    const uint32_t u[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(u[i] << 16);
-        v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-    }
-}
-template <typename T> struct RawOf { using type = uint4; };
-template <> struct RawOf<float> { using type = Raw8f; };
-
-// Sum over the LPR lanes of a row group of NB per-lane partials (one per head of a block of NB heads), in the order of the
-// xor butterfly (adjacent lanes first: a balanced pairwise tree over the row's 8-channel chunks). The first log2(NB) levels
-// are "transposing": a lane keeps half of its values and hands the other half to its partner, so the block costs
-// log2(NB) + ... shuffles in all instead of NB log2(LPR) (the additions are the same, and IEEE addition commutes, so the
-// bits are those of the plain butterfly). On return p[0] of lane `sub` is the complete sum of head bitrev(sub mod NB) of
-// the block (the same value in every lane of the group with those low bits).
-template <int NB, int LPR>
-__device__ __forceinline__ void block_reduce(float (&p)[NB], int sub) {
-    int keep = NB >> 1;
-#pragma unroll
-    for (int m = 1; m < LPR; m <<= 1) {
-        if (keep >= 1) {
-            const bool up = (sub & m) != 0;
-#pragma unroll
-            for (int q = 0; q < NB / 2; ++q) {
-                if (q < keep) {
-                    const float stay = up ? p[q + keep] : p[q];
-                    const float give = up ? p[q] : p[q + keep];
-                    p[q] = __fadd_rn(stay, __shfl_xor_sync(0xffffffffu, give, m));
-                }
-            }
-            keep >>= 1;
-        } else {
-            p[0] = __fadd_rn(p[0], __shfl_xor_sync(0xffffffffu, p[0], m));
-        }
-    }
-}
-
 // One CTA: tiles of kRows consecutive keys of one (batch, KV head), taken in turn with the other CTAs of that pair (grid-
 // stride); writes delta for the G query heads of the group. A group of D/8 lanes owns a row: each lane forms the fma chain
 // over its 8 channels, an xor butterfly adds adjacent partials pairwise (IEEE addition commutes, so every lane of the group
