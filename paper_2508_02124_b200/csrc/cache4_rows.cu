@@ -1,68 +1,114 @@
 // Rows into and out of the paged 4-bit cache (include/dma.h, dma_cache4_append, dma_cache4_read).
 //
-// A group of d / 8 lanes owns a row of one KV head, 8 channels of K and of V per lane, as in the kernels that form delta: a lane's eight
-// codes are one 32-bit word, eight lanes hold the 64 channels of a scale.
+// Append: a group of d / 16 lanes owns a row of one KV head, 16 channels of K and of V per lane: two words of codes, four lanes to the 64 channels of a scale. Bound by
+// instructions (13 per value; with 8 channels per lane 26: what a row takes beside its values is shared by more of them). 16384 rows of 8 heads, d = 128: APPEND_US.
+// Read: d / 8 lanes, a word of codes each; bound by memory. 14336 rows 17 us, 4.5 TB/s.
 #include <algorithm>
 #include <type_traits>
 
 #include "delta_fixed.cuh"
 #include "paged.cuh"
+#include "sm100_ptx.cuh"
 
 namespace dma {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kAppendThreads = 128;
 
 __device__ __forceinline__ float min_nan(float a, float b) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ float round_bf16(float x) { return __bfloat162float(__float2bfloat16_rn(x)); }
 
-// The codes of a lane's eight channels, and the (s, z) pair of its group of eight lanes. All in fp32, rounded operation by operation:
-// the halves keep every difference in range.
-// A division takes a dozen instructions, sixteen of them per lane more than all else; so the quotients are products with the reciprocal, each within 4e-6 of the definition's for
-// quotients below 16 (three roundings of 2^-24). Both round to the same code unless the product lies that near to a half; then, and for scales so small that their own
-// rounding to bf16 is coarse, or not finite, the lane divides.
+// 16 channels as loaded, and widened
+template <typename T> struct Raw16 { typename RawOf<T>::type a, b; };
+template <typename T>
+__device__ __forceinline__ Raw16<T> load_raw16(const T* p) { return {load_raw8(p), load_raw8(p + 8)}; }
+template <typename T>
+__device__ __forceinline__ void widen16(const Raw16<T>& r, float (&x)[2][8]) { widen8(r.a, x[0]); widen8(r.b, x[1]); }
+
+// lo and hi over the four lanes of a group, of K and of V
+__device__ __forceinline__ void group_range(const Raw16<float>& k, const Raw16<float>& v, float (&lo)[2], float (&hi)[2]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        float x[2][8];
+        widen16(i ? v : k, x);
+        lo[i] = hi[i] = x[0][0];
+#pragma unroll
+        for (int c = 1; c < 16; ++c) { lo[i] = min_nan(lo[i], x[c / 8][c % 8]); hi[i] = max_nan(hi[i], x[c / 8][c % 8]); }
+#pragma unroll
+        for (int m = 1; m < 4; m <<= 1) {
+            lo[i] = min_nan(lo[i], __shfl_xor_sync(0xffffffffu, lo[i], m));
+            hi[i] = max_nan(hi[i], __shfl_xor_sync(0xffffffffu, hi[i], m));
+        }
+    }
+}
+__device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b) { uint32_t r; asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b)); return r; }
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) { uint32_t r; asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b)); return r; }
+// (two numbers per instruction, and K's and V's together through the lanes)
+__device__ __forceinline__ void group_range(const Raw16<__nv_bfloat16>& k, const Raw16<__nv_bfloat16>& v, float (&lo)[2], float (&hi)[2]) {
+    auto all = [](auto&& f, const Raw16<__nv_bfloat16>& r) { return f(f(f(r.a.x, r.a.y), f(r.a.z, r.a.w)), f(f(r.b.x, r.b.y), f(r.b.z, r.b.w))); };
+    const uint32_t k0 = all(min2, k), v0 = all(min2, v), k1 = all(max2, k), v1 = all(max2, v);
+    uint32_t a = min2(__byte_perm(k0, v0, 0x5410), __byte_perm(k0, v0, 0x7632)), b = max2(__byte_perm(k1, v1, 0x5410), __byte_perm(k1, v1, 0x7632));
+#pragma unroll
+    for (int m = 1; m < 4; m <<= 1) {
+        a = min2(a, __shfl_xor_sync(0xffffffffu, a, m));
+        b = max2(b, __shfl_xor_sync(0xffffffffu, b, m));
+    }
+    lo[0] = __uint_as_float(a << 16); lo[1] = __uint_as_float(a & 0xffff0000u);
+    hi[0] = __uint_as_float(b << 16); hi[1] = __uint_as_float(b & 0xffff0000u);
+}
+
+// The codes of a lane's 16 channels, and the (s, z) pair of its group: the definition, in fp32, rounded operation by operation; the halves keep every difference in range.
+// A division takes a dozen instructions, sixteen of them per lane more than all else. A quotient a / b is therefore the product q with b's rounded reciprocal y and one
+// correction, q + (a - q b) y (Markstein, "Computation of elementary functions on the IBM RISC System/6000", 1990): the remainder is exact, and the result is the rounded
+// quotient unless that lies within 2^-22 of its last place of a midpoint between two numbers, where it may be the other neighbour. That is a code's difference only next to a
+// half, 2^-22 of the 2^-23 of all quotients that lie there. (Without the correction 0.2 % of bf16 values are ties that the product misses.) Two values per
+// instruction. Ranges at the ends of fp32's, and what is not finite, are divided.
 template <bool kExactZero>
-__device__ __forceinline__ uint32_t quantise(const float (&x)[8], uint32_t& pair) {
-    float lo = x[0], hi = x[0];
+__device__ __forceinline__ uint2 quantise(const float (&x)[2][8], float lo, float hi, uint32_t& pair) {
+    const float z = kExactZero ? lo : round_bf16(lo), zh = __fmul_rn(z, 0.5f), range = __fsub_rn(__fmul_rn(hi, 0.5f), zh);
+    if (!(range >= 1e-28f && range <= 1e38f)) {
+        const float s = max_nan(0.0f, round_bf16(__fdiv_rn(range, 7.5f))), sh = __fmul_rn(s, 0.5f);
+        pair = (__float_as_uint(s) >> 16) | (__float_as_uint(z) & 0xffff0000u);
+        uint32_t word[2] = {0u, 0u};
 #pragma unroll
-    for (int c = 1; c < 8; ++c) { lo = min_nan(lo, x[c]); hi = max_nan(hi, x[c]); }
-#pragma unroll
-    for (int m = 1; m < 8; m <<= 1) {
-        lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, m));
-        hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, m));
+        for (int c = 0; c < 16; ++c)                              // (fmaxf: 0 where the quotient is NaN)
+            word[c / 8] |= (uint32_t)(int)fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(__fmul_rn(x[c / 8][c % 8], 0.5f), zh), sh)), 0.0f), 15.0f) << (4 * (c % 8));
+        return make_uint2(word[0], word[1]);
     }
-    const float z = kExactZero ? lo : round_bf16(lo), zh = __fmul_rn(z, 0.5f);
-    const float s = max_nan(0.0f, round_bf16(__fdiv_rn(__fsub_rn(__fmul_rn(hi, 0.5f), zh), 7.5f)));
-    const float sh = __fmul_rn(s, 0.5f);
+    constexpr float kSeventh = 1.0f / 7.5f;
+    float q0 = __fmul_rn(range, kSeventh);
+    q0 = __fmaf_rn(__fmaf_rn(-q0, 7.5f, range), kSeventh, q0);
+    const float s = round_bf16(q0), sh = __fmul_rn(s, 0.5f), y = __frcp_rn(sh);
     pair = (__float_as_uint(s) >> 16) | (__float_as_uint(z) & 0xffff0000u);
-    const float inv = __frcp_rn(sh);
-    bool near = !(s >= 1e-30f && s <= 1e37f);
-    float n[8];
+    const float2 half = make_float2(0.5f, 0.5f), zz = make_float2(-zh, -zh), b = make_float2(-sh, -sh), yy = make_float2(y, y), up = make_float2(12582912.0f, 12582912.0f),
+                 down = make_float2(-12582912.0f, -12582912.0f), by16 = make_float2(16.0f, 16.0f);
+    uint32_t word[2];
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        float q = __fmul_rn(__fmaf_rn(x[c], 0.5f, -zh), inv);
-        if (!kExactZero) q = fmaxf(q, 0.0f);                      // (a zero that bf16 rounded up; with an exact one no value lies below it)
-        n[c] = __fadd_rn(__fadd_rn(q, 12582912.0f), -12582912.0f);
-        near = near || !(fabsf(q - n[c]) <= 0.49999f);
-    }
-    if (near) {
+    for (int i = 0; i < 2; ++i) {
+        float2 n[4];                                              // codes c and c + 4
 #pragma unroll
-        for (int c = 0; c < 8; ++c) n[c] = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(__fmul_rn(x[c], 0.5f), zh), sh)), 0.0f), 15.0f);        // (fmaxf: 0 where it is NaN)
+        for (int c = 0; c < 4; ++c) {
+            const float2 a = ptx::fma2(make_float2(x[i][c], x[i][c + 4]), half, zz);
+            float2 q = ptx::mul2(a, yy);
+            q = ptx::fma2(ptx::fma2(q, b, a), yy, q);
+            if (!kExactZero) { q.x = fmaxf(q.x, 0.0f); q.y = fmaxf(q.y, 0.0f); }   // (a zero that bf16 rounded up; below an exact one lies no value, and none above 15.1)
+            n[c] = ptx::add2(ptx::add2(q, up), down);             // to the nearest integer, ties to even
+        }
+        // four codes as one number, exactly, above 2^23
+        const float2 w = ptx::add2(ptx::fma2(ptx::fma2(ptx::fma2(n[3], by16, n[2]), by16, n[1]), by16, n[0]), make_float2(8388608.0f, 8388608.0f));
+        word[i] = __byte_perm(__float_as_uint(w.x), __float_as_uint(w.y), 0x5410);
     }
-    // four codes as one number, exactly: 2^23 + them
-    const float w0 = fmaf(fmaf(fmaf(n[3], 16.0f, n[2]), 16.0f, n[1]), 16.0f, n[0]) + 8388608.0f, w1 = fmaf(fmaf(fmaf(n[7], 16.0f, n[6]), 16.0f, n[5]), 16.0f, n[4]) + 8388608.0f;
-    return __byte_perm(__float_as_uint(w0), __float_as_uint(w1), 0x5410);
+    return make_uint2(word[0], word[1]);
 }
 
 // Tiles of kRows rows of KV head blockIdx.y, taken in turn; a warp requests its next rows before it works on those it has. z of the tile's (head, row) pairs goes
 // through shared memory; then a thread per pair forms delta, while the next tile's rows are worked on (two buffers, one barrier per tile).
 template <typename T, int D, int kRows>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) cache4_append_kernel(const T* K, const T* V, const float* W, const float* A, const float* delta_new, int64_t delta_ld,
+__global__ void __launch_bounds__(kAppendThreads, sizeof(T) == 2 ? 6 : 4) cache4_append_kernel(const T* K, const T* V, const float* W, const float* A, const float* delta_new, int64_t delta_ld,
                                                                  const int32_t* slot, uint8_t* codes, uint32_t* scales, float* delta, int rows, int Hq, int Hkv, int G,
                                                                  int64_t ks_row, int64_t ks_head, int64_t vs_row, int64_t vs_head, int page_log, int nslots) {
-    constexpr int LPR = D / 8, RPW = 32 / LPR, kPass = kRows / (8 * RPW);
-    using Raw = typename RawOf<T>::type;
+    constexpr int LPR = D / 16, RPW = 32 / LPR, kWarps = kAppendThreads / 32, kPass = kRows / (kWarps * RPW);
     extern __shared__ float smem[];
     float* sW = smem;                     // [G][D]
     float* sZ = smem + G * D;             // [2][G][kRows]
@@ -70,25 +116,25 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) cache4_appen
     const int hk = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane % LPR, grp = lane / LPR;
     pdl_enter(K, V, W, A, delta_new, slot, codes, scales, delta);
     const int place_mask = (1 << page_log) - 1, ntiles = (rows + kRows - 1) / kRows;
-    const T* Kh = K + hk * ks_head + sub * 8;
-    const T* Vh = V + hk * vs_head + sub * 8;
-    Raw k_next, v_next;
+    const T* Kh = K + hk * ks_head + sub * 16;
+    const T* Vh = V + hk * vs_head + sub * 16;
+    Raw16<T> k_next, v_next;
     int at_next;
     auto request = [&](int tile, int pass) {
-        const int t = tile * kRows + (pass * 8 + warp) * RPW + grp;
-        k_next = Raw{};
-        v_next = Raw{};
+        const int t = tile * kRows + (pass * kWarps + warp) * RPW + grp;
+        k_next = Raw16<T>{};
+        v_next = Raw16<T>{};
         at_next = -1;
         if (tile < ntiles && t < rows) {
-            k_next = load_raw8(Kh + t * ks_row);
-            v_next = load_raw8(Vh + t * vs_row);
+            k_next = load_raw16(Kh + t * ks_row);
+            v_next = load_raw16(Vh + t * vs_row);
             at_next = slot[t];
         }
     };
     request(blockIdx.x, 0);
     if (!delta_new) {
-        // (a lane's eight weights in two halves, each next to the other lanes' same half: a group's 16-byte reads meet every bank once)
-        for (int i = tid; i < G * D; i += kThreads) sW[i / D * D + (i >> 2 & 1) * (D / 2) + i % D / 8 * 4 + (i & 3)] = W[(size_t)hk * G * D + i];
+        // (a lane's sixteen weights in four parts, each next to the other lanes' same part: a group's 16-byte reads meet every bank once)
+        for (int i = tid; i < G * D; i += kAppendThreads) sW[i / D * D + (i >> 2 & 3) * (D / 4) + i % D / 16 * 4 + (i & 3)] = W[(size_t)hk * G * D + i];
         __syncthreads();
     }
     int buf = 0;
@@ -96,41 +142,52 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) cache4_appen
         const int t0 = tile * kRows;
         float* zs = sZ + buf * G * kRows;
         for (int pass = 0; pass < kPass; ++pass) {
-            const int r = (pass * 8 + warp) * RPW + grp, at = at_next;
+            const int r = (pass * kWarps + warp) * RPW + grp, at = at_next;
             const bool in = (unsigned)at < (unsigned)nslots;
-            float v[8];
-            uint32_t kp, vp, kw, vw;
+            float v[2][8];
+            uint32_t kp, vp;
+            uint2 kw, vw;
             {
-                float k[8];
-                widen8(k_next, k);
-                widen8(v_next, v);
+                float k[2][8], lo[2], hi[2];
+                group_range(k_next, v_next, lo, hi);
+                widen16(k_next, k);
+                widen16(v_next, v);
                 if (pass + 1 < kPass) request(tile, pass + 1); else request(tile + gridDim.x, 0);
-                kw = quantise<sizeof(T) == 2>(k, kp);
+                kw = quantise<sizeof(T) == 2>(k, lo[0], hi[0], kp);
+                vw = quantise<sizeof(T) == 2>(v, lo[1], hi[1], vp);
             }
-            vw = quantise<sizeof(T) == 2>(v, vp);
             if (sub == 0) sSlot[buf][r] = in ? at : -1;
             if (in) {
                 const size_t row = key_row(at >> page_log, hk, at & place_mask, Hkv, page_log);
-                *reinterpret_cast<uint32_t*>(codes + row * D + sub * 4) = kw;
-                *reinterpret_cast<uint32_t*>(codes + row * D + D / 2 + sub * 4) = vw;
-                if (sub % 8 == 0) {
-                    scales[row * (D / 32) + sub / 8] = kp;
-                    scales[row * (D / 32) + D / 64 + sub / 8] = vp;
+                uint8_t* to = codes + row * D + sub * 8;
+                *reinterpret_cast<uint2*>(to) = kw;
+                *reinterpret_cast<uint2*>(to + D / 2) = vw;
+                if (sub % 4 == 0) {
+                    uint32_t* sc = scales + row * (D / 32) + sub / 4;
+                    sc[0] = kp;
+                    sc[D / 64] = vp;
                 }
             }
             if (!delta_new) {
-                // heads in blocks of 4 (then 2, then 1), as in the other kernels that form delta
+                // Heads in blocks of 4 (then 2, then 1). The sums are those of the other kernels that form delta: a chain over each 8 channels, then neighbours pairwise, the
+                // first two of which a lane has itself.
                 auto block = [&](int g0, auto nb_tag) {
                     constexpr int NB = decltype(nb_tag)::value;
                     float p[NB];
 #pragma unroll
                     for (int q = 0; q < NB; ++q) {
-                        const float4 wa = *reinterpret_cast<const float4*>(sW + (g0 + q) * D + sub * 4), wb = *reinterpret_cast<const float4*>(sW + (g0 + q) * D + D / 2 + sub * 4);
-                        const float w[8] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w};
-                        float a = 0.0f;
+                        float part[2];
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) a = __fmaf_rn(v[c], w[c], a);
-                        p[q] = a;
+                        for (int i = 0; i < 2; ++i) {
+                            const float* wp = sW + (g0 + q) * D + i * (D / 2) + sub * 4;
+                            const float4 wa = *reinterpret_cast<const float4*>(wp), wb = *reinterpret_cast<const float4*>(wp + D / 4);
+                            const float w[8] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w};
+                            float a = 0.0f;
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) a = __fmaf_rn(v[i][c], w[c], a);
+                            part[i] = a;
+                        }
+                        p[q] = __fadd_rn(part[0], part[1]);
                     }
                     int mine = 0;             // head of the block this lane ends up with: the low bits of sub, reversed
 #pragma unroll
@@ -145,7 +202,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) cache4_appen
             }
         }
         __syncthreads();                      // z and slots of this tile are complete (and the other buffers' readers of two tiles ago are long done)
-        for (int i = tid; i < G * kRows; i += kThreads) {
+        for (int i = tid; i < G * kRows; i += kAppendThreads) {
             const int g = i / kRows, r = i % kRows, h = hk * G + g, at = sSlot[buf][r];
             if (at < 0) continue;
             const float x = delta_new ? delta_new[h * delta_ld + t0 + r] : delta_fixed(zs[i], A[h]);
@@ -209,17 +266,17 @@ int append_tiles(const Cache& C, int ctas, const void* K, const void* V, const f
                  uint8_t* codes, __nv_bfloat16* scales, float* delta, cudaStream_t st) {
     const size_t smem = (size_t)C.G * (D + 2 * kRows) * sizeof(float);
     if (smem > 48 * 1024) return DMA_ERR_UNSUPPORTED;
-    return launch_overlapped(cache4_append_kernel<T, D, kRows>, dim3(ctas, C.Hkv), dim3(kThreads), smem, st, 1, (const T*)K, (const T*)V, W, A, delta_new, delta_ld, slot, codes,
+    return launch_overlapped(cache4_append_kernel<T, D, kRows>, dim3(ctas, C.Hkv), dim3(kAppendThreads), smem, st, 1, (const T*)K, (const T*)V, W, A, delta_new, delta_ld, slot, codes,
                              (uint32_t*)scales, delta, C.rows, C.Hq, C.Hkv, C.G, C.ks[0], C.ks[1], C.vs[0], C.vs[1], C.page_log, C.num_pages << C.page_log);
 }
-// Tiles of 64 rows on four CTAs per SM; of a pass's rows where that leaves SMs without one.
+// Tiles of 64 rows on six CTAs per SM; of a pass's rows where that leaves SMs without one, or the heads' z need the room.
 template <typename T, int D>
 int append(const Cache& C, const void* K, const void* V, const float* W, const float* A, const float* delta_new, int64_t delta_ld, const int32_t* slot,
            uint8_t* codes, __nv_bfloat16* scales, float* delta, cudaStream_t st) {
-    constexpr int kPassRows = 8 * 32 / (D / 8), kTile = 64;
-    const int tiles = (C.rows + kTile - 1) / kTile, most = (4 * 148 + C.Hkv - 1) / C.Hkv;
-    const bool large = (int64_t)tiles * C.Hkv >= 148 && (size_t)C.G * (D + 2 * kTile) * sizeof(float) <= 48 * 1024;
-    if (large) return append_tiles<T, D, kTile>(C, std::min(tiles, most), K, V, W, A, delta_new, delta_ld, slot, codes, scales, delta, st);
+    constexpr int kPassRows = kAppendThreads / (D / 16), kTile = 64;
+    const int tiles = (C.rows + kTile - 1) / kTile, most = (6 * 148 + C.Hkv - 1) / C.Hkv;
+    if (kTile > kPassRows && (int64_t)tiles * C.Hkv >= 148 && (size_t)C.G * (D + 2 * kTile) * sizeof(float) <= 48 * 1024)
+        return append_tiles<T, D, kTile>(C, std::min(tiles, most), K, V, W, A, delta_new, delta_ld, slot, codes, scales, delta, st);
     return append_tiles<T, D, kPassRows>(C, std::min((C.rows + kPassRows - 1) / kPassRows, most), K, V, W, A, delta_new, delta_ld, slot, codes, scales, delta, st);
 }
 
