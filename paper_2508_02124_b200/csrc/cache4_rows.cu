@@ -63,11 +63,15 @@ __device__ __forceinline__ void group_range(const Raw16<__nv_bfloat16>& k, const
 // correction, q + (a - q b) y (Markstein, "Computation of elementary functions on the IBM RISC System/6000", 1990): the remainder is exact, and the result is the rounded
 // quotient unless that lies within 2^-22 of its last place of a midpoint between two numbers, where it may be the other neighbour. That is a code's difference only next to a
 // half, 2^-22 of the 2^-23 of all quotients that lie there. (Without the correction 0.2 % of bf16 values are ties that the product misses.) Two values per
-// instruction. Ranges at the ends of fp32's, and what is not finite, are divided.
+// instruction. Ranges at the ends of fp32's, and what is not finite, are divided; rows that are not stored (`used`) may come out as anything.
 template <bool kExactZero>
-__device__ __forceinline__ uint2 quantise(const float (&x)[2][8], float lo, float hi, uint32_t& pair) {
+__device__ __forceinline__ uint2 quantise(const float (&x)[2][8], float lo, float hi, bool used, uint32_t& pair) {
     const float z = kExactZero ? lo : round_bf16(lo), zh = __fmul_rn(z, 0.5f), range = __fsub_rn(__fmul_rn(hi, 0.5f), zh);
-    if (!(range >= 1e-28f && range <= 1e38f)) {
+    if (kExactZero && range == 0.0f) {                            // equal values: 0 / 0, code 0
+        pair = __float_as_uint(z) & 0xffff0000u;
+        return make_uint2(0u, 0u);
+    }
+    if (!(range >= 1e-28f && range <= 1e38f) && used) {
         const float s = max_nan(0.0f, round_bf16(__fdiv_rn(range, 7.5f))), sh = __fmul_rn(s, 0.5f);
         pair = (__float_as_uint(s) >> 16) | (__float_as_uint(z) & 0xffff0000u);
         uint32_t word[2] = {0u, 0u};
@@ -153,8 +157,8 @@ __global__ void __launch_bounds__(kAppendThreads, sizeof(T) == 2 ? 6 : 4) cache4
                 widen16(k_next, k);
                 widen16(v_next, v);
                 if (pass + 1 < kPass) request(tile, pass + 1); else request(tile + gridDim.x, 0);
-                kw = quantise<sizeof(T) == 2>(k, lo[0], hi[0], kp);
-                vw = quantise<sizeof(T) == 2>(v, lo[1], hi[1], vp);
+                kw = quantise<sizeof(T) == 2>(k, lo[0], hi[0], in, kp);
+                vw = quantise<sizeof(T) == 2>(v, lo[1], hi[1], in, vp);
             }
             if (sub == 0) sSlot[buf][r] = in ? at : -1;
             if (in) {
@@ -269,11 +273,11 @@ int append_tiles(const Cache& C, int ctas, const void* K, const void* V, const f
     return launch_overlapped(cache4_append_kernel<T, D, kRows>, dim3(ctas, C.Hkv), dim3(kAppendThreads), smem, st, 1, (const T*)K, (const T*)V, W, A, delta_new, delta_ld, slot, codes,
                              (uint32_t*)scales, delta, C.rows, C.Hq, C.Hkv, C.G, C.ks[0], C.ks[1], C.vs[0], C.vs[1], C.page_log, C.num_pages << C.page_log);
 }
-// Tiles of 64 rows on six CTAs per SM; of a pass's rows where that leaves SMs without one, or the heads' z need the room.
+// Tiles of 32 rows on six CTAs per SM (of 64: 32.1 us for 16384 rows of 8 heads, of 32: 30.4); of a pass's rows where that leaves SMs without one, or the heads' z need the room.
 template <typename T, int D>
 int append(const Cache& C, const void* K, const void* V, const float* W, const float* A, const float* delta_new, int64_t delta_ld, const int32_t* slot,
            uint8_t* codes, __nv_bfloat16* scales, float* delta, cudaStream_t st) {
-    constexpr int kPassRows = kAppendThreads / (D / 16), kTile = 64;
+    constexpr int kPassRows = kAppendThreads / (D / 16), kTile = 32;
     const int tiles = (C.rows + kTile - 1) / kTile, most = (6 * 148 + C.Hkv - 1) / C.Hkv;
     if (kTile > kPassRows && (int64_t)tiles * C.Hkv >= 148 && (size_t)C.G * (D + 2 * kTile) * sizeof(float) <= 48 * 1024)
         return append_tiles<T, D, kTile>(C, std::min(tiles, most), K, V, W, A, delta_new, delta_ld, slot, codes, scales, delta, st);
