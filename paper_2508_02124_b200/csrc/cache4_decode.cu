@@ -702,7 +702,7 @@ struct AttnShape {
     using Query = uint2[NG][4][32];                               // operand fragments, the same for every warp
     static constexpr size_t kBytes = sizeof(Warp) * kWarps > sizeof(Merge) ? sizeof(Warp) * kWarps : sizeof(Merge);
 };
-constexpr int kAttnCtas = 4 * 148;
+constexpr int kAttnCtas = 3 * 148;
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
 __device__ __forceinline__ void cp8(uint32_t dst, const void* src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory"); }
@@ -955,7 +955,7 @@ __device__ __forceinline__ int warp_find(const int32_t* first, int n, int x) {
 }
 
 template <int D, int kH>
-__global__ void __launch_bounds__(kThreads, 4) attn_kernel(AttnArgs A) {
+__global__ void __launch_bounds__(kThreads, 3) attn_kernel(AttnArgs A) {
     using Sh = AttnShape<D, kH>;
     constexpr int NG = Sh::NG, kCols = Sh::kCols, kPitch = Sh::kPitch;
     extern __shared__ __align__(16) uint8_t attn_smem[];
@@ -972,7 +972,7 @@ __global__ void __launch_bounds__(kThreads, 4) attn_kernel(AttnArgs A) {
     const int cta = blockIdx.x;
     if (A.plan.ustart) {
         U = A.plan.ustart[A.rows];
-        E = min((int)gridDim.x, max(U / 4, 1));                   // (four units at least)
+        E = min((int)gridDim.x, max(U / 2, 1));                   // (four units at least)
         if (cta >= E || U == 0) return;
         at = (int)((int64_t)cta * U / E);
         until = (int)((int64_t)(cta + 1) * U / E);
@@ -1003,6 +1003,29 @@ __global__ void __launch_bounds__(kThreads, 4) attn_kernel(AttnArgs A) {
         }
         const int hk = i / A.hb, h0 = hk * A.G + (i % A.hb) * A.hpb, heads = min(A.hpb, (hk + 1) * A.G - h0);
         const int32_t* pages = R.table + seq * R.ld;
+        // 64 keys per turn, a lane's two neighbouring keys in every head, requested kAhead turns before they are tested
+        constexpr int kAhead = kH <= 4 ? 2 : 1;
+        float2 dl[kAhead][kH];
+        int page[kAhead];
+        auto page_of = [&](int j) {
+            if (j >= k1) return -1;
+            const int p = pages[j >> R.page_log];
+            return (unsigned)p < (unsigned)R.num_pages ? p : -1;
+        };
+        const float* plane = R.delta + ((size_t)h0 << R.page_log);
+        auto request = [&](int a, int j, int p) {
+            page[a] = p;
+            const float* src = plane + (size_t)p * ((uint32_t)R.Hq << R.page_log) + (j & R.mask());
+#pragma unroll
+            for (int h = 0; h < kH; ++h) {
+                dl[a][h] = make_float2(0.0f, 0.0f);
+                if (p >= 0 && h < heads) dl[a][h] = *reinterpret_cast<const float2*>(src + (h << R.page_log));
+            }
+        };
+        int j = k0 + warp * 64;
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) request(a, j + a * kWarps * 64 + 2 * lane, page_of(j + a * kWarps * 64 + 2 * lane));
+        int after = page_of(j + kAhead * kWarps * 64 + 2 * lane);
         unsigned long long least[kH];
 #pragma unroll
         for (int h = 0; h < kH; ++h) least[h] = h >= heads ? ~0ull : A.weakest ? A.weakest[t * R.Hq + h0 + h] : 0ull;
@@ -1096,29 +1119,6 @@ __global__ void __launch_bounds__(kThreads, 4) attn_kernel(AttnArgs A) {
                 if constexpr (D == 128) cp16(dst + lane * kPitch + D, src); else cp8(dst + lane * kPitch + D, src);
             }
         };
-        // 64 keys per turn, a lane's two neighbouring keys in every head, requested kAhead turns before they are tested
-        constexpr int kAhead = kH <= 4 ? 2 : 1;
-        float2 dl[kAhead][kH];
-        int page[kAhead];
-        auto page_of = [&](int j) {
-            if (j >= k1) return -1;
-            const int p = pages[j >> R.page_log];
-            return (unsigned)p < (unsigned)R.num_pages ? p : -1;
-        };
-        const float* plane = R.delta + ((size_t)h0 << R.page_log);
-        auto request = [&](int a, int j, int p) {
-            page[a] = p;
-            const float* src = plane + (size_t)p * ((uint32_t)R.Hq << R.page_log) + (j & R.mask());
-#pragma unroll
-            for (int h = 0; h < kH; ++h) {
-                dl[a][h] = make_float2(0.0f, 0.0f);
-                if (p >= 0 && h < heads) dl[a][h] = *reinterpret_cast<const float2*>(src + (h << R.page_log));
-            }
-        };
-        int j = k0 + warp * 64;
-#pragma unroll
-        for (int a = 0; a < kAhead; ++a) request(a, j + a * kWarps * 64 + 2 * lane, page_of(j + a * kWarps * 64 + 2 * lane));
-        int after = page_of(j + kAhead * kWarps * 64 + 2 * lane);
         while (true) {
             // keys are queued until a batch is full
             while (j < k1 && tail - issued * kBatch < kBatch) {
@@ -1215,6 +1215,12 @@ __global__ void __launch_bounds__(kThreads, 4) attn_kernel(AttnArgs A) {
         const bool whole = !A.plan.ustart || (u0 >= begin && u1 <= until);
         const int item = t * per_row + i;
         float* slot = A.partial + (size_t)(2 * cta + (u0 > begin ? 1 : 0)) * kCols * (D + 2);
+        auto write_out = [&](int h, int c, float top, float sum, const float (&v)[4]) {
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            __nv_bfloat162 lo = __floats2bfloat162_rn(v[0] * inv, v[1] * inv), hi = __floats2bfloat162_rn(v[2] * inv, v[3] * inv);
+            *reinterpret_cast<uint2*>(A.o + t * A.os_row + (h0 + h) * A.os_head + c) = make_uint2(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi));
+            if (c == 0) A.lse[t * R.Hq + h0 + h] = sum == 0.0f ? -INFINITY : top + logf(sum);
+        };
         // thread: four channels of a head
         for (int e = tid; e < heads * (D / 4); e += kThreads) {
             const int h = e / (D / 4), c = e % (D / 4) * 4;
@@ -1230,10 +1236,7 @@ __global__ void __launch_bounds__(kThreads, 4) attn_kernel(AttnArgs A) {
                 v[0] = fmaf(a.x, f, v[0]); v[1] = fmaf(a.y, f, v[1]); v[2] = fmaf(a.z, f, v[2]); v[3] = fmaf(a.w, f, v[3]);
             }
             if (whole) {
-                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                __nv_bfloat162 lo = __floats2bfloat162_rn(v[0] * inv, v[1] * inv), hi = __floats2bfloat162_rn(v[2] * inv, v[3] * inv);
-                *reinterpret_cast<uint2*>(A.o + t * A.os_row + (h0 + h) * A.os_head + c) = make_uint2(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi));
-                if (c == 0) A.lse[t * R.Hq + h0 + h] = sum == 0.0f ? -INFINITY : top + logf(sum);
+                write_out(h, c, top, sum, v);
             } else {
                 *reinterpret_cast<float4*>(slot + 2 * kCols + h * D + c) = make_float4(v[0], v[1], v[2], v[3]);
                 if (c == 0) { slot[2 * h] = top; slot[2 * h + 1] = sum; }
@@ -1248,27 +1251,51 @@ __global__ void __launch_bounds__(kThreads, 4) attn_kernel(AttnArgs A) {
             __syncthreads();
             if (sTicket == pieces - 1) {
                 __threadfence();
-                auto piece = [&](int c) {
-                    const int first = (int)((int64_t)c * U / E);
-                    return A.partial + (size_t)(2 * c + (u0 > first ? 1 : 0)) * kCols * (D + 2);
-                };
-                for (int e = tid; e < heads * (D / 4); e += kThreads) {
-                    const int h = e / (D / 4), c = e % (D / 4) * 4;
-                    float top = -3.4e38f;
-                    for (int x = c0; x <= c1; ++x) top = fmaxf(top, __ldcg(piece(x) + 2 * h));
-                    float sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-                    for (int x = c0; x <= c1; ++x) {
-                        const float* s = piece(x);
-                        const float f = ex2f((__ldcg(s + 2 * h) - top) * kLog2e);
-                        const float4 a = __ldcg(reinterpret_cast<const float4*>(s + 2 * kCols + h * D + c));
-                        sum = fmaf(__ldcg(s + 2 * h + 1), f, sum);
-                        v[0] = fmaf(a.x, f, v[0]); v[1] = fmaf(a.y, f, v[1]); v[2] = fmaf(a.z, f, v[2]); v[3] = fmaf(a.w, f, v[3]);
+                // (only the first piece can lie in its CTA's second place)
+                constexpr int kSlot = kCols * (D + 2);
+                const float* head_piece = A.partial + (size_t)(2 * c0 + (u0 > (int)((int64_t)c0 * U / E) ? 1 : 0)) * kSlot;
+                const float* rest = A.partial + (size_t)2 * c0 * kSlot;
+                auto piece = [&](int x) { return x == 0 ? head_piece : rest + (size_t)2 * x * kSlot; };
+                // maxima and sums of a chunk of pieces by a thread each, then every piece's values
+                constexpr int kChunk = kThreads / kCols;
+                float2* sml = reinterpret_cast<float2*>(attn_smem);
+                float top[2], sum[2], v[2][4];
+                constexpr int kTurns = kCols * D / 4 / kThreads < 1 ? 1 : kCols * D / 4 / kThreads;   // (head, four channels) pairs of a thread
+#pragma unroll
+                for (int n = 0; n < kTurns; ++n) {
+                    top[n] = -3.4e38f;
+                    sum[n] = v[n][0] = v[n][1] = v[n][2] = v[n][3] = 0.0f;
+                }
+                for (int x0 = 0; x0 < pieces; x0 += kChunk) {
+                    const int count = min(kChunk, pieces - x0);
+                    __syncthreads();
+                    if (tid < count * kCols) sml[tid] = __ldcg(reinterpret_cast<const float2*>(piece(x0 + tid / kCols)) + tid % kCols);
+                    __syncthreads();
+#pragma unroll
+                    for (int n = 0; n < kTurns; ++n) {
+                        const int e = tid + n * kThreads, h = e / (D / 4), c = e % (D / 4) * 4;
+                        if (h >= heads) continue;
+                        float most = top[n];
+                        for (int x = 0; x < count; ++x) most = fmaxf(most, sml[x * kCols + h].x);
+                        const float fade = ex2f((top[n] - most) * kLog2e);
+                        top[n] = most;
+                        sum[n] *= fade;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) v[n][k] *= fade;
+#pragma unroll 8
+                        for (int x = 0; x < count; ++x) {
+                            const float2 ml = sml[x * kCols + h];
+                            const float f = ex2f((ml.x - most) * kLog2e);
+                            const float4 a = __ldcg(reinterpret_cast<const float4*>(piece(x0 + x) + 2 * kCols + h * D + c));
+                            sum[n] = fmaf(ml.y, f, sum[n]);
+                            v[n][0] = fmaf(a.x, f, v[n][0]); v[n][1] = fmaf(a.y, f, v[n][1]); v[n][2] = fmaf(a.z, f, v[n][2]); v[n][3] = fmaf(a.w, f, v[n][3]);
+                        }
                     }
-                    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                    __nv_bfloat162 lo = __floats2bfloat162_rn(v[0] * inv, v[1] * inv), hi = __floats2bfloat162_rn(v[2] * inv, v[3] * inv);
-                    *reinterpret_cast<uint2*>(A.o + t * A.os_row + (h0 + h) * A.os_head + c) = make_uint2(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi));
-                    if (c == 0) A.lse[t * R.Hq + h0 + h] = sum == 0.0f ? -INFINITY : top + logf(sum);
+                }
+#pragma unroll
+                for (int n = 0; n < kTurns; ++n) {
+                    const int e = tid + n * kThreads, h = e / (D / 4), c = e % (D / 4) * 4;
+                    if (h < heads) write_out(h, c, top[n], sum[n], v[n]);
                 }
             }
         }
