@@ -8,6 +8,7 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <climits>
 #include <type_traits>
 
 #include "paged.cuh"
@@ -1003,32 +1004,44 @@ __global__ void __launch_bounds__(kThreads, 3) attn_kernel(AttnArgs A) {
         }
         const int hk = i / A.hb, h0 = hk * A.G + (i % A.hb) * A.hpb, heads = min(A.hpb, (hk + 1) * A.G - h0);
         const int32_t* pages = R.table + seq * R.ld;
-        // 64 keys per turn, a lane's two neighbouring keys in every head, requested kAhead turns before they are tested
-        constexpr int kAhead = kH <= 4 ? 2 : 1;
-        float2 dl[kAhead][kH];
-        int page[kAhead];
+        // 64 keys per turn, a lane's two neighbouring keys in every head, requested a turn before they are tested, and their page two
+        float2 dl[kH] = {};                                       // (of a lane without a page, or a head that is none: not looked at)
+        int page;
         auto page_of = [&](int j) {
             if (j >= k1) return -1;
             const int p = pages[j >> R.page_log];
             return (unsigned)p < (unsigned)R.num_pages ? p : -1;
         };
         const float* plane = R.delta + ((size_t)h0 << R.page_log);
-        auto request = [&](int a, int j, int p) {
-            page[a] = p;
+        auto request = [&](int j, int p) {
+            page = p;
             const float* src = plane + (size_t)p * ((uint32_t)R.Hq << R.page_log) + (j & R.mask());
 #pragma unroll
             for (int h = 0; h < kH; ++h) {
-                dl[a][h] = make_float2(0.0f, 0.0f);
-                if (p >= 0 && h < heads) dl[a][h] = *reinterpret_cast<const float2*>(src + (h << R.page_log));
+                if (p >= 0 && h < heads) dl[h] = *reinterpret_cast<const float2*>(src + (h << R.page_log));
             }
         };
         int j = k0 + warp * 64;
+        request(j + 2 * lane, page_of(j + 2 * lane));
+        int after = page_of(j + kWarps * 64 + 2 * lane);
+        // A head keeps the patterns above its weakest key's, and those equal to it up to that key's index: least[h], the pattern or, past the index, the next one. The turn
+        // that the index lies in (first_mixed and later ones, in turns that are none's) is tested key by key. (delta > 0: 1 keeps every key, and an absent one reads as 0.)
+        uint32_t least[kH];
+        int first_mixed = INT_MAX;
+        auto weakest_of = [&](int h, int& last) {
+            const unsigned long long k = A.weakest && h < heads ? A.weakest[t * R.Hq + h0 + h] : 0ull;
+            last = k ? (int)(0xFFFFFFFFu - (uint32_t)k) : INT_MAX;
+            return h < heads ? max((uint32_t)(k >> 32), 1u) : 0xFFFFFFFFu;
+        };
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) request(a, j + a * kWarps * 64 + 2 * lane, page_of(j + a * kWarps * 64 + 2 * lane));
-        int after = page_of(j + kAhead * kWarps * 64 + 2 * lane);
-        unsigned long long least[kH];
-#pragma unroll
-        for (int h = 0; h < kH; ++h) least[h] = h >= heads ? ~0ull : A.weakest ? A.weakest[t * R.Hq + h0 + h] : 0ull;
+        for (int h = 0; h < kH; ++h) {
+            int last;
+            least[h] = weakest_of(h, last);
+            if (least[h] != 0xFFFFFFFFu) {
+                least[h] += k0 > last;
+                if (k0 <= last) first_mixed = min(first_mixed, last);
+            }
+        }
         // queries: column r of the operand is head r % kCols; channels in the order that the codes come in
         WarpState<D> W;
         {
@@ -1127,39 +1140,45 @@ __global__ void __launch_bounds__(kThreads, 3) attn_kernel(AttnArgs A) {
                 bool any[2] = {false, false};
 #pragma unroll
                 for (int h = 0; h < kCols; ++h) b[0][h] = b[1][h] = -INFINITY;
-#pragma unroll
-                for (int h = 0; h < kH; ++h) {
-                    const bool k0h = order_key(__float_as_uint(dl[0][h].x) & 0x7FFFFFFFu, key) >= least[h], k1h = order_key(__float_as_uint(dl[0][h].y) & 0x7FFFFFFFu, key + 1) >= least[h];
-                    b[0][h] = k0h ? dl[0][h].x : -INFINITY;
-                    b[1][h] = k1h ? dl[0][h].y : -INFINITY;
+                auto test = [&](int h, uint32_t least0, uint32_t least1) {
+                    const bool k0h = __float_as_uint(dl[h].x) >= least0, k1h = __float_as_uint(dl[h].y) >= least1;
+                    b[0][h] = k0h ? dl[h].x : -INFINITY;
+                    b[1][h] = k1h ? dl[h].y : -INFINITY;
                     any[0] = any[0] || k0h;
                     any[1] = any[1] || k1h;
-                }
-                any[0] = any[0] && page[0] >= 0 && key < k1;
-                any[1] = any[1] && page[0] >= 0 && key + 1 < k1;
-                const uint32_t ballot[2] = {__ballot_sync(0xffffffffu, any[0]), __ballot_sync(0xffffffffu, any[1])}, below = (1u << lane) - 1u;
-                const size_t off = (size_t)(uint32_t)page[0] * page_bytes + (head_bytes + (uint32_t)(key & R.mask()) * D);
-                int to = tail + __popc(ballot[0] & below);
+                };
+                if (j + 63 < first_mixed) {
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    if (any[e]) {
-                        S.off[to % kRing] = off + e * D;
-                        float4* dst = reinterpret_cast<float4*>(S.bias[to % kRing]);
-                        dst[0] = make_float4(b[e][0], b[e][1], b[e][2], b[e][3]);
-                        if constexpr (kCols == 8) dst[1] = make_float4(b[e][4], b[e][5], b[e][6], b[e][7]);
+                    for (int h = 0; h < kH; ++h) test(h, least[h], least[h]);
+                } else {
+                    first_mixed = INT_MAX;
+#pragma unroll
+                    for (int h = 0; h < kH; ++h) {
+                        int last;
+                        const uint32_t u = weakest_of(h, last), past = u == 0xFFFFFFFFu ? 0u : 1u;
+                        test(h, key > last ? u + past : u, key + 1 > last ? u + past : u);
+                        const int next = j + kWarps * 64;
+                        least[h] = next > last ? u + past : u;
+                        if (next <= last) first_mixed = min(first_mixed, last);
                     }
-                    if (e == 0) to = tail + __popc(ballot[0]) + __popc(ballot[1] & below);
                 }
-                tail += __popc(ballot[0]) + __popc(ballot[1]);
+                any[0] = any[0] && page >= 0;
+                any[1] = any[1] && page >= 0 && key + 1 < k1;
+                const uint32_t ballot[2] = {__ballot_sync(0xffffffffu, any[0]), __ballot_sync(0xffffffffu, any[1])}, below = (1u << lane) - 1u;
+                const size_t off = (size_t)(uint32_t)page * page_bytes + (head_bytes + (uint32_t)(key & R.mask()) * D);
+                const int n0 = __popc(ballot[0]);
+                auto queue = [&](int to, size_t at, const float (&v)[kCols]) {
+                    S.off[to % kRing] = at;
+                    float4* dst = reinterpret_cast<float4*>(S.bias[to % kRing]);
+                    dst[0] = make_float4(v[0], v[1], v[2], v[3]);
+                    if constexpr (kCols == 8) dst[1] = make_float4(v[4], v[5], v[6], v[7]);
+                };
+                if (any[0]) queue(tail + __popc(ballot[0] & below), off, b[0]);
+                if (any[1]) queue(tail + n0 + __popc(ballot[1] & below), off + D, b[1]);
+                tail += n0 + __popc(ballot[1]);
                 j += kWarps * 64;
-#pragma unroll
-                for (int a = 0; a + 1 < kAhead; ++a) {
-                    page[a] = page[a + 1];
-#pragma unroll
-                    for (int h = 0; h < kH; ++h) dl[a][h] = dl[a + 1][h];
-                }
-                request(kAhead - 1, j + (kAhead - 1) * kWarps * 64 + 2 * lane, after);
-                after = page_of(j + kAhead * kWarps * 64 + 2 * lane);
+                request(j + 2 * lane, after);
+                after = page_of(j + kWarps * 64 + 2 * lane);
             }
             // the next batch is requested, the one before it is used; behind the last one an empty group keeps the count
             const bool more = tail > issued * kBatch;
