@@ -37,16 +37,16 @@ struct Rows {
     }
 };
 
-// By radix passes of eight bits over the row, each of which reads it again (from the L2).
+// Equal weights, of which the first by index are kept: radix passes of eight bits of the index, each of which reads the row again (from the L2).
 struct RadixShared { int hist[256]; int bin, before, count; };
-// the bin of the need-th in descending (down) or ascending order
-__device__ __forceinline__ void radix_pick(RadixShared& S, bool down, int need) {
+// the bin of the need-th
+__device__ __forceinline__ void radix_pick(RadixShared& S, int need) {
     const int tid = threadIdx.x;
     __syncthreads();
     if (tid < 32) {
         int c[8], sum = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { c[i] = S.hist[down ? 255 - (8 * tid + i) : 8 * tid + i]; sum += c[i]; }
+        for (int i = 0; i < 8; ++i) { c[i] = S.hist[8 * tid + i]; sum += c[i]; }
         int incl = sum;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -56,7 +56,7 @@ __device__ __forceinline__ void radix_pick(RadixShared& S, bool down, int need) 
         int before = incl - sum;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (before < need && need <= before + c[i]) { S.bin = down ? 255 - (8 * tid + i) : 8 * tid + i; S.before = before; S.count = c[i]; }
+            if (before < need && need <= before + c[i]) { S.bin = 8 * tid + i; S.before = before; S.count = c[i]; }
             before += c[i];
         }
     }
@@ -75,31 +75,12 @@ __device__ __noinline__ int radix_index(RadixShared& S, Load load, int n, uint32
         radix_clear(S);
         for (int j = threadIdx.x; j < n; j += blockDim.x)
             if (load(j) == u && (shift == 24 || (j ^ j_lo) >> (shift + 8) == 0)) atomicAdd(&S.hist[j >> shift & 255], 1);
-        radix_pick(S, false, need);
+        radix_pick(S, need);
         j_lo |= S.bin << shift;
         need -= S.before;
     }
     return j_lo;
 }
-// the order key of the weakest of the row's `keep` best
-template <typename Load>
-__device__ __noinline__ unsigned long long radix_select(RadixShared& S, Load load, int n, int keep) {
-    int need = keep;
-    uint32_t u = 0u;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        radix_clear(S);
-        for (int j = threadIdx.x; j < n; j += blockDim.x) {
-            const uint32_t v = load(j);
-            if (shift == 24 || (v ^ u) >> (shift + 8) == 0) atomicAdd(&S.hist[v >> shift & 255u], 1);
-        }
-        radix_pick(S, true, need);
-        u |= (uint32_t)S.bin << shift;
-        need -= S.before;
-        if (S.count == need) return order_key(u, INT32_MAX);      // the whole bin is kept
-    }
-    return order_key(u, radix_index(S, load, n, u, need));
-}
-
 // What every row's attention is cut by: units of about the same work, dealt out to the CTAs in equal shares. ustart[t]: units before row t, over all its
 // `per_row` items. A key costs its test, and its expansion where some head of the group keeps it; the heads' kept keys are taken to be independent.
 // (By keys alone, rows that keep all theirs took up to twice a long row's time.)
@@ -151,10 +132,10 @@ __global__ void __launch_bounds__(1024) plan_kernel(Rows R, int rows, Plan P) {
 
 // The weakest kept key of a (row, query head). A sample brackets its delta (4.5 standard deviations of the sample's rank to either side); one sweep over the row
 // counts the keys above the bracket and notes those inside, a few per cent, each thread in slots of its own; the need-th of these is found by
-// a histogram over the bracket and a ranking of the bin's keys. Rows of up to kSample keys are their own sample: the bracket is one bin. Where
-// the bracket misses or holds too many (weights that crowd, equal weights) radix_select takes the row.
+// a histogram over the bracket and a ranking of the bin's keys. Rows of up to kSample keys are their own sample: the bracket is one bin. A bracket that misses, or holds too
+// many (weights that crowd), is replaced by a bin of a histogram of the row, and the row is swept again; equal weights are counted by index.
 // Many rows: 256 threads each, so that an SM works on several and their barriers and round trips hide each other; fewer long ones: 512.
-constexpr int kOwn = 20, kShared = 512, kRank = 128;     // slots per thread, overflow slots, most keys ranked against each other
+constexpr int kOwn = 12, kShared = 512, kRank = 128;     // slots per thread, overflow slots, most keys ranked against each other
 constexpr int kBins = 1024;
 template <int NT>
 struct alignas(16) HeldShared {
@@ -293,13 +274,24 @@ __global__ void __launch_bounds__(NT, 1024 / NT) select_kernel(Rows R, int rows,
     uint32_t lo = 0u, hi = 0x7FFFFFFFu;
     {
         uint32_t u[kPer], umin = 0x7FFFFFFFu, umax = 0u;
+        // four neighbours from each of kSample / 4 scattered places (single keys take four times the sectors, which were the larger part of what the kernel waited for)
         const bool whole = n <= kSample;
-        const uint32_t step = (uint32_t)n / kSample;
+        const uint32_t quads = (uint32_t)n / 4, step = quads / (kSample / 4);
+        uint32_t at[kPer / 4];
+        int pg[kPer / 4];
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) {
+        for (int k = 0; k < kPer / 4; ++k) {
             const uint32_t i = k * NT + tid;
-            const uint32_t j = whole ? i : (uint32_t)((uint64_t)i * (uint32_t)n / kSample) + (((i * 2654435761u) >> 16) * step >> 16);
-            u[k] = j < (uint32_t)n ? load(j) : 0xFFFFFFFFu;
+            at[k] = 4 * (whole ? i : (uint32_t)((uint64_t)i * quads / (kSample / 4)) + (((i * 2654435761u) >> 16) * step >> 16));
+            pg[k] = at[k] < (uint32_t)n ? pages[at[k] >> R.page_log] : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < kPer / 4; ++k) {
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if ((unsigned)pg[k] < (unsigned)R.num_pages) v = *reinterpret_cast<const uint4*>(plane + (size_t)pg[k] * stride + (at[k] & (uint32_t)R.mask()));
+            const uint32_t four[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[4 * k + e] = at[k] + e < (uint32_t)n ? four[e] & 0x7FFFFFFFu : 0xFFFFFFFFu;
         }
 #pragma unroll
         for (int k = 0; k < kPer; ++k)
@@ -322,41 +314,52 @@ __global__ void __launch_bounds__(NT, 1024 / NT) select_kernel(Rows R, int rows,
         if (S.bin[0] >= 0 && r0 >= 1) hi = min(umin + ((uint32_t)(S.bin[0] + 1) << shift) - 1u, 0x7FFFFFFFu);
         if (S.bin[1] >= 0) lo = umin + ((uint32_t)S.bin[1] << shift);
     }
-    // sweep: four neighbouring keys of a page per thread and step. What lies inside is noted by predicated stores, without a branch per key, and what lies below
-    // is counted by the sign of its distance (with a branch and two comparisons per key, the sweep was 50 of the 62 instructions that 32 keys took).
-    uint32_t below = 0u, seen = 0u;
-    int extra = 0;
-    uint2 *own = S.own + tid, *const own_end = own + (kOwn - 4) * NT;
-    const uint32_t width = hi - lo, beyond = lo > 0u ? 0u : 0xFFFFFFFFu;          // beyond: below the bracket, wherever that is
+    // f(patterns, index of the first) for four neighbouring keys of a page per thread and step; keys beyond the row read as `beyond`
     const int chunks = (n + 3) / 4;
-    constexpr int kAhead = 4;
-    int page[kAhead];
-    auto pages_at = [&](int i0) {
+    auto sweep = [&](uint32_t beyond, auto&& f) {
+        constexpr int kAhead = 4;
+        int page[kAhead];
+        auto pages_at = [&](int i0) {
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int i = i0 + k * NT + tid;
-            page[k] = i < chunks ? pages[(4 * i) >> R.page_log] : -1;
+            for (int k = 0; k < kAhead; ++k) {
+                const int i = i0 + k * NT + tid;
+                page[k] = i < chunks ? pages[(4 * i) >> R.page_log] : -1;
+            }
+        };
+        pages_at(0);
+        for (int i0 = 0; i0 < chunks; i0 += NT * kAhead) {
+            uint4 u[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                u[k] = make_uint4(0u, 0u, 0u, 0u);
+                if ((unsigned)page[k] < (unsigned)R.num_pages) u[k] = *reinterpret_cast<const uint4*>(plane + (size_t)page[k] * stride + (4 * (i0 + k * NT + tid) & R.mask()));
+            }
+            pages_at(i0 + NT * kAhead);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int j = 4 * (i0 + k * NT + tid);
+                uint32_t v[4] = {u[k].x & 0x7FFFFFFFu, u[k].y & 0x7FFFFFFFu, u[k].z & 0x7FFFFFFFu, u[k].w & 0x7FFFFFFFu};
+                if (j + 4 > n) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (j + e >= n) v[e] = beyond;
+                }
+                f(v, j);
+            }
         }
     };
-    pages_at(0);
-    for (int i0 = 0; i0 < chunks; i0 += NT * kAhead) {
-        uint4 u[kAhead];
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            u[k] = make_uint4(0u, 0u, 0u, 0u);
-            if ((unsigned)page[k] < (unsigned)R.num_pages) u[k] = *reinterpret_cast<const uint4*>(plane + (size_t)page[k] * stride + (4 * (i0 + k * NT + tid) & R.mask()));
-        }
-        pages_at(i0 + NT * kAhead);
-        seen += 4 * kAhead;
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int j = 4 * (i0 + k * NT + tid);
-            uint32_t v[4] = {u[k].x & 0x7FFFFFFFu, u[k].y & 0x7FFFFFFFu, u[k].z & 0x7FFFFFFFu, u[k].w & 0x7FFFFFFFu};
-            if (j + 4 > n) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (j + e >= n) v[e] = beyond;
-            }
+    uint2* own;
+    int inside, need, nmore;
+    for (;;) {
+        // What lies inside the bracket is noted by predicated stores, without a branch per key, and what lies below is counted by the sign of its distance (with a branch
+        // and two comparisons per key, the sweep was 50 of the 62 instructions that 32 keys took).
+        uint32_t below = 0u, seen = 0u;
+        int extra = 0;
+        own = S.own + tid;
+        uint2* const own_end = own + (kOwn - 4) * NT;
+        const uint32_t width = hi - lo;
+        sweep(lo > 0u ? 0u : 0xFFFFFFFFu, [&](const uint32_t (&v)[4], int j) {        // (beyond the row: below the bracket, wherever that is)
+            seen += 4;
             if (own <= own_end) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -376,40 +379,59 @@ __global__ void __launch_bounds__(NT, 1024 / NT) select_kernel(Rows R, int rows,
                     }
                 }
             }
+        });
+        const int mine = (int)(own - (S.own + tid)) / NT + extra;
+        const int sum_above = __reduce_add_sync(0xffffffffu, (int)(seen - below) - mine), sum_in = __reduce_add_sync(0xffffffffu, mine);
+        if (lane == 0) { S.above[warp] = sum_above; S.part[warp] = sum_in; }
+        __syncthreads();
+        inside = __reduce_add_sync(0xffffffffu, lane < kWarps ? S.part[lane] : 0);
+        need = w - __reduce_add_sync(0xffffffffu, lane < kWarps ? S.above[lane] : 0);
+        nmore = S.nmore;
+        __syncthreads();                                          // (part, above and nmore have been read)
+        if (need >= 1 && need <= inside && nmore <= kShared) break;
+        // The bracket missed, or holds too many: the part of the row that holds the threshold, by rank r in it, divided into bins; then once more with the bin.
+        int r = need;
+        if (need < 1) { lo = hi + 1u; hi = 0x7FFFFFFFu; r = w; }
+        else if (need > inside) { hi = lo - 1u; lo = 0u; r = need - inside; }
+        if (lo == hi) {                                           // equal weights: by their indices
+            const int j = radix_index(S.radix, load, n, lo, r);
+            if (tid == 0) weakest[item] = order_key(lo, j);
+            return;
         }
-    }
-    const int mine = (int)(own - (S.own + tid)) / NT;
-    const int sum_above = __reduce_add_sync(0xffffffffu, (int)(seen - below) - mine - extra), sum_in = __reduce_add_sync(0xffffffffu, mine + extra);
-    if (lane == 0) { S.above[warp] = sum_above; S.part[warp] = sum_in; }
-    __syncthreads();
-    const int inside = __reduce_add_sync(0xffffffffu, lane < kWarps ? S.part[lane] : 0);
-    int need = w - __reduce_add_sync(0xffffffffu, lane < kWarps ? S.above[lane] : 0);
-    const int nmore = S.nmore;
-    unsigned long long found;
-    if (need < 1 || need > inside || nmore > kShared) {
-        found = radix_select(S.radix, load, n, w);
-    } else {
-        __syncthreads();                                          // (part and above have been read)
-        auto inside_keys = [&](auto&& f) {
-            for (int i = 0; i < mine; ++i) f(S.own[i * NT + tid]);
-            for (int i = tid; i < nmore; i += NT) f(S.more[i]);
-        };
-        // the bin of the bracket that holds it, then the order keys of that bin
+        if (tid == 0) S.nmore = 0;
         const int shift = shift_of(hi - lo);
-        inside_keys([&](uint2 x) { atomicAdd(&S.hist[(x.x - lo) >> shift], 1); });
+        sweep(0xFFFFFFFFu, [&](const uint32_t (&v)[4], int) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (v[e] - lo <= hi - lo) atomicAdd(&S.hist[(v[e] - lo) >> shift], 1);
+        });
         __syncthreads();
         int excl, c[kBins / NT], bin, before, count;
         scan_bins<NT>(S, S.hist, excl, c);
-        if (bin_of<NT>(need, excl, c, bin, before, count)) { S.bin[0] = bin; S.need = need - before; S.count = count; }
+        if (bin_of<NT>(r, excl, c, bin, before, count)) S.bin[0] = bin;
         __syncthreads();
-        const uint32_t low = lo + ((uint32_t)S.bin[0] << shift);
-        need = S.need;
-        count = S.count;
-        __syncthreads();
-        found = find_weakest<NT>(S, [&](auto&& f) {
-            inside_keys([&](uint2 x) { if ((x.x - low) >> shift == 0u) f(order_key(x.x, (int)x.y)); });
-        }, (unsigned long long)low << 32, 32 + shift - 10, 1 << 10, count, need);
+        lo += (uint32_t)S.bin[0] << shift;
+        hi = min(hi, lo + ((1u << shift) - 1u));
     }
+    auto inside_keys = [&](auto&& f) {
+        for (uint2* x = S.own + tid; x < own; x += NT) f(*x);
+        for (int i = tid; i < nmore; i += NT) f(S.more[i]);
+    };
+    // the bin of the bracket that holds it, then the order keys of that bin
+    const int shift = shift_of(hi - lo);
+    inside_keys([&](uint2 x) { atomicAdd(&S.hist[(x.x - lo) >> shift], 1); });
+    __syncthreads();
+    int excl, c[kBins / NT], bin, before, count;
+    scan_bins<NT>(S, S.hist, excl, c);
+    if (bin_of<NT>(need, excl, c, bin, before, count)) { S.bin[0] = bin; S.need = need - before; S.count = count; }
+    __syncthreads();
+    const uint32_t low = lo + ((uint32_t)S.bin[0] << shift);
+    need = S.need;
+    count = S.count;
+    __syncthreads();
+    const unsigned long long found = find_weakest<NT>(S, [&](auto&& f) {
+        inside_keys([&](uint2 x) { if ((x.x - low) >> shift == 0u) f(order_key(x.x, (int)x.y)); });
+    }, (unsigned long long)low << 32, 32 + shift - 10, 1 << 10, count, need);
     if (tid == 0) weakest[item] = found;
 }
 
@@ -1360,7 +1382,6 @@ int select(const Cache& C, const Rows& R, unsigned long long* weakest, const Pla
     auto stream = [&](auto nt, auto kernel) { return select_launch(kernel, nt, sizeof(SelectShared<nt>), 1, C, R, weakest, plan, st); };
     auto held = [&](auto nt, auto kernel, int cluster) { return select_launch(kernel, nt, sizeof(ClusterShared<nt>), cluster, C, R, weakest, plan, st); };
     using std::integral_constant;
-    constexpr integral_constant<int, 128> t128{};
     constexpr integral_constant<int, 256> t256{};
     constexpr integral_constant<int, 512> t512{};
     constexpr integral_constant<int, 1024> t1024{};
@@ -1368,7 +1389,7 @@ int select(const Cache& C, const Rows& R, unsigned long long* weakest, const Pla
     const int items = C.rows * C.Hq;
     if (items >= 3 * 148) {
         if (capacity <= 2 * K) return held(t256, select_held_kernel<256, 8>, 1);
-        return stream(t128, select_kernel<128, 8>);
+        return stream(t256, select_kernel<256, 8>);
     }
     if (capacity <= 4 * K) return held(t1024, select_held_kernel<1024, 4>, 1);
     if (capacity <= 8 * K) return held(t1024, select_held_kernel<1024, 8>, 1);
