@@ -149,11 +149,12 @@ struct alignas(16) HeldShared {
     unsigned long long found;
 };
 template <int NT>
-struct alignas(16) SelectShared : HeldShared<NT> {
-    uint2 own[kOwn * NT], more[kShared];                          // (pattern, index) of keys inside the bracket
-};
-template <int NT>
 struct alignas(16) ClusterShared : HeldShared<NT> { int sum[kBins]; };       // the whole row's bins
+template <int NT>
+struct alignas(16) SelectShared : ClusterShared<NT> {
+    uint2 own[kOwn * NT], more[kShared];                          // (pattern, index) of keys inside the bracket
+    int total[2][3];                                              // this CTA's keys above the bracket and inside, and its overflow; of the last two sweeps
+};
 __device__ __forceinline__ int shift_of(uint32_t width) { return max(0, 22 - __clz((int)width)); }       // kBins bins over width + 1 patterns
 
 // The descending running count of the bins in hist: a thread's bins are kBins - 1 - tid kBins / NT and those below it, `excl` keys lie above them. The bins are zeroed again. One barrier.
@@ -242,24 +243,26 @@ __device__ __forceinline__ unsigned long long find_weakest(HeldShared<NT>& S, Ea
     return rank_candidates<NT>(S, count, need);
 }
 
-template <int NT, int kPer>
+template <int NT, int kPer, bool kCluster>
 __global__ void __launch_bounds__(NT, 1024 / NT) select_kernel(Rows R, int rows, int w, unsigned long long* weakest, Plan P) {
     extern __shared__ __align__(16) uint8_t select_smem[];
     SelectShared<NT>& S = *reinterpret_cast<SelectShared<NT>*>(select_smem);
     constexpr int kSample = NT * kPer, kWarps = NT / 32;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nrank = kCluster ? (int)cluster.num_blocks() : 1, rank = kCluster ? (int)cluster.block_rank() : 0;
     for (int i = tid; i < kBins; i += NT) S.hist[i] = 0;
     if (tid == 0) { S.ncand = S.nmore = 0; S.bin[0] = S.bin[1] = -1; }
     pdl_enter(R.table, R.seq, R.pos, R.delta, weakest, P.ustart, P.tickets);
-    if (P.ustart && blockIdx.x == 0) {
-        make_plan<NT>(R, rows, P);
+    int item = blockIdx.x / nrank;
+    if (P.ustart && item-- == 0) {
+        if (rank == 0) make_plan<NT>(R, rows, P);
         return;
     }
-    const int item = blockIdx.x - (P.ustart ? 1 : 0), t = item / R.Hq, h = item % R.Hq;
+    const int t = item / R.Hq, h = item % R.Hq;
     int r;
     const int n = R.visible(t, r);
     if (n <= w) {                                                 // every key
-        if (tid == 0) weakest[item] = 0ull;
+        if (tid == 0 && rank == 0) weakest[item] = 0ull;
         return;
     }
     const int32_t* pages = R.table + r * R.ld;
@@ -270,8 +273,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) select_kernel(Rows R, int rows,
         if ((unsigned)page >= (unsigned)R.num_pages) return 0u;
         return __float_as_uint(plane[(size_t)page * stride + (j & R.mask())]) & 0x7FFFFFFFu;
     };
-    // sample
+    // sample (by every CTA of a cluster, the same one)
     uint32_t lo = 0u, hi = 0x7FFFFFFFu;
+    bool collect;
     {
         uint32_t u[kPer], umin = 0x7FFFFFFFu, umax = 0u;
         // four neighbours from each of kSample / 4 scattered places (single keys take four times the sectors, which were the larger part of what the kernel waited for)
@@ -310,6 +314,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) select_kernel(Rows R, int rows,
         if (bin_of<NT>(r0, excl, c, bin, before, count)) S.bin[0] = bin;
         if (bin_of<NT>(r1, excl, c, bin, before, count)) S.bin[1] = bin;
         __syncthreads();
+        // Expected inside: the row's part of the sample's ranks between r0 and r1. Where that is more than the slots take, the bracket's bins are counted first.
+        collect = whole || (float)n * (float)(r1 - r0) <= 0.75f * kSample * (float)((kOwn - 4) * NT) * (float)nrank;
         // (a rank beyond the sample: no bracket on that side)
         if (S.bin[0] >= 0 && r0 >= 1) hi = min(umin + ((uint32_t)(S.bin[0] + 1) << shift) - 1u, 0x7FFFFFFFu);
         if (S.bin[1] >= 0) lo = umin + ((uint32_t)S.bin[1] << shift);
@@ -326,15 +332,16 @@ __global__ void __launch_bounds__(NT, 1024 / NT) select_kernel(Rows R, int rows,
                 page[k] = i < chunks ? pages[(4 * i) >> R.page_log] : -1;
             }
         };
-        pages_at(0);
-        for (int i0 = 0; i0 < chunks; i0 += NT * kAhead) {
+        const int step = NT * kAhead * nrank;
+        pages_at(rank * NT * kAhead);
+        for (int i0 = rank * NT * kAhead; i0 < chunks; i0 += step) {
             uint4 u[kAhead];
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {
                 u[k] = make_uint4(0u, 0u, 0u, 0u);
                 if ((unsigned)page[k] < (unsigned)R.num_pages) u[k] = *reinterpret_cast<const uint4*>(plane + (size_t)page[k] * stride + (4 * (i0 + k * NT + tid) & R.mask()));
             }
-            pages_at(i0 + NT * kAhead);
+            pages_at(i0 + step);
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {
                 const int j = 4 * (i0 + k * NT + tid);
@@ -349,89 +356,166 @@ __global__ void __launch_bounds__(NT, 1024 / NT) select_kernel(Rows R, int rows,
         }
     };
     uint2* own;
-    int inside, need, nmore;
-    for (;;) {
-        // What lies inside the bracket is noted by predicated stores, without a branch per key, and what lies below is counted by the sign of its distance (with a branch
-        // and two comparisons per key, the sweep was 50 of the 62 instructions that 32 keys took).
-        uint32_t below = 0u, seen = 0u;
-        int extra = 0;
-        own = S.own + tid;
-        uint2* const own_end = own + (kOwn - 4) * NT;
-        const uint32_t width = hi - lo;
-        sweep(lo > 0u ? 0u : 0xFFFFFFFFu, [&](const uint32_t (&v)[4], int j) {        // (beyond the row: below the bracket, wherever that is)
-            seen += 4;
-            if (own <= own_end) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t d = v[e] - lo;
-                    below += d >> 31;
-                    if (d <= width) { *own = make_uint2(v[e], (uint32_t)(j + e)); own += NT; }
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t d = v[e] - lo;
-                    below += d >> 31;
-                    if (d <= width) {
-                        const int at = atomicAdd(&S.nmore, 1);
-                        if (at < kShared) S.more[at] = make_uint2(v[e], (uint32_t)(j + e));
-                        ++extra;
-                    }
-                }
-            }
-        });
-        const int mine = (int)(own - (S.own + tid)) / NT + extra;
-        const int sum_above = __reduce_add_sync(0xffffffffu, (int)(seen - below) - mine), sum_in = __reduce_add_sync(0xffffffffu, mine);
-        if (lane == 0) { S.above[warp] = sum_above; S.part[warp] = sum_in; }
-        __syncthreads();
-        inside = __reduce_add_sync(0xffffffffu, lane < kWarps ? S.part[lane] : 0);
-        need = w - __reduce_add_sync(0xffffffffu, lane < kWarps ? S.above[lane] : 0);
-        nmore = S.nmore;
-        __syncthreads();                                          // (part, above and nmore have been read)
-        if (need >= 1 && need <= inside && nmore <= kShared) break;
-        // The bracket missed, or holds too many: the part of the row that holds the threshold, by rank r in it, divided into bins; then once more with the bin.
-        int r = need;
-        if (need < 1) { lo = hi + 1u; hi = 0x7FFFFFFFu; r = w; }
-        else if (need > inside) { hi = lo - 1u; lo = 0u; r = need - inside; }
-        if (lo == hi) {                                           // equal weights: by their indices
-            const int j = radix_index(S.radix, load, n, lo, r);
-            if (tid == 0) weakest[item] = order_key(lo, j);
+    int need, nmore, count, shift;
+    unsigned long long found;
+    int* bins = S.hist;                                           // of the whole row, after a merge
+    auto merge = [&]() {
+        if (nrank == 1) {
+            __syncthreads();
             return;
         }
-        if (tid == 0) S.nmore = 0;
-        const int shift = shift_of(hi - lo);
-        sweep(0xFFFFFFFFu, [&](const uint32_t (&v)[4], int) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (v[e] - lo <= hi - lo) atomicAdd(&S.hist[(v[e] - lo) >> shift], 1);
-        });
+        bins = S.sum;
+        cluster.sync();
+        for (int i = tid; i < kBins; i += NT) {
+            int all = 0;
+            for (int q = 0; q < nrank; ++q) all += cluster.map_shared_rank(S.hist, q)[i];
+            S.sum[i] = all;
+        }
+        cluster.sync();
+        for (int i = tid; i < kBins; i += NT) S.hist[i] = 0;
         __syncthreads();
-        int excl, c[kBins / NT], bin, before, count;
-        scan_bins<NT>(S, S.hist, excl, c);
-        if (bin_of<NT>(r, excl, c, bin, before, count)) S.bin[0] = bin;
+    };
+    // the bin that holds the need-th: lo of it, its keys, and the rank in it
+    auto narrow = [&]() {
+        int excl, c[kBins / NT], bin, before, in_bin;
+        scan_bins<NT>(S, bins, excl, c);
+        if (bin_of<NT>(need, excl, c, bin, before, in_bin)) { S.bin[0] = bin; S.need = need - before; S.count = in_bin; }
         __syncthreads();
         lo += (uint32_t)S.bin[0] << shift;
-        hi = min(hi, lo + ((1u << shift) - 1u));
-    }
-    auto inside_keys = [&](auto&& f) {
-        for (uint2* x = S.own + tid; x < own; x += NT) f(*x);
-        for (int i = tid; i < nmore; i += NT) f(S.more[i]);
+        need = S.need;
+        count = S.count;
+        __syncthreads();
     };
-    // the bin of the bracket that holds it, then the order keys of that bin
-    const int shift = shift_of(hi - lo);
-    inside_keys([&](uint2 x) { atomicAdd(&S.hist[(x.x - lo) >> shift], 1); });
-    __syncthreads();
-    int excl, c[kBins / NT], bin, before, count;
-    scan_bins<NT>(S, S.hist, excl, c);
-    if (bin_of<NT>(need, excl, c, bin, before, count)) { S.bin[0] = bin; S.need = need - before; S.count = count; }
-    __syncthreads();
-    const uint32_t low = lo + ((uint32_t)S.bin[0] << shift);
-    need = S.need;
-    count = S.count;
-    __syncthreads();
-    const unsigned long long found = find_weakest<NT>(S, [&](auto&& f) {
-        inside_keys([&](uint2 x) { if ((x.x - low) >> shift == 0u) f(order_key(x.x, (int)x.y)); });
-    }, (unsigned long long)low << 32, 32 + shift - 10, 1 << 10, count, need);
+    auto equal_weights = [&]() {                                  // by their indices
+        if (rank != 0) return;
+        const int j = radix_index(S.radix, load, n, lo, need);
+        if (tid == 0) weakest[item] = order_key(lo, j);
+    };
+    for (int turn = 0;; ++turn) {
+        // One sweep: what lies below the bracket is counted by the sign of its distance; what lies inside goes into bins, or is noted by predicated stores, without a branch
+        // per key (with a branch and two comparisons per key, the sweep was 50 of the 62 instructions that 32 keys took).
+        if (turn == 16) {                                         // (five narrow any row to one pattern: weights that change under the call)
+            if (nrank > 1) cluster.sync();
+            found = order_key(lo, INT32_MAX);
+            if (rank != 0) return;
+            break;
+        }
+        uint32_t below = 0u, seen = 0u;
+        int in = 0;
+        own = S.own + tid;
+        uint2* const own_end = own + (kOwn - 4) * NT;
+        const uint32_t width = hi - lo, beyond = lo > 0u ? 0u : 0xFFFFFFFFu;      // (below the bracket, wherever that is)
+        shift = shift_of(width);
+        if (collect) {
+            sweep(beyond, [&](const uint32_t (&v)[4], int j) {
+                seen += 4;
+                if (own <= own_end) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t d = v[e] - lo;
+                        below += d >> 31;
+                        if (d <= width) { *own = make_uint2(v[e], (uint32_t)(j + e)); own += NT; }
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t d = v[e] - lo;
+                        below += d >> 31;
+                        if (d <= width) {
+                            const int at = atomicAdd(&S.nmore, 1);
+                            if (at < kShared) S.more[at] = make_uint2(v[e], (uint32_t)(j + e));
+                            ++in;
+                        }
+                    }
+                }
+            });
+            in += (int)(own - (S.own + tid)) / NT;
+        } else {
+            sweep(beyond, [&](const uint32_t (&v)[4], int) {
+                seen += 4;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t d = v[e] - lo;
+                    below += d >> 31;
+                    if (d <= width) { atomicAdd(&S.hist[d >> shift], 1); ++in; }
+                }
+            });
+        }
+        const int sum_above = __reduce_add_sync(0xffffffffu, (int)(seen - below) - in), sum_in = __reduce_add_sync(0xffffffffu, in);
+        if (lane == 0) { S.above[warp] = sum_above; S.part[warp] = sum_in; }
+        __syncthreads();
+        int inside = __reduce_add_sync(0xffffffffu, lane < kWarps ? S.part[lane] : 0), above = __reduce_add_sync(0xffffffffu, lane < kWarps ? S.above[lane] : 0);
+        nmore = S.nmore;
+        bool over = nmore > kShared;
+        if (nrank > 1) {
+            int* mine = S.total[turn & 1];
+            if (tid == 0) { mine[0] = above; mine[1] = inside; mine[2] = over; }
+            cluster.sync();
+            above = inside = 0;
+            for (int q = 0; q < nrank; ++q) {
+                const int* x = cluster.map_shared_rank(mine, q);
+                above += x[0];
+                inside += x[1];
+                over = over || x[2];
+            }
+        }
+        __syncthreads();                                          // (part, above and nmore have been read)
+        need = w - above;
+        if (need < 1 || need > inside) {                          // the bracket missed: the part of the row beside it, by bins
+            if (!collect)
+                for (int i = tid; i < kBins; i += NT) S.hist[i] = 0;
+            if (need < 1) { lo = hi + 1u; hi = 0x7FFFFFFFu; } else { hi = lo - 1u; lo = 0u; }
+            if (tid == 0) S.nmore = 0;
+            collect = false;
+            __syncthreads();
+            continue;
+        }
+        if (lo == hi && (!collect || over)) {                     // equal weights
+            if (nrank > 1) cluster.sync();                        // (no CTA leaves while another may still read its totals)
+            equal_weights();
+            return;
+        }
+        if (!collect) {                                           // the threshold's bin is the new bracket
+            merge();
+            narrow();
+            hi = min(hi, lo + ((1u << shift) - 1u));
+            collect = lo == hi ? false : (int64_t)count <= (int64_t)(kOwn - 4) * NT * nrank / 2;
+            if (lo == hi && count <= kRank) collect = true;
+            continue;
+        }
+        if (over) {                                               // too many (weights that crowd): by bins
+            if (tid == 0) S.nmore = 0;
+            collect = false;
+            __syncthreads();
+            continue;
+        }
+        // the keys inside: the bin that holds the need-th, then its order keys
+        auto inside_keys = [&](auto&& f) {
+            for (uint2* x = S.own + tid; x < own; x += NT) f(*x);
+            for (int i = tid; i < nmore; i += NT) f(S.more[i]);
+        };
+        inside_keys([&](uint2 x) { atomicAdd(&S.hist[(x.x - lo) >> shift], 1); });
+        merge();
+        narrow();
+        if (nrank == 1) {
+            found = find_weakest<NT>(S, [&](auto&& f) {
+                inside_keys([&](uint2 x) { if ((x.x - lo) >> shift == 0u) f(order_key(x.x, (int)x.y)); });
+            }, (unsigned long long)lo << 32, 32 + shift - 10, 1 << 10, count, need);
+            break;
+        }
+        if (count <= kRank) {                                     // they meet in the first CTA
+            SelectShared<NT>* first = cluster.map_shared_rank(&S, 0);
+            inside_keys([&](uint2 x) { if ((x.x - lo) >> shift == 0u) first->cand[atomicAdd(&first->ncand, 1)] = order_key(x.x, (int)x.y); });
+            cluster.sync();
+            if (rank != 0) return;
+            found = rank_candidates<NT>(S, count, need);
+            break;
+        }
+        hi = min(hi, lo + ((1u << shift) - 1u));                  // a bin that holds many: swept again
+        if (tid == 0) S.nmore = 0;
+        collect = false;
+        __syncthreads();
+    }
     if (tid == 0) weakest[item] = found;
 }
 
@@ -1379,7 +1463,7 @@ int select_launch(void (*kernel)(Rows, int, int, unsigned long long*, Plan), int
     return launch_overlapped(kernel, dim3((unsigned)((C.rows * C.Hq + (plan.ustart ? 1 : 0)) * cluster)), dim3(threads), bytes, st, cluster, R, C.rows, C.w, weakest, plan);
 }
 int select(const Cache& C, const Rows& R, unsigned long long* weakest, const Plan& plan, int64_t capacity, cudaStream_t st) {
-    auto stream = [&](auto nt, auto kernel) { return select_launch(kernel, nt, sizeof(SelectShared<nt>), 1, C, R, weakest, plan, st); };
+    auto stream = [&](auto nt, auto kernel, int cluster) { return select_launch(kernel, nt, sizeof(SelectShared<nt>), cluster, C, R, weakest, plan, st); };
     auto held = [&](auto nt, auto kernel, int cluster) { return select_launch(kernel, nt, sizeof(ClusterShared<nt>), cluster, C, R, weakest, plan, st); };
     using std::integral_constant;
     constexpr integral_constant<int, 256> t256{};
@@ -1389,13 +1473,17 @@ int select(const Cache& C, const Rows& R, unsigned long long* weakest, const Pla
     const int items = C.rows * C.Hq;
     if (items >= 3 * 148) {
         if (capacity <= 2 * K) return held(t256, select_held_kernel<256, 8>, 1);
-        return stream(t256, select_kernel<256, 8>);
+        if (capacity <= 4 * K) return held(t256, select_held_kernel<256, 16>, 1);
+        if (capacity <= 32 * K) return stream(t256, select_kernel<256, 8, false>, 1);
+        return stream(t512, select_kernel<512, 8, false>, 1);
     }
     if (capacity <= 4 * K) return held(t1024, select_held_kernel<1024, 4>, 1);
     if (capacity <= 8 * K) return held(t1024, select_held_kernel<1024, 8>, 1);
     if (capacity <= 16 * K) return held(t1024, select_held_kernel<1024, 16>, 1);
-    if (capacity <= 256 * K && items * (capacity / (32 * K)) <= 148) return held(t1024, select_held_kernel<1024, 32>, capacity <= 32 * K ? 1 : capacity <= 64 * K ? 2 : capacity <= 128 * K ? 4 : 8);
-    return stream(t512, select_kernel<512, 8>);
+    if (capacity <= 32 * K) return held(t1024, select_held_kernel<1024, 32>, 1);
+    int cluster = 1;
+    while (cluster < 8 && items * cluster * 2 <= 2 * 148 && capacity / cluster > 32 * K) cluster *= 2;
+    return cluster == 1 ? stream(t512, select_kernel<512, 8, false>, 1) : stream(t512, select_kernel<512, 8, true>, cluster);
 }
 
 }  // namespace

@@ -441,6 +441,31 @@ def test_decode_long(Hq, Hkv, d, page, w, lens, dtype):
     decode_case(Hq, Hkv, d, page, w, lens, dtype, seed=w)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("kind", ["random", "few", "equal", "ramp", "outlier", "segments", "zero"])
+@pytest.mark.parametrize("n,rows,w", [(3000, 1, 700), (9001, 1, 9000), (20000, 1, 20), (33001, 1, 5000), (70001, 3, 3000), (300007, 1, 40000), (2100, 230, 500), (5003, 230, 40), (33100, 230, 8000)])
+def test_decode_selection_of_crowded_weights(n, rows, w, kind, dtype):
+    """The kept set where the selection changes its form (row length, few or many rows) and where weights crowd: few values, one value, weights that rise along the row, one far
+    above the others, long stretches of one value, weights of the smallest exponent. Drafts share one sequence; the plain implementation takes the last rows."""
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    Hq, Hkv, d, page = 2, 1, 64, 64
+    blocks = -(-n // page)
+    c, *arrays = pool_of(Hq, Hkv, d, page, blocks, rows, dt, nseq=1, blocks=blocks, w=w)
+    vals, weights = filled(c, *arrays, n + w)
+    rng = np.random.RandomState(n)
+    keys = blocks * page
+    x = {"random": lambda: 1 + rng.rand(keys), "few": lambda: 1 + rng.randint(0, 7, keys) / 4, "equal": lambda: np.full(keys, 1.0), "ramp": lambda: 1 + np.arange(keys) / keys,
+         "outlier": lambda: np.where(np.arange(keys) == n // 2, 80.0, 1 + rng.rand(keys) / 1000), "segments": lambda: 1 + rng.randint(0, 9, keys // 512 + 1).repeat(512)[:keys] / 8,
+         "zero": lambda: 1e-37 * (1 + rng.rand(keys))}[kind]
+    dl = np.stack([x(), x()[::-1]]).astype(np.float32)                     # [Hq, keys]
+    arrays[2].copy_(torch.from_numpy(dl.reshape(Hq, blocks, page).transpose(1, 0, 2).copy()))
+    pos = [n - 1 - t % 7 for t in range(rows)]
+    q = torch.randn(rows, Hq, d, generator=torch.Generator().manual_seed(n)).to(dt).cuda()
+    table = np.arange(blocks, dtype=np.int32)[None]
+    o, lse = dma.dma_cache4_decode(c, q, *arrays, i32(table), i32([0] * rows), i32(pos))
+    check_decode(c, q, arrays, vals, dl.T, table, [0] * rows, pos, o, lse, w, rows=[rows - 1] if rows < 4 else [0, rows - 1])
+
+
 def test_decode_many_rows():
     """More rows than the chip holds CTAs; the plain implementation takes some of them."""
     rng = np.random.RandomState(8)
