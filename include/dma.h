@@ -277,7 +277,7 @@ typedef struct {
     int32_t dtype;               /* element type of q, K, V, o: DMA_BF16 | DMA_FP32                               */
     int32_t page_size;           /* keys per page: 16, 32, 64, 128 or 256                                         */
     int32_t num_pages;           /* pages of the pool; num_pages * page_size < 2^31                               */
-    int32_t max_blocks;          /* pages that a sequence may hold; max_blocks * page_size < 2^31                 */
+    int32_t max_blocks;          /* pages that a sequence may hold; max_blocks * page_size <= 2^30                */
     int32_t nseq;                /* sequences: rows of block_table                                                */
     int32_t rows;                /* rows (tokens) of this call, >= 1                                              */
     int32_t flags;               /* DMA_FLAG_SIMT: dma_cache4_decode on the CUDA cores also for bf16; others refused */
@@ -337,7 +337,8 @@ int dma_cache4_read(const dma_cache_t* c, const void* codes, const void* scales,
  * o = 0, lse = -inf; a row whose row_seq is outside [0, nseq) (padding) is left as it is. Only the kept keys' codes are read (those
  * that some head of a group keeps). Results depend on the call's rows and lengths in the last bits (where long rows are cut),
  * and are the same bits from run to run.
- * ws: dma_cache4_decode_workspace() bytes, a size that does not fall as rows, Hq or max_blocks grow. */
+ * ws: dma_cache4_decode_workspace() bytes, a size that does not fall as rows, Hq or max_blocks grow. It serves one call at a time: calls that may overlap
+ * on the GPU (streams, captured graphs that replay side by side) need one each. */
 int dma_cache4_decode_workspace(const dma_cache_t* c, size_t* bytes);
 int dma_cache4_decode(const dma_cache_t* c, const void* q, const void* codes, const void* scales, const float* delta,
                       const int32_t* block_table, const int32_t* row_seq, const int32_t* row_pos, void* o, float* lse, void* ws,

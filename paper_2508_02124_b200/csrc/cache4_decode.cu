@@ -643,7 +643,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) select_held_kernel(Rows R, int 
 constexpr int kSimtWarps = 4;
 template <typename T, int D>
 __global__ void __launch_bounds__(32 * kSimtWarps) simt_attn_kernel(Rows R, const T* q, const uint8_t* codes, const uint32_t* scales, const unsigned long long* weakest,
-                                                                    T* o, float* lse, float* partial, int Hkv, int G, float scale, int64_t qs_row, int64_t qs_head,
+                                                                    T* o, float* lse, float* partial, int32_t* status, int Hkv, int G, float scale, int64_t qs_row, int64_t qs_head,
                                                                     int64_t os_row, int64_t os_head) {
     constexpr int C = D / 8;                                      // channels of a lane
     __shared__ size_t sRow[kSimtWarps][32];
@@ -651,7 +651,8 @@ __global__ void __launch_bounds__(32 * kSimtWarps) simt_attn_kernel(Rows R, cons
     __shared__ float sM[kSimtWarps], sL[kSimtWarps], sO[kSimtWarps][D];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane & 7, grp = lane >> 3;
     const int item = blockIdx.x, t = item / R.Hq, h = item % R.Hq, hk = h / G, split = blockIdx.y, nsplit = gridDim.y;
-    pdl_enter(R.table, R.seq, R.pos, R.delta, q, codes, scales, weakest, o, lse, partial);
+    pdl_enter(R.table, R.seq, R.pos, R.delta, q, codes, scales, weakest, o, lse, partial, status);
+    if (item == 0 && split == 0 && tid == 0) *status = 0;
     int r;
     const int n = R.visible(t, r);
     if (n < 0) return;
@@ -1039,6 +1040,7 @@ struct AttnArgs {
     const unsigned long long* weakest;
     __nv_bfloat16* o;
     float *lse, *partial;
+    int32_t* status;
     Plan plan;
     int Hkv, G, hb, hpb;                                          // heads of a group, blocks that they come in, heads per block
     float scale;
@@ -1073,7 +1075,8 @@ __global__ void __launch_bounds__(kThreads, 3) attn_kernel(AttnArgs A) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, t4 = lane & 3;
     auto& S = reinterpret_cast<typename Sh::Warp*>(attn_smem)[warp];
     Rows& R = A.R;
-    pdl_enter(R.table, R.seq, R.pos, R.delta, A.q, A.codes, A.scales, A.weakest, A.o, A.lse, A.partial, A.plan.ustart, A.plan.tickets);
+    pdl_enter(R.table, R.seq, R.pos, R.delta, A.q, A.codes, A.scales, A.weakest, A.o, A.lse, A.partial, A.status, A.plan.ustart, A.plan.tickets);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *A.status = 0;
     const int per_row = A.Hkv * A.hb;
     int at = 0, until = 1, E = 1, U = 1;                          // units of this CTA; without a plan the CTA's item
     const int cta = blockIdx.x;
@@ -1442,10 +1445,10 @@ size_t plan_bytes(const Cache& C) { return round256(((size_t)C.rows + 1 + (size_
 
 template <typename T, int D>
 int simt_decode(const Cache& C, const Rows& R, const void* q, const uint8_t* codes, const __nv_bfloat16* scales, const unsigned long long* weakest, void* o, float* lse,
-                float* partial, cudaStream_t st) {
+                float* partial, int32_t* status, cudaStream_t st) {
     const int items = C.rows * C.Hq, splits = simt_splits(C);
     const int rc = launch_overlapped(simt_attn_kernel<T, D>, dim3(items, splits), dim3(32 * kSimtWarps), 0, st, 1, R, (const T*)q, codes, (const uint32_t*)scales,
-                                     weakest, (T*)o, lse, partial, C.Hkv, C.G, C.scale, C.qs[0], C.qs[1], C.os[0], C.os[1]);
+                                     weakest, (T*)o, lse, partial, status, C.Hkv, C.G, C.scale, C.qs[0], C.qs[1], C.os[0], C.os[1]);
     if (rc || splits == 1) return rc;
     return launch_overlapped(simt_combine_kernel<T, D>, dim3(items), dim3(D), 0, st, 1, R, partial, (T*)o, lse, splits, C.os[0], C.os[1]);
 }
@@ -1519,10 +1522,10 @@ int launch_cache4_decode(const Cache& C, const void* q, const uint8_t* codes, co
     if (!tensor) {
         auto f = C.dtype == DMA_BF16 ? (C.d == 128 ? simt_decode<__nv_bfloat16, 128> : simt_decode<__nv_bfloat16, 64>)
                                      : (C.d == 128 ? simt_decode<float, 128> : simt_decode<float, 64>);
-        return f(C, R, q, codes, scales, weakest, o, lse, partial, st);
+        return f(C, R, q, codes, scales, weakest, o, lse, partial, (int32_t*)ws, st);
     }
     const int hpb = (C.G + hb - 1) / hb, grid = plan.ustart ? kAttnCtas : C.rows * per_row;
-    const AttnArgs A{R, (const __nv_bfloat16*)q, codes, (const uint8_t*)scales, weakest, (__nv_bfloat16*)o, lse, partial, plan, C.Hkv, C.G, hb, hpb, C.scale,
+    const AttnArgs A{R, (const __nv_bfloat16*)q, codes, (const uint8_t*)scales, weakest, (__nv_bfloat16*)o, lse, partial, (int32_t*)ws, plan, C.Hkv, C.G, hb, hpb, C.scale,
                      C.qs[0], C.qs[1], C.os[0], C.os[1], C.rows};
     if (C.d == 128) return hpb == 1 ? tc_decode<128, 1>(A, grid, st) : hpb == 2 ? tc_decode<128, 2>(A, grid, st) : hpb <= 4 ? tc_decode<128, 4>(A, grid, st) : tc_decode<128, 8>(A, grid, st);
     return hpb == 1 ? tc_decode<64, 1>(A, grid, st) : hpb == 2 ? tc_decode<64, 2>(A, grid, st) : hpb <= 4 ? tc_decode<64, 4>(A, grid, st) : tc_decode<64, 8>(A, grid, st);

@@ -11,7 +11,7 @@ int resolve_pages(const dma_cache_t* c, Cache* o) {
     int lg = 4;
     while (lg < 8 && (1 << lg) != c->page_size) ++lg;
     if ((1 << lg) != c->page_size) return DMA_ERR_UNSUPPORTED;
-    if (((int64_t)c->num_pages << lg) > INT32_MAX || ((int64_t)c->max_blocks << lg) > INT32_MAX) return DMA_ERR_SHAPE;
+    if (((int64_t)c->num_pages << lg) > INT32_MAX || ((int64_t)c->max_blocks << lg) > (1 << 30)) return DMA_ERR_SHAPE;
     if (c->table_ld != 0 && c->table_ld < c->max_blocks) return DMA_ERR_SHAPE;
     o->page_size = c->page_size; o->page_log = lg; o->num_pages = c->num_pages; o->max_blocks = c->max_blocks;
     o->nseq = c->nseq; o->rows = c->rows;

@@ -32,7 +32,7 @@ def test_struct_layout_and_sizes(lib):
 
 @pytest.mark.parametrize("kw,code", [
     (dict(Hq=3), -2), (dict(Hkv=0), -2), (dict(w=0), -2), (dict(rows=0), -2), (dict(nseq=0), -2), (dict(num_pages=0), -2), (dict(max_blocks=0), -2),
-    (dict(num_pages=1 << 26), -2), (dict(max_blocks=1 << 26), -2), (dict(rows=1 << 29), -2), (dict(softmax_scale=-1.0), -2), (dict(softmax_scale=float("nan")), -2),
+    (dict(num_pages=1 << 26), -2), (dict(max_blocks=1 << 26), -2), (dict(max_blocks=(1 << 25) + 1), -2), (dict(rows=1 << 29), -2), (dict(softmax_scale=-1.0), -2), (dict(softmax_scale=float("nan")), -2),
     (dict(page_size=48), -4), (dict(page_size=8), -4), (dict(page_size=512), -4), (dict(page_size=0), -4), (dict(d=96), -4), (dict(flags=8), -4), (dict(flags=64), -4),
     (dict(Hq=131072, Hkv=65536), -2)])
 def test_refused_descriptors(lib, kw, code):
