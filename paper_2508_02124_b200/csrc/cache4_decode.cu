@@ -169,9 +169,10 @@ __global__ void __launch_bounds__(D) simt_combine_kernel(Rows R, const float* pa
 //            scale goes into the weight, P s as a half, scaled by a power of two per head and group that follows its largest (WarpState); that rounding, at most 2^-11 of a
 //            weight, is the kernel's largest after the output's (its error against 64 bits grows by a sixth). z P is summed in fp32.
 //            With up to four heads the operand's columns 4 to 7 hold the same heads again, and their lanes take the second 16 keys through the softmax.
-// 64 rows of 1 to 16K keys, 32 / 8 heads of 128, w = 2048: 113 us for 414 MB (with one instance of this code for every use 285, with codes as bf16 numbers less 128 210). Half
-// of the issue slots, 55 % of the integer pipe: with all pages in the L2 it is 110 us, without the attending 90, with 8 or 16 warps per SM 133 and 118. Batches of 256
-// rows of 4096 keys, whose heads keep more of the same keys, run at 4.4 TB/s.
+// 64 rows of 1 to 16K keys, 32 / 8 heads of 128, w = 2048: 113 us for 414 MB read, 780 instructions per 32 keys of a union. 53 % of the issue slots, 54 % of the integer pipe, 18 % of the
+// tensor pipe: with all pages in the L2 it is 110 us, without the attending 90. Twelve warps per SM: sixteen, with stages that are swizzled to fit, 118; eight with three
+// stages 133 where twelve took 119. Codes as bf16 numbers and weights in a high and a low part 210 where this form took 165. 256 rows of 4096 keys, w = 1024: 240 us,
+// 4.4 TB/s.
 // (tcgen05 needs 64 rows of A at least, of which a decoding step has the group's 1 to 8 heads or, turned around, the keys: then the expanded codes would
 // have to go through shared memory once more. mma.sync takes them from the registers that the expansion leaves them in, and its rate is not what bounds this kernel.)
 constexpr int kBatch = 32, kStages = 2;

@@ -7,8 +7,8 @@
 //   plan_kernel          the attention's shares of the work, where nothing is selected (else the selection's first CTA makes them)
 //
 // Measured, 32 heads, us: one row of 16384 keys 6.6, of 262144 25, of 1048576 54 (by one CTA per row 118 and 522); 64 rows of 1 to 16K 41; 256 of 4096 72 (by a sample and a sweep 113), 48
-// of 65536 137. Bound by barriers and round trips where there are few rows, by instructions (some 35 per 32 keys, the fixed part of a row included) where there are many;
-// the weights' bytes alone would take a tenth to a third of it. All weights equal 8 (one row of 16384) to 44 (64 rows), ten values 12 to 128.
+// of 65536 137. Bound by barriers and round trips where there are few rows, by instructions where there are many (64 rows: 64 % of the issue slots, 43 per 32 keys, the fixed part
+// of a row included; the weights' bytes alone would take a fifth of the time). All weights equal: 8 for the one row, 44 for the 64; quarters of whole numbers: 12 and 128.
 #include <cooperative_groups.h>
 
 #include <algorithm>

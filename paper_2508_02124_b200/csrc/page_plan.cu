@@ -5,7 +5,7 @@
 // request, 1024 requests at a time; a thread per page taken, per page given back and per row then finds its request by a search in the sums.
 // Every CTA forms the sums, which takes it less time than waiting for another's, and takes its share of the pages and rows: a row's page is its table's entry or, where the call
 // takes it, the ring's, so that no CTA waits for another's writes. One CTA where there is little to write.
-// Bound by latency: three dependent trips to memory (lengths, ring or table, maps) and the barriers of the sums. us: 64 requests of a decoding step 5.5; 1000 requests, 50 000 rows and
+// Bound by latency: three dependent trips to memory (lengths, ring or table, maps) and the barriers of the sums. us: 64 requests of a decoding step 5.3; 1000 requests, 50 000 rows and
 // as many pages given back 7.9 (by one CTA 51, and its rows by a second kernel 6).
 #include <algorithm>
 #include <climits>
