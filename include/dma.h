@@ -278,7 +278,7 @@ typedef struct {
     int32_t page_size;           /* keys per page: 16, 32, 64, 128 or 256                                         */
     int32_t num_pages;           /* pages of the pool; num_pages * page_size < 2^31                               */
     int32_t max_blocks;          /* pages that a sequence may hold; max_blocks * page_size <= 2^30                */
-    int32_t nseq;                /* sequences: rows of block_table                                                */
+    int32_t nseq;                /* sequences: rows of block_table; at most 2^30                                  */
     int32_t rows;                /* rows (tokens) of this call, >= 1                                              */
     int32_t flags;               /* DMA_FLAG_SIMT: dma_cache4_decode on the CUDA cores also for bf16; others refused */
     float softmax_scale;         /* 0 -> 1/sqrt(d)                                                                */
@@ -318,7 +318,8 @@ int dma_page_plan(const dma_cache_t* c, const int32_t* lens, const int32_t* want
  *     z = bf16(min x),  s = max(0, bf16((max x / 2 - z / 2) / 7.5)),  n = min(15, max(0, rint((x / 2 - z / 2) / (s / 2))))
  *   (ties to even; n = 0 where the quotient is NaN, so with s = 0 too). 64 channels that hold a NaN, an infinity or a value that bf16 rounds to one read back as NaN.
  *   delta: of the row's V as given (not as held), the bits of dma_mask_build: W_delta [Hq, d], A [Hq]. Or, with delta_new not
- *   NULL, delta_new[h * delta_ld + t] as it is (dma_mask_build's bias, or dma_delta_range's output for the full weights);
+ *   NULL, delta_new[h * delta_ld + t] as it is (dma_mask_build's bias, or dma_delta_range's output for the full weights;
+ *   weights are greater than 0: what dma_cache4_decode keeps of keys with others is not defined);
  *   W_delta and A are then not read. Hq / Hkv at most 76 (d = 128) or 96 (d = 64); DMA_ERR_UNSUPPORTED beyond. */
 int dma_cache4_append(const dma_cache_t* c, const void* K, const void* V, const float* W_delta, const float* A, const float* delta_new,
                       int64_t delta_ld, const int32_t* slot, void* codes, void* scales, float* delta, void* cuda_stream);

@@ -8,6 +8,7 @@ namespace dma {
 int resolve_pages(const dma_cache_t* c, Cache* o) {
     if (!c) return DMA_ERR_NULL;
     if (c->rows < 1 || c->nseq < 1 || c->num_pages < 1 || c->max_blocks < 1) return DMA_ERR_SHAPE;
+    if (c->nseq > (1 << 30)) return DMA_ERR_SHAPE;                 // (the plan counts them by 1024, in 32 bits)
     int lg = 4;
     while (lg < 8 && (1 << lg) != c->page_size) ++lg;
     if ((1 << lg) != c->page_size) return DMA_ERR_UNSUPPORTED;

@@ -178,3 +178,12 @@ def test_the_plain_implementation():
     o, lse, _ = ref.decode(q, K, V, dl, 100, 0.125)
     e = np.exp(K[:, 0] @ q.T * 0.125 + dl.T)
     assert np.allclose(o, (e / e.sum(0)).T @ V[:, 0]) and np.allclose(lse, np.log(e.sum(0)))
+
+
+def test_most_sequences():
+    """A plan takes 1024 sequences a turn in 32 bits: 2^30 of them at most."""
+    c = dma.cache(Hq=1, Hkv=1, d=64, w=1, rows=1, nseq=1 << 30, page_size=16, num_pages=1, max_blocks=1)
+    assert dma.dma_cache4_bytes(c) == (16 * 64, 16 * 8, 16 * 4)
+    c.nseq = (1 << 30) + 1
+    with pytest.raises(RuntimeError):
+        dma.dma_cache4_bytes(c)
