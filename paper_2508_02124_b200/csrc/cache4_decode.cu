@@ -171,8 +171,8 @@ __global__ void __launch_bounds__(D) simt_combine_kernel(Rows R, const float* pa
 //            With up to four heads the operand's columns 4 to 7 hold the same heads again, and their lanes take the second 16 keys through the softmax.
 // 64 rows of 1 to 16K keys, 32 / 8 heads of 128, w = 2048: 113 us for 414 MB read, 780 instructions per 32 keys of a union. 53 % of the issue slots, 54 % of the integer pipe, 18 % of the
 // tensor pipe: with all pages in the L2 it is 110 us, without the attending 90. Twelve warps per SM: sixteen, with stages that are swizzled to fit, 118; eight with three
-// stages 133 where twelve took 119. Codes as bf16 numbers and weights in a high and a low part 210 where this form took 165. 256 rows of 4096 keys, w = 1024: 240 us,
-// 4.4 TB/s.
+// stages 133 where twelve took 119. Codes as bf16 numbers and weights in a high and a low part 210 where this form took 165. 256 rows of 4096 keys, w = 1024: 221 us,
+// 4.7 TB/s.
 // (tcgen05 needs 64 rows of A at least, of which a decoding step has the group's 1 to 8 heads or, turned around, the keys: then the expanded codes would
 // have to go through shared memory once more. mma.sync takes them from the registers that the expansion leaves them in, and its rate is not what bounds this kernel.)
 constexpr int kBatch = 32, kStages = 2;
@@ -447,7 +447,7 @@ __device__ __forceinline__ int warp_find(const int32_t* first, int n, int x) {
 }
 
 template <int D, int kH, int kW>
-__global__ void __launch_bounds__(32 * kW, kW == 4 ? 3 : 2) attn_kernel(AttnArgs A) {
+__global__ void __launch_bounds__(32 * kW, kW == 4 ? 3 : D == 64 ? 2 : 1) attn_kernel(AttnArgs A) {
     using Sh = AttnShape<D, kH, kW>;
     constexpr int kWarps = kW, kThreads = 32 * kW, NG = Sh::NG, kCols = Sh::kCols, kPitch = Sh::kPitch;
     extern __shared__ __align__(16) uint8_t attn_smem[];
@@ -465,7 +465,7 @@ __global__ void __launch_bounds__(32 * kW, kW == 4 ? 3 : 2) attn_kernel(AttnArgs
     const int cta = blockIdx.x;
     if (A.plan.ustart) {
         U = A.plan.ustart[A.rows];
-        E = min((int)gridDim.x, max(U / 2, 1));                   // (four units at least)
+        E = min((int)gridDim.x, max(U / 2, 1));                   // (two units at least)
         if (cta >= E || U == 0) return;
         at = (int)((int64_t)cta * U / E);
         until = (int)((int64_t)(cta + 1) * U / E);
@@ -842,10 +842,11 @@ int attn_launch(const AttnArgs& A, int grid, cudaStream_t st) {
     if (cudaFuncSetAttribute(attn_kernel<D, kH, kW>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return DMA_ERR_CUDA;
     return launch_overlapped(attn_kernel<D, kH, kW>, dim3(grid), dim3(32 * kW), bytes, st, 1, A);
 }
-// Eight warps per CTA where every CTA has one short row and all of them run at once with less than four warps per scheduler.
+// Eight warps per CTA where every CTA has one short row and all of them run at once: an SM has one of 128 channels or two of 64 (rows of 1000 keys, 8 KV heads; us of four warps and of eight:
+// d = 128, 16 rows 13.4 and 12.0, 20 rows 16.5 and 17.2; d = 64, 16 rows 10.5 and 8.8, 30 rows 12.4 and 12.2, 48 rows of 4 KV heads 11.7 and 10.7).
 template <int D, int kH>
 int tc_decode(const AttnArgs& A, int grid, cudaStream_t st) {
-    return !A.plan.ustart && grid <= 2 * 148 ? attn_launch<D, kH, 8>(A, grid, st) : attn_launch<D, kH, 4>(A, grid, st);
+    return !A.plan.ustart && grid <= (D == 64 ? 2 : 1) * 148 ? attn_launch<D, kH, 8>(A, grid, st) : attn_launch<D, kH, 4>(A, grid, st);
 }
 
 }  // namespace
@@ -862,9 +863,13 @@ int launch_cache4_decode(const Cache& C, const void* q, const uint8_t* codes, co
     const bool tensor = C.dtype == DMA_BF16 && !(C.flags & DMA_FLAG_SIMT);
     const int hb = head_blocks(C), per_row = C.Hkv * hb;
     unsigned long long* weakest = nullptr;
+    // (units of 256 keys: 64 rows of 16K 157 us, of 512 159; one row of 16K 14.7, of 128 15.1, of 512 17.9)
     Plan plan{nullptr, nullptr, per_row, 8, (C.G + hb - 1) / hb, C.w};
     char* at = (char*)ws + kWsHeaderBytes;
-    if (tensor && capacity > 1024) {
+    // The work is dealt out where rows may be long, unless short ones come in numbers that even out by themselves (us dealt out and by a CTA per item, 8 KV heads, w half the row:
+    // one row of 1024 keys 13.0 and 11.6, of 1536 13.0 and 14.9; 64 rows of up to 4096 57 and 62, 256 rows of up to 4096 189 and 185, of 4096 301 and 280, of 2048 172 and 155).
+    const bool even = capacity <= 1024 || (capacity <= 4096 && (int64_t)C.rows * per_row >= 4 * kAttnCtas);
+    if (tensor && !even) {
         plan.ustart = reinterpret_cast<int32_t*>(at + weakest_bytes(C));
         plan.tickets = plan.ustart + C.rows + 1;
         while ((int64_t)C.rows * per_row > INT32_MAX / ((capacity >> plan.unit_log) + 2)) ++plan.unit_log;

@@ -6,9 +6,9 @@
 //   select_kernel        longer ones, by a sample and a sweep; a cluster per row where there are few
 //   plan_kernel          the attention's shares of the work, where nothing is selected (else the selection's first CTA makes them)
 //
-// Measured, 32 heads, us: one row of 16384 keys 6.6, of 262144 25, of 1048576 54 (by one CTA per row 118 and 522); 64 rows of 1 to 16K 41; 256 of 4096 72 (by a sample and a sweep 113), 48
-// of 65536 137. Bound by barriers and round trips where there are few rows, by instructions where there are many (64 rows: 64 % of the issue slots, 43 per 32 keys, the fixed part
-// of a row included; the weights' bytes alone would take a fifth of the time). All weights equal: 8 for the one row, 44 for the 64; quarters of whole numbers: 12 and 128.
+// Measured, 32 heads, us: one row of 16384 keys 6.0, of 262144 25, of 1048576 49; 64 rows of 1 to 16K 41; 256 of 4096 68; 64 of 65536 178. Bound by barriers and round trips where there
+// are few rows, by instructions where there are many (64 rows of 1 to 16K: 64 % of the issue slots, 43 per 32 keys, the fixed part of a row included; the weights' bytes alone would take
+// a fifth of the time). All weights equal: 7 for the one row, 48 for the 64; quarters of whole numbers: 12 and 120.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -70,8 +70,9 @@ __global__ void __launch_bounds__(1024) plan_kernel(Rows R, int rows, Plan P) {
 // counts the keys above the bracket and notes those inside, a few per cent, each thread in slots of its own; the need-th of these is found by
 // a histogram over the bracket and a ranking of the bin's keys. Rows of up to kSample keys are their own sample: the bracket is one bin. A bracket that misses, or holds too
 // many (weights that crowd), is replaced by a bin of a histogram of the row, and the row is swept again; equal weights are counted by index.
-// Many rows: 256 threads each, so that an SM works on several and their barriers and round trips hide each other; fewer long ones: 512.
-constexpr int kOwn = 12, kShared = 512, kRank = 128;     // slots per thread, overflow slots, most keys ranked against each other
+constexpr int kShared = 512, kRank = 128;                // overflow slots, most keys ranked against each other
+// slots per thread (512 threads of 12: rows of 64K, w = 8192, are swept twice, 277 us for 64 rows; of 20: 181)
+__host__ __device__ constexpr int own_slots(int threads) { return threads == 256 ? 16 : 20; }
 constexpr int kBins = 1024;
 template <int NT>
 struct alignas(16) HeldShared {
@@ -80,16 +81,23 @@ struct alignas(16) HeldShared {
     uint32_t wmin[NT / 32], wmax[NT / 32];
     int part[NT / 32], above[NT / 32];
     int bin[2], need, count, ncand, nmore;
-    uint32_t umin, umax;
     unsigned long long found;
 };
-template <int NT>
-struct alignas(16) ClusterShared : HeldShared<NT> { int sum[kBins]; };       // the whole row's bins
-template <int NT>
-struct alignas(16) SelectShared : ClusterShared<NT> {
-    uint2 own[kOwn * NT], more[kShared];                          // (pattern, index) of keys inside the bracket
+template <int NT, bool kCluster>
+struct alignas(16) SelectShared : HeldShared<NT> {
+    int sum[kCluster ? kBins : 1];                                // a cluster's row's bins
+    uint2 own[own_slots(NT) * NT], more[kShared];                          // (pattern, index) of keys inside the bracket
     int total[2][3];                                              // this CTA's keys above the bracket and inside, and its overflow; of the last two sweeps
 };
+// The bracket's ranks of the sample, to either side of the expected one; and whether the slots take the row's part between them, with a quarter to spare.
+constexpr int kPer = 8;                                           // a thread's keys of the sample
+__host__ __device__ __forceinline__ float bracket(int n, int w, int sample) {
+    const float q = (float)w / (float)n;
+    return 4.5f * sqrtf(q * (float)sample * (1.0f - q)) + 4.0f;
+}
+__host__ __device__ __forceinline__ bool collects(int n, float dev, int threads, int sample, int ctas) {
+    return (float)n * (2.0f * dev + 1.0f) <= 0.75f * (float)sample * (float)((own_slots(threads) - 4) * threads) * (float)ctas;
+}
 __device__ __forceinline__ int shift_of(uint32_t width) { return max(0, 22 - __clz((int)width)); }       // kBins bins over width + 1 patterns
 
 // The descending running count of the bins in hist: a thread's bins are kBins - 1 - tid kBins / NT and those below it, `excl` keys lie above them. The bins are zeroed again. One barrier.
@@ -178,11 +186,11 @@ __device__ __forceinline__ unsigned long long find_weakest(HeldShared<NT>& S, Ea
     return rank_candidates<NT>(S, count, need);
 }
 
-template <int NT, int kPer, bool kCluster>
+template <int NT, bool kCluster>
 __global__ void __launch_bounds__(NT, 1024 / NT) select_kernel(Rows R, int rows, int w, unsigned long long* weakest, Plan P) {
     extern __shared__ __align__(16) uint8_t select_smem[];
-    SelectShared<NT>& S = *reinterpret_cast<SelectShared<NT>*>(select_smem);
-    constexpr int kSample = NT * kPer, kWarps = NT / 32;
+    SelectShared<NT, kCluster>& S = *reinterpret_cast<SelectShared<NT, kCluster>*>(select_smem);
+    constexpr int kSample = kPer * NT, kWarps = NT / 32, kOwn = own_slots(NT);
     cg::cluster_group cluster = cg::this_cluster();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nrank = kCluster ? (int)cluster.num_blocks() : 1, rank = kCluster ? (int)cluster.block_rank() : 0;
     for (int i = tid; i < kBins; i += NT) S.hist[i] = 0;
@@ -238,14 +246,14 @@ __global__ void __launch_bounds__(NT, 1024 / NT) select_kernel(Rows R, int rows,
         __syncthreads();
         int excl, c[kBins / NT];
         scan_bins<NT>(S, S.hist, excl, c);
-        const float q = (float)w / (float)n, mid = q * kSample, dev = 4.5f * sqrtf(mid * (1.0f - q)) + 4.0f;
+        const float mid = (float)w / (float)n * kSample, dev = bracket(n, w, kSample);
         const int r0 = whole ? w : (int)(mid - dev), r1 = whole ? w : (int)(mid + dev) + 1;
         int bin, before, count;
         if (bin_of<NT>(r0, excl, c, bin, before, count)) S.bin[0] = bin;
         if (bin_of<NT>(r1, excl, c, bin, before, count)) S.bin[1] = bin;
         __syncthreads();
-        // Expected inside: the row's part of the sample's ranks between r0 and r1. Where that is more than the slots take, the bracket's bins are counted first.
-        collect = whole || (float)n * (float)(r1 - r0) <= 0.75f * kSample * (float)((kOwn - 4) * NT) * (float)nrank;
+        // (where the slots do not take what lies inside, the bracket's bins are counted first)
+        collect = whole || collects(n, dev, NT, kSample, nrank);
         // (a rank beyond the sample: no bracket on that side)
         if (S.bin[0] >= 0 && r0 >= 1) hi = min(umin + ((uint32_t)(S.bin[0] + 1) << shift) - 1u, 0x7FFFFFFFu);
         if (S.bin[1] >= 0) lo = umin + ((uint32_t)S.bin[1] << shift);
@@ -453,7 +461,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) select_kernel(Rows R, int rows,
             break;
         }
         if (count <= kRank) {                                     // they meet in the first CTA
-            SelectShared<NT>* first = cluster.map_shared_rank(&S, 0);
+            SelectShared<NT, kCluster>* first = cluster.map_shared_rank(&S, 0);
             inside_keys([&](uint2 x) { if ((x.x - lo) >> shift == 0u) first->cand[atomicAdd(&first->ncand, 1)] = order_key(x.x, (int)x.y); });
             cluster.sync();
             if (rank != 0) return;
@@ -468,35 +476,34 @@ __global__ void __launch_bounds__(NT, 1024 / NT) select_kernel(Rows R, int rows,
     if (tid == 0) weakest[item] = found;
 }
 
-// The same for rows that the registers hold: NT threads with kKeys keys each, and where there are few rows up to eight such CTAs as a cluster. The row is read in one go, a
+// The same for rows that the registers hold: NT threads with kKeys keys each. The row is read in one go, a
 // histogram of all its keys over their range finds the threshold's bin, and that bin is ranked: a third of the sample's and the sweep's instructions, and fewer
 // barriers and round trips, which is what counts for few rows.
 template <int NT, int kKeys>
 __global__ void __launch_bounds__(NT, 1024 / NT) select_held_kernel(Rows R, int rows, int w, unsigned long long* weakest, Plan P) {
     static_assert(NT <= kBins, "a thread has a bin at least");
     extern __shared__ __align__(16) uint8_t select_smem[];
-    ClusterShared<NT>& S = *reinterpret_cast<ClusterShared<NT>*>(select_smem);
-    cg::cluster_group cluster = cg::this_cluster();
-    const int tid = threadIdx.x, nrank = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    HeldShared<NT>& S = *reinterpret_cast<HeldShared<NT>*>(select_smem);
+    const int tid = threadIdx.x;
     for (int i = tid; i < kBins; i += NT) S.hist[i] = 0;
     if (tid == 0) S.ncand = 0;
     pdl_enter(R.table, R.seq, R.pos, R.delta, weakest, P.ustart, P.tickets);
-    int item = blockIdx.x / nrank;
+    int item = blockIdx.x;
     if (P.ustart && item-- == 0) {
-        if (rank == 0) make_plan<NT>(R, rows, P);
+        make_plan<NT>(R, rows, P);
         return;
     }
     const int t = item / R.Hq, h = item % R.Hq;
     int r;
     const int n = R.visible(t, r);
     if (n <= w) {                                                 // every key
-        if (tid == 0 && rank == 0) weakest[item] = 0ull;
+        if (tid == 0) weakest[item] = 0ull;
         return;
     }
     const int32_t* pages = R.table + r * R.ld;
     const float* plane = R.delta + ((size_t)h << R.page_log);
     const int stride = R.Hq << R.page_log;
-    auto index = [&](int k) { return 4 * (((k >> 2) * nrank + rank) * NT + tid) + (k & 3); };
+    auto index = [&](int k) { return 4 * ((k >> 2) * NT + tid) + (k & 3); };
     constexpr uint32_t kNone = 0xFFFFFFFFu;
     constexpr int kTogether = kKeys < 16 ? kKeys : 16;            // keys of a thread on their way at a time
     uint32_t u[kKeys], umin = 0x7FFFFFFFu, umax = 0u;
@@ -522,14 +529,6 @@ __global__ void __launch_bounds__(NT, 1024 / NT) select_held_kernel(Rows R, int 
         umax = (uint32_t)max((int)umax, (int)u[k]);
     }
     range_of<NT>(S, umin, umax);                                  // (its barrier: the histogram is zero)
-    if (nrank > 1) {
-        if (tid == 0) { S.umin = umin; S.umax = umax; }
-        cluster.sync();
-        for (int q = 0; q < nrank; ++q) {
-            umin = min(umin, *cluster.map_shared_rank(&S.umin, q));
-            umax = max(umax, *cluster.map_shared_rank(&S.umax, q));
-        }
-    }
     // the bin that holds the need-th, then, while it holds many keys of several patterns, the bins of its own range
     uint32_t lo = umin, nbins = kBins, pattern = 0u;
     int shift = shift_of(umax - umin), need = w, count;
@@ -541,21 +540,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) select_held_kernel(Rows R, int 
             if (bin < nbins) atomicAdd(&S.hist[bin], 1);
         }
         int excl, c[kBins / NT], bin, before, in_bin;
-        if (nrank > 1) {
-            // the bins of the whole row in `sum`, which nobody else reads; then, when all have read them, this CTA's are zeroed
-            cluster.sync();
-            for (int i = tid; i < kBins; i += NT) {
-                int all = 0;
-                for (int q = 0; q < nrank; ++q) all += cluster.map_shared_rank(S.hist, q)[i];
-                S.sum[i] = all;
-            }
-            cluster.sync();
-            for (int i = tid; i < kBins; i += NT) S.hist[i] = 0;
-            scan_bins<NT>(S, S.sum, excl, c);
-        } else {
-            __syncthreads();
-            scan_bins<NT>(S, S.hist, excl, c);
-        }
+        __syncthreads();
+        scan_bins<NT>(S, S.hist, excl, c);
         if (bin_of<NT>(need, excl, c, bin, before, in_bin)) { S.bin[0] = bin; S.need = need - before; S.count = in_bin; }
         __syncthreads();
         lo += (uint32_t)S.bin[0] << shift;
@@ -577,16 +563,11 @@ __global__ void __launch_bounds__(NT, 1024 / NT) select_held_kernel(Rows R, int 
         }
         __syncthreads();                                          // (bin, need and count have been read)
     }
-    unsigned long long found;
-    {
-        ClusterShared<NT>* first = nrank > 1 ? cluster.map_shared_rank(&S, 0) : &S;
 #pragma unroll
-        for (int k = 0; k < kKeys; ++k)
-            if ((u[k] - lo) >> shift == 0u) first->cand[atomicAdd(&first->ncand, 1)] = order_key(by_index ? pattern : u[k], index(k));
-        if (nrank > 1) cluster.sync(); else __syncthreads();
-        if (rank != 0) return;
-        found = rank_candidates<NT>(S, count, need);
-    }
+    for (int k = 0; k < kKeys; ++k)
+        if ((u[k] - lo) >> shift == 0u) S.cand[atomicAdd(&S.ncand, 1)] = order_key(by_index ? pattern : u[k], index(k));
+    __syncthreads();
+    const unsigned long long found = rank_candidates<NT>(S, count, need);
     if (tid == 0) weakest[item] = found;
 }
 
@@ -597,29 +578,35 @@ int select_launch(void (*kernel)(Rows, int, int, unsigned long long*, Plan), int
 }
 }  // namespace
 
+// The form by the table's capacity, which bounds the rows' lengths (and with w their brackets), and by the number of (row, head) items. us of one form and of
+// the next, 32 heads, rows of the capacity, w a quarter of it:
+//   up to 2K     held by 256 threads; by 1024 for 13 rows 4.5 against 9.2, for one row 3.7 against 3.9
+//   up to 4K     held by 1024 threads where every item has an SM (4 rows 4.1; by 256 4.7), else by 256 (5 rows 4.8 against 6.2; 13 rows 6.6 against 11.5)
+//   up to 16K    held by 1024 threads where two items per SM are all (one row of 16K 6.3; swept 7.8. 9 rows 13.6 against 14.0; 10 rows 17.7 against 17.1)
+//   beyond       swept: by 256 threads where there are many items and the bracket fits their slots (64 rows of 16K 57; by 512 70), else by 512 (64 rows of 32K 108 against 144), whose
+//                cluster is as large as the bracket needs (9 rows of 256K, w = 8192: two CTAs 92, one, which sweeps twice, 133; 32 of 128K, w = 32K: 208 against 267). Where no cluster's slots would do,
+//                256 threads again (64 rows of 64K, two sweeps 264 against 281).
+//                Few rows take larger clusters: of 16K keys per CTA where an SM has one (one row of 64K: four CTAs 12.5, two 14.0, eight 16.6), of 32K where it has two (2 rows of 128K:
+//                four 22.7, two 24.6; 4 rows of 32K: two 18.8, one 14.5; one row of 256K: eight 24.6, two 36).
 int launch_cache4_select(const Cache& C, const Rows& R, unsigned long long* weakest, const Plan& plan, cudaStream_t st) {
-    const int64_t capacity = (int64_t)C.max_blocks << C.page_log;
-    auto stream = [&](auto nt, auto kernel, int cluster) { return select_launch(kernel, nt, sizeof(SelectShared<nt>), cluster, C, R, weakest, plan, st); };
-    auto held = [&](auto nt, auto kernel, int cluster) { return select_launch(kernel, nt, sizeof(ClusterShared<nt>), cluster, C, R, weakest, plan, st); };
-    using std::integral_constant;
-    constexpr integral_constant<int, 256> t256{};
-    constexpr integral_constant<int, 512> t512{};
-    constexpr integral_constant<int, 1024> t1024{};
-    constexpr int K = 1024;
-    const int items = C.rows * C.Hq;
-    if (items >= 3 * 148) {
-        if (capacity <= 2 * K) return held(t256, select_held_kernel<256, 8>, 1);
-        if (capacity <= 4 * K) return held(t256, select_held_kernel<256, 16>, 1);
-        if (capacity <= 32 * K) return stream(t256, select_kernel<256, 8, false>, 1);
-        return stream(t512, select_kernel<512, 8, false>, 1);
-    }
-    if (capacity <= 4 * K) return held(t1024, select_held_kernel<1024, 4>, 1);
-    if (capacity <= 8 * K) return held(t1024, select_held_kernel<1024, 8>, 1);
-    if (capacity <= 16 * K) return held(t1024, select_held_kernel<1024, 16>, 1);
-    if (capacity <= 32 * K) return held(t1024, select_held_kernel<1024, 32>, 1);
+    constexpr int K = 1024, kSms = 148;
+    const int capacity = C.max_blocks << C.page_log, items = C.rows * C.Hq;
+    auto held = [&](auto nt, auto kernel) { return select_launch(kernel, nt, sizeof(HeldShared<nt>), 1, C, R, weakest, plan, st); };
+    constexpr std::integral_constant<int, 256> t256{};
+    constexpr std::integral_constant<int, 1024> t1024{};
+    if (capacity <= 2 * K) return held(t256, select_held_kernel<256, 8>);
+    if (capacity <= 4 * K) return items <= kSms ? held(t1024, select_held_kernel<1024, 4>) : held(t256, select_held_kernel<256, 16>);
+    const bool few = items <= 2 * kSms;
+    if (few && capacity <= 8 * K) return held(t1024, select_held_kernel<1024, 8>);
+    if (few && capacity <= 16 * K) return held(t1024, select_held_kernel<1024, 16>);
+    auto fits = [&](int threads, int ctas) { return collects(capacity, bracket(capacity, C.w, kPer * threads), threads, kPer * threads, ctas); };
     int cluster = 1;
-    while (cluster < 8 && items * cluster * 2 <= 2 * 148 && capacity / cluster > 32 * K) cluster *= 2;
-    return cluster == 1 ? stream(t512, select_kernel<512, 8, false>, 1) : stream(t512, select_kernel<512, 8, true>, cluster);
+    while (cluster < 8 && !fits(512, cluster)) cluster *= 2;
+    const bool one_sweep = fits(512, cluster);
+    if (!few && (fits(256, 1) || !one_sweep)) return select_launch(select_kernel<256, false>, 256, sizeof(SelectShared<256, false>), 1, C, R, weakest, plan, st);
+    while (cluster < 8 && items * cluster * 2 <= 2 * kSms && capacity / (2 * cluster) >= (items * cluster * 2 <= kSms ? 16 : 32) * K) cluster *= 2;
+    if (cluster == 1) return select_launch(select_kernel<512, false>, 512, sizeof(SelectShared<512, false>), 1, C, R, weakest, plan, st);
+    return select_launch(select_kernel<512, true>, 512, sizeof(SelectShared<512, true>), cluster, C, R, weakest, plan, st);
 }
 
 int launch_cache4_plan(const Cache& C, const Rows& R, const Plan& plan, cudaStream_t st) {

@@ -614,3 +614,61 @@ def test_two_streams_and_two_workspaces():
     for x, runs in zip(alone, got):
         for y in runs:
             assert torch.equal(x[0], y[0]) and torch.equal(x[1], y[1])
+
+
+@pytest.mark.parametrize("kind", ["random", "few", "equal", "segments"])
+@pytest.mark.parametrize("n,rows,w", [
+    (3000, 150, 700), (7001, 120, 3000),                                   # held by 256 threads, or by 1024
+    (16001, 160, 8000), (40000, 160, 12000),                               # swept by 256 threads, by 512
+    (131000, 160, 40000), (140000, 20, 30000),                             # by clusters, of many rows and of few
+    (1000003, 1, 300000), (1000003, 150, 300000)])                         # no bracket fits: two sweeps, by a cluster of eight and by 256 threads
+def test_decode_selection_by_every_form(n, rows, w, kind):
+    """Forms that lengths, windows and numbers of rows lead to. The kept set from a stable sort, the sums in 64 bits on the device; the tolerances as above."""
+    Hq, Hkv, d, page = 2, 1, 64, 64
+    blocks, half = -(-n // page), torch.finfo(torch.bfloat16).eps / 2
+    keys, g = blocks * page, torch.Generator("cuda").manual_seed(n)
+    c = dma.cache(Hq, Hkv, d, w=w, rows=rows, nseq=1, page_size=page, num_pages=blocks, max_blocks=blocks)
+    codes, scales, delta = dma.cache4(c, "cuda")
+    codes.random_(0, 256, generator=g)
+    scales.copy_(torch.randn(scales.shape, generator=g, device="cuda"))
+    scales[..., 0] = scales[..., 0].abs() / 8
+    x = torch.rand(Hq, keys, generator=g, device="cuda")
+    dl = {"random": 1 + x, "few": 1 + (8 * x).floor() / 8, "equal": torch.ones_like(x), "segments": 1 + (16 * x[:, ::512]).floor().repeat_interleave(512, 1)[:, :keys] / 16}[kind]
+    delta.copy_(dl.view(Hq, blocks, page).transpose(0, 1))
+    q = torch.randn(rows, Hq, d, generator=g, device="cuda").bfloat16()
+    o, lse = dma.dma_cache4_decode(c, q, codes, scales, delta, i32(np.arange(blocks)[None]), i32([0] * rows), i32([n - 1 - t for t in range(rows)]))
+    for t in {0, rows - 1}:
+        for h in range(Hq):
+            j = torch.sort(dl[h, :n - t], descending=True, stable=True)[1][:w]
+            at, place = j // page, j % page
+            nib, sc = codes[at, 0, place], scales[at, 0, place].double()
+            kv = torch.stack([nib & 15, nib >> 4], -1).flatten(2).double() * sc[:, :, :, 0] + sc[:, :, :, 1]
+            bias, qd = dl[h, j].double(), q[t, h].double() / math.sqrt(d)
+            score = kv[:, 0] @ qd + bias
+            big = ((kv[:, 0] - sc[:, 0, :, 1]).abs() + sc[:, 0, :, 1].abs()) @ qd.abs() + bias.abs()
+            p = torch.softmax(score, 0)
+            exact, u = p @ kv[:, 1], 2.0 ** -24
+            e = (128 + 8) * u * float(big.max())
+            pv = p @ (kv[:, 1] - sc[:, 1, :, 1] + sc[:, 1, :, 1].abs())
+            lim = (2 * e + (w + 64) * u) * pv + torch.finfo(torch.float16).eps / 2 * (p @ (kv[:, 1] - sc[:, 1, :, 1])) + half * exact.abs() + 1e-30
+            err = (o[t, h].double() - exact).abs()
+            assert (err <= lim).all(), (t, h, float((err / lim).max()))
+            want = float(torch.logsumexp(score, 0))
+            assert abs(float(lse[t, h]) - want) <= e + (w + 64) * u + 2.0 ** -23 * abs(want), (t, h)
+
+
+@pytest.mark.parametrize("w", [500, 4096])
+def test_decode_by_a_cta_per_item(w):
+    """So many rows of a short table that the work is not dealt out."""
+    decode_case(4, 2, 64, 64, w, [4096, 3001, 2500, 101, 1024, 4095, 333, 1999, 2050], drafts=100, check=list(range(0, 900, 61)), seed=w)
+
+
+@pytest.mark.parametrize("dtype,lens", [("bf16", [300]), ("bf16", [5000]), ("fp32", [300]), ("fp32", [5000])])
+def test_decode_clears_the_status(dtype, lens):
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    blocks = -(-lens[0] // 64)
+    c, *arrays = pool_of(2, 1, 64, 64, blocks, 1, dt, nseq=1, blocks=blocks, w=100)
+    filled(c, *arrays, 1)
+    ws = torch.full((dma.dma_cache4_decode_workspace(c),), 0xAB, dtype=torch.uint8, device="cuda")
+    dma.dma_cache4_decode(c, torch.ones(1, 2, 64, dtype=dt, device="cuda"), *arrays, i32(np.arange(blocks)[None]), i32([0]), i32([lens[0] - 1]), ws=ws)
+    assert dma.dma_read_status(ws) == 0
