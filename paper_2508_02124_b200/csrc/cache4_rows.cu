@@ -274,13 +274,14 @@ int append_tiles(const Cache& C, int ctas, const void* K, const void* V, const f
     return launch_overlapped(cache4_append_kernel<T, D, kRows>, dim3(ctas, C.Hkv), dim3(kAppendThreads), smem, st, 1, (const T*)K, (const T*)V, W, A, delta_new, delta_ld, slot, codes,
                              (uint32_t*)scales, delta, C.rows, C.Hq, C.Hkv, C.G, C.ks[0], C.ks[1], C.vs[0], C.vs[1], C.page_log, C.num_pages << C.page_log);
 }
-// Tiles of 32 rows on six CTAs per SM (of 64: 32.1 us for 16384 rows of 8 heads, of 32: 30.4); of a pass's rows where that leaves SMs without one, or the heads' z need the room.
+// Tiles of 32 rows on six CTAs per SM where there are three per SM (us of 64, 32 and, a pass's, 8 rows, d = 128: 16384 rows of 8 heads 32.1, 30.4 and 32.5, 2048 rows -, 6.5 and 7.0, 1024 rows -, 5.2
+// and 4.6); of a pass's rows where there are fewer, or the heads' z need the room.
 template <typename T, int D>
 int append(const Cache& C, const void* K, const void* V, const float* W, const float* A, const float* delta_new, int64_t delta_ld, const int32_t* slot,
            uint8_t* codes, __nv_bfloat16* scales, float* delta, cudaStream_t st) {
     constexpr int kPassRows = kAppendThreads / (D / 16), kTile = 32;
     const int tiles = (C.rows + kTile - 1) / kTile, most = (6 * 148 + C.Hkv - 1) / C.Hkv;
-    if (kTile > kPassRows && (int64_t)tiles * C.Hkv >= 148 && (size_t)C.G * (D + 2 * kTile) * sizeof(float) <= 48 * 1024)
+    if (kTile > kPassRows && (int64_t)tiles * C.Hkv >= 3 * 148 && (size_t)C.G * (D + 2 * kTile) * sizeof(float) <= 48 * 1024)
         return append_tiles<T, D, kTile>(C, std::min(tiles, most), K, V, W, A, delta_new, delta_ld, slot, codes, scales, delta, st);
     return append_tiles<T, D, kPassRows>(C, std::min((C.rows + kPassRows - 1) / kPassRows, most), K, V, W, A, delta_new, delta_ld, slot, codes, scales, delta, st);
 }
