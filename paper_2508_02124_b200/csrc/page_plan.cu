@@ -158,12 +158,14 @@ bool apart(const int32_t* a, const int32_t* b, size_t n) { return a + n <= b || 
 
 int launch_page_plan(const Cache& C, const int32_t* lens, const int32_t* want, int32_t* table, int32_t* ring, const int32_t* pool, int32_t* lens_out,
                      int32_t* pool_out, int32_t* cu, int32_t* row_seq, int32_t* row_pos, int32_t* slot, cudaStream_t st) {
-    // Several CTAs where there may be much to write, a thread per row or page (us of one CTA and of 16: 64 requests that bring 4096 rows and hold up to 512 pages 8.6 and 6.9, 256 of them 14.4
-    // and 7.2, 16 that bring 8192 rows 7.9 and 6.1; decoding steps of 64 to 1000 requests 5.3 to 6.6 either way: one, which needs no second kernel where lengths are updated in place).
+    // Lengths and pool that are updated in place are written when every CTA has read them: by a second kernel where there are several.
+    const bool in_place = !(apart(lens, lens_out, C.nseq) && apart(want, lens_out, C.nseq) && apart(pool, pool_out, 4));
+    // Several CTAs where there may be much to write, a thread per row or page (us of one CTA and of this many, replayed: 64 requests that bring 4096 rows and hold up to 512 pages 7.3 and 5.1, in
+    // place, with 2 to set it up, 9.3 and 10.6; 16 that bring 8192 rows 9.3 and 4.9, in place 11.2 and 10.5; decoding steps of 64 to 1000 requests the same either way).
     const int64_t most = (int64_t)C.rows + (int64_t)C.nseq * C.max_blocks;
-    const int ctas = C.rows <= 1024 && most <= 64 * 1024 ? 1 : (int)std::min<int64_t>(148, (most + kPlanThreads - 1) / kPlanThreads);
-    // Lengths and pool that are updated in place are written when every CTA has read them.
-    const bool two = ctas > 1 && !(apart(lens, lens_out, C.nseq) && apart(want, lens_out, C.nseq) && apart(pool, pool_out, 4));
+    const bool little = C.rows <= (in_place ? 4096 : 1024) && most <= 64 * 1024;
+    const int ctas = little ? 1 : (int)std::min<int64_t>(148, (most + kPlanThreads - 1) / kPlanThreads);
+    const bool two = ctas > 1 && in_place;
     int rc = launch_overlapped(page_plan_kernel, dim3(ctas), dim3(kPlanThreads), 0, st, 1, lens, want, table, ring, pool, lens_out, pool_out, cu, row_seq, row_pos,
                                slot, C.nseq, C.rows, C.page_log, C.num_pages, C.max_blocks, C.table_ld, !two, true);
     if (rc || !two) return rc;
