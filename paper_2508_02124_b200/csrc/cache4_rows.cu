@@ -3,7 +3,7 @@
 // Append: a group of d / 16 lanes owns a row of one KV head, 16 channels of K and of V per lane: two words of codes, four lanes to the 64 channels of a scale. Bound by
 // instructions (61 % of the issue slots, 18 per warp and 32 values). 16384 rows of 8 heads, d = 128: 31 us, 2.9 TB/s (57 with divisions beside ties, 45 with 8 channels
 // per lane: what a row takes beside its values is shared by fewer of them).
-// Read: d / 8 lanes, a word of codes each; bound by memory. 14336 rows 17 us, 4.5 TB/s.
+// Read: d / 8 lanes, a word of codes each; bound by memory. 14336 rows 16.6 us, 4.7 TB/s.
 #include <algorithm>
 #include <type_traits>
 
@@ -243,19 +243,36 @@ template <typename T, int D, int kRows>
 __global__ void __launch_bounds__(kThreads) cache4_read_kernel(const uint8_t* codes, const uint32_t* scales, const float* delta, const int32_t* slot, T* K, T* V,
                                                                float* delta_out, int64_t delta_ld, int rows, int Hq, int Hkv, int G, int64_t ks_row, int64_t ks_head,
                                                                int64_t vs_row, int64_t vs_head, int page_log, int nslots) {
-    constexpr int LPR = D / 8, RPW = 32 / LPR;
+    constexpr int LPR = D / 8, RPW = 32 / LPR, kTurns = kRows / (8 * RPW), kTogether = sizeof(T) == 2 ? kTurns : 1;      // (rows of a lane; requested at once)
     const int hk = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane % LPR, grp = lane / LPR;
     pdl_enter(codes, scales, delta, slot, K, V, delta_out);
     const int place_mask = (1 << page_log) - 1, t0 = blockIdx.x * kRows, n = min(kRows, rows - t0);
-    for (int r = warp * RPW + grp; r < n; r += 8 * RPW) {
-        const int t = t0 + r, at = slot[t];
-        if ((unsigned)at >= (unsigned)nslots) continue;
-        const size_t row = key_row(at >> page_log, hk, at & place_mask, Hkv, page_log);
-        float k[8], v[8];
-        expand(*reinterpret_cast<const uint32_t*>(codes + row * D + sub * 4), scales[row * (D / 32) + sub / 8], k);
-        expand(*reinterpret_cast<const uint32_t*>(codes + row * D + D / 2 + sub * 4), scales[row * (D / 32) + D / 64 + sub / 8], v);
-        store8(K + t * ks_row + hk * ks_head + sub * 8, k);
-        store8(V + t * vs_row + hk * vs_head + sub * 8, v);
+#pragma unroll 1
+    for (int i0 = 0; i0 < kTurns; i0 += kTogether) {
+        int at[kTogether];
+        uint32_t kw[kTogether], vw[kTogether], kp[kTogether], vp[kTogether];
+        auto row_of = [&](int i) { return ((i0 + i) * 8 + warp) * RPW + grp; };
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i) at[i] = row_of(i) < n ? slot[t0 + row_of(i)] : -1;
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i) {
+            if ((unsigned)at[i] >= (unsigned)nslots) continue;
+            const size_t row = key_row(at[i] >> page_log, hk, at[i] & place_mask, Hkv, page_log);
+            kw[i] = *reinterpret_cast<const uint32_t*>(codes + row * D + sub * 4);
+            vw[i] = *reinterpret_cast<const uint32_t*>(codes + row * D + D / 2 + sub * 4);
+            kp[i] = scales[row * (D / 32) + sub / 8];
+            vp[i] = scales[row * (D / 32) + D / 64 + sub / 8];
+        }
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i) {
+            if ((unsigned)at[i] >= (unsigned)nslots) continue;
+            const int t = t0 + row_of(i);
+            float k[8], v[8];
+            expand(kw[i], kp[i], k);
+            expand(vw[i], vp[i], v);
+            store8(K + t * ks_row + hk * ks_head + sub * 8, k);
+            store8(V + t * vs_row + hk * vs_head + sub * 8, v);
+        }
     }
     if (!delta_out) return;
     for (int i = tid; i < G * kRows; i += kThreads) {
@@ -286,13 +303,21 @@ int append(const Cache& C, const void* K, const void* V, const float* W, const f
     return append_tiles<T, D, kPassRows>(C, std::min((C.rows + kPassRows - 1) / kPassRows, most), K, V, W, A, delta_new, delta_ld, slot, codes, scales, delta, st);
 }
 
-template <typename T, int D>
-int read(const Cache& C, const uint8_t* codes, const __nv_bfloat16* scales, const float* delta, const int32_t* slot, void* K, void* V, float* delta_out,
-         int64_t delta_ld, cudaStream_t st) {
-    constexpr int kRows = 32;
+template <typename T, int D, int kRows>
+int read_tiles(const Cache& C, const uint8_t* codes, const __nv_bfloat16* scales, const float* delta, const int32_t* slot, void* K, void* V, float* delta_out,
+               int64_t delta_ld, cudaStream_t st) {
     return launch_overlapped(cache4_read_kernel<T, D, kRows>, dim3((C.rows + kRows - 1) / kRows, C.Hkv), dim3(kThreads), 0, st, 1, codes, (const uint32_t*)scales, delta,
                              slot, (T*)K, (T*)V, delta_out, delta_ld, C.rows, C.Hq, C.Hkv, C.G, C.ks[0], C.ks[1], C.vs[0], C.vs[1], C.page_log,
                              C.num_pages << C.page_log);
+}
+// A lane has one row where the chip holds all CTAs at once, else two (us of one and of two, 8 heads: d = 128, 64 rows 1.8 and 2.1, 2000 rows 3.3 and 3.5, 32768 rows 38.9 and 34.5; d = 64 22.8 and
+// 20.3). bf16 rows are requested together (one after the other 36.4 with d = 128), fp32 ones are not (d = 128: 65.3, together 68.8).
+template <typename T, int D>
+int read(const Cache& C, const uint8_t* codes, const __nv_bfloat16* scales, const float* delta, const int32_t* slot, void* K, void* V, float* delta_out,
+         int64_t delta_ld, cudaStream_t st) {
+    constexpr int kPass = kThreads / (D / 8);
+    if ((int64_t)((C.rows + kPass - 1) / kPass) * C.Hkv > 8 * 148) return read_tiles<T, D, 2 * kPass>(C, codes, scales, delta, slot, K, V, delta_out, delta_ld, st);
+    return read_tiles<T, D, kPass>(C, codes, scales, delta, slot, K, V, delta_out, delta_ld, st);
 }
 
 }  // namespace
