@@ -7,7 +7,7 @@
 //   plan_kernel          the attention's shares of the work, where nothing is selected (else the selection's first CTA makes them)
 //
 // Measured, 32 heads, us: one row of 16384 keys 6.0, of 262144 25, of 1048576 49; 64 rows of 1 to 16K 41; 256 of 4096 68; 64 of 65536 178. Bound by barriers and round trips where there
-// are few rows, by instructions where there are many (64 rows of 1 to 16K: 64 % of the issue slots, 43 per 32 keys, the fixed part of a row included; the weights' bytes alone would take
+// are few rows, by instructions where there are many (64 rows of 1 to 16K: 63 % of the issue slots, 43 per 32 keys, the fixed part of a row included; the weights' bytes alone would take
 // a fifth of the time). All weights equal: 7 for the one row, 48 for the 64; quarters of whole numbers: 12 and 120.
 #include <cooperative_groups.h>
 
