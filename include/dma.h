@@ -324,9 +324,10 @@ int dma_page_plan(const dma_cache_t* c, const int32_t* lens, const int32_t* want
 int dma_cache4_append(const dma_cache_t* c, const void* K, const void* V, const float* W_delta, const float* A, const float* delta_new,
                       int64_t delta_ld, const int32_t* slot, void* codes, void* scales, float* delta, void* cuda_stream);
 
-/* Reads rows back: K, V [rows, Hkv, d] (k_stride, v_stride) get z + s n, formed in fp32 and rounded once; delta_out, if not NULL,
+/* Reads rows back: K, V [rows, Hkv, d] get z + s n, formed in fp32 and rounded once; delta_out, if not NULL,
  * gets [Hq, delta_ld >= rows] (dma_decode's and dma_mask_build's layout for one batch entry). Rows whose slot lies outside the
- * pool are left as they are. */
+ * pool are left as they are. k_stride and v_stride are those of this call's K and V: a descriptor that served dma_cache4_append
+ * with the strides of its rows gets those of the arrays read into first (the Python binding takes them from the tensors). */
 int dma_cache4_read(const dma_cache_t* c, const void* codes, const void* scales, const float* delta, const int32_t* slot, void* K,
                     void* V, float* delta_out, int64_t delta_ld, void* cuda_stream);
 

@@ -187,3 +187,58 @@ def test_most_sequences():
     c.nseq = (1 << 30) + 1
     with pytest.raises(RuntimeError):
         dma.dma_cache4_bytes(c)
+
+
+def test_read_goes_by_its_outputs_own_strides(monkeypatch):
+    """A descriptor that holds the strides of a projection's output, for dma_cache4_append, reads into arrays of any layout: the library gets the outputs' strides, and the
+    descriptor stays as it is."""
+    monkeypatch.setattr(dma, "_raw_device", lambda: -1)
+    monkeypatch.setattr(dma, "_stream", lambda: 0)
+    seen = []
+
+    def call(name, c, *a):
+        seen.append((tuple(c._obj.k_stride), tuple(c._obj.v_stride), a[4], a[5]))
+    monkeypatch.setattr(dma, "_call", call)
+    bf16 = dict(dtype=torch.bfloat16)
+    c = cache()
+    arrays, slot = dma.cache4(c, "cpu"), torch.zeros(3, dtype=torch.int32)
+    flat, wide = torch.zeros(3, 2, 128, **bf16), torch.zeros(3, 8, 128, **bf16)
+    dense = ((0, 0), (256, 128))
+    for strides in ((0, 0), (1024, 128), (256, 128)):
+        c.k_stride[:] = c.v_stride[:] = strides
+        for K, V, kst, vst in ((None, None, dense, dense), (flat, None, dense, dense), (wide[:, 4:6], wide[:, 6:], ((1024, 128),), ((1024, 128),)),
+                               (flat, wide[:, ::4], dense, ((1024, 512),)), (wide[:, :2, :128], flat, ((1024, 128),), dense)):
+            k, v, _ = dma.dma_cache4_read(c, *arrays, slot, K, V)
+            got = seen.pop()
+            assert got[0] in kst and got[1] in vst and got[2:] == (k.data_ptr(), v.data_ptr())
+            assert tuple(c.k_stride) == tuple(c.v_stride) == strides
+    # strides that mean nothing, of one row or one head, do not reach the library's check of strides
+    c = cache(rows=1, Hkv=1, Hq=4)
+    arrays = dma.cache4(c, "cpu")
+    for one in (torch.zeros(1, 1, 128, **bf16), torch.zeros(1, 1, 128, **bf16).as_strided((1, 1, 128), (3, 5, 1)), torch.zeros(9, 128, **bf16)[:1, None]):
+        dma.dma_cache4_read(c, *arrays, slot[:1], one, one)
+        got = seen.pop()
+        assert all(s == (0, 0) or min(s) > 0 and s[0] % 8 == s[1] % 8 == 0 for s in got[:2])
+    c = cache(rows=3, Hkv=1, Hq=4)
+    dma.dma_cache4_read(c, *dma.cache4(c, "cpu"), slot, wide[:, 5:6], wide[:, 5].unsqueeze(1).as_strided((3, 1, 128), (1024, 1, 1)))
+    assert all(s[0] == 1024 and s[1] > 0 and s[1] % 8 == 0 for s in seen.pop()[:2])
+    c = cache()
+    arrays = dma.cache4(c, "cpu")
+    for bad in (flat.float(), flat[:2], flat[:, :1], flat[..., :64], torch.zeros(3, 2, 256, **bf16)[..., ::2], torch.zeros(3, 256, **bf16)):
+        for kw in (dict(K=bad), dict(V=bad)):
+            with pytest.raises((TypeError, ValueError)):
+                dma.dma_cache4_read(c, *arrays, slot, **kw)
+    assert not seen
+
+
+def test_read_refuses_output_strides_that_the_library_cannot_write(lib, monkeypatch):
+    """Rows or heads on top of each other, or off the alignment: the library's own refusal."""
+    monkeypatch.setattr(dma, "_raw_device", lambda: -1)
+    monkeypatch.setattr(dma, "_stream", lambda: 0)
+    c = cache()
+    arrays, slot = dma.cache4(c, "cpu"), torch.zeros(3, dtype=torch.int32)
+    for bad in (torch.zeros(1, 2, 128, dtype=torch.bfloat16).expand(3, 2, 128), torch.zeros(3, 1, 128, dtype=torch.bfloat16).expand(3, 2, 128),
+                torch.zeros(3, 2, 132, dtype=torch.bfloat16)[..., :128]):
+        with pytest.raises(dma.DmaError) as e:
+            dma.dma_cache4_read(c, *arrays, slot, K=bad)
+        assert e.value.status == -3

@@ -672,3 +672,27 @@ def test_decode_clears_the_status(dtype, lens):
     ws = torch.full((dma.dma_cache4_decode_workspace(c),), 0xAB, dtype=torch.uint8, device="cuda")
     dma.dma_cache4_decode(c, torch.ones(1, 2, 64, dtype=dt, device="cuda"), *arrays, i32(np.arange(blocks)[None]), i32([0]), i32([lens[0] - 1]), ws=ws)
     assert dma.dma_read_status(ws) == 0
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,rows,dtype", [(8, 2, 128, 70, "bf16"), (4, 1, 64, 1, "bf16"), (4, 4, 64, 33, "fp32")])
+def test_append_from_a_projection_and_read_into_arrays_by_one_descriptor(Hq, Hkv, d, rows, dtype):
+    """Rows written from a slice of [rows, Hq + 2 Hkv, d] and read back, through the same descriptor, into contiguous arrays, new ones and a slice of another width: the same bits,
+    and what a descriptor without strides writes and reads."""
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    page, pages, g = 16, 9, torch.Generator().manual_seed(rows)
+    qkv = torch.randn(rows, Hq + 2 * Hkv, d, generator=g).to(dt).cuda()
+    K, V = qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
+    W, A = (torch.randn(Hq, d, generator=g) / math.sqrt(d)).cuda(), (torch.rand(Hq, generator=g) + 0.5).cuda()
+    slot = torch.randperm(pages * page, generator=g)[:rows].int().cuda()
+    c, *arrays = pool_of(Hq, Hkv, d, page, pages, rows, dt)
+    c.k_stride[:], c.v_stride[:] = K.stride()[:2], V.stride()[:2]
+    dma.dma_cache4_append(c, K, V, slot, *arrays, W, A)
+    plain, *same = pool_of(Hq, Hkv, d, page, pages, rows, dt)
+    dma.dma_cache4_append(plain, K.contiguous(), V.contiguous(), slot, *same, W, A)
+    want = dma.dma_cache4_read(plain, *same, slot)
+    into = [torch.full((rows, Hkv, d), 7.0, dtype=dt, device="cuda") for _ in range(2)]
+    wide = torch.full((rows, 2 * Hkv + 1, d + 8), 7.0, dtype=dt, device="cuda")
+    for got in (dma.dma_cache4_read(c, *arrays, slot), dma.dma_cache4_read(c, *arrays, slot, *into), dma.dma_cache4_read(c, *arrays, slot, wide[:, :Hkv, :d], into[1])):
+        assert all(torch.equal(bits(a), bits(b)) for a, b in zip(got, want))
+    assert (wide[:, Hkv:] == 7.0).all() and (wide[..., d:] == 7.0).all()
+    assert tuple(c.k_stride) == K.stride()[:2]
