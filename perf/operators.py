@@ -216,10 +216,9 @@ def prepare(case, seed):
             s["c"] = dma.cache(case["Hq"], case["Hkv"], case["d"], w=case.get("w", 1), dtype=_dtype(case), rows=case["rows"], page_size=case["page"],
                                num_pages=s["pages"], nseq=s["table"].shape[0] if kind == "decode" else 1,
                                max_blocks=s["table"].shape[1] if kind == "decode" else 1)
-        if kind == "append":                 # its rows are written from the projection's output and read back as arrays of their own
-            s["c_in"] = type(s["c"]).from_buffer_copy(s["c"])
-            s["c_in"].k_stride[:] = s["K"].stride()[:2]
-            s["c_in"].v_stride[:] = s["V"].stride()[:2]
+        if kind == "append":
+            s["c"].k_stride[:] = s["K"].stride()[:2]
+            s["c"].v_stride[:] = s["V"].stride()[:2]
         if kind == "decode":
             s["ws"] = torch.empty(dma.dma_cache4_decode_workspace(s["c"]), dtype=torch.uint8, device="cuda")
     return s
@@ -243,7 +242,7 @@ def _own_plan(s):
 
 def _own_append(s):
     from paper_2508_02124_b200 import binding as dma
-    dma.dma_cache4_append(s["c_in"], s["K"], s["V"], s["slot"], s["codes"], s["scales"], s["delta"], W_delta=s["W"], A=s["A"])
+    dma.dma_cache4_append(s["c"], s["K"], s["V"], s["slot"], s["codes"], s["scales"], s["delta"], W_delta=s["W"], A=s["A"])
     return _own_read(s)
 
 
