@@ -179,9 +179,10 @@ __global__ void __launch_bounds__(D) simt_combine_kernel(Rows R, const float* pa
 //            codes of a word take a shift and four masks. A group of 64 channels is a chain of four products, whose sum takes the group's scale, and with the query's own sum
 //            over the group its zero, in fp32; the query goes in as halves, scaled by a power of two per head (its 8 bits survive down to 2^-27 of the head's largest
 //            channel; the products of 16 n take q / 16). Nothing of K is rounded. Softmax in registers, with a running maximum per warp and head. Of V the
-//            scale goes into the weight, P s as a half, scaled by a power of two per head and group that follows its largest (WarpState); that rounding, at most 2^-11 of a
-//            weight, is the kernel's largest after the output's (its error against 64 bits grows by a sixth). z P is summed in fp32.
-//            With up to four heads the operand's columns 4 to 7 hold the same heads again, and their lanes take the second 16 keys through the softmax.
+//            scale goes into the weight, P s in two halves, its rounding and what that leaves, scaled by a power of two per head and group that follows the largest
+//            (WarpState): 2^-22 of a weight, and of the small ones 2^-31 of the largest, which is less than the sums' own rounding in fp32. z P is summed in fp32.
+//            With up to four heads the operand's columns 4 to 7 hold the same heads again: their lanes take the second 16 keys through the softmax, and in the
+//            products of V they hold the low halves (one half per weight took the same time: 64 rows of 1 to 16K keys, whole call, 158 and 156 us).
 // 64 rows of 1 to 16K keys, 32 / 8 heads of 128, w = 2048: 113 us for 414 MB read, 780 instructions per 32 keys of a union. 53 % of the issue slots, 54 % of the integer pipe, 18 % of the
 // tensor pipe: with all pages in the L2 it is 110 us, without the attending 90. Twelve warps per SM: sixteen, with stages that are swizzled to fit, 118; eight with three
 // stages 133 where twelve took 119. Codes as bf16 numbers and weights in a high and a low part 210 where this form took 165. 256 rows of 4096 keys, w = 1024: 221 us,
@@ -400,17 +401,25 @@ __device__ __forceinline__ void attend(WarpState<D>& W, const uint2 (&q)[D / kGr
     const uint8_t* vrow = data + ra * kPitch + D / 2 + 4 * r;
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-        uint32_t b[2][2];
+        // hi + lo is the weight to 2^-22 of it
+        uint32_t b[2][2], low[2][2];
 #pragma unroll
-        for (int i = 0; i < kSets; ++i) {
-            b[i][0] = turn8x8(halves(w[i][g][0] * W.f[g][0], w[i][g][1] * W.f[g][1]));
-            b[i][1] = turn8x8(halves(w[i][g][2] * W.f[g][0], w[i][g][3] * W.f[g][1]));
-        }
-        if constexpr (kSets == 1) {                               // (columns 0 to 3 hold the first 16 keys' weights, 4 to 7 the others': zeros for the other product)
-            b[1][0] = lane < 16 ? 0u : b[0][0];
-            b[1][1] = lane < 16 ? 0u : b[0][1];
-            b[0][0] = lane < 16 ? b[0][0] : 0u;
-            b[0][1] = lane < 16 ? b[0][1] : 0u;
+        for (int i = 0; i < kSets; ++i)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float x0 = w[i][g][2 * e] * W.f[g][0], x1 = w[i][g][2 * e + 1] * W.f[g][1];
+                const uint32_t hi = halves(x0, x1);
+                const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+                b[i][e] = turn8x8(hi);
+                low[i][e] = turn8x8(halves(x0 - back.x, x1 - back.y));
+            }
+        if constexpr (kSets == 1) {                               // (columns 0 to 3 hold the first 16 keys' weights, 4 to 7 the others': a product takes its keys' high parts in these, their low parts in those)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t other_low = __shfl_xor_sync(0xffffffffu, low[0][e], 16);
+                b[1][e] = lane < 16 ? other_low : b[0][e];
+                b[0][e] = lane < 16 ? b[0][e] : other_low;
+            }
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -423,7 +432,10 @@ __device__ __forceinline__ void attend(WarpState<D>& W, const uint2 (&q)[D / kGr
             expand_word(__byte_perm(wc, wd, 0x5410), a2);
             expand_word(__byte_perm(wc, wd, 0x7632), a3);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) mma16816(W.o[g][j], a0[j], a1[j], a2[j], a3[j], b[i][0], b[i][1]);
+            for (int j = 0; j < 4; ++j) {
+                mma16816(W.o[g][j], a0[j], a1[j], a2[j], a3[j], b[i][0], b[i][1]);
+                if constexpr (kSets == 2) mma16816(W.o[g][j], a0[j], a1[j], a2[j], a3[j], low[i][0], low[i][1]);
+            }
         }
     }
 }

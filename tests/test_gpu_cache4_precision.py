@@ -1,0 +1,79 @@
+"""GPU tests of what dma_cache4_decode keeps of its numbers: weights of scales of any sign and size, weights and queries in full. The exact results are formed in 64 bits on the
+device; the tolerances are those of fp32 sums."""
+import math
+
+import pytest
+import torch
+
+from paper_2508_02124_b200 import binding as dma
+
+pytestmark = pytest.mark.gpu
+I32 = dict(dtype=torch.int32, device="cuda")
+U = 2.0 ** -24                                                             # half a step of fp32
+
+
+def a_cache(Hq, Hkv, d, page, lens, w, dtype, seed, flags=0):
+    """A pool with random codes and ordinary scales, zeros and weights, a row per sequence, and its call's arguments."""
+    g = torch.Generator("cuda").manual_seed(seed)
+    nseq, blocks = len(lens), -(-max(lens) // page)
+    pages = nseq * blocks
+    c = dma.cache(Hq, Hkv, d, w=w, dtype=dtype, rows=nseq, nseq=nseq, page_size=page, num_pages=pages, max_blocks=blocks, flags=flags)
+    codes, scales, delta = dma.cache4(c, "cuda")
+    codes.random_(0, 256, generator=g)
+    scales.copy_(torch.randn(scales.shape, generator=g, device="cuda"))
+    scales[..., 0] = scales[..., 0].abs() / 4 + 0.05
+    delta.copy_(torch.exp(torch.nn.functional.softplus(torch.randn(delta.shape, generator=g, device="cuda")) / 4))
+    table = torch.randperm(pages, generator=g, device="cuda").int().view(nseq, blocks)
+    q = torch.randn(nseq, Hq, d, generator=g, device="cuda").to(dtype)
+    return c, q, (codes, scales, delta), (table, torch.arange(nseq, **I32), torch.tensor(lens, **I32) - 1)
+
+
+def check(c, q, arrays, plan, o, lse, exact_scores=False):
+    """A score is a sum of 2 d products and a few more operations: at most 136 U of the sum of its terms' magnitudes (`big`) off, where no query is 0; of a query 0 it is the bias,
+    and what is left is an exponential's, of 2^-22, and its argument's rounding. The sums of n weights and values are off by at most (n + 64) U of the sum of theirs. bf16 elements'
+    values go through the tensor cores as codes by weights p s in two halves: 2^-22 of a weight, and 2^-24 in units of which the largest weight of the row's head and group is 2^7 or more:
+    2^-31 of that one, times a code of up to 15."""
+    codes, scales, delta = arrays
+    table, seq, pos = plan
+    page, G = c.page_size, c.Hq // c.Hkv
+    half = torch.finfo(q.dtype).eps / 2
+    for t in range(c.rows):
+        n = int(pos[t]) + 1
+        j = torch.arange(n, device="cuda")
+        at, place = table[int(seq[t])][j // page].long(), j % page
+        for h in range(c.Hq):
+            dl = delta[at, h, place]
+            kept = torch.sort(dl, descending=True, stable=True)[1][:c.w]
+            nib, sc = codes[at[kept], h // G, place[kept]], scales[at[kept], h // G, place[kept]].double()
+            n4 = torch.stack([nib & 15, nib >> 4], -1).flatten(2).double()   # [kept, 2, d]
+            s, z = sc[..., 0].repeat_interleave(64, -1), sc[..., 1].repeat_interleave(64, -1)
+            bias, qd = dl[kept].double(), q[t, h].double() / math.sqrt(c.d)
+            score = (n4[:, 0] * s[:, 0] + z[:, 0]) @ qd + bias
+            big = float(((n4[:, 0] * s[:, 0].abs() + z[:, 0].abs()) @ qd.abs() + bias.abs()).max())
+            p = torch.softmax(score, 0)
+            exact = p @ (n4[:, 1] * s[:, 1] + z[:, 1])
+            e = 8 * U * big + 2.0 ** -22 if exact_scores else 136 * U * big
+            ps = p[:, None] * s[:, 1].abs()
+            lim = (2 * e + (len(kept) + 64) * U) * (p @ (n4[:, 1] * s[:, 1].abs() + z[:, 1].abs())) + 2.0 ** -22 * (ps * n4[:, 1]).sum(0) + len(kept) * 15 * 2.0 ** -31 * ps.max(0)[0]
+            lim = lim + half * exact.abs() + 1e-38
+            err = (o[t, h].double() - exact).abs()
+            assert (err <= lim).all(), (t, h, n, float((err / lim).max()))
+            want = float(torch.logsumexp(score, 0))
+            assert abs(float(lse[t, h]) - want) <= e + (len(kept) + 64) * U + 2.0 ** -23 * abs(want), (t, h, n)
+
+
+SHAPES = [(1, 1, 64), (4, 2, 128), (4, 1, 64), (8, 2, 128), (5, 1, 64), (8, 1, 128)]         # one, two, up to four and up to eight heads of a group
+
+
+@pytest.mark.parametrize("gate", [0.25, 3.0])
+@pytest.mark.parametrize("lens,w", [([40, 300, 3], 200), ([900, 5000], 700), ([20000], 16000)])
+@pytest.mark.parametrize("Hq,Hkv,d", SHAPES)
+def test_weights_keep_their_bits(Hq, Hkv, d, lens, w, gate):
+    """Queries of 0, so that the scores are the weights delta to the bit and what the values' sums lose is seen: values far larger than their sums. Nearly equal weights, and weights
+    over many powers of two."""
+    c, q, arrays, plan = a_cache(Hq, Hkv, d, 64, lens, w, torch.bfloat16, d + w)
+    arrays[2].copy_(torch.exp(arrays[2].log() * 4 * gate))
+    arrays[1][..., 1].copy_(-7.5 * arrays[1][..., 0])                      # values on both sides of zero
+    q.zero_()
+    o, lse = dma.dma_cache4_decode(c, q, *arrays, *plan)
+    check(c, q, arrays, plan, o, lse, exact_scores=True)
