@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(D) simt_combine_kernel(Rows R, const float* pa
 //            over the group its zero, in fp32; the query goes in as halves, scaled by a power of two per head (its 8 bits survive down to 2^-27 of the head's largest
 //            channel; the products of 16 n take q / 16). Nothing of K is rounded. Softmax in registers, with a running maximum per warp and head. Of V the
 //            scale goes into the weight, P s in two halves, its rounding and what that leaves, scaled by a power of two per head and group that follows the largest
-//            (WarpState): 2^-22 of a weight, and of the small ones 2^-31 of the largest, which is less than the sums' own rounding in fp32. z P is summed in fp32.
+//            (WarpState): 2^-22 of a weight, and of the small ones 2^-32 of the largest, which is less than the sums' own rounding in fp32. z P is summed in fp32.
 //            With up to four heads the operand's columns 4 to 7 hold the same heads again: their lanes take the second 16 keys through the softmax, and in the
 //            products of V they hold the low halves (one half per weight took the same time: 64 rows of 1 to 16K keys, whole call, 158 and 156 us).
 // 64 rows of 1 to 16K keys, 32 / 8 heads of 128, w = 2048: 113 us for 414 MB read, 780 instructions per 32 keys of a union. 53 % of the issue slots, 54 % of the integer pipe, 18 % of the
@@ -375,7 +375,7 @@ __device__ __forceinline__ void attend(WarpState<D>& W, const uint2 (&q)[D / kGr
                 W.oz[g][0] = fmaf(p[0], za, fmaf(p[2], zb, W.oz[g][0]));
                 W.oz[g][1] = fmaf(p[1], za, fmaf(p[3], zb, W.oz[g][1]));
             }
-            most = fmaxf(most, fmaxf(fmaxf(w[i][g][0], w[i][g][2]) * W.f[g][0], fmaxf(w[i][g][1], w[i][g][3]) * W.f[g][1]));
+            most = fmaxf(most, fmaxf(fmaxf(fabsf(w[i][g][0]), fabsf(w[i][g][2])) * W.f[g][0], fmaxf(fabsf(w[i][g][1]), fabsf(w[i][g][3])) * W.f[g][1]));
         }
     }
     move = move || __any_sync(0xffffffffu, most > 32768.0f);
@@ -384,8 +384,8 @@ __device__ __forceinline__ void attend(WarpState<D>& W, const uint2 (&q)[D / kGr
         for (int g = 0; g < NG; ++g)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                float top = fmaxf(w[0][g][e], w[0][g][e + 2]);
-                if constexpr (kSets == 2) top = fmaxf(top, fmaxf(w[1][g][e], w[1][g][e + 2]));
+                float top = fmaxf(fabsf(w[0][g][e]), fabsf(w[0][g][e + 2]));             // (scales of the caller's may be negative)
+                if constexpr (kSets == 2) top = fmaxf(top, fmaxf(fabsf(w[1][g][e]), fabsf(w[1][g][e + 2])));
                 top = fmaxf(over_keys(top), W.wref[g][e] * fade[e]);
                 W.wref[g][e] = top;
                 const int up = 7 + 127 - (int)(__float_as_uint(top) >> 23);

@@ -77,3 +77,18 @@ def test_weights_keep_their_bits(Hq, Hkv, d, lens, w, gate):
     q.zero_()
     o, lse = dma.dma_cache4_decode(c, q, *arrays, *plan)
     check(c, q, arrays, plan, o, lse, exact_scores=True)
+
+
+@pytest.mark.parametrize("flags", [0, dma.DMA_FLAG_SIMT])
+@pytest.mark.parametrize("size", [2.0 ** -30, 1.0, 2.0 ** 30])
+@pytest.mark.parametrize("sign", ["negative", "mixed"])
+@pytest.mark.parametrize("Hq,Hkv,d", SHAPES)
+def test_scales_of_any_sign_and_size(Hq, Hkv, d, sign, size, flags):
+    """Arrays are the caller's: a code n stands for z + s n whatever the sign of s."""
+    c, q, arrays, plan = a_cache(Hq, Hkv, d, 32, [1, 40, 300, 3000], 700, torch.bfloat16, d + Hq, flags)
+    g = torch.Generator("cuda").manual_seed(1)
+    s = arrays[1][..., 0]
+    s.mul_(-1.0 if sign == "negative" else torch.randint(0, 2, s.shape, generator=g, device="cuda") * 2.0 - 1.0)
+    arrays[1][:, :, :, 1].mul_(size)                                       # V's scales and zeros
+    o, lse = dma.dma_cache4_decode(c, q, *arrays, *plan)
+    check(c, q, arrays, plan, o, lse)
