@@ -10,6 +10,7 @@
 #include <climits>
 
 #include "cache4_decode.cuh"
+#include "sm100_ptx.cuh"
 
 namespace dma {
 namespace {
@@ -177,8 +178,8 @@ __global__ void __launch_bounds__(D) simt_combine_kernel(Rows R, const float* pa
 //   attend   S^T = K q^T and O^T += V^T P^T by mma.m16n8k16 (keys, then channels, by heads). What bounds this kernel is the integer pipe that expands the codes, so they are
 //            expanded as little as possible: a code n in the lowest mantissa bits of a half is the subnormal number n 2^-24, exactly, and four bits higher 16 n 2^-24; eight
 //            codes of a word take a shift and four masks. A group of 64 channels is a chain of four products, whose sum takes the group's scale, and with the query's own sum
-//            over the group its zero, in fp32; the query goes in as halves, scaled by a power of two per head (its 8 bits survive down to 2^-27 of the head's largest
-//            channel; the products of 16 n take q / 16). Nothing of K is rounded. Softmax in registers, with a running maximum per warp and head. Of V the
+//            over the group its zero, in fp32; the query goes in as halves, scaled by a power of two per head and group (its 8 bits survive down to 2^-27 of the largest
+//            channel there, and what is lost below that is less than the rounding of the sums; the products of 16 n take q / 16). Nothing of K is rounded. Softmax in registers, with a running maximum per warp and head. Of V the
 //            scale goes into the weight, P s in two halves, its rounding and what that leaves, scaled by a power of two per head and group that follows the largest
 //            (WarpState): 2^-22 of a weight, and of the small ones 2^-32 of the largest, which is less than the sums' own rounding in fp32. z P is summed in fp32.
 //            With up to four heads the operand's columns 4 to 7 hold the same heads again: their lanes take the second 16 keys through the softmax, and in the
@@ -247,7 +248,7 @@ template <int D>
 struct WarpState {
     static constexpr int NG = D / kGroup;
     float o[NG][4][4], oz[NG][2], f[NG][2], wref[NG][2], m[2], l[2];
-    float qsum[NG][2], scale[2];
+    float qsum[NG][2], scale[NG][2];
 };
 
 // 32 keys of a stage. odd (of the warp): some scale is not finite; a head that does not keep the key is to get nothing of it. One instance of this code per kernel:
@@ -299,22 +300,18 @@ __device__ __forceinline__ void attend(WarpState<D>& W, const uint2 (&q)[D / kGr
             pa[0] = a.x; pa[1] = a.y;
             pb[0] = b.x; pb[1] = b.y;
         }
-        float dot[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        const float2 ba = *reinterpret_cast<const float2*>(&bias[key][col]), bb = *reinterpret_cast<const float2*>(&bias[key + 8][col]);
+        float2 xa = ba, xb = bb;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
             const float sa = pair_s(pa[g]), za = pair_z(pa[g]), sb = pair_s(pb[g]), zb = pair_z(pb[g]);
-            dot[0] = fmaf(sa, c[i][g][0], fmaf(za, W.qsum[g][0], dot[0]));
-            dot[1] = fmaf(sa, c[i][g][1], fmaf(za, W.qsum[g][1], dot[1]));
-            dot[2] = fmaf(sb, c[i][g][2], fmaf(zb, W.qsum[g][0], dot[2]));
-            dot[3] = fmaf(sb, c[i][g][3], fmaf(zb, W.qsum[g][1], dot[3]));
+            const float2 qs = make_float2(W.qsum[g][0], W.qsum[g][1]), sc = make_float2(W.scale[g][0], W.scale[g][1]);
+            xa = ptx::fma2(ptx::fma2(make_float2(sa, sa), make_float2(c[i][g][0], c[i][g][1]), ptx::mul2(make_float2(za, za), qs)), sc, xa);
+            xb = ptx::fma2(ptx::fma2(make_float2(sb, sb), make_float2(c[i][g][2], c[i][g][3]), ptx::mul2(make_float2(zb, zb), qs)), sc, xb);
             sv[i][0][g] = pa[NG + g];
             sv[i][1][g] = pb[NG + g];
         }
-        const float2 ba = *reinterpret_cast<const float2*>(&bias[key][col]), bb = *reinterpret_cast<const float2*>(&bias[key + 8][col]);
-        x[i][0] = fmaf(dot[0], W.scale[0], ba.x);
-        x[i][1] = fmaf(dot[1], W.scale[1], ba.y);
-        x[i][2] = fmaf(dot[2], W.scale[0], bb.x);
-        x[i][3] = fmaf(dot[3], W.scale[1], bb.y);
+        x[i][0] = xa.x; x[i][1] = xa.y; x[i][2] = xb.x; x[i][3] = xb.y;
         if (odd) {                                                // (values of a group without finite scale are NaN, or infinities of both signs)
             bool na = false, nb = false;
 #pragma unroll
@@ -564,7 +561,6 @@ __global__ void __launch_bounds__(32 * kW, kW == 4 ? 3 : D == 64 ? 2 : 1) attn_k
         {
             const int h = r % kCols;
             uint4 raw[NG][2];
-            uint32_t big = 0u;
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
                 raw[g][0] = raw[g][1] = make_uint4(0u, 0u, 0u, 0u);
@@ -573,20 +569,21 @@ __global__ void __launch_bounds__(32 * kW, kW == 4 ? 3 : D == 64 ? 2 : 1) attn_k
                     raw[g][0] = src[0];
                     raw[g][1] = src[1];
                 }
+            }
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                uint32_t big = 0u;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const uint32_t v[4] = {raw[g][e].x, raw[g][e].y, raw[g][e].z, raw[g][e].w};
 #pragma unroll
                     for (int k = 0; k < 4; ++k) big = max(big, max(v[k] & 0x7fff0000u, v[k] << 16 & 0x7fff0000u));
                 }
-            }
-            big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
-            big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
-            // the head's power of two brings its largest channel to 2^14 .. 2^15
-            const int up = max(-113, min(100, 127 + 14 - (int)(big >> 23)));
-            const float k = __uint_as_float((uint32_t)(127 + up) << 23), even = k, odd_k = k * 0.0625f;
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
+                big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
+                big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
+                // the power of two of the head's group brings its largest channel to 2^14 .. 2^15
+                const int up = max(-113, min(100, 127 + 14 - (int)(big >> 23)));
+                const float k = __uint_as_float((uint32_t)(127 + up) << 23), even = k, odd_k = k * 0.0625f;
                 float sum = 0.0f;
                 uint32_t frag[4][2];
 #pragma unroll
@@ -607,17 +604,17 @@ __global__ void __launch_bounds__(32 * kW, kW == 4 ? 3 : D == 64 ? 2 : 1) attn_k
                 sum += __shfl_xor_sync(0xffffffffu, sum, 2);
                 // (in the products' units: codes 2^-24, queries k)
                 sum *= k * 0x1p-24f;
+                const float unit = A.scale / k * 0x1p24f;
                 W.qsum[g][0] = __shfl_sync(0xffffffffu, sum, 8 * t4);
                 W.qsum[g][1] = __shfl_sync(0xffffffffu, sum, 8 * t4 + 4);
+                W.scale[g][0] = __shfl_sync(0xffffffffu, unit, 8 * t4);
+                W.scale[g][1] = __shfl_sync(0xffffffffu, unit, 8 * t4 + 4);
                 W.oz[g][0] = W.oz[g][1] = 0.0f;
                 W.f[g][0] = W.f[g][1] = 1.0f;
                 W.wref[g][0] = W.wref[g][1] = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) W.o[g][j][0] = W.o[g][j][1] = W.o[g][j][2] = W.o[g][j][3] = 0.0f;
             }
-            const float unit = A.scale / k * 0x1p24f;
-            W.scale[0] = __shfl_sync(0xffffffffu, unit, 8 * t4);
-            W.scale[1] = __shfl_sync(0xffffffffu, unit, 8 * t4 + 4);
             W.m[0] = W.m[1] = -3.4e38f;
             W.l[0] = W.l[1] = 0.0f;
         }

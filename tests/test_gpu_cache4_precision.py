@@ -92,3 +92,17 @@ def test_scales_of_any_sign_and_size(Hq, Hkv, d, sign, size, flags):
     arrays[1][:, :, :, 1].mul_(size)                                       # V's scales and zeros
     o, lse = dma.dma_cache4_decode(c, q, *arrays, *plan)
     check(c, q, arrays, plan, o, lse)
+
+
+@pytest.mark.parametrize("flags", [0, dma.DMA_FLAG_SIMT])
+@pytest.mark.parametrize("lens,w", [([40, 300, 3], 200), ([900, 5000], 700)])
+@pytest.mark.parametrize("Hq,Hkv", [(2, 2), (4, 2), (4, 1), (8, 1)])
+def test_queries_keep_the_channels_of_every_group(Hq, Hkv, lens, w, flags):
+    """Channels of one group far above the other's where the keys' scales are as far below: both count."""
+    c, q, arrays, plan = a_cache(Hq, Hkv, 128, 32, lens, w, torch.bfloat16, Hq + w, flags)
+    q[:, ::2, :64] *= 2.0 ** 40
+    q[:, 1::2, :64] *= 2.0 ** 60
+    arrays[1][:, :, :, 0, 0] *= 2.0 ** -60
+    q[0, 0, 64:] *= 2.0 ** -40
+    o, lse = dma.dma_cache4_decode(c, q, *arrays, *plan)
+    check(c, q, arrays, plan, o, lse)
