@@ -283,11 +283,16 @@ __global__ void __launch_bounds__(kThreads) cache4_read_kernel(const uint8_t* co
     }
 }
 
+// What a CTA of the append takes beside its sSlot, and what no opt-in is needed for.
+constexpr size_t append_smem(int G, int d, int rows) { return (size_t)G * (d + 2 * rows) * sizeof(float); }
+constexpr size_t append_room(int rows) { return 48 * 1024 - 2 * rows * sizeof(int); }
+
 template <typename T, int D, int kRows>
 int append_tiles(const Cache& C, int ctas, const void* K, const void* V, const float* W, const float* A, const float* delta_new, int64_t delta_ld, const int32_t* slot,
                  uint8_t* codes, __nv_bfloat16* scales, float* delta, cudaStream_t st) {
-    const size_t smem = (size_t)C.G * (D + 2 * kRows) * sizeof(float);
-    if (smem > 48 * 1024) return DMA_ERR_UNSUPPORTED;
+    const size_t smem = append_smem(C.G, D, kRows);
+    if (smem > append_room(kRows) &&
+        cudaFuncSetAttribute(cache4_append_kernel<T, D, kRows>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return DMA_ERR_CUDA;
     return launch_overlapped(cache4_append_kernel<T, D, kRows>, dim3(ctas, C.Hkv), dim3(kAppendThreads), smem, st, 1, (const T*)K, (const T*)V, W, A, delta_new, delta_ld, slot, codes,
                              (uint32_t*)scales, delta, C.rows, C.Hq, C.Hkv, C.G, C.ks[0], C.ks[1], C.vs[0], C.vs[1], C.page_log, C.num_pages << C.page_log);
 }
@@ -298,7 +303,7 @@ int append(const Cache& C, const void* K, const void* V, const float* W, const f
            uint8_t* codes, __nv_bfloat16* scales, float* delta, cudaStream_t st) {
     constexpr int kPassRows = kAppendThreads / (D / 16), kTile = 32;
     const int tiles = (C.rows + kTile - 1) / kTile, most = (6 * 148 + C.Hkv - 1) / C.Hkv;
-    if (kTile > kPassRows && (int64_t)tiles * C.Hkv >= 3 * 148 && (size_t)C.G * (D + 2 * kTile) * sizeof(float) <= 48 * 1024)
+    if (kTile > kPassRows && (int64_t)tiles * C.Hkv >= 3 * 148 && append_smem(C.G, D, kTile) <= append_room(kTile))
         return append_tiles<T, D, kTile>(C, std::min(tiles, most), K, V, W, A, delta_new, delta_ld, slot, codes, scales, delta, st);
     return append_tiles<T, D, kPassRows>(C, std::min((C.rows + kPassRows - 1) / kPassRows, most), K, V, W, A, delta_new, delta_ld, slot, codes, scales, delta, st);
 }

@@ -7,6 +7,9 @@ namespace dma {
 
 constexpr int kGroup = 64;             // channels that share a scale and a zero
 
+// query heads of a group that dma_cache4_append takes: their sampling weights and z lie in 48 KB of shared memory
+constexpr int append_heads(int d) { return d == 128 ? 76 : 96; }
+
 // dma_cache_t with defaults resolved
 struct Cache {
     int Hq, Hkv, G, d, w, dtype, flags;

@@ -99,6 +99,7 @@ int dma_cache4_append(const dma_cache_t* c, const void* K, const void* V, const 
     if (!K || !V || !slot || !codes || !scales || !delta || (!delta_new && (!W_delta || !A))) return DMA_ERR_NULL;
     if (!aligned(16, K, V, W_delta, codes, scales, delta) || !aligned(4, A, delta_new, slot)) return DMA_ERR_ALIGN;
     if (delta_new && delta_ld < C.rows) return DMA_ERR_SHAPE;
+    if (C.G > append_heads(C.d)) return DMA_ERR_UNSUPPORTED;
     if ((rc = sm100())) return rc;
     return launch_cache4_append(C, K, V, W_delta, A, delta_new, delta_ld, slot, (uint8_t*)codes, (__nv_bfloat16*)scales, delta, (cudaStream_t)cuda_stream);
 }

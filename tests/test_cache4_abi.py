@@ -242,3 +242,13 @@ def test_read_refuses_output_strides_that_the_library_cannot_write(lib, monkeypa
         with pytest.raises(dma.DmaError) as e:
             dma.dma_cache4_read(c, *arrays, slot, K=bad)
         assert e.value.status == -3
+
+
+@pytest.mark.parametrize("d,most", [(128, 76), (64, 96)])
+def test_most_heads_per_group_of_an_append(lib, d, most):
+    """Refused before anything touches a device; as many as documented are not."""
+    a = 4096
+    for Hq, Hkv in ((most + 1, 1), (2 * most + 2, 2)):
+        assert dma._typed_fn("dma_cache4_append")(ctypes.byref(cache(Hq=Hq, Hkv=Hkv, d=d)), a, a, a, a, 0, 0, a, a, a, a, 0) == -4
+    if not torch.cuda.is_available():
+        assert dma._typed_fn("dma_cache4_append")(ctypes.byref(cache(Hq=most, Hkv=1, d=d)), a, a, a, a, 0, 0, a, a, a, a, 0) == -6

@@ -696,3 +696,37 @@ def test_append_from_a_projection_and_read_into_arrays_by_one_descriptor(Hq, Hkv
         assert all(torch.equal(bits(a), bits(b)) for a, b in zip(got, want))
     assert (wide[:, Hkv:] == 7.0).all() and (wide[..., d:] == 7.0).all()
     assert tuple(c.k_stride) == K.stride()[:2]
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,rows", [(64, 1, 128, 15000), (128, 2, 128, 8000), (64, 1, 128, 9), (76, 1, 128, 15000), (76, 1, 128, 5), (96, 1, 64, 40), (96, 1, 64, 9000), (95, 1, 64, 3)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_append_of_as_many_heads_per_group_as_documented(Hq, Hkv, d, rows, dtype):
+    """Up to Hq / Hkv = 76 (d = 128) and 96 (d = 64), prompts and steps: the bits of the weights, and the values of a call with one query head."""
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    page, g = 64, torch.Generator().manual_seed(Hq + rows)
+    pages = rows // page + 1
+    K, V = (torch.randn(rows, Hkv, d, generator=g).to(dt).cuda() for _ in range(2))
+    W, A = torch.randn(Hq, d, generator=g) / math.sqrt(d), torch.rand(Hq, generator=g) + 0.5
+    slot = torch.randperm(pages * page, generator=g)[:rows].int().cuda()
+    c, *arrays = pool_of(Hq, Hkv, d, page, pages, rows, dt)
+    dma.dma_cache4_append(c, K, V, slot, *arrays, W.cuda(), A.cuda())
+    K1, V1, delta = dma.dma_cache4_read(c, *arrays, slot)
+    some = sorted({0, 1, rows // 2, rows - 1} & set(range(rows)))
+    _, dl = oracle.delta(V[some].float().cpu().numpy()[None], W.numpy(), A.numpy(), Hq)
+    assert np.array_equal(delta[:, some].cpu().numpy().view(np.uint32), np.ascontiguousarray(dl[0]).view(np.uint32))
+    one, *few = pool_of(Hkv, Hkv, d, page, pages, rows, dt)
+    dma.dma_cache4_append(one, K, V, slot, *few, W[::Hq // Hkv].cuda().contiguous(), A[::Hq // Hkv].cuda().contiguous())
+    K2, V2, first = dma.dma_cache4_read(one, *few, slot)
+    assert torch.equal(bits(K1), bits(K2)) and torch.equal(bits(V1), bits(V2)) and torch.equal(bits(delta[::Hq // Hkv]), bits(first))
+    given = torch.rand(Hq, rows, generator=g).cuda()
+    dma.dma_cache4_append(c, K, V, slot, *arrays, delta_new=given)
+    assert torch.equal(bits(dma.dma_cache4_read(c, *arrays, slot)[2]), bits(given))
+
+
+@pytest.mark.parametrize("Hq,d", [(77, 128), (97, 64)])
+def test_append_refuses_more_heads_per_group(Hq, d):
+    c, *arrays = pool_of(Hq, 1, d, 16, 2, 3)
+    K = torch.zeros(3, 1, d, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(dma.DmaError) as e:
+        dma.dma_cache4_append(c, K, K, i32([0, 1, 2]), *arrays, torch.zeros(Hq, d, device="cuda"), torch.zeros(Hq, device="cuda"))
+    assert e.value.status == -4
