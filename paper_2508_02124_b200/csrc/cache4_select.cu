@@ -66,6 +66,9 @@ __global__ void __launch_bounds__(1024) plan_kernel(Rows R, int rows, Plan P) {
     make_plan<1024>(R, rows, P);
 }
 
+// (the pattern of keys in pages outside the pool: fewer than w others, which are all kept)
+__device__ __forceinline__ unsigned long long threshold(unsigned long long found) { return found >> 32 ? found : 0ull; }
+
 // The weakest kept key of a (row, query head). A sample brackets its delta (4.5 standard deviations of the sample's rank to either side); one sweep over the row
 // counts the keys above the bracket and notes those inside, a few per cent, each thread in slots of its own; the need-th of these is found by
 // a histogram over the bracket and a ranking of the bin's keys. Rows of up to kSample keys are their own sample: the bracket is one bin. A bracket that misses, or holds too
@@ -473,7 +476,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) select_kernel(Rows R, int rows,
         collect = false;
         __syncthreads();
     }
-    if (tid == 0) weakest[item] = found;
+    if (tid == 0) weakest[item] = threshold(found);
 }
 
 // The same for rows that the registers hold: NT threads with kKeys keys each. The row is read in one go, a
@@ -568,7 +571,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) select_held_kernel(Rows R, int 
         if ((u[k] - lo) >> shift == 0u) S.cand[atomicAdd(&S.ncand, 1)] = order_key(by_index ? pattern : u[k], index(k));
     __syncthreads();
     const unsigned long long found = rank_candidates<NT>(S, count, need);
-    if (tid == 0) weakest[item] = found;
+    if (tid == 0) weakest[item] = threshold(found);
 }
 
 int select_launch(void (*kernel)(Rows, int, int, unsigned long long*, Plan), int threads, size_t bytes, int cluster, const Cache& C, const Rows& R,
