@@ -577,7 +577,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) select_held_kernel(Rows R, int 
 int select_launch(void (*kernel)(Rows, int, int, unsigned long long*, Plan), int threads, size_t bytes, int cluster, const Cache& C, const Rows& R,
                   unsigned long long* weakest, const Plan& plan, cudaStream_t st) {
     if (bytes > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return DMA_ERR_CUDA;
-    return launch_overlapped(kernel, dim3((unsigned)((C.rows * C.Hq + (plan.ustart ? 1 : 0)) * cluster)), dim3(threads), bytes, st, cluster, R, C.rows, C.w, weakest, plan);
+    return launch_overlapped(kernel, dim3((unsigned)(((int64_t)C.rows * C.Hq + (plan.ustart ? 1 : 0)) * cluster)), dim3(threads), bytes, st, cluster, R, C.rows, C.w, weakest, plan);
 }
 }  // namespace
 
@@ -587,13 +587,14 @@ int select_launch(void (*kernel)(Rows, int, int, unsigned long long*, Plan), int
 //   up to 4K     held by 1024 threads where every item has an SM (4 rows 4.1; by 256 4.7), else by 256 (5 rows 4.8 against 6.2; 13 rows 6.6 against 11.5)
 //   up to 16K    held by 1024 threads where two items per SM are all (one row of 16K 6.3; swept 7.8. 9 rows 13.6 against 14.0; 10 rows 17.7 against 17.1)
 //   beyond       swept: by 256 threads where there are many items and the bracket fits their slots (64 rows of 16K 57; by 512 70), else by 512 (64 rows of 32K 108 against 144), whose
-//                cluster is as large as the bracket needs (9 rows of 256K, w = 8192: two CTAs 92, one, which sweeps twice, 133; 32 of 128K, w = 32K: 208 against 267). Where no cluster's slots would do,
-//                256 threads again (64 rows of 64K, two sweeps 264 against 281).
+//                cluster is as large as the bracket needs (9 rows of 256K, w = 8192: two CTAs 92, one, which sweeps twice, 133; 32 of 128K, w = 32K: 208 against 267). Where no cluster's slots would do, or a
+//                grid does not take so many clusters, 256 threads again (64 rows of 64K, two sweeps 264 against 281).
 //                Few rows take larger clusters: of 16K keys per CTA where an SM has one (one row of 64K: four CTAs 12.5, two 14.0, eight 16.6), of 32K where it has two (2 rows of 128K:
 //                four 22.7, two 24.6; 4 rows of 32K: two 18.8, one 14.5; one row of 256K: eight 24.6, two 36).
 int launch_cache4_select(const Cache& C, const Rows& R, unsigned long long* weakest, const Plan& plan, cudaStream_t st) {
     constexpr int K = 1024, kSms = 148;
-    const int capacity = C.max_blocks << C.page_log, items = C.rows * C.Hq;
+    const int capacity = C.max_blocks << C.page_log;
+    const int64_t items = (int64_t)C.rows * C.Hq;
     auto held = [&](auto nt, auto kernel) { return select_launch(kernel, nt, sizeof(HeldShared<nt>), 1, C, R, weakest, plan, st); };
     constexpr std::integral_constant<int, 256> t256{};
     constexpr std::integral_constant<int, 1024> t1024{};
@@ -605,7 +606,7 @@ int launch_cache4_select(const Cache& C, const Rows& R, unsigned long long* weak
     auto fits = [&](int threads, int ctas) { return collects(capacity, bracket(capacity, C.w, kPer * threads), threads, kPer * threads, ctas); };
     int cluster = 1;
     while (cluster < 8 && !fits(512, cluster)) cluster *= 2;
-    const bool one_sweep = fits(512, cluster);
+    const bool one_sweep = fits(512, cluster) && (items + 1) * cluster <= INT32_MAX;       // (what a grid takes)
     if (!few && (fits(256, 1) || !one_sweep)) return select_launch(select_kernel<256, false>, 256, sizeof(SelectShared<256, false>), 1, C, R, weakest, plan, st);
     while (cluster < 8 && items * cluster * 2 <= 2 * kSms && capacity / (2 * cluster) >= (items * cluster * 2 <= kSms ? 16 : 32) * K) cluster *= 2;
     if (cluster == 1) return select_launch(select_kernel<512, false>, 512, sizeof(SelectShared<512, false>), 1, C, R, weakest, plan, st);

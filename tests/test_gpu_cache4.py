@@ -730,3 +730,28 @@ def test_append_refuses_more_heads_per_group(Hq, d):
     with pytest.raises(dma.DmaError) as e:
         dma.dma_cache4_append(c, K, K, i32([0, 1, 2]), *arrays, torch.zeros(Hq, d, device="cuda"), torch.zeros(Hq, device="cuda"))
     assert e.value.status == -4
+
+
+def test_decode_of_more_items_than_a_grid_of_clusters_takes():
+    """2^28 rows by heads, all but two rows of no sequence, of a length that the selection would take by clusters of eight: 2^31 CTAs. The two rows are what they are in a call of
+    their own, within a step of bf16 of each other; the others stay as they are. (Overlapping queries and outputs, so that they fit; the two rows' lie apart.)"""
+    Hq, d, page, blocks, rows, w = 64, 64, 256, 1954, 1 << 22, 250000
+    real = [5, 3000000]
+    c, *arrays = pool_of(Hq, 1, d, page, blocks, rows, nseq=1, blocks=blocks, w=w, fill=False)
+    g = torch.Generator("cuda").manual_seed(1)
+    arrays[0].random_(0, 256, generator=g)
+    arrays[1].copy_(torch.rand(arrays[1].shape, generator=g, device="cuda"))
+    arrays[2].copy_(1 + torch.rand(arrays[2].shape, generator=g, device="cuda"))
+    table = torch.arange(blocks, **I32)[None]
+    flat = torch.randn(rows * 8 + Hq * d, generator=g, device="cuda").bfloat16()
+    q, o = flat.as_strided((rows, Hq, d), (8, d, 1)), torch.full_like(flat, 7.0).as_strided((rows, Hq, d), (8, d, 1))
+    c.q_stride[:] = c.o_stride[:] = (8, d)
+    lse, seq, pos = torch.full((rows, Hq), 7.0, device="cuda"), torch.full((rows,), -1, **I32), torch.full((rows,), blocks * page - 1, **I32)
+    seq[real] = 0
+    dma.dma_cache4_decode(c, q, *arrays, table, seq, pos, o, lse)
+    alone = dma.cache(Hq, 1, d, w=w, rows=2, nseq=1, page_size=page, num_pages=blocks, max_blocks=blocks)
+    o2, lse2 = dma.dma_cache4_decode(alone, q[real].contiguous(), *arrays, table, seq[real], pos[real])
+    # (each is within half a step of the exact value and what fp32 sums leave)
+    assert ((o[real].float() - o2.float()).abs() <= 2 * torch.finfo(torch.bfloat16).eps * o2.float().abs()).all() and ((lse[real] - lse2).abs() <= 2.0 ** -12).all()
+    lse[real] = 7.0
+    assert bool((lse == 7.0).all())
