@@ -15,6 +15,7 @@
 #include <type_traits>
 
 #include "cache4_decode.cuh"
+#include "cache4_sample.h"
 
 namespace dma {
 namespace {
@@ -221,13 +222,13 @@ __global__ void __launch_bounds__(NT, 1024 / NT) select_kernel(Rows R, int rows,
         uint32_t u[kPer], umin = 0x7FFFFFFFu, umax = 0u;
         // four neighbours from each of kSample / 4 scattered places (single keys take four times the sectors, which were the larger part of what the kernel waited for)
         const bool whole = n <= kSample;
-        const uint32_t quads = (uint32_t)n / 4, step = quads / (kSample / 4);
+        const uint32_t quads = (uint32_t)n / 4;
         uint32_t at[kPer / 4];
         int pg[kPer / 4];
 #pragma unroll
         for (int k = 0; k < kPer / 4; ++k) {
             const uint32_t i = k * NT + tid;
-            at[k] = 4 * (whole ? i : (uint32_t)((uint64_t)i * quads / (kSample / 4)) + (((i * 2654435761u) >> 16) * step >> 16));
+            at[k] = 4 * (whole ? i : sample_quad(i, quads, kSample / 4));
             pg[k] = at[k] < (uint32_t)n ? pages[at[k] >> R.page_log] : -1;
         }
 #pragma unroll

@@ -67,3 +67,43 @@ def test_decode_of_tables_with_holes(n, rows, w, holes, weights, dtype):
             assert (err <= lim).all(), (t, h, len(k), float((err / lim).max()))
             want = float(torch.logsumexp(score, 0))
             assert abs(float(lse[t, h]) - want) <= e + (len(k) + 64) * U + 2.0 ** -23 * abs(want), (t, h)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_decode_of_a_row_of_more_than_a_quarter_of_2_30_keys(dtype):
+    """2^28 + 1001 keys, whose pages come back again and again; every seventh page is outside the pool."""
+    Hq, d, page, pages, n, w = 1, 64, 256, 1000, (1 << 28) + 1001, 5000
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    blocks, half, g = -(-n // page), torch.finfo(dt).eps / 2, torch.Generator("cuda").manual_seed(3)
+    c = dma.cache(Hq, 1, d, w=w, dtype=dt, rows=1, nseq=1, page_size=page, num_pages=pages, max_blocks=blocks)
+    codes, scales, delta = dma.cache4(c, "cuda")
+    codes.random_(0, 256, generator=g)
+    scales.copy_(torch.rand(scales.shape, generator=g, device="cuda"))
+    delta.copy_(1 + torch.rand(delta.shape, generator=g, device="cuda"))
+    at = torch.arange(blocks, device="cuda")
+    table = torch.where(at % 7 == 3, -1, torch.randint(0, pages, (blocks,), generator=g, device="cuda")).int()
+    q = torch.randn(1, Hq, d, generator=g, device="cuda").to(dt)
+    o, lse = dma.dma_cache4_decode(c, q, codes, scales, delta, table[None], torch.zeros(1, **I32), torch.tensor([n - 1], **I32))
+    # the window's weakest key has the weight of the largest patterns that hold w keys: copies of a page's key have one weight
+    count = torch.bincount(table[:-1][table[:-1] >= 0].long(), minlength=pages)[:, None].expand(pages, page).clone()
+    count[table[-1].long(), :n - (blocks - 1) * page] += 1                    # (the last page is not whole)
+    by, order = torch.sort(delta[:, 0].flatten(), descending=True, stable=True)
+    upto = count.flatten()[order].cumsum(0)
+    last = int((upto >= w).nonzero()[0])
+    weakest = by[last]
+    assert int((by == weakest).sum()) == 1
+    whole = order[:last]                                                       # these are kept with all their copies, the weakest's with the first ones (their values are alike)
+    times = torch.cat([count.flatten()[whole], (w - (upto[last - 1] if last else 0)).view(1).to(count.dtype)]).double()
+    k = order[:last + 1]
+    nib, sc = codes[k // page, 0, k % page], scales[k // page, 0, k % page].double()
+    n4 = torch.stack([nib & 15, nib >> 4], -1).flatten(2).double()
+    kv = n4 * sc[:, :, :, 0] + sc[:, :, :, 1]
+    bias, qd = delta[k // page, 0, k % page].double(), q[0, 0].double() / math.sqrt(d)
+    score = kv[:, 0] @ qd + bias
+    e = 136 * U * float((kv[:, 0] @ qd.abs() + bias).max())
+    top = score.max()
+    p = torch.exp(score - top) * times
+    total = p.sum()
+    exact, want = (p / total) @ kv[:, 1], float(top + total.log())
+    lim = (2 * e + (w + 64) * U) * exact + 2.0 ** -22 * exact + w * 15 * 2.0 ** -31 + half * exact
+    assert ((o[0, 0].double() - exact).abs() <= lim).all() and abs(float(lse[0, 0]) - want) <= e + (w + 64) * U + 2.0 ** -23 * abs(want)
