@@ -252,3 +252,25 @@ def test_most_heads_per_group_of_an_append(lib, d, most):
         assert dma._typed_fn("dma_cache4_append")(ctypes.byref(cache(Hq=Hq, Hkv=Hkv, d=d)), a, a, a, a, 0, 0, a, a, a, a, 0) == -4
     if not torch.cuda.is_available():
         assert dma._typed_fn("dma_cache4_append")(ctypes.byref(cache(Hq=most, Hkv=1, d=d)), a, a, a, a, 0, 0, a, a, a, a, 0) == -6
+
+
+def ends_of_the_range():
+    """fp32 groups with values between bf16's largest number (3.3895e38) and fp32's: at the top, at the bottom, at both ends."""
+    x = np.random.RandomState(3).rand(4, 64).astype(np.float32)
+    x[0, 7] = 3.4e38
+    x[1, 9] = -3.4e38
+    x[2, 3], x[2, 4] = 3.4e38, -3.38e38
+    x[3, 3], x[3, 4] = 3.4e38, -3.4e38
+    return x
+
+
+def test_values_between_the_largest_numbers_of_bf16_and_of_fp32():
+    """Only a smallest value that bf16 rounds to -inf makes a group NaN; a largest one enters its scale as it is."""
+    n, s, z = ref.quantise(ends_of_the_range())
+    v = ref.values(n, s, z)
+    assert np.isinf(ref.bf16(np.float32(3.4e38))) and np.isfinite(s[0]) and np.isfinite(v[0]).all()
+    assert abs(v[0, 7] / 3.4e38 - 1) <= 2.0 ** -8 and (v[0, :7] == z[0, 0]).all()
+    assert np.isnan(v[1]).all() and np.isnan(v[3]).all()
+    with np.errstate(over="ignore"):
+        back = v[2].astype(np.float32)
+    assert not np.isnan(back).any() and np.isfinite(back[4]) and (np.isfinite(back) | (n[2] == 15)).all()

@@ -755,3 +755,19 @@ def test_decode_of_more_items_than_a_grid_of_clusters_takes():
     assert ((o[real].float() - o2.float()).abs() <= 2 * torch.finfo(torch.bfloat16).eps * o2.float().abs()).all() and ((lse[real] - lse2).abs() <= 2.0 ** -12).all()
     lse[real] = 7.0
     assert bool((lse == 7.0).all())
+
+
+def test_append_at_the_end_of_fp32s_range():
+    """Values between bf16's largest number and fp32's: codes, scales and what is read back are the plain implementation's."""
+    from test_cache4_abi import ends_of_the_range
+    x = ends_of_the_range()
+    n, s, z = ref.quantise(x)
+    c, *arrays = pool_of(1, 1, 64, 16, 1, 4, torch.float32)
+    K, slot = torch.from_numpy(x).cuda()[:, None], i32([3, 0, 9, 15])
+    dma.dma_cache4_append(c, K, K, slot, *arrays, delta_new=torch.ones(1, 4, device="cuda"))
+    sc = arrays[1][0, 0, [3, 0, 9, 15], :, 0].float().cpu().numpy()        # [row, K or V, (s, z)]
+    with np.errstate(over="ignore"):
+        back = ref.values(n, s, z).astype(np.float32)
+    for i, got in enumerate(dma.dma_cache4_read(c, *arrays, slot)[:2]):
+        assert np.array_equal(sc[:, i, 0], s[:, 0], equal_nan=True) and np.array_equal(sc[:, i, 1], z[:, 0], equal_nan=True)
+        assert np.array_equal(got[:, 0].cpu().numpy(), back, equal_nan=True)
