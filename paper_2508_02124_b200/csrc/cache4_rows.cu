@@ -61,9 +61,10 @@ __device__ __forceinline__ void group_range(const Raw16<__nv_bfloat16>& k, const
 
 // The codes of a lane's 16 channels, and the (s, z) pair of its group: the definition, in fp32, rounded operation by operation; the halves keep every difference in range.
 // A division takes a dozen instructions, sixteen of them per lane more than all else. A quotient a / b is therefore the product q with b's rounded reciprocal y and one
-// correction, q + (a - q b) y (Markstein, "Computation of elementary functions on the IBM RISC System/6000", 1990): the remainder is exact, and the result is the rounded
-// quotient unless that lies within 2^-22 of its last place of a midpoint between two numbers, where it may be the other neighbour. That is a code's difference only next to a
-// half, 2^-22 of the 2^-23 of all quotients that lie there. (Without the correction 0.2 % of bf16 values are ties that the product misses.) Two values per
+// correction, q + (a - q b) y (Markstein, "Computation of elementary functions on the IBM RISC System/6000", 1990). The remainder is exact, and before its own rounding the sum is
+// within 2^-45 of the quotient, so that it rounds to the quotient's rounding unless the quotient is as near to a midpoint between two numbers. It never is: b is half a bf16 number
+// or 7.5, of 8 bits at most, a has 24, and a midpoint m has 25 with its last one set. m b then has 25 bits at least without trailing zeros, is not a, and as multiples of one unit
+// below 2^33 the two differ by 2^-33 at least. So the codes are the divisions' bits. (Without the correction 0.2 % of bf16 values are ties that the product misses.) Two values per
 // instruction. Ranges at the ends of fp32's, and what is not finite, are divided; rows that are not stored (`used`) may come out as anything.
 template <bool kExactZero>
 __device__ __forceinline__ uint2 quantise(const float (&x)[2][8], float lo, float hi, bool used, uint32_t& pair) {

@@ -771,3 +771,24 @@ def test_append_at_the_end_of_fp32s_range():
     for i, got in enumerate(dma.dma_cache4_read(c, *arrays, slot)[:2]):
         assert np.array_equal(sc[:, i, 0], s[:, 0], equal_nan=True) and np.array_equal(sc[:, i, 1], z[:, 0], equal_nan=True)
         assert np.array_equal(got[:, 0].cpu().numpy(), back, equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("zero", [0.0, -1.7, 3.0, 1e-3, -1e30])
+def test_append_codes_next_to_halves(zero, dtype):
+    """Values at the middle between two codes and at its neighbours, for 4000 scales of any mantissa: the codes are those of the rounded quotient, which the kernel forms by a product
+    and one correction."""
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    rng, rows, f = np.random.RandomState(5), 4000, np.float32
+    s = ref.bf16((1 + rng.rand(rows)).astype(f) * f(2.0) ** rng.randint(-20, 20, rows).astype(f) * f(max(abs(zero), 1.0) if abs(zero) > 1e9 else 1.0))
+    mid = (f(zero) + (np.arange(15, dtype=f) + f(0.5)) * s[:, None]).astype(f)             # [rows, 15]
+    x = np.concatenate([mid, np.nextafter(mid, f(np.inf)), np.nextafter(mid, -f(np.inf)), np.nextafter(np.nextafter(mid, f(np.inf)), f(np.inf)),
+                        np.full((rows, 2), zero, f), (f(zero) + 15 * s[:, None] * np.array([1.0, 0.999], f)).astype(f)], 1)
+    assert x.shape == (rows, 64)
+    x = torch.from_numpy(x).to(dt)
+    K = torch.stack([x, x.flip(0)], 1).cuda()                                                  # [rows, 2, 64]
+    c, *arrays = pool_of(2, 2, 64, 256, 16, rows, dt)
+    dma.dma_cache4_append(c, K, K, torch.arange(rows, **I32), *arrays, delta_new=torch.ones(2, rows, device="cuda"))
+    n, sc, _ = ref.quantise(K.float().cpu().numpy())
+    got = ref.unpack(arrays[0].cpu().numpy().transpose(0, 2, 1, 3, 4).reshape(-1, 2, 2, 32)[:rows])
+    assert np.isfinite(sc).all() and np.array_equal(got[:, :, 0], n) and np.array_equal(got[:, :, 1], n)
