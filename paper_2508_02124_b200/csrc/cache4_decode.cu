@@ -610,7 +610,7 @@ __global__ void __launch_bounds__(32 * kW, kW == 4 ? 3 : D == 64 ? 2 : 1) attn_k
                 W.scale[g][0] = __shfl_sync(0xffffffffu, unit, 8 * t4);
                 W.scale[g][1] = __shfl_sync(0xffffffffu, unit, 8 * t4 + 4);
                 W.oz[g][0] = W.oz[g][1] = 0.0f;
-                W.f[g][0] = W.f[g][1] = 1.0f;
+                W.f[g][0] = W.f[g][1] = 0x1p100f;                 // (whatever weight comes first passes the half's range by it, and sets the power)
                 W.wref[g][0] = W.wref[g][1] = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) W.o[g][j][0] = W.o[g][j][1] = W.o[g][j][2] = W.o[g][j][3] = 0.0f;
@@ -729,11 +729,11 @@ __global__ void __launch_bounds__(32 * kW, kW == 4 ? 3 : D == 64 ? 2 : 1) attn_k
         for (int g = 0; g < NG; ++g)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float unit = 0x1p24f / W.f[g][e & 1];
+                const float unit = 1.0f / W.f[g][e & 1];
                 float v[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    v[j] = W.o[g][j][e] * (j & 1 ? unit * 0.0625f : unit);
+                    v[j] = W.o[g][j][e] * unit * (j & 1 ? 0x1p20f : 0x1p24f);
                     if (kH <= 4) v[j] += __shfl_xor_sync(0xffffffffu, v[j], 2);
                     v[j] += W.oz[g][e & 1];
                 }

@@ -106,3 +106,18 @@ def test_queries_keep_the_channels_of_every_group(Hq, Hkv, lens, w, flags):
     q[0, 0, 64:] *= 2.0 ** -40
     o, lse = dma.dma_cache4_decode(c, q, *arrays, *plan)
     check(c, q, arrays, plan, o, lse)
+
+
+@pytest.mark.parametrize("flags", [0, dma.DMA_FLAG_SIMT])
+@pytest.mark.parametrize("size", [2.0 ** -80, 2.0 ** -40, 2.0 ** -20, 1.0, 2.0 ** 40, 2.0 ** 98])
+@pytest.mark.parametrize("Hq,Hkv,d", SHAPES)
+def test_scales_that_begin_with_zero(Hq, Hkv, d, size, flags):
+    """The first keys' values are constant (scale 0), as padding's are, and the later ones' scales of any size."""
+    lens = [300, 900, 3000]
+    c, q, arrays, plan = a_cache(Hq, Hkv, d, 32, lens, 4000, torch.bfloat16, d + Hq, flags)
+    for r, n in enumerate(lens):
+        pages = plan[0][r].long()
+        arrays[1][pages, :, :, 1] *= size
+        arrays[1][pages[:n // 64], :, :, 1] = 0.0                          # half of the row's keys
+    o, lse = dma.dma_cache4_decode(c, q, *arrays, *plan)
+    check(c, q, arrays, plan, o, lse)
