@@ -327,7 +327,9 @@ int dma_cache4_append(const dma_cache_t* c, const void* K, const void* V, const 
                       int64_t delta_ld, const int32_t* slot, void* codes, void* scales, float* delta, void* cuda_stream);
 
 /* Reads rows back: K, V [rows, Hkv, d] get z + s n, formed in fp32 and rounded once; delta_out, if not NULL,
- * gets [Hq, delta_ld >= rows] (dma_decode's and dma_mask_build's layout for one batch entry). Rows whose slot lies outside the
+ * gets [Hq, delta_ld >= rows] (dma_decode's and dma_mask_build's layout for one batch entry). They serve dma_decode, and
+ * dma_attn_fwd_chunk where the window holds every key (bias = delta_out, expiry = p->L): expiry rows of a smaller window come from
+ * dma_mask_build, which forms weights from V, and no call forms them from weights that are stored. Rows whose slot lies outside the
  * pool are left as they are. k_stride and v_stride are those of this call's K and V: a descriptor that served dma_cache4_append
  * with the strides of its rows gets those of the arrays read into first (the Python binding takes them from the tensors). */
 int dma_cache4_read(const dma_cache_t* c, const void* codes, const void* scales, const float* delta, const int32_t* slot, void* K,
@@ -340,7 +342,10 @@ int dma_cache4_read(const dma_cache_t* c, const void* codes, const void* scales,
  * max_blocks pages, and keys in pages whose number is outside the pool, are not visible. A row that sees no key gets
  * o = 0, lse = -inf; a row whose row_seq is outside [0, nseq) (padding) is left as it is. Only the kept keys' codes are read (those
  * that some head of a group keeps). Results depend on the call's rows and lengths in the last bits (where long rows are cut),
- * and are the same bits from run to run.
+ * and are the same bits from run to run. The kernels' forms, and so the time, go by the table's width (max_blocks * page_size), w and
+ * rows, never by lengths that only the device knows: a table much wider than its longest row costs some us per call. On the tensor
+ * cores (bf16 without DMA_FLAG_SIMT) q times the softmax scale, and the pages' scales, are to stay below 2^100 in magnitude: beyond,
+ * a row may come out as NaN where the CUDA cores' is finite.
  * ws: dma_cache4_decode_workspace() bytes, a size that does not fall as rows, Hq or max_blocks grow. It serves one call at a time: calls that may overlap
  * on the GPU (streams, captured graphs that replay side by side) need one each. */
 int dma_cache4_decode_workspace(const dma_cache_t* c, size_t* bytes);

@@ -175,19 +175,21 @@ __global__ void __launch_bounds__(D) simt_combine_kernel(Rows R, const float* pa
 //   scan     a lane per key tests its weight against every head's weakest kept key; keys that some head keeps are queued, with the heads' biases
 //            (-inf where a head drops the key), so that a key that several heads keep is read and expanded once
 //   gather   32 queued keys at a time, codes and scales, by cp.async into one of the warp's stages while the stage before is used
-//   attend   S^T = K q^T and O^T += V^T P^T by mma.m16n8k16 (keys, then channels, by heads). What bounds this kernel is the integer pipe that expands the codes, so they are
-//            expanded as little as possible: a code n in the lowest mantissa bits of a half is the subnormal number n 2^-24, exactly, and four bits higher 16 n 2^-24; eight
+//   attend   S^T = K q^T and O^T += V^T P^T by mma.m16n8k16 (keys, then channels, by heads). The codes are expanded as little as
+//            possible: a code n in the lowest mantissa bits of a half is the subnormal number n 2^-24, exactly, and four bits higher 16 n 2^-24; eight
 //            codes of a word take a shift and four masks. A group of 64 channels is a chain of four products, whose sum takes the group's scale, and with the query's own sum
 //            over the group its zero, in fp32; the query goes in as halves, scaled by a power of two per head and group (its 8 bits survive down to 2^-27 of the largest
 //            channel there, and what is lost below that is less than the rounding of the sums; the products of 16 n take q / 16). Nothing of K is rounded. Softmax in registers, with a running maximum per warp and head. Of V the
 //            scale goes into the weight, P s in two halves, its rounding and what that leaves, scaled by a power of two per head and group that follows the largest
 //            (WarpState): 2^-22 of a weight, and of the small ones 2^-32 of the largest, which is less than the sums' own rounding in fp32. z P is summed in fp32.
 //            With up to four heads the operand's columns 4 to 7 hold the same heads again: their lanes take the second 16 keys through the softmax, and in the
-//            products of V they hold the low halves (one half per weight took the same time: 64 rows of 1 to 16K keys, whole call, 158 and 156 us).
-// 64 rows of 1 to 16K keys, 32 / 8 heads of 128, w = 2048: 113 us for 414 MB read, 780 instructions per 32 keys of a union. 53 % of the issue slots, 54 % of the integer pipe, 18 % of the
-// tensor pipe: with all pages in the L2 it is 110 us, without the attending 90. Twelve warps per SM: sixteen, with stages that are swizzled to fit, 118; eight with three
-// stages 133 where twelve took 119. Codes as bf16 numbers and weights in a high and a low part 210 where this form took 165. 256 rows of 4096 keys, w = 1024: 221 us,
-// 4.7 TB/s.
+//            products of V they hold the low halves (the 64 rows below: 115.2 us, with one half per weight 113.6; with eight heads per group, whose low halves are products of their
+//            own, 182 and 169).
+// 64 rows of 1 to 16K keys, 32 / 8 heads of 128, w = 2048: 117 us for 414 MB read, 3.6 TB/s, 800 instructions per 32 keys of a union. No unit is at its limit: 53 % of the issue
+// slots, 53 % of the integer pipe, 17 % of the tensor pipe. What the time is made of is the chain of test, queue and gather that every warp goes through before it attends, with three
+// warps per scheduler to take turns: without the attending 90 us; with all pages in the L2 3 us less than from memory. Twelve warps per SM: sixteen, with stages that are swizzled to
+// fit, 118 where twelve took 113; eight with three stages 133 where twelve took 119. Codes as bf16 numbers and weights in two parts of bf16 210 where subnormal halves took 165. 256
+// rows of 4096 keys, w = 1024: 228 us, 4.6 TB/s.
 // (tcgen05 needs 64 rows of A at least, of which a decoding step has the group's 1 to 8 heads or, turned around, the keys: then the expanded codes would
 // have to go through shared memory once more. mma.sync takes them from the registers that the expansion leaves them in, and its rate is not what bounds this kernel.)
 constexpr int kBatch = 32, kStages = 2;
@@ -252,7 +254,7 @@ struct WarpState {
 };
 
 // 32 keys of a stage. odd (of the warp): some scale is not finite; a head that does not keep the key is to get nothing of it. One instance of this code per kernel:
-// with six, a warp waited 4.2 cycles per instruction for the instruction itself (285 us at the 64 rows above; with one, 210).
+// with six, a warp waited 4.2 cycles per instruction for the instruction itself (an earlier form, at the 64 rows above: 285 us, with one 210).
 template <int D, int kH>
 __device__ __forceinline__ void attend(WarpState<D>& W, const uint2 (&q)[D / kGroup][4][32], const uint8_t* data, const float (*bias)[kH <= 4 ? 4 : 8], bool odd) {
     constexpr int NG = D / kGroup, kPitch = key_pitch(D), kCols = kH <= 4 ? 4 : 8, kSets = kH <= 4 ? 1 : 2;       // sets of 16 keys by 8 columns that a lane takes through the softmax
@@ -867,7 +869,7 @@ int attn_launch(const AttnArgs& A, int grid, cudaStream_t st) {
     return launch_overlapped(attn_kernel<D, kH, kW>, dim3(grid), dim3(32 * kW), bytes, st, 1, A);
 }
 // Eight warps per CTA where every CTA has one short row and all of them run at once: an SM has one of 128 channels or two of 64 (rows of 1000 keys, 8 KV heads; us of four warps and of eight:
-// d = 128, 16 rows 13.4 and 12.0, 20 rows 16.5 and 17.2; d = 64, 16 rows 10.5 and 8.8, 30 rows 12.4 and 12.2, 48 rows of 4 KV heads 11.7 and 10.7).
+// d = 128, 16 rows 13.9 and 11.8, 20 rows 16.9 and 21.6; d = 64, 16 rows 10.9 and 9.1, 30 rows 12.6 and 12.2, 48 rows of 4 KV heads 12.5 and 12.0).
 template <int D, int kH>
 int tc_decode(const AttnArgs& A, int grid, cudaStream_t st) {
     return !A.plan.ustart && grid <= (D == 64 ? 2 : 1) * 148 ? attn_launch<D, kH, 8>(A, grid, st) : attn_launch<D, kH, 4>(A, grid, st);
@@ -887,11 +889,11 @@ int launch_cache4_decode(const Cache& C, const void* q, const uint8_t* codes, co
     const bool tensor = C.dtype == DMA_BF16 && !(C.flags & DMA_FLAG_SIMT);
     const int hb = head_blocks(C), per_row = C.Hkv * hb;
     unsigned long long* weakest = nullptr;
-    // (units of 256 keys: 64 rows of 16K 157 us, of 512 159; one row of 16K 14.7, of 128 15.1, of 512 17.9)
+    // (units of 256 keys: 64 rows of 16K 161 us, of 512 163; one row of 16K 15.5, of 128 16.4, of 512 18.2)
     Plan plan{nullptr, nullptr, per_row, 8, (C.G + hb - 1) / hb, C.w};
     char* at = (char*)ws + kWsHeaderBytes;
     // The work is dealt out where rows may be long, unless short ones come in numbers that even out by themselves (us dealt out and by a CTA per item, 8 KV heads, w half the row:
-    // one row of 1024 keys 13.0 and 11.6, of 1536 13.0 and 14.9; 64 rows of up to 4096 57 and 62, 256 rows of up to 4096 189 and 185, of 4096 301 and 280, of 2048 172 and 155).
+    // one row of 1024 keys 12.2 and 11.0, of 1536 13.3 and 14.3; 64 rows of up to 4096 60 and 64, 256 rows of up to 4096 194 and 189, of 4096 310 and 289, of 2048 177 and 160).
     const bool even = capacity <= 1024 || (capacity <= 4096 && (int64_t)C.rows * per_row >= 4 * kAttnCtas);
     if (tensor && !even) {
         plan.ustart = reinterpret_cast<int32_t*>(at + weakest_bytes(C));

@@ -1,9 +1,9 @@
 // Rows into and out of the paged 4-bit cache (include/dma.h, dma_cache4_append, dma_cache4_read).
 //
 // Append: a group of d / 16 lanes owns a row of one KV head, 16 channels of K and of V per lane: two words of codes, four lanes to the 64 channels of a scale. Bound by
-// instructions (61 % of the issue slots, 18 per warp and 32 values). 16384 rows of 8 heads, d = 128: 31 us, 2.9 TB/s (57 with divisions beside ties, 45 with 8 channels
-// per lane: what a row takes beside its values is shared by fewer of them).
-// Read: d / 8 lanes, a word of codes each; bound by memory. 14336 rows 16.6 us, 4.7 TB/s.
+// latency: 61 % of the issue slots and 32 % of the warps active, neither memory nor a pipe at its limit; 18 instructions per warp and 32 values. 16384 rows of 8 heads, d = 128: 31 us,
+// 2.9 TB/s, where the bytes alone take 13 (57 with divisions beside ties, 45 with 8 channels per lane: what a row takes beside its values is shared by fewer of them).
+// Read: d / 8 lanes, a word of codes each. 14336 rows 16.6 us, 4.7 TB/s: below the copy's rate by the two dependent trips, slot and codes, that every CTA of several waves begins with.
 #include <algorithm>
 #include <type_traits>
 

@@ -792,3 +792,34 @@ def test_append_codes_next_to_halves(zero, dtype):
     n, sc, _ = ref.quantise(K.float().cpu().numpy())
     got = ref.unpack(arrays[0].cpu().numpy().transpose(0, 2, 1, 3, 4).reshape(-1, 2, 2, 32)[:rows])
     assert np.isfinite(sc).all() and np.array_equal(got[:, :, 0], n) and np.array_equal(got[:, :, 1], n)
+
+
+@pytest.mark.parametrize("d,dtype", [(128, "bf16"), (64, "bf16"), (64, "fp32")])
+def test_read_prefix_under_a_chunk_of_queries(d, dtype):
+    """A prompt's last rows over its cached keys where the window holds every key, so that none expires: dma_attn_fwd_chunk over what dma_cache4_read gives, and dma_cache4_decode
+    with a row per token, are within their roundings of each other."""
+    Hq, Hkv, page, L, n0 = 8, 2, 32, 300, 211
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    half, u, g = torch.finfo(dt).eps / 2, 2.0 ** -24, torch.Generator().manual_seed(d)
+    q, K, V = (torch.randn(L, h, d, generator=g).to(dt).cuda() for h in (Hq, Hkv, Hkv))
+    W, A = (torch.randn(Hq, d, generator=g) / math.sqrt(d)).cuda(), (torch.rand(Hq, generator=g) / 4 + 0.1).cuda()
+    c, *arrays = pool_of(Hq, Hkv, d, page, 12, L, dt, blocks=12, w=L)
+    table = torch.randperm(12, generator=g).int().cuda()
+    j = torch.arange(L, device="cuda")
+    slot = table[j // page] * page + (j % page).int()
+    dma.dma_cache4_append(c, K, V, slot, *arrays, W, A)
+    Kc, Vc, delta = dma.dma_cache4_read(c, *arrays, slot)
+    O, lse = dma.dma_attn_fwd_chunk(dma.problem(1, Hq, Hkv, L, d, L, dtype=dt), n0, q[None, n0:], Kc[None], Vc[None], delta[None], torch.full((1, Hq, L), L, **I32))
+    c.rows = L - n0
+    o, l = dma.dma_cache4_decode(c, q[n0:], *arrays, table[None], torch.zeros(L - n0, **I32), j[n0:].int())
+    k, v = (x.double().repeat_interleave(Hq // Hkv, 1).transpose(0, 1) for x in (Kc, Vc))          # [Hq, L, d]
+    qd, seen = q[n0:].double().transpose(0, 1), j <= j[n0:, None]
+    bias = delta.double()[:, None]
+    p = torch.softmax((qd @ k.transpose(1, 2) / math.sqrt(d) + bias).masked_fill(~seen, -math.inf), -1)
+    big = float((qd.abs() @ k.abs().transpose(1, 2) / math.sqrt(d) + bias).max())
+    pv = (p @ v.abs()).transpose(0, 1)
+    # bf16: K's rounding on the way out moves a score by half a step of its terms, V's a value, P's rounding a weight, and each result has its own. fp32: the sums of both (z and s n
+    # apart, up to six times the values)
+    lim = (2 * half * big + 4 * half) * pv + 2 * (2 * 136 * u * big + (L + 64) * u) * 6 * pv
+    assert ((O[0].double() - o.double()).abs() <= lim).all()
+    assert ((lse[0].t().double() - l.double()).abs() <= half * big + 2 * 136 * u * big + (L + 64) * u).all()
