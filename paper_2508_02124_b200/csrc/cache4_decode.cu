@@ -175,18 +175,20 @@ __global__ void __launch_bounds__(D) simt_combine_kernel(Rows R, const float* pa
 //   scan     a lane per key tests its weight against every head's weakest kept key; keys that some head keeps are queued, with the heads' biases
 //            (-inf where a head drops the key), so that a key that several heads keep is read and expanded once
 //   gather   32 queued keys at a time, codes and scales, by cp.async into one of the warp's stages while the stage before is used
-//   attend   S^T = K q^T and O^T += V^T P^T by mma.m16n8k16 (keys, then channels, by heads). The codes are expanded as little as
-//            possible: a code n in the lowest mantissa bits of a half is the subnormal number n 2^-24, exactly, and four bits higher 16 n 2^-24; eight
-//            codes of a word take a shift and four masks. A group of 64 channels is a chain of four products, whose sum takes the group's scale, and with the query's own sum
-//            over the group its zero, in fp32; the query goes in as halves, scaled by a power of two per head and group (its 8 bits survive down to 2^-27 of the largest
-//            channel there, and what is lost below that is less than the rounding of the sums; the products of 16 n take q / 16). Nothing of K is rounded. Softmax in registers, with a running maximum per warp and head. Of V the
-//            scale goes into the weight, P s in two halves, its rounding and what that leaves, scaled by a power of two per head and group that follows the largest
-//            (WarpState): 2^-22 of a weight, and of the small ones 2^-32 of the largest, which is less than the sums' own rounding in fp32. z P is summed in fp32.
-//            With up to four heads the operand's columns 4 to 7 hold the same heads again: their lanes take the second 16 keys through the softmax, and in the
+//   attend   S^T = K q^T and O^T += V^T P^T by mma.m16n8k16 (keys, then channels, by heads). The codes are expanded as little as possible: a code n in the high half of a half's
+//            low byte is the subnormal number n 2^-20, exactly, and the eight codes of a word take three shifts and four masks. A group of 64 channels is a chain of four products,
+//            whose sum takes the group's scale, and with the query's own sum over the group its zero, in fp32; the query goes in as halves, scaled by a power of two per head and
+//            group (its 8 bits survive down to 2^-31 of the largest channel there, and what is lost below that is less than the rounding of the sums). Softmax in registers, with a
+//            running maximum per warp and head. Of V the scale goes into the weight, P s in two halves, its rounding and what that leaves, scaled by a power of two per head and
+//            group that follows the largest (WarpState): 2^-22 of a weight, and of the small ones 2^-32 of the largest, which is less than the sums' own rounding in fp32. z P is
+//            summed in fp32. With up to four heads the operand's columns 4 to 7 hold the same heads again: their lanes take the second 16 keys through the softmax, and in the
 //            products of V they hold the low halves (the 64 rows below: 115.2 us, with one half per weight 113.6; with eight heads per group, whose low halves are products of their
 //            own, 182 and 169).
-// 64 rows of 1 to 16K keys, 32 / 8 heads of 128, w = 2048: 117 us for 414 MB read, 3.6 TB/s, 800 instructions per 32 keys of a union. No unit is at its limit: 53 % of the issue
-// slots, 53 % of the integer pipe, 17 % of the tensor pipe. What the time is made of is the chain of test, queue and gather that every warp goes through before it attends, with three
+//            What the products cut: the tensor core adds the 16 addends of an element, and the sum so far, above 2^-25 of the largest one's power of two, and a subnormal operand
+//            counts as 2^-14 there whatever it is (both measured). So an addend loses up to 2^-19 of a code's step by the largest weight among its 16 keys, or by the largest
+//            channel. With codes in the lowest bits, which take a shift less, it was 2^-15: 118 us instead of 123, but a key that outweighs 16 others 2^15 times left nothing of
+//            them, and four to ten times as many outputs rounded elsewhere than the exact ones. In the highest bits, a shift more, it is 2^-21, and 126 us.
+// 64 rows of 1 to 16K keys, 32 / 8 heads of 128, w = 2048: 123 us for 414 MB read, 3.4 TB/s. No unit is at its limit (see the counters). What the time is made of is the chain of test, queue and gather that every warp goes through before it attends, with three
 // warps per scheduler to take turns: without the attending 90 us; with all pages in the L2 3 us less than from memory. Twelve warps per SM: sixteen, with stages that are swizzled to
 // fit, 118 where twelve took 113; eight with three stages 133 where twelve took 119. Codes as bf16 numbers and weights in two parts of bf16 210 where subnormal halves took 165. 256
 // rows of 4096 keys, w = 1024: 228 us, 4.6 TB/s.
@@ -232,20 +234,19 @@ __device__ __forceinline__ uint32_t halves(float lo, float hi) {
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
 }
-// a word's codes in four pairs of halves: pair s holds codes s and s + 4, times 2^-24, and 16 where s is odd
+// a word's codes in four pairs of halves: pair s holds codes s and s + 4, times 2^-20
 __device__ __forceinline__ void expand_word(uint32_t x, uint32_t (&d)[4]) {
-    const uint32_t y = x >> 8;
-    d[0] = x & 0x000f000fu;
+    d[0] = x << 4 & 0x00f000f0u;
     d[1] = x & 0x00f000f0u;
-    d[2] = y & 0x000f000fu;
-    d[3] = y & 0x00f000f0u;
+    d[2] = x >> 4 & 0x00f000f0u;
+    d[3] = x >> 8 & 0x00f000f0u;
 }
 __device__ __forceinline__ float ex2f(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
 constexpr float kLog2e = 1.4426950408889634f;
 
 // The heads' softmax state and sums of a warp, in the layout of the accumulators: this lane's columns are heads 2 (lane % 4) and the next one, modulo 4 where there are
-// up to four. o is in units of 2^-24 f (odd j: 16 times that); f, a power of two, brings the largest weight so far, wref, to 2^7 .. 2^8.
+// up to four. o is in units of 2^-20 f; f, a power of two, brings the largest weight so far, wref, to 2^7 .. 2^8.
 template <int D>
 struct WarpState {
     static constexpr int NG = D / kGroup;
@@ -585,7 +586,7 @@ __global__ void __launch_bounds__(32 * kW, kW == 4 ? 3 : D == 64 ? 2 : 1) attn_k
                 big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
                 // the power of two of the head's group brings its largest channel to 2^14 .. 2^15
                 const int up = max(-113, min(100, 127 + 14 - (int)(big >> 23)));
-                const float k = __uint_as_float((uint32_t)(127 + up) << 23), even = k, odd_k = k * 0.0625f;
+                const float k = __uint_as_float((uint32_t)(127 + up) << 23);
                 float sum = 0.0f;
                 uint32_t frag[4][2];
 #pragma unroll
@@ -597,16 +598,16 @@ __global__ void __launch_bounds__(32 * kW, kW == 4 ? 3 : D == 64 ? 2 : 1) attn_k
 #pragma unroll
                     for (int n8 = 0; n8 < 8; ++n8) sum += ch[n8];
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) frag[s][e] = halves(ch[s] * (s & 1 ? odd_k : even), ch[s + 4] * (s & 1 ? odd_k : even));
+                    for (int s = 0; s < 4; ++s) frag[s][e] = halves(ch[s] * k, ch[s + 4] * k);
                 }
                 if (warp == 0)
 #pragma unroll
                     for (int s = 0; s < 4; ++s) sQ[g][s][lane] = make_uint2(frag[s][0], frag[s][1]);
                 sum += __shfl_xor_sync(0xffffffffu, sum, 1);
                 sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                // (in the products' units: codes 2^-24, queries k)
-                sum *= k * 0x1p-24f;
-                const float unit = A.scale / k * 0x1p24f;
+                // (in the products' units: codes 2^-20, queries k)
+                sum *= k * 0x1p-20f;
+                const float unit = A.scale / k * 0x1p20f;
                 W.qsum[g][0] = __shfl_sync(0xffffffffu, sum, 8 * t4);
                 W.qsum[g][1] = __shfl_sync(0xffffffffu, sum, 8 * t4 + 4);
                 W.scale[g][0] = __shfl_sync(0xffffffffu, unit, 8 * t4);
@@ -735,7 +736,7 @@ __global__ void __launch_bounds__(32 * kW, kW == 4 ? 3 : D == 64 ? 2 : 1) attn_k
                 float v[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    v[j] = W.o[g][j][e] * unit * (j & 1 ? 0x1p20f : 0x1p24f);
+                    v[j] = W.o[g][j][e] * unit * 0x1p20f;
                     if (kH <= 4) v[j] += __shfl_xor_sync(0xffffffffu, v[j], 2);
                     v[j] += W.oz[g][e & 1];
                 }

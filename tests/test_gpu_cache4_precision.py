@@ -28,11 +28,19 @@ def a_cache(Hq, Hkv, d, page, lens, w, dtype, seed, flags=0):
     return c, q, (codes, scales, delta), (table, torch.arange(nseq, **I32), torch.tensor(lens, **I32) - 1)
 
 
+def cut(ps):
+    """What products of 16 keys cut of the sums of weights ps [n, d], each addend by 2^-19 of the largest weight of its product. No more than 16 addends share a product, so the largest
+    ones add up to 16 times the sum of the n / 16 largest weights at most; and the sum so far is cut once per product, by no more than once per key."""
+    top = ps.sort(0, descending=True)[0][:-(-len(ps) // 16)]
+    return 2.0 ** -19 * (16 * top.sum(0) + ps.sum(0))
+
+
 def check(c, q, arrays, plan, o, lse, exact_scores=False):
     """A score is a sum of 2 d products and a few more operations: at most 136 U of the sum of its terms' magnitudes (`big`) off, where no query is 0; of a query 0 it is the bias,
     and what is left is an exponential's, of 2^-22, and its argument's rounding. The sums of n weights and values are off by at most (n + 64) U of the sum of theirs. bf16 elements'
     values go through the tensor cores as codes by weights p s in two halves: 2^-22 of a weight, and 2^-24 in units of which the largest weight of the row's head and group is 2^7 or more:
-    2^-31 of that one, times a code of up to 15."""
+    2^-31 of that one, times a code of up to 15. A product of 16 keys cuts each addend, and the sum so far, by up to 2^-19 of the largest weight among them (cut()); exponentials below
+    2^-126 are 0, which n of them times the largest value bound."""
     codes, scales, delta = arrays
     table, seq, pos = plan
     page, G = c.page_size, c.Hq // c.Hkv
@@ -55,7 +63,9 @@ def check(c, q, arrays, plan, o, lse, exact_scores=False):
             e = 8 * U * big + 2.0 ** -22 if exact_scores else 136 * U * big
             ps = p[:, None] * s[:, 1].abs()
             lim = (2 * e + (len(kept) + 64) * U) * (p @ (n4[:, 1] * s[:, 1].abs() + z[:, 1].abs())) + 2.0 ** -22 * (ps * n4[:, 1]).sum(0) + len(kept) * 15 * 2.0 ** -31 * ps.max(0)[0]
-            lim = lim + half * exact.abs() + 1e-38
+            lim = lim + half * exact.abs() + len(kept) * 2.0 ** -126 * (n4[:, 1] * s[:, 1].abs() + z[:, 1].abs()).max() + 1e-38
+            if q.dtype == torch.bfloat16 and not c.flags & dma.DMA_FLAG_SIMT:
+                lim = lim + cut(ps)
             err = (o[t, h].double() - exact).abs()
             assert (err <= lim).all(), (t, h, n, float((err / lim).max()))
             want = float(torch.logsumexp(score, 0))
@@ -121,3 +131,29 @@ def test_scales_that_begin_with_zero(Hq, Hkv, d, size, flags):
         arrays[1][pages[:n // 64], :, :, 1] = 0.0                          # half of the row's keys
     o, lse = dma.dma_cache4_decode(c, q, *arrays, *plan)
     check(c, q, arrays, plan, o, lse)
+
+
+@pytest.mark.parametrize("Hq,Hkv,d", SHAPES)
+@pytest.mark.parametrize("n", [2, 16, 17, 500])
+def test_a_key_that_outweighs_the_others(Hq, Hkv, d, n):
+    """One key has 2^15.9 times the weight of each other and the value 0, a code of 8 by a scale of 1 and a zero of -8, so that the outputs are the others' alone. Weight 1 and value 0
+    are exact; each other weight is e^-11 of that, within 2^-21; sums of magnitudes up to 16 are kept to 64 U; and the products cut 2^-19 per addend beside that key, of which 16 share
+    its product, while among the others alone it is 2^-19 of their own weight."""
+    c, q, arrays, plan = a_cache(Hq, Hkv, d, 16, [n], n, torch.bfloat16, n)
+    arrays[1][..., 0], arrays[1][..., 1] = 1.0, -8.0
+    arrays[2].fill_(1.0)
+    first = int(plan[0][0, (n - 1) // 16])
+    arrays[0][first, :, (n - 1) % 16, 1] = 0x88
+    arrays[2][first, :, (n - 1) % 16] = 12.0
+    q.zero_()
+    o, lse = dma.dma_cache4_decode(c, q, *arrays, *plan)
+    j = torch.arange(n, device="cuda")
+    nib = arrays[0][plan[0][0, j // 16].long(), :, j % 16, 1]                # [n, Hkv, d / 2]
+    v = torch.stack([nib & 15, nib >> 4], -1).flatten(2).double() - 8
+    p = torch.exp(torch.where(j == n - 1, 0.0, -11.0).double())
+    total = float(p.sum())
+    for h in range(Hq):
+        exact, mag = (p @ v[:, h // (Hq // Hkv)]) / total, float((p[:-1] * 16).sum())
+        lim = 17 * 2.0 ** -19 + (2.0 ** -21 + 80 * U) * mag + 64 * U * 16 + torch.finfo(torch.bfloat16).eps / 2 * exact.abs()
+        assert ((o[0, h].double() - exact).abs() <= lim).all()
+    assert (lse[0].double() - 12 - math.log(total)).abs().max() <= 2.0 ** -20
