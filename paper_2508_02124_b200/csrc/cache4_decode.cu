@@ -187,7 +187,9 @@ __global__ void __launch_bounds__(D) simt_combine_kernel(Rows R, const float* pa
 //            What the products cut: the tensor core adds the 16 addends of an element, and the sum so far, above 2^-25 of the largest one's power of two, and a subnormal operand
 //            counts as 2^-14 there whatever it is (both measured). So an addend loses up to 2^-19 of a code's step by the largest weight among its 16 keys, or by the largest
 //            channel. With codes in the lowest bits, which take a shift less, it was 2^-15: 118 us instead of 123, but a key that outweighs 16 others 2^15 times left nothing of
-//            them, and four to ten times as many outputs rounded elsewhere than the exact ones. In the highest bits, a shift more, it is 2^-21, and 126 us.
+//            them. In the highest bits, a shift more, it is 2^-21, and 126 us. Sums of V begin anew with every 32 keys and are added in fp32, to nearest (125 us): one chain of products
+//            over all keys is cut at each of them, always towards zero, and the codes' part and the zeros' nearly cancel (of 64K kept keys' outputs 25 % then rounded elsewhere than
+//            the exact ones, now 1.5 %; of 2048 kept of 16K 0.5 and 0.2 %).
 // 64 rows of 1 to 16K keys, 32 / 8 heads of 128, w = 2048: 123 us for 414 MB read, 3.4 TB/s. No unit is at its limit (see the counters). What the time is made of is the chain of test, queue and gather that every warp goes through before it attends, with three
 // warps per scheduler to take turns: without the attending 90 us; with all pages in the L2 3 us less than from memory. Twelve warps per SM: sixteen, with stages that are swizzled to
 // fit, 118 where twelve took 113; eight with three stages 133 where twelve took 119. Codes as bf16 numbers and weights in two parts of bf16 210 where subnormal halves took 165. 256
@@ -421,6 +423,7 @@ __device__ __forceinline__ void attend(WarpState<D>& W, const uint2 (&q)[D / kGr
                 b[0][e] = lane < 16 ? b[0][e] : other_low;
             }
         }
+        float sum[4][4] = {};                                     // of the 32 keys: what the products cut stays relative to these, and fp32 additions round to nearest
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint8_t* v = vrow + 16 * i * kPitch + g * 32;
@@ -433,10 +436,17 @@ __device__ __forceinline__ void attend(WarpState<D>& W, const uint2 (&q)[D / kGr
             expand_word(__byte_perm(wc, wd, 0x7632), a3);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                mma16816(W.o[g][j], a0[j], a1[j], a2[j], a3[j], b[i][0], b[i][1]);
-                if constexpr (kSets == 2) mma16816(W.o[g][j], a0[j], a1[j], a2[j], a3[j], low[i][0], low[i][1]);
+                mma16816(sum[j], a0[j], a1[j], a2[j], a3[j], b[i][0], b[i][1]);
+                if constexpr (kSets == 2) mma16816(sum[j], a0[j], a1[j], a2[j], a3[j], low[i][0], low[i][1]);
             }
         }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                const float2 x = ptx::add2(make_float2(W.o[g][j][e], W.o[g][j][e + 1]), make_float2(sum[j][e], sum[j][e + 1]));
+                W.o[g][j][e] = x.x; W.o[g][j][e + 1] = x.y;
+            }
     }
 }
 

@@ -157,3 +157,27 @@ def test_a_key_that_outweighs_the_others(Hq, Hkv, d, n):
         lim = 17 * 2.0 ** -19 + (2.0 ** -21 + 80 * U) * mag + 64 * U * 16 + torch.finfo(torch.bfloat16).eps / 2 * exact.abs()
         assert ((o[0, h].double() - exact).abs() <= lim).all()
     assert (lse[0].double() - 12 - math.log(total)).abs().max() <= 2.0 ** -20
+
+
+@pytest.mark.parametrize("Hq,Hkv,d", [(16, 4, 128), (32, 4, 128), (32, 4, 64)])
+def test_long_sums_have_no_drift(Hq, Hkv, d):
+    """Rows of tens of thousands of kept keys whose values are as often above zero as below, so many rows that a warp sums thousands of keys: the codes' sums and the zeros' nearly
+    cancel, so that sums cut towards zero would show as outputs that are too low by more than their own rounding. The mean error, in parts of p (|z| + s n): two cuts of 2^-25 per 32
+    keys at most, and six standard deviations of the mean of the outputs' roundings, which are uniform in half a step to either side."""
+    n, rows = 40000, 64
+    c, q, arrays, plan = a_cache(Hq, Hkv, d, 64, [n], 1 << 20, torch.bfloat16, d)
+    arrays[1][..., 1].copy_(-7.5 * arrays[1][..., 0])
+    c.rows = rows                                                          # of one sequence, the same one
+    o, _ = dma.dma_cache4_decode(c, torch.zeros(rows, Hq, d, dtype=torch.bfloat16, device="cuda"), *arrays, plan[0], torch.zeros(rows, **I32), plan[2].expand(rows).contiguous())
+    off, spread, j = [], [], torch.arange(n, device="cuda")
+    at, place = plan[0][0, j // 64].long(), j % 64
+    for h in range(Hq):
+        nib, sc = arrays[0][at, h // (Hq // Hkv), place, 1], arrays[1][at, h // (Hq // Hkv), place, 1].double()
+        n4 = torch.stack([nib & 15, nib >> 4], -1).flatten(1).double()       # [n, d]
+        s, z = sc[..., 0].repeat_interleave(64, -1), sc[..., 1].repeat_interleave(64, -1)
+        p = torch.softmax(arrays[2][at, h, place].double(), 0)
+        mag, x = p @ (n4 * s + z.abs()), o[0, h].double()
+        off.append((x - p @ (n4 * s + z)) / mag)
+        spread.append((torch.exp2(torch.floor(torch.log2(x.abs().clamp_min(1e-30))) - 7) / mag) ** 2 / 12)
+    off, spread = torch.cat(off), torch.cat(spread)
+    assert abs(float(off.mean())) <= 2 * 2.0 ** -25 + 6 * float(spread.sum().sqrt()) / len(off)
