@@ -182,18 +182,17 @@ __global__ void __launch_bounds__(D) simt_combine_kernel(Rows R, const float* pa
 //            running maximum per warp and head. Of V the scale goes into the weight, P s in two halves, its rounding and what that leaves, scaled by a power of two per head and
 //            group that follows the largest (WarpState): 2^-22 of a weight, and of the small ones 2^-32 of the largest, which is less than the sums' own rounding in fp32. z P is
 //            summed in fp32. With up to four heads the operand's columns 4 to 7 hold the same heads again: their lanes take the second 16 keys through the softmax, and in the
-//            products of V they hold the low halves (the 64 rows below: 115.2 us, with one half per weight 113.6; with eight heads per group, whose low halves are products of their
-//            own, 182 and 169).
+//            products of V they hold the low halves (one half per weight was 1.4 % faster; with eight heads per group, whose low halves are products of their own, 7 %).
 //            What the products cut: the tensor core adds the 16 addends of an element, and the sum so far, above 2^-25 of the largest one's power of two, and a subnormal operand
 //            counts as 2^-14 there whatever it is (both measured). So an addend loses up to 2^-19 of a code's step by the largest weight among its 16 keys, or by the largest
 //            channel. With codes in the lowest bits, which take a shift less, it was 2^-15: 118 us instead of 123, but a key that outweighs 16 others 2^15 times left nothing of
 //            them. In the highest bits, a shift more, it is 2^-21, and 126 us. Sums of V begin anew with every 32 keys and are added in fp32, to nearest (125 us): one chain of products
 //            over all keys is cut at each of them, always towards zero, and the codes' part and the zeros' nearly cancel (of 64K kept keys' outputs 25 % then rounded elsewhere than
 //            the exact ones, now 1.5 %; of 2048 kept of 16K 0.5 and 0.2 %).
-// 64 rows of 1 to 16K keys, 32 / 8 heads of 128, w = 2048: 123 us for 414 MB read, 3.4 TB/s. No unit is at its limit (see the counters). What the time is made of is the chain of test, queue and gather that every warp goes through before it attends, with three
-// warps per scheduler to take turns: without the attending 90 us; with all pages in the L2 3 us less than from memory. Twelve warps per SM: sixteen, with stages that are swizzled to
-// fit, 118 where twelve took 113; eight with three stages 133 where twelve took 119. Codes as bf16 numbers and weights in two parts of bf16 210 where subnormal halves took 165. 256
-// rows of 4096 keys, w = 1024: 228 us, 4.6 TB/s.
+// 64 rows of 1 to 16K keys, 32 / 8 heads of 128, w = 2048: 125 us for 414 MB read, 3.3 TB/s, 890 instructions per 32 keys of a union. No unit is at its limit: 55 % of the issue
+// slots, 54 % of the integer pipe, 16 % of the tensor pipe. What the time is made of is the chain of test, queue and gather that every warp goes through before it attends, with three
+// warps per scheduler to take turns: without the attending 89 us. (Of an earlier form at 113 us: with all pages in the L2 110; sixteen warps per SM instead of twelve, with stages
+// that are swizzled to fit, 118; eight with three stages 133 where twelve took 119.) 256 rows of 4096 keys, w = 1024: 247 us, 4.2 TB/s.
 // (tcgen05 needs 64 rows of A at least, of which a decoding step has the group's 1 to 8 heads or, turned around, the keys: then the expanded codes would
 // have to go through shared memory once more. mma.sync takes them from the registers that the expansion leaves them in, and its rate is not what bounds this kernel.)
 constexpr int kBatch = 32, kStages = 2;
@@ -880,7 +879,7 @@ int attn_launch(const AttnArgs& A, int grid, cudaStream_t st) {
     return launch_overlapped(attn_kernel<D, kH, kW>, dim3(grid), dim3(32 * kW), bytes, st, 1, A);
 }
 // Eight warps per CTA where every CTA has one short row and all of them run at once: an SM has one of 128 channels or two of 64 (rows of 1000 keys, 8 KV heads; us of four warps and of eight:
-// d = 128, 16 rows 13.9 and 11.8, 20 rows 16.9 and 21.6; d = 64, 16 rows 10.9 and 9.1, 30 rows 12.6 and 12.2, 48 rows of 4 KV heads 12.5 and 12.0).
+// d = 128, 16 rows 15.1 and 12.3, 20 rows 18.1 and 22.6; d = 64, 16 rows 11.4 and 9.6, 30 rows 13.2 and 12.8, 48 rows of 4 KV heads 13.3 and 12.7).
 template <int D, int kH>
 int tc_decode(const AttnArgs& A, int grid, cudaStream_t st) {
     return !A.plan.ustart && grid <= (D == 64 ? 2 : 1) * 148 ? attn_launch<D, kH, 8>(A, grid, st) : attn_launch<D, kH, 4>(A, grid, st);
@@ -900,11 +899,11 @@ int launch_cache4_decode(const Cache& C, const void* q, const uint8_t* codes, co
     const bool tensor = C.dtype == DMA_BF16 && !(C.flags & DMA_FLAG_SIMT);
     const int hb = head_blocks(C), per_row = C.Hkv * hb;
     unsigned long long* weakest = nullptr;
-    // (units of 256 keys: 64 rows of 16K 161 us, of 512 163; one row of 16K 15.5, of 128 16.4, of 512 18.2)
+    // (units of 256 keys: 64 rows of 16K 174 us, of 512 175; one row of 16K 15.7, of 128 16.5, of 512 19.3)
     Plan plan{nullptr, nullptr, per_row, 8, (C.G + hb - 1) / hb, C.w};
     char* at = (char*)ws + kWsHeaderBytes;
     // The work is dealt out where rows may be long, unless short ones come in numbers that even out by themselves (us dealt out and by a CTA per item, 8 KV heads, w half the row:
-    // one row of 1024 keys 12.2 and 11.0, of 1536 13.3 and 14.3; 64 rows of up to 4096 60 and 64, 256 rows of up to 4096 194 and 189, of 4096 310 and 289, of 2048 177 and 160).
+    // one row of 1024 keys 14.1 and 11.8, of 1536 13.7 and 15.2; 64 rows of up to 4096 65 and 69, 256 rows of up to 4096 209 and 206, of 4096 338 and 314, of 2048 193 and 174).
     const bool even = capacity <= 1024 || (capacity <= 4096 && (int64_t)C.rows * per_row >= 4 * kAttnCtas);
     if (tensor && !even) {
         plan.ustart = reinterpret_cast<int32_t*>(at + weakest_bytes(C));
