@@ -318,7 +318,7 @@ int dma_page_plan(const dma_cache_t* c, const int32_t* lens, const int32_t* want
  *     z = bf16(min x),  s = max(0, bf16((max x / 2 - z / 2) / 7.5)),  n = min(15, max(0, rint((x / 2 - z / 2) / (s / 2))))
  *   (ties to even; n = 0 where the quotient is NaN, so with s = 0 too). 64 channels that hold a NaN or an infinity, or whose
  *   smallest value bf16 rounds to -inf, read back as NaN. A largest value beyond bf16's range is no such case: it takes part in s
- *   as it is; where z + s n then passes fp32's range, that channel alone reads back as an infinity.
+ *   as it is; where z + s n then passes fp32's range, those channels alone read back as infinities.
  *   delta: of the row's V as given (not as held), the bits of dma_mask_build: W_delta [Hq, d], A [Hq]. Or, with delta_new not
  *   NULL, delta_new[h * delta_ld + t] as it is (dma_mask_build's bias, or dma_delta_range's output for the full weights;
  *   weights are greater than 0: what dma_cache4_decode keeps of keys with others is not defined);

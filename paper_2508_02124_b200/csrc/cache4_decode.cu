@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(D) simt_combine_kernel(Rows R, const float* pa
 //            products of V they hold the low halves (one half per weight was 1.4 % faster; with eight heads per group, whose low halves are products of their own, 7 %).
 //            What the products cut: the tensor core adds the 16 addends of an element, and the sum so far, above 2^-25 of the largest one's power of two, and a subnormal operand
 //            counts as 2^-14 there whatever it is (both measured). So an addend loses up to 2^-19 of a code's step by the largest weight among its 16 keys, or by the largest
-//            channel. With codes in the lowest bits, which take a shift less, it was 2^-15: 118 us instead of 123, but a key that outweighs 16 others 2^15 times left nothing of
+//            channel. With codes in the lowest bits, which take two shifts less, it was 2^-15: 118 us instead of 123, but a key that outweighs 16 others 2^15 times left nothing of
 //            them. In the highest bits, a shift more, it is 2^-21, and 126 us. Sums of V begin anew with every 32 keys and are added in fp32, to nearest (125 us): one chain of products
 //            over all keys is cut at each of them, always towards zero, and the codes' part and the zeros' nearly cancel (of 64K kept keys' outputs 25 % then rounded elsewhere than
 //            the exact ones, now 1.5 %; of 2048 kept of 16K 0.5 and 0.2 %).
@@ -622,7 +622,7 @@ __global__ void __launch_bounds__(32 * kW, kW == 4 ? 3 : D == 64 ? 2 : 1) attn_k
                 W.scale[g][0] = __shfl_sync(0xffffffffu, unit, 8 * t4);
                 W.scale[g][1] = __shfl_sync(0xffffffffu, unit, 8 * t4 + 4);
                 W.oz[g][0] = W.oz[g][1] = 0.0f;
-                W.f[g][0] = W.f[g][1] = 0x1p100f;                 // (whatever weight comes first passes the half's range by it, and sets the power)
+                W.f[g][0] = W.f[g][1] = 0x1p126f;                 // (whatever weight comes first passes the half's range by it, and sets the power)
                 W.wref[g][0] = W.wref[g][1] = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) W.o[g][j][0] = W.o[g][j][1] = W.o[g][j][2] = W.o[g][j][3] = 0.0f;

@@ -119,7 +119,7 @@ def test_queries_keep_the_channels_of_every_group(Hq, Hkv, lens, w, flags):
 
 
 @pytest.mark.parametrize("flags", [0, dma.DMA_FLAG_SIMT])
-@pytest.mark.parametrize("size", [2.0 ** -80, 2.0 ** -40, 2.0 ** -20, 1.0, 2.0 ** 40, 2.0 ** 98])
+@pytest.mark.parametrize("size", [2.0 ** -104, 2.0 ** -80, 2.0 ** -40, 2.0 ** -20, 1.0, 2.0 ** 40, 2.0 ** 98])
 @pytest.mark.parametrize("Hq,Hkv,d", SHAPES)
 def test_scales_that_begin_with_zero(Hq, Hkv, d, size, flags):
     """The first keys' values are constant (scale 0), as padding's are, and the later ones' scales of any size."""
