@@ -353,6 +353,69 @@ int dma_cache4_decode(const dma_cache_t* c, const void* q, const void* codes, co
                       const int32_t* block_table, const int32_t* row_seq, const int32_t* row_pos, void* o, float* lse, void* ws,
                       size_t ws_bytes, void* cuda_stream);
 
+/* ---- A paged cache in the element type, and requests that share a long prefix --------------------------------------------
+ * (A property of the library, like the 4-bit cache above, whose descriptor, pages, slots, rows and page plan it shares.)
+ *   kv      dtype [num_pages, Hkv, page_size, 2, d]     a key's K row, then its V row
+ *   delta   fp32  [num_pages, Hq, page_size]            the keys' dynamic weights
+ * A prefix is a sequence that other sequences stand behind: a system prompt, a document, a conversation that is sampled several
+ * times. Its keys lie in the pool once. Row t of sequence row_seq[t] sees the keys of its prefix row_prefix[t] and, behind them, the keys
+ * 0 .. row_pos[t] of its own sequence: block tables, lengths and positions are each sequence's own, as dma_page_plan keeps them, and
+ * a key's place in the row's context is the prefix' length plus its own position. row_prefix outside [0, nprefix): no prefix.
+ * Weights are greater than 0 and no NaN, as in the 4-bit cache; with others it is not defined which keys are kept. */
+
+/* Bytes of the two arrays (any pointer may be NULL). */
+int dma_cache_bytes(const dma_cache_t* c, size_t* kv, size_t* delta);
+
+/* HOST. The rotation of a position m (Sec. 3, App. A listing: the rotary embedding between the projections and the cache): pair i of the first `rot`
+ * channels of a head, (x, y), becomes scale (x cos a - y sin a, x sin a + y cos a) with a = m inv_freq[i]; the other channels stay. */
+typedef struct {
+    const float* inv_freq;       /* DEVICE, [rot / 2]                                                             */
+    int32_t rot;                 /* channels that are rotated: a multiple of 16, at most d                        */
+    int32_t interleaved;         /* 0: pair i is (i, i + rot / 2); 1: (2 i, 2 i + 1)                              */
+    float scale;                 /* 0 -> 1                                                                        */
+} dma_rotation_t;
+
+/* A step's rows into the cache: K rotated, V as it is, delta of V as dma_cache4_append forms it (the bits of dma_mask_build with W_delta, A;
+ * or delta_new); and q rotated by the same positions.
+ *   q, K, V   [rows, Hq or Hkv, d] (q_stride, k_stride, v_stride)
+ *   rotation  NULL: K as it is; q, q_out, row_pos, row_prefix and prefix_len are then not read (q and q_out have to be NULL)
+ *   q         NULL: only K is rotated. q_out has o_stride; it may be q, with the same strides
+ *   row_pos   [rows]; row t is rotated by row_pos[t] + prefix_len[row_prefix[t]] (a length below 0 counts as 0). row_pos[t] < 0, as behind a plan's
+ *             last row: the row is skipped altogether
+ *   row_prefix, prefix_len   [rows], [nprefix]; both NULL: no prefixes
+ *   slot      [rows]; K, V and delta of a row whose slot is outside the pool are not written (its q is). Slots of one call are distinct.
+ * Angles are formed in 64 bits and reduced to a turn before they are rounded to fp32; the rotation is fp32, rounded once. */
+int dma_cache_append(const dma_cache_t* c, const dma_rotation_t* rotation, const void* q, const void* K, const void* V, const float* W_delta,
+                     const float* A, const float* delta_new, int64_t delta_ld, const int32_t* slot, const int32_t* row_pos,
+                     const int32_t* row_prefix, const int32_t* prefix_len, int32_t nprefix, void* q_out, void* kv, float* delta, void* cuda_stream);
+
+/* The order of prefixes, once when a prefix has been appended (or has grown): of each of c->nseq prefixes and every query head the min(w, visible)
+ * keys with the largest delta, largest first, ties to the lower position. What the rows behind the prefix keep of it is the beginning of this list.
+ *   block_table [nseq, table_ld], prefix_len [nseq]: the prefixes' own. Keys in pages whose number is outside the pool are not visible;
+ *               lengths are brought into [0, max_blocks * page_size]
+ *   order_slot, order_weight [nseq, Hq, order_ld]: slot and delta of each; entries behind the last one are left as they are.
+ *               order_ld >= min(w, max_blocks * page_size)
+ *   order_len [nseq]: min(w, visible)
+ * Reads Hq, Hkv, w, pages, nseq, table_ld. ws: dma_prefix_order_workspace() bytes, for one call at a time; a size that does not fall as nseq, Hq,
+ * max_blocks or w grow. */
+int dma_prefix_order_workspace(const dma_cache_t* c, size_t* bytes);
+int dma_prefix_order(const dma_cache_t* c, const float* delta, const int32_t* block_table, const int32_t* prefix_len, int32_t* order_slot,
+                     float* order_weight, int64_t order_ld, int32_t* order_len, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/* Decoding over the pages, behind prefixes: dma_decode for every row over the keys of its prefix and its own keys 0 .. row_pos[t] (none if
+ * row_pos[t] < 0). Every query head keeps the min(w, visible) keys with the largest delta (ties to the lower place in the context) and
+ *   o[t, h] = softmax(q . K_sel^T scale + delta_sel) V_sel,  lse[t, h] its log-sum-exp (natural log)
+ * q and o have q_stride and o_stride; lse [rows, Hq]. order_*: of nprefix prefixes, of dma_prefix_order with the same Hq, pool and w (0 prefixes: the four
+ * pointers are not read). All rows of a prefix attend to its keys together: the listed keys are read once per 128 rows and query
+ * head. Rows in no order; a row that sees no key gets o = 0, lse = -inf; a row whose row_seq is outside [0, nseq) is left as it is.
+ * Results depend on the call's rows and prefixes in the last bits, and are the same bits from run to run.
+ * ws: dma_cache_decode_workspace() bytes, a size that does not fall as rows, Hq, max_blocks or nprefix grow. It serves one call at a time: calls that may
+ * overlap on the GPU need one each. */
+int dma_cache_decode_workspace(const dma_cache_t* c, int32_t nprefix, size_t* bytes);
+int dma_cache_decode(const dma_cache_t* c, const void* q, const void* kv, const float* delta, const int32_t* block_table, const int32_t* row_seq,
+                     const int32_t* row_pos, const int32_t* row_prefix, int32_t nprefix, const int32_t* order_slot, const float* order_weight,
+                     int64_t order_ld, const int32_t* order_len, void* o, float* lse, void* ws, size_t ws_bytes, void* cuda_stream);
+
 /* The whole hot path on HOST buffers (all contiguous, default strides only): copies Q,K,V,(dO),W_delta,A into the
  * caller's device arena, runs dma_mask_build, dma_attn_fwd and, if `backward` != 0, dma_attn_bwd on the stream,
  * copies O, lse (and dQ,dK,dV,dM) back and synchronises the stream before returning. The copies run on two helper

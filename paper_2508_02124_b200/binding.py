@@ -23,7 +23,8 @@ ENTRY_POINTS = ("dma_query_workspace", "dma_bitmap_words", "dma_mask_build", "dm
                 "dma_mask_bwd_workspace", "dma_mask_bwd", "dma_delta_range", "dma_decode_workspace", "dma_decode",
                 "dma_mask_build_varlen", "dma_decode_state_bytes", "dma_decode_state_init", "dma_decode_step",
                 "dma_attn_fwd_chunk", "dma_kernel_timing", "dma_kernel_timing_read",
-                "dma_cache4_bytes", "dma_page_plan", "dma_cache4_append", "dma_cache4_read", "dma_cache4_decode_workspace", "dma_cache4_decode")
+                "dma_cache4_bytes", "dma_page_plan", "dma_cache4_append", "dma_cache4_read", "dma_cache4_decode_workspace", "dma_cache4_decode",
+                "dma_cache_bytes", "dma_cache_append", "dma_prefix_order_workspace", "dma_prefix_order", "dma_cache_decode_workspace", "dma_cache_decode")
 
 
 class DmaError(RuntimeError):
@@ -50,6 +51,11 @@ class dma_cache_t(ctypes.Structure):
                 ("v_stride", ctypes.c_int64 * 2), ("o_stride", ctypes.c_int64 * 2)]
 
 
+class dma_rotation_t(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("rot", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+_STRIDES, _STRIDES_AT = struct.Struct("8q"), dma_cache_t.q_stride.offset      # of q, K, V and o
 _KV_STRIDES, _KV_AT = struct.Struct("4q"), dma_cache_t.k_stride.offset       # k_stride and v_stride at once: a tenth of the time of two ctypes arrays
 
 
@@ -122,7 +128,8 @@ _SIGNATURES = {
     "dma_attn_bwd": "Pvvvvvvvvvvvvvvzv", "dma_delta_range": "Pvvvvliiv", "dma_decode": "Pvvvvlvvvvzv",
     "dma_decode_state_init": "Pvlvvzv", "dma_decode_step": "Pvvvvlvvvvzv", "dma_step_host": "Pivvvvvvvvvvvvvzv",
     "dma_page_plan": "vvvvvvvvvvvvv", "dma_cache4_append": "vvvvvvlvvvvv", "dma_cache4_read": "vvvvvvvvlv",
-    "dma_cache4_decode": "vvvvvvvvvvvzv", "dma_read_status": "vv", "dma_selftest_wait_timeout": "vzv"}
+    "dma_cache4_decode": "vvvvvvvvvvvzv", "dma_cache_append": "vvvvvvvvlvvvvivvvv", "dma_prefix_order": "vvvvvvlvvzv",
+    "dma_cache_decode": "vvvvvvvvivvlvvvvzv", "dma_read_status": "vv", "dma_selftest_wait_timeout": "vzv"}
 _KINDS = {"P": ctypes.POINTER(dma_problem_t), "v": ctypes.c_void_p, "i": ctypes.c_int32, "l": ctypes.c_int64, "z": ctypes.c_size_t}
 _typed = {}                  # name -> function object with typed parameters
 _typed_lib = None            # a handle of its own: the function objects of lib() stay untyped
@@ -515,6 +522,156 @@ def dma_cache4_decode(c, q, codes, scales, delta, block_table, row_seq, row_pos,
     _call("dma_cache4_decode", ctypes.byref(c), _row_major("q", q, dt, rows, heads, d, c.q_stride, dev), *_pool(c, codes, scales, delta, heads, c.Hkv, d, dev),
           _table(c, block_table, dev), _flat("row_seq", row_seq, torch.int32, rows, dev), _flat("row_pos", row_pos, torch.int32, rows, dev),
           _row_major("o", o, dt, rows, heads, d, c.o_stride, dev), _flat("lse", lse, torch.float32, rows * heads, dev), _flat("ws", ws, torch.uint8, 0, dev), ws.numel(), _stream())
+    return o, lse
+
+
+# ---- the paged cache in the element type, and shared prefixes ----
+
+def _rows(name, t, dtype, rows, heads, d, dev):
+    """Address, row and head strides of [rows, heads, d] in its own layout. A stride that no second row or head takes is the contiguous one."""
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: {t.dtype} where {dtype} is taken")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the call runs on cuda:{dev}")
+    shape = t.shape
+    if shape != (rows, heads, d) and (len(shape) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != d):
+        raise ValueError(f"{name}: shape {tuple(shape)} where [{rows}, {heads}, {d}] is taken")
+    row, head, one = t.stride()
+    if one != 1:
+        raise ValueError(f"{name}: strides {t.stride()}, the channels of a head lie side by side")
+    row, head = row if rows > 1 else heads * d, head if heads > 1 else d
+    if row <= 0 or head <= 0:
+        raise ValueError(f"{name}: strides {t.stride()}, rows and heads on top of each other")
+    return t.data_ptr(), row, head
+
+
+def _with_strides(c, *strides):
+    """The descriptor with these strides of q, K, V and o: itself, or a copy."""
+    if _STRIDES.unpack_from(c, _STRIDES_AT) != strides:
+        c = dma_cache_t.from_buffer_copy(c)
+        _STRIDES.pack_into(c, _STRIDES_AT, *strides)
+    return c
+
+
+def dma_cache_bytes(c):
+    """Bytes of (kv, delta)."""
+    n = [ctypes.c_size_t() for _ in range(2)]
+    _check(lib().dma_cache_bytes(ctypes.byref(c), *map(ctypes.byref, n)), "dma_cache_bytes")
+    return tuple(x.value for x in n)
+
+
+def cache_kv(c, device):
+    """Arrays of the descriptor's pool in the element type: (kv, delta fp32), zero-filled."""
+    return (torch.zeros(c.num_pages, c.Hkv, c.page_size, 2, c.d, dtype=torch.bfloat16 if c.dtype == DMA_BF16 else torch.float32, device=device),
+            torch.zeros(c.num_pages, c.Hq, c.page_size, dtype=torch.float32, device=device))
+
+
+def _kv_pool(c, kv, delta, dt, dev):
+    keys = c.num_pages * c.page_size
+    return _flat("kv", kv, dt, keys * c.Hkv * 2 * c.d, dev), _flat("delta", delta, torch.float32, keys * c.Hq, dev)
+
+
+def dma_cache_append(c, K, V, slot, kv, delta, W_delta=None, A=None, delta_new=None, q=None, q_out=None, row_pos=None, row_prefix=None, prefix_len=None, inv_freq=None,
+                     interleaved=False, rot_scale=0.0):
+    """Writes the rows K, V [rows, Hkv, d] into their slots, K rotated by the rows' positions with the frequencies inv_freq [rot / 2] (None: as it is), with the dynamic
+    weights of V (W_delta [Hq, d], A [Hq]) or those given as delta_new [Hq, >= rows]. Returns q [rows, Hq, d] rotated (q_out: where, may be q itself), None without q. Tensors
+    of rows are taken in their own layout, whatever the descriptor's strides are."""
+    dev, rows, heads, kv_heads, d, dt, i32 = _here(), c.rows, c.Hq, c.Hkv, c.d, torch.bfloat16 if c.dtype == DMA_BF16 else torch.float32, torch.int32
+    given, ld, w, a = None, 0, None, None
+    if delta_new is not None:
+        given, ld = _by_head("delta_new", delta_new, heads, rows, dev)
+    elif W_delta is None or A is None:
+        raise ValueError("either W_delta and A or delta_new")
+    else:
+        w, a = _flat("W_delta", W_delta, torch.float32, heads * d, dev), _flat("A", A, torch.float32, heads, dev)
+    k, k_row, k_head = _rows("K", K, dt, rows, kv_heads, d, dev)
+    v, v_row, v_head = _rows("V", V, dt, rows, kv_heads, d, dev)
+    turn, pos, pre, length, npre = None, None, None, None, 0
+    if inv_freq is not None:
+        if row_pos is None or (row_prefix is None) != (prefix_len is None):
+            raise ValueError("a rotation takes row_pos, and row_prefix with prefix_len or neither")
+        turn = dma_rotation_t(_flat("inv_freq", inv_freq, torch.float32, 1, dev), 2 * inv_freq.numel(), int(interleaved), rot_scale)
+        pos = _flat("row_pos", row_pos, i32, rows, dev)
+        if row_prefix is not None:
+            pre, npre = _flat("row_prefix", row_prefix, i32, rows, dev), prefix_len.numel()
+            length = _flat("prefix_len", prefix_len, i32, npre, dev)
+    elif q is not None:
+        raise ValueError("q is taken to be rotated: inv_freq")
+    at, q_row, q_head, out, o_row, o_head = None, 0, 0, None, 0, 0
+    if q is not None:
+        at, q_row, q_head = _rows("q", q, dt, rows, heads, d, dev)
+        if q_out is None:
+            q_out = torch.empty(rows, heads, d, dtype=dt, device=q.device)
+        out, o_row, o_head = _rows("q_out", q_out, dt, rows, heads, d, dev)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    c = _with_strides(c, q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head)
+    _call("dma_cache_append", ctypes.byref(c), None if turn is None else ctypes.byref(turn), at, k, v, w, a, given, ld, _flat("slot", slot, i32, rows, dev), pos, pre, length, npre,
+          out, *_kv_pool(c, kv, delta, dt, dev), _stream())
+    return q_out
+
+
+def dma_prefix_order_workspace(c):
+    n = ctypes.c_size_t()
+    _check(lib().dma_prefix_order_workspace(ctypes.byref(c), ctypes.byref(n)), "dma_prefix_order_workspace")
+    return n.value
+
+
+def dma_prefix_order(c, delta, block_table, prefix_len, order_slot=None, order_weight=None, order_len=None, ws=None):
+    """The lists of c.nseq prefixes, for dma_cache_decode: (order_slot int32 [nseq, Hq, ld], order_weight fp32 [nseq, Hq, ld], order_len int32 [nseq])."""
+    dev, n, heads, i32 = _here(), c.nseq, c.Hq, torch.int32
+    ld = min(c.w, c.max_blocks * c.page_size)
+    if order_slot is None:
+        order_slot = torch.empty(n, heads, ld, dtype=i32, device=delta.device)
+    if order_weight is None:
+        order_weight = torch.empty_like(order_slot, dtype=torch.float32)
+    if order_len is None:
+        order_len = torch.empty(n, dtype=i32, device=delta.device)
+    slot, weight, length, ld = _order(n, heads, order_slot, order_weight, order_len, dev)
+    if ws is None:
+        ws = _ws(dma_prefix_order_workspace(c), delta.device)
+    _call("dma_prefix_order", ctypes.byref(c), _flat("delta", delta, torch.float32, c.num_pages * c.page_size * heads, dev), _table(c, block_table, dev),
+          _flat("prefix_len", prefix_len, i32, n, dev), slot, weight, ld, length, _flat("ws", ws, torch.uint8, 0, dev), ws.numel(), _stream())
+    return order_slot, order_weight, order_len
+
+
+def _order(n, heads, slot, weight, length, dev):
+    """Addresses of the lists, and the entries between two heads'."""
+    shape = slot.shape
+    if len(shape) != 3 or shape[0] < n or shape[1] != heads or weight.shape != shape:
+        raise ValueError(f"order: {tuple(shape)} and {tuple(weight.shape)} where two of [{n}, {heads}, entries] are taken")
+    return (_flat("order_slot", slot, torch.int32, 0, dev), _flat("order_weight", weight, torch.float32, 0, dev), _flat("order_len", length, torch.int32, n, dev), shape[2])
+
+
+def dma_cache_decode_workspace(c, nprefix=0):
+    n = ctypes.c_size_t()
+    _check(lib().dma_cache_decode_workspace(ctypes.byref(c), nprefix, ctypes.byref(n)), "dma_cache_decode_workspace")
+    return n.value
+
+
+def dma_cache_decode(c, q, kv, delta, block_table, row_seq, row_pos, row_prefix=None, order=None, o=None, lse=None, ws=None):
+    """One step over the pages for every row, behind the prefix row_prefix [rows] of those whose lists are given (order: what dma_prefix_order returned; None: no
+    prefixes); returns (o [rows, Hq, d], lse [rows, Hq]). q and o are taken in their own layout, whatever the descriptor's strides are."""
+    dev, rows, heads, d, dt, i32 = _here(), c.rows, c.Hq, c.d, torch.bfloat16 if c.dtype == DMA_BF16 else torch.float32, torch.int32
+    if (row_prefix is None) != (order is None):
+        raise ValueError("row_prefix and order go together")
+    if o is None:
+        o = torch.empty(rows, heads, d, dtype=dt, device=q.device)
+    if lse is None:
+        lse = torch.empty(rows, heads, dtype=torch.float32, device=q.device)
+    pre, npre, slot, weight, length, ld = None, 0, None, None, None, 0
+    if order is not None:
+        npre = order[0].shape[0]
+        slot, weight, length, ld = _order(npre, heads, *order, dev)
+        pre = _flat("row_prefix", row_prefix, i32, rows, dev)
+    if ws is None:
+        ws = _ws(dma_cache_decode_workspace(c, npre), q.device)
+    at, q_row, q_head = _rows("q", q, dt, rows, heads, d, dev)
+    out, o_row, o_head = _rows("o", o, dt, rows, heads, d, dev)
+    c = _with_strides(c, q_row, q_head, 0, 0, 0, 0, o_row, o_head)
+    _call("dma_cache_decode", ctypes.byref(c), at, *_kv_pool(c, kv, delta, dt, dev), _table(c, block_table, dev), _flat("row_seq", row_seq, i32, rows, dev),
+          _flat("row_pos", row_pos, i32, rows, dev), pre, npre, slot, weight, ld, length, out, _flat("lse", lse, torch.float32, rows * heads, dev),
+          _flat("ws", ws, torch.uint8, 0, dev), ws.numel(), _stream())
     return o, lse
 
 

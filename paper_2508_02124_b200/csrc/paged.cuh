@@ -1,4 +1,4 @@
-// The paged 4-bit cache (include/dma.h, dma_cache_t): resolved descriptor, launchers, addressing of pages and slots.
+// The paged caches (include/dma.h, dma_cache_t): resolved descriptor, launchers, addressing of pages and slots.
 #pragma once
 
 #include "common.cuh"
@@ -32,7 +32,25 @@ size_t cache4_decode_ws_bytes(const Cache& C);
 int launch_cache4_decode(const Cache& C, const void* q, const uint8_t* codes, const __nv_bfloat16* scales, const float* delta, const int32_t* table,
                          const int32_t* row_seq, const int32_t* row_pos, void* o, float* lse, void* ws, cudaStream_t st);
 
-// Key rows of the pool: row (page, head, place) of codes takes d bytes (K's codes, V's), of scales 2 d / 64 pairs of bf16.
+// dma_rotation_t with defaults resolved; no frequencies: nothing is rotated
+struct Rotation {
+    const float* inv_freq;
+    int rot, interleaved;
+    float scale;
+};
+int launch_cache_append(const Cache& C, const Rotation& rot, const void* q, const void* K, const void* V, const float* W, const float* A, const float* delta_new,
+                        int64_t delta_ld, const int32_t* slot, const int32_t* pos, const int32_t* prefix, const int32_t* prefix_len, int nprefix, void* q_out, void* kv,
+                        float* delta, cudaStream_t st);
+size_t prefix_order_ws_bytes(const Cache& C);              // of C.nseq prefixes
+int launch_prefix_order(const Cache& C, const float* delta, const int32_t* table, const int32_t* len, int32_t* slot, float* weight, int64_t order_ld, int32_t* order_len,
+                        void* ws, cudaStream_t st);
+size_t cache_decode_ws_bytes(const Cache& C, int nprefix);
+int launch_cache_decode(const Cache& C, const void* q, const void* kv, const float* delta, const int32_t* table, const int32_t* row_seq, const int32_t* row_pos,
+                        const int32_t* row_prefix, int nprefix, const int32_t* order_slot, const float* order_weight, int64_t order_ld, const int32_t* order_len,
+                        void* o, float* lse, void* ws, cudaStream_t st);
+
+// Key rows of the pool: row (page, head, place) of codes takes d bytes (K's codes, V's), of scales 2 d / 64 pairs of bf16; of a cache
+// in the element type 2 d elements.
 __device__ __forceinline__ size_t key_row(int page, int head, int place, int Hkv, int page_log) {
     return (((size_t)page * Hkv + head) << page_log) + place;
 }

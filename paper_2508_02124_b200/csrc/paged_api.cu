@@ -1,4 +1,5 @@
-// C-ABI entry points of the paged 4-bit cache (include/dma.h): argument validation, defaults, dispatch.
+// C-ABI entry points of the paged caches (include/dma.h): argument validation, defaults, dispatch.
+#include <algorithm>
 #include <cmath>
 
 #include "paged.cuh"
@@ -137,6 +138,104 @@ int dma_cache4_decode(const dma_cache_t* c, const void* q, const void* codes, co
     if ((rc = sm100())) return rc;
     return launch_cache4_decode(C, q, (const uint8_t*)codes, (const __nv_bfloat16*)scales, delta, block_table, row_seq, row_pos, o, lse, ws,
                                 (cudaStream_t)cuda_stream);
+}
+
+int dma_cache_bytes(const dma_cache_t* c, size_t* kv, size_t* delta) {
+    Cache C;
+    const int rc = resolve_cache(c, &C);
+    if (rc) return rc;
+    const size_t keys = (size_t)C.num_pages << C.page_log;
+    if (kv) *kv = keys * C.Hkv * 2 * C.d * (C.dtype == DMA_BF16 ? 2 : 4);
+    if (delta) *delta = keys * C.Hq * sizeof(float);
+    return DMA_OK;
+}
+
+int dma_cache_append(const dma_cache_t* c, const dma_rotation_t* rotation, const void* q, const void* K, const void* V, const float* W_delta,
+                     const float* A, const float* delta_new, int64_t delta_ld, const int32_t* slot, const int32_t* row_pos,
+                     const int32_t* row_prefix, const int32_t* prefix_len, int32_t nprefix, void* q_out, void* kv, float* delta, void* cuda_stream) {
+    Cache C;
+    int rc = resolve_cache(c, &C);
+    if (rc) return rc;
+    if (!K || !V || !slot || !kv || !delta || (!delta_new && (!W_delta || !A)) || (q == nullptr) != (q_out == nullptr)) return DMA_ERR_NULL;
+    Rotation rot = {};
+    if (rotation) {
+        if (!rotation->inv_freq || !row_pos || (row_prefix == nullptr) != (prefix_len == nullptr)) return DMA_ERR_NULL;
+        if (rotation->rot < 16 || rotation->rot > C.d || nprefix < 0 || !std::isfinite(rotation->scale)) return DMA_ERR_SHAPE;
+        if (rotation->rot % 16) return DMA_ERR_UNSUPPORTED;
+        rot = {rotation->inv_freq, rotation->rot, rotation->interleaved != 0, rotation->scale != 0.0f ? rotation->scale : 1.0f};
+    } else {
+        if (q) return DMA_ERR_UNSUPPORTED;
+        row_pos = row_prefix = prefix_len = nullptr;
+    }
+    if (q && q == q_out && C.rows * C.Hq > 1 && (C.qs[0] != C.os[0] || C.qs[1] != C.os[1])) return DMA_ERR_SHAPE;
+    if (!aligned(16, q, K, V, W_delta, q_out, kv, delta) || !aligned(4, A, delta_new, slot, rot.inv_freq, row_pos, row_prefix, prefix_len)) return DMA_ERR_ALIGN;
+    if (delta_new && delta_ld < C.rows) return DMA_ERR_SHAPE;
+    if ((rc = sm100())) return rc;
+    return launch_cache_append(C, rot, q, K, V, W_delta, A, delta_new, delta_ld, slot, row_pos, row_prefix, prefix_len, nprefix, q_out, kv, delta, (cudaStream_t)cuda_stream);
+}
+
+// A prefix' list and its sorted chunks are counted in 32 bits.
+static int resolve_order(const dma_cache_t* c, Cache* C) {
+    const int rc = resolve_cache(c, C);
+    if (rc) return rc;
+    const int64_t items = (int64_t)C->nseq * C->Hq;
+    if (items > INT32_MAX / 2 || items * ((((int64_t)C->max_blocks << C->page_log) + 4095) / 4096) > INT32_MAX) return DMA_ERR_SHAPE;
+    return DMA_OK;
+}
+
+int dma_prefix_order_workspace(const dma_cache_t* c, size_t* bytes) {
+    Cache C;
+    const int rc = resolve_order(c, &C);
+    if (rc) return rc;
+    if (!bytes) return DMA_ERR_NULL;
+    *bytes = prefix_order_ws_bytes(C);
+    return DMA_OK;
+}
+
+int dma_prefix_order(const dma_cache_t* c, const float* delta, const int32_t* block_table, const int32_t* prefix_len, int32_t* order_slot,
+                     float* order_weight, int64_t order_ld, int32_t* order_len, void* ws, size_t ws_bytes, void* cuda_stream) {
+    Cache C;
+    int rc = resolve_order(c, &C);
+    if (rc) return rc;
+    if (!delta || !block_table || !prefix_len || !order_slot || !order_weight || !order_len) return DMA_ERR_NULL;
+    if (!aligned(16, delta) || !aligned(4, block_table, prefix_len, order_slot, order_weight, order_len)) return DMA_ERR_ALIGN;
+    if (order_ld < std::min<int64_t>(C.w, (int64_t)C.max_blocks << C.page_log)) return DMA_ERR_SHAPE;
+    if (!ws || ws_bytes < prefix_order_ws_bytes(C) || !aligned(16, ws)) return DMA_ERR_WORKSPACE;
+    if ((rc = sm100())) return rc;
+    return launch_prefix_order(C, delta, block_table, prefix_len, order_slot, order_weight, order_ld, order_len, ws, (cudaStream_t)cuda_stream);
+}
+
+// CTAs are counted in 32 bits.
+static int resolve_decode(const dma_cache_t* c, int32_t nprefix, Cache* C) {
+    const int rc = resolve_cache(c, C);
+    if (rc) return rc;
+    return nprefix < 0 || nprefix > (1 << 30) ? DMA_ERR_SHAPE : DMA_OK;
+}
+
+int dma_cache_decode_workspace(const dma_cache_t* c, int32_t nprefix, size_t* bytes) {
+    Cache C;
+    const int rc = resolve_decode(c, nprefix, &C);
+    if (rc) return rc;
+    if (!bytes) return DMA_ERR_NULL;
+    *bytes = cache_decode_ws_bytes(C, nprefix);
+    return DMA_OK;
+}
+
+int dma_cache_decode(const dma_cache_t* c, const void* q, const void* kv, const float* delta, const int32_t* block_table, const int32_t* row_seq,
+                     const int32_t* row_pos, const int32_t* row_prefix, int32_t nprefix, const int32_t* order_slot, const float* order_weight,
+                     int64_t order_ld, const int32_t* order_len, void* o, float* lse, void* ws, size_t ws_bytes, void* cuda_stream) {
+    Cache C;
+    int rc = resolve_decode(c, nprefix, &C);
+    if (rc) return rc;
+    if (!q || !kv || !delta || !block_table || !row_seq || !row_pos || !o || !lse) return DMA_ERR_NULL;
+    if (nprefix > 0 && (!row_prefix || !order_slot || !order_weight || !order_len)) return DMA_ERR_NULL;
+    if (!aligned(16, q, kv, delta, o) || !aligned(4, block_table, row_seq, row_pos, lse)) return DMA_ERR_ALIGN;
+    if (nprefix > 0 && !aligned(4, row_prefix, order_slot, order_weight, order_len)) return DMA_ERR_ALIGN;
+    if (nprefix > 0 && order_ld < 1) return DMA_ERR_SHAPE;
+    if (!ws || ws_bytes < cache_decode_ws_bytes(C, nprefix) || !aligned(16, ws)) return DMA_ERR_WORKSPACE;
+    if ((rc = sm100())) return rc;
+    return launch_cache_decode(C, q, kv, delta, block_table, row_seq, row_pos, row_prefix, nprefix, order_slot, order_weight, order_ld, order_len, o, lse, ws,
+                               (cudaStream_t)cuda_stream);
 }
 
 }  // extern "C"
