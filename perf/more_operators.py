@@ -213,7 +213,7 @@ def prepare(case, seed):
                                num_pages=s["pages"], max_blocks=s["table"].shape[1])
             s["ws"] = workspace(dma.dma_cache_decode_workspace(s["c"], case["n"]))
             if not case["first"]:
-                dma.dma_prefix_order(s["cp"], s["delta"], s["prefix_table"], s["lens"], *s["order"], ws=s["wsp"])
+                s["order"] = dma.dma_prefix_order(s["cp"], s["delta"], s["prefix_table"], s["lens"], ws=s["wsp"])
     return s
 
 
