@@ -115,8 +115,9 @@ __global__ void __launch_bounds__(256) simt_sum_kernel(DecodeArgs A) {
 struct Layout {
     size_t cut, piece, first, members, tiles, ntiles, total;
     int pieces, tile_rows, max_tiles;
+    bool simt;
     Layout(const Cache& C, int nprefix) {
-        const bool simt = true;
+        simt = C.dtype != DMA_BF16 || (C.flags & DMA_FLAG_SIMT);
         tile_rows = simt ? kWarps : 128;
         pieces = simt ? 1 + kSplits : 1;
         max_tiles = (int)std::min<int64_t>(C.rows, (int64_t)nprefix + C.rows / tile_rows);
@@ -157,7 +158,7 @@ int launch_cache_decode(const Cache& C, const void* q, const void* kv, const flo
                           L.pieces, (int*)(p + L.first), (int*)(p + L.members), (int4*)(p + L.tiles), (int*)(p + L.ntiles), L.tile_rows};
     const int rc = launch_own_keys(C, A, st);
     if (rc || nprefix == 0) return rc;
-    return launch_prefix_simt(C, A, L.max_tiles, st);
+    return L.simt ? launch_prefix_simt(C, A, L.max_tiles, st) : launch_prefix_tc(C, A, L.max_tiles, st);
 }
 
 }  // namespace dma

@@ -45,7 +45,8 @@ struct DecodeArgs {
 
 // Attention over the rows' own keys, and what each keeps of its prefix: the row's last part where it has no prefix, else its first piece.
 int launch_own_keys(const Cache& C, const DecodeArgs& A, cudaStream_t st);
-// Attention over the prefixes and the sum of the pieces
+// Attention over the prefixes and the sum of the pieces; on the tensor cores tiles of 128 rows and one piece
 int launch_prefix_simt(const Cache& C, const DecodeArgs& A, int max_tiles, cudaStream_t st);
+int launch_prefix_tc(const Cache& C, const DecodeArgs& A, int max_tiles, cudaStream_t st);
 
 }  // namespace dma
