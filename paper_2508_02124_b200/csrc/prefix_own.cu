@@ -5,6 +5,7 @@
 // keys, a bisection over their order keys between the weights around the cut. Where the list has w entries, own keys that do not exceed its last cannot be kept and are left out
 // at once: of n own keys behind a prefix of N about n w / N remain. They lie in shared memory, where every count is a sweep by one warp.
 #include <algorithm>
+#include <type_traits>
 
 #include "cache4_decode.cuh"
 #include "delta_fixed.cuh"
@@ -18,10 +19,9 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 
 // A team of 1, 2, 4 or 8 warps has a (row, head), each warp a part of the own keys.
 struct OwnShared {
-    uint64_t full[kWarps];
-    int part[2][kWarps], seen[kWarps], cands[kWarps];
-    float m[kWarps], l[kWarps];
-    int abort_flag, drain_flag;
+    unsigned long long least[kWarps];
+    int part[2][kWarps], cands[kWarps], cut[kWarps];
+    float m[kWarps], l[kWarps], all_m[kWarps][8], all_l[kWarps][8];
 };
 
 __device__ __forceinline__ void team_sync(int id, int threads) {
@@ -32,9 +32,6 @@ __device__ __forceinline__ float warp_max(float x) {              // (NaN only w
     float y;
     asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
     return y;
-}
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(ptx::smem_u32(bar)) : "memory");
 }
 template <bool kTrans>
 __device__ __forceinline__ void ldmatrix(uint32_t (&r)[4], uint32_t addr) {
@@ -188,26 +185,128 @@ struct Attend<__nv_bfloat16, D> {
     }
 };
 
-__device__ void group_rows(const DecodeArgs& A) {
-    __shared__ int part[kWarps], tile_part[kWarps], turn[kThreads];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    auto prefix_of = [&](int t) {
-        int r, n;
-        return A.own(t, r) < 0 ? -1 : A.listed(t, n);
-    };
+// All of a group's heads, up to eight, over the same keys (bf16): S = Q K^T and O = P V with the heads as the rows 0-7, and in the rows 8-15 what p leaves when it is rounded.
+template <int D>
+struct AttendAll {
+    static constexpr int kStage = 16, kPitch = 2 * D * 2 + 16;
+    uint32_t q[D / 16][2];
+    float acc[D / 8][4], m = -INFINITY, l = 0.0f, c1;              // of row lane / 4; m in log2 units
+    __device__ __forceinline__ void start(const __nv_bfloat16* row, bool real, float scale, int lane) {
+        c1 = scale * 1.4426950408889634f;
+#pragma unroll
+        for (int x = 0; x < D / 8; ++x)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) acc[x][y] = 0.0f;
+#pragma unroll
+        for (int x = 0; x < D / 16; ++x)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) q[x][y] = real ? *reinterpret_cast<const uint32_t*>(row + x * 16 + y * 8 + (lane & 3) * 2) : 0u;
+    }
+    // bias: of the lane's head, for the keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9 with c = lane % 4
+    __device__ __forceinline__ void stage(uint8_t* keys, const float (&bias)[4], int count, int lane) {
+        if (count < kStage) {                                     // (0 times what lies there must be 0)
+            for (int i = count * (D / 8) + lane; i < kStage * (D / 8); i += 32) *reinterpret_cast<uint4*>(keys + i / (D / 8) * kPitch + D * 2 + i % (D / 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            __syncwarp();
+        }
+        const uint32_t base = ptx::smem_u32(keys), at_k = base + ((lane & 7) + (lane >> 4) * 8) * kPitch + ((lane >> 3) & 1) * 16;
+        const uint32_t at_v = base + ((lane & 7) + ((lane >> 3) & 1) * 8) * kPitch + D * 2 + (lane >> 4) * 16;
+        float s[2][4] = {};
+#pragma unroll
+        for (int x = 0; x < D / 16; ++x) {
+            uint32_t b[4];
+            ldmatrix<false>(b, at_k + x * 32);
+            const uint32_t a[4] = {q[x][0], 0u, q[x][1], 0u};
+            mma_16816(s[0], a, b[0], b[1]);
+            mma_16816(s[1], a, b[2], b[3]);
+        }
+        float x[4], top = m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int e = (lane & 3) * 2 + (i >> 1) * 8 + (i & 1);
+            x[i] = e < count ? fmaf(s[i >> 1][i & 1], c1, bias[i] * 1.4426950408889634f) : -INFINITY;
+            top = fmaxf(top, x[i]);
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        if (__any_sync(0xffffffffu, top > m)) {
+            const float fade = m == -INFINITY ? 1.0f : ptx::ex2(m - top);
+            l *= fade;
+#pragma unroll
+            for (int y = 0; y < D / 8; ++y)
+#pragma unroll
+                for (int z = 0; z < 4; ++z) acc[y][z] *= fade;
+            m = top;
+        }
+        const float ref = m == -INFINITY ? 0.0f : m;
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            p[i] = ptx::ex2(x[i] - ref);
+            l += p[i];
+        }
+        const uint32_t h0 = ptx::pack_bf16(p[0], p[1]), h1 = ptx::pack_bf16(p[2], p[3]);
+        const uint32_t a[4] = {h0, ptx::pack_bf16(p[0] - __uint_as_float(h0 << 16), p[1] - __uint_as_float(h0 & 0xffff0000u)),
+                               h1, ptx::pack_bf16(p[2] - __uint_as_float(h1 << 16), p[3] - __uint_as_float(h1 & 0xffff0000u))};
+#pragma unroll
+        for (int y = 0; y < D / 16; ++y) {
+            uint32_t b[4];
+            ldmatrix<true>(b, at_v + y * 32);
+            mma_16816(acc[2 * y], a, b[0], b[1]);
+            mma_16816(acc[2 * y + 1], a, b[2], b[3]);
+        }
+    }
+    // o [8][D] to shared memory; (m, l) of the lane's head, natural units
+    __device__ __forceinline__ void end(float* o, int lane) {
+        l += __shfl_xor_sync(0xffffffffu, l, 1);
+        l += __shfl_xor_sync(0xffffffffu, l, 2);
+        m = m == -INFINITY ? m : m * 0.6931471805599453f;
+#pragma unroll
+        for (int y = 0; y < D / 8; ++y)
+#pragma unroll
+            for (int z = 0; z < 2; ++z)                           // (an infinite value's second part is not a number)
+                o[(lane >> 2) * D + y * 8 + (lane & 3) * 2 + z] = isfinite(acc[y][z]) ? acc[y][z] + acc[y][z + 2] : acc[y][z];
+    }
+};
+
+// The rows by prefix, in the order of rows, and tiles of them.
+__device__ void group_rows(const DecodeArgs& A, int* turn) {       // turn: kTogether per thread
+    constexpr int kTogether = 4;                                  // rows of a thread requested together
+    __shared__ int part[kWarps], tile_part[kWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x;
     if (A.nprefix == 0) {
         if (tid == 0) *A.ntiles = 0;
         return;
     }
-    for (int i = tid; i <= A.nprefix; i += kThreads) A.first[i] = 0;
+    // f(row, its prefix or -1) for kTogether rows at a time, thread by thread
+    auto turns = [&](auto f) {
+        for (int b = 0; b < A.rows; b += threads * kTogether) {
+            int r[kTogether], g[kTogether], n[kTogether];
+#pragma unroll
+            for (int i = 0; i < kTogether; ++i) {
+                const int t = b + i * threads + tid;
+                r[i] = g[i] = -1;
+                if (t < A.rows) { r[i] = A.seq[t]; g[i] = A.prefix[t]; }
+            }
+#pragma unroll
+            for (int i = 0; i < kTogether; ++i) {
+                if ((unsigned)r[i] >= (unsigned)A.nseq || (unsigned)g[i] >= (unsigned)A.nprefix) g[i] = -1;
+                n[i] = g[i] >= 0 ? A.order_len[g[i]] : 0;
+            }
+#pragma unroll
+            for (int i = 0; i < kTogether; ++i) g[i] = n[i] > 0 ? g[i] : -1;
+            f(b, g);
+        }
+    };
+    for (int i = tid; i <= A.nprefix; i += threads) A.first[i] = 0;
     __syncthreads();
-    for (int t = tid; t < A.rows; t += kThreads) {
-        const int g = prefix_of(t);
-        if (g >= 0) atomicAdd(&A.first[g], 1);
-    }
+    turns([&](int, const int (&g)[kTogether]) {
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i)
+            if (g[i] >= 0) atomicAdd(&A.first[g[i]], 1);
+    });
     __syncthreads();
     int row_carry = 0, tile_carry = 0;
-    for (int b = 0; b < A.nprefix; b += kThreads) {
+    for (int b = 0; b < A.nprefix; b += threads) {
         const int g = b + tid, n = g < A.nprefix ? __ldcg(&A.first[g]) : 0, nt = (n + A.tile_rows - 1) / A.tile_rows;
         int x = n, y = nt;
 #pragma unroll
@@ -218,7 +317,7 @@ __device__ void group_rows(const DecodeArgs& A) {
         if (lane == 31) { part[warp] = x; tile_part[warp] = y; }
         __syncthreads();
         int before = 0, tiles_before = 0, all = 0, all_tiles = 0;
-        for (int i = 0; i < kWarps; ++i) {
+        for (int i = 0; i < threads / 32; ++i) {
             before += i < warp ? part[i] : 0;
             tiles_before += i < warp ? tile_part[i] : 0;
             all += part[i];
@@ -235,207 +334,319 @@ __device__ void group_rows(const DecodeArgs& A) {
         __syncthreads();
     }
     if (tid == 0) *A.ntiles = tile_carry;
-    // in the order of rows: a turn's rows of the same prefix follow one another, the first of them moves the prefix' start on
-    for (int b = 0; b < A.rows; b += kThreads) {
-        const int t = b + tid, g = t < A.rows ? prefix_of(t) : -1;
-        turn[tid] = g;
+    // a turn's rows of the same prefix follow one another, the first of them moves the prefix' start on
+    turns([&](int b, const int (&g)[kTogether]) {
+        const int count = min(A.rows - b, threads * kTogether);
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i) turn[i * threads + tid] = g[i];
         __syncthreads();
-        int rank = 0, same = 0;
-        if (g >= 0)
-            for (int i = 0; i < kThreads; ++i) {
-                same += turn[i] == g;
-                rank += turn[i] == g && i < tid;
+        int rank[kTogether] = {}, same[kTogether] = {}, start[kTogether];
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i) start[i] = g[i] >= 0 ? __ldcg(&A.first[g[i]]) : 0;
+        for (int e = 0; e < count; ++e) {
+            const int x = turn[e];
+#pragma unroll
+            for (int i = 0; i < kTogether; ++i) {
+                same[i] += x == g[i];
+                rank[i] += x == g[i] && e < i * threads + tid;
             }
-        int start = 0;
-        if (g >= 0) start = __ldcg(&A.first[g]);
-        __syncthreads();
-        if (g >= 0) {
-            A.members[start + rank] = t;
-            if (rank == 0) __stcg(&A.first[g], start + same);
         }
         __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i)
+            if (g[i] >= 0) {
+                A.members[start[i] + rank[i]] = b + i * threads + tid;
+                if (rank[i] == 0) __stcg(&A.first[g[i]], start[i] + same[i]);
+            }
+        __syncthreads();
+    });
+}
+
+// R * 32 numbers of a warp in descending order, number i * 32 + lane in v[i].
+template <int R>
+__device__ __forceinline__ void sort_down(uint32_t (&v)[R], int lane) {
+    auto lanes = [&](int k, int j) {                              // pairs that j < 32 lanes part, in runs of k
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const uint32_t o = __shfl_xor_sync(0xffffffffu, v[i], j);
+            const bool up = ((lane & j) == 0) == (((i * 32 + lane) & k) == 0);
+            v[i] = up ? max(v[i], o) : min(v[i], o);
+        }
+    };
+#pragma unroll 1
+    for (int k = 2; k <= 32; k *= 2)
+#pragma unroll 1
+        for (int j = k / 2; j > 0; j /= 2) lanes(k, j);
+#pragma unroll
+    for (int k = 64; k <= 32 * R; k *= 2) {
+#pragma unroll
+        for (int j = k / 2; j >= 32; j /= 2)
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                if (!(i & (j / 32))) {
+                    const int o = i | (j / 32);
+                    const uint32_t a = v[i], b = v[o];
+                    const bool down = ((i * 32) & k) == 0;
+                    v[i] = down ? max(a, b) : min(a, b);
+                    v[o] = down ? min(a, b) : max(a, b);
+                }
+#pragma unroll 1
+        for (int j = 16; j > 0; j /= 2) lanes(k, j);
     }
 }
 
-// One CTA per kWarps / team (row, head)s; the last one groups the rows by prefix.
+// The sums of a row's own keys, D / 32 channels per lane: its piece, or its result where there is no prefix.
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int team, int room) {
-    constexpr int kBatch = 4, kHeld = 4;                          // 128 keys each, requested together; candidates, and entries of the order, that a lane holds
+__device__ __forceinline__ void write_own(const DecodeArgs& A, int t, int h, bool behind, int cut, float top, float sum, const float (&o)[D / 32], int lane) {
+    if (behind) {
+        float* out = A.piece_of(t, h, 0, D);
+#pragma unroll
+        for (int x = 0; x < D / 32; ++x) out[2 + lane + 32 * x] = o[x];
+        if (lane == 0) {
+            out[0] = top;
+            out[1] = sum;
+            A.cut[t * A.Hq + h] = cut;
+        }
+    } else {
+        T* out = (T*)A.o + t * A.os_row + h * A.os_head;
+#pragma unroll
+        for (int x = 0; x < D / 32; ++x) store_as(out + lane + 32 * x, sum == 0.0f ? 0.0f : o[x] / sum);
+        if (lane == 0) A.lse[t * A.Hq + h] = sum == 0.0f ? -INFINITY : top + logf(sum);
+    }
+}
+
+// A CTA per (row, KV head); the last one groups the rows by prefix. The group's heads each have a warp or a team of them (kTeams; else up to eight heads at a time, the others
+// in turn). Where a row keeps all keys whatever their weights, the warps share its own keys, all heads together.
+template <typename T, int D, bool kTeams>
+__global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warps_per_head, int room) {
     using At = Attend<T, D>;
-    extern __shared__ __align__(16) uint8_t dynamic[];            // [kWarps][At::kStage][At::kPitch] keys, [kWarps][room]: (pattern of delta, position), then (delta, slot) of the kept ones
+    extern __shared__ __align__(16) uint8_t dynamic[];            // of each warp [At::kStage][At::kPitch] keys, [room]: (pattern of delta, slot) of candidates by position, then of the kept ones
     __shared__ OwnShared S;
-    __shared__ float sO[kWarps][D];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid < kWarps) ptx::mbar_init(&S.full[tid], 1);
-    if (tid == 0) S.abort_flag = S.drain_flag = 0;
-    ptx::fence_barrier_init();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x / 32, team = kTeams ? warps_per_head : 1;
     pdl_enter(A.q, A.kv, A.delta, A.table, A.seq, A.pos, A.prefix, A.order_slot, A.order_len, A.order_weight, A.o, A.lse, A.status, A.cut, A.piece, A.first, A.members, A.tiles, A.ntiles);
-    __syncthreads();
     if (blockIdx.x == gridDim.x - 1) {
         if (tid < kWsHeaderBytes / 4) A.status[tid] = 0;
-        group_rows(A);
+        group_rows(A, reinterpret_cast<int*>(dynamic));
         return;
     }
-    const int in_team = warp % team, leader = warp - in_team, teams = kWarps / team, bar = 1 + warp / team;
-    const int64_t item = (int64_t)blockIdx.x * teams + warp / team;
-    if (item >= (int64_t)A.rows * A.Hq) return;                   // (a team's barrier counts its own warps only)
-    const int t = (int)(item / A.Hq), h = (int)(item % A.Hq), hk = h / A.G;
+    const int t = blockIdx.x / A.Hkv, hk = blockIdx.x % A.Hkv;
     const int r = A.seq[t], p = A.pos[t], g = A.nprefix ? A.prefix[t] : -1;
     if ((unsigned)r >= (unsigned)A.nseq) return;
     const int n = min(max(p, -1), (A.max_blocks << A.page_log) - 1) + 1;
     const int32_t* pages = A.table + r * A.ld;
-    const int mask = (1 << A.page_log) - 1, seg = (n + team * 128 - 1) / (team * 128) * 128, j0 = min(n, in_team * seg), j1 = min(n, j0 + seg);
+    const int mask = (1 << A.page_log) - 1;
     const T* kv = (const T*)A.kv;
-    uint8_t* keys_at = dynamic + warp * (At::kStage * At::kPitch);
-    uint2* found = reinterpret_cast<uint2*>(dynamic + kWarps * (At::kStage * At::kPitch));
-    uint2* mine = found + warp * room;
-    auto page_of = [&](int j) {                                   // -1: outside the pool, or no key
-        int page = j < j1 ? pages[j >> A.page_log] : -1;
-        return (unsigned)page < (unsigned)A.num_pages ? page : -1;
-    };
-    auto delta_at = [&](int page, int j) { return A.delta + (((size_t)page * A.Hq + h) << A.page_log) + (j & mask); };
-    // f(position, page, pattern, is a key) for the part's keys, four side by side per lane (in one page, since pages have 16 keys and more)
-    auto sweep = [&](auto f) {
-        int page[kBatch], next[kBatch];
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) next[i] = page_of(j0 + 128 * i + 4 * lane);
-#pragma unroll 1
-        for (int b = j0; b < j1; b += 128 * kBatch) {
-            uint4 u[kBatch];
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                page[i] = next[i];
-                if (page[i] >= 0) u[i] = *reinterpret_cast<const uint4*>(delta_at(page[i], b + 128 * i + 4 * lane));
-            }
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) next[i] = page_of(b + 128 * (kBatch + i) + 4 * lane);
-            f(b, page, u);
-        }
-    };
+    constexpr int kStageBytes = At::kStage * At::kPitch;
+    uint8_t* keys_at = dynamic + warp * kStageBytes;
     int listed = 0;
     if ((unsigned)g < (unsigned)A.nprefix) listed = (int)max((int64_t)0, min((int64_t)min(A.order_len[g], A.w), A.order_ld));
     const bool behind = listed > 0, floored = listed == A.w;      // (as DecodeArgs::listed)
-    const float* weight = A.order_weight + ((int64_t)g * A.Hq + h) * A.order_ld;
-    // the last entries of the order, from the end on
-    uint32_t held[kHeld];
+    constexpr int kParts = 2 * D * (int)sizeof(T) / 16, kTogether = kParts < 32 ? 32 / kParts : 1;       // 16-byte parts of a key, keys per instruction
+
+    if constexpr (sizeof(T) == 2) {
+        if ((int64_t)listed + n <= A.w) {
+            for (int g0 = 0; g0 < A.G; g0 += 8) {
+                const int mine = g0 + (lane >> 2), h = hk * A.G + mine;
+                const bool real = mine < A.G;
+                AttendAll<D> at;
+                at.start((const T*)A.q + t * A.qs_row + h * A.qs_head, real, A.scale, lane);
+                // 16 keys at a time, side by side in one page, turn by turn of the warps
+                int next = warp * 16 < n ? pages[warp * 16 >> A.page_log] : -1;
+#pragma unroll 1
+                for (int j = warp * 16; j < n; j += warps * 16) {
+                    const int page = next, count = min(n - j, 16);
+                    next = j + warps * 16 < n ? pages[(j + warps * 16) >> A.page_log] : -1;
+                    if ((unsigned)page >= (unsigned)A.num_pages) continue;
+                    const uint8_t* from = (const uint8_t*)(kv + key_row(page, hk, j & mask, A.Hkv, A.page_log) * (2 * D));
+                    const uint32_t to = ptx::smem_u32(keys_at);
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) held[i] = listed - 1 - 32 * i - lane >= 0 ? __float_as_uint(weight[listed - 1 - 32 * i - lane]) & 0x7FFFFFFFu : 0u;
-    const uint32_t floor = __shfl_sync(0xffffffffu, held[0], 0);
-    auto word = [](const uint4& u, int x) { return (x == 0 ? u.x : x == 1 ? u.y : x == 2 ? u.z : u.w) & 0x7FFFFFFFu; };
-    // what may be kept
-    int c = 0, seen = 0;
-    sweep([&](int b, const int (&page)[kBatch], const uint4 (&u)[kBatch]) {
-        uint32_t flags = 0;
+                    for (int i = lane; i < 16 * kParts; i += 32)
+                        if (i / kParts < count) ptx::cp_async16_at(to + i / kParts * At::kPitch + i % kParts * 16, from + i * 16);
+                    float bias[4] = {};
+                    const float* delta = A.delta + (((size_t)page * A.Hq + h) << A.page_log) + (j & mask) + (lane & 3) * 2;
+                    if (real) {
+                        const float2 u = *reinterpret_cast<const float2*>(delta), v = *reinterpret_cast<const float2*>(delta + 8);
+                        bias[0] = u.x; bias[1] = u.y; bias[2] = v.x; bias[3] = v.y;
+                    }
+                    ptx::cp_async_wait_all();
+                    __syncwarp();
+                    at.stage(keys_at, bias, count, lane);
+                    __syncwarp();
+                }
+                float* o = reinterpret_cast<float*>(keys_at);     // [8][D]
+                at.end(o, lane);
+                if ((lane & 3) == 0) {
+                    S.all_m[warp][lane >> 2] = at.m;
+                    S.all_l[warp][lane >> 2] = at.l;
+                }
+                __syncthreads();
+                for (int y = warp; y < min(8, A.G - g0); y += warps) {
+                    const int head = hk * A.G + g0 + y;
+                    float top = -INFINITY, sum = 0.0f, out[D / 32] = {};
+                    for (int w = 0; w < warps; ++w) top = fmaxf(top, S.all_m[w][y]);
+                    for (int w = 0; w < warps; ++w) {
+                        const float wm = S.all_m[w][y], wl = S.all_l[w][y], f = wm == -INFINITY ? (wl == 0.0f ? 0.0f : 1.0f) : expf(wm - top);
+                        if (f == 0.0f) continue;
+                        sum += wl * f;
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const bool there = page[i] >= 0 && b + 128 * i + 4 * lane + x < j1;
-                seen += there;
-                flags |= (uint32_t)(there && (!floored || word(u[i], x) > floor)) << (4 * i + x);
+                        for (int x = 0; x < D / 32; ++x) out[x] += reinterpret_cast<const float*>(dynamic + w * kStageBytes)[y * D + lane + 32 * x] * f;
+                    }
+                    write_own<T, D>(A, t, head, behind, listed, top, sum, out, lane);
+                }
+                __syncthreads();
             }
-        const int mine_count = __popc(flags);
-        int at = mine_count;
+            return;
+        }
+    }
+    const int in_team = kTeams ? warp % team : 0, leader = warp - in_team, bar = 1 + warp / team;
+    uint2* found = reinterpret_cast<uint2*>(dynamic + warps * kStageBytes);
+    uint2* mine = found + warp * room;
+    const int seg = (n + team * 64 - 1) / (team * 64) * 64, j0 = min(n, in_team * seg), j1 = min(n, j0 + seg);
+#pragma unroll 1
+    for (int head = warp / team; head < A.G; head += warps / team) {
+    const int h = hk * A.G + head;
+    const float* weight = A.order_weight + ((int64_t)g * A.Hq + h) * A.order_ld;
+    // f(position, slot, patterns) for the part's keys, 512 at a time: a lane has 16 of them, side by side in one page (pages have 16 keys and more). Patterns of places without a key: -2
+    auto sweep = [&](auto f) {
+        auto page_of = [&](int j) { return j < j1 ? pages[j >> A.page_log] : -1; };
+        int next = page_of(j0 + 16 * lane);
+#pragma unroll 1
+        for (int b = j0; b < j1; b += 512) {
+            const int j = b + 16 * lane, page = next, slot = (page << A.page_log) + (j & mask);
+            const bool there = (unsigned)page < (unsigned)A.num_pages;
+            int u[16];
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                int4 x = make_int4(-2, -2, -2, -2);
+                if (there) x = *reinterpret_cast<const int4*>(A.delta + (((size_t)page * A.Hq + h) << A.page_log) + (j & mask) + i);
+                u[i] = x.x; u[i + 1] = x.y; u[i + 2] = x.z; u[i + 3] = x.w;
+            }
+            next = page_of(j + 512);
+            if (b + 512 > j1)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) u[i] = j + i < j1 ? u[i] : -2;
+            f(j, slot, u);
+        }
+    };
+    At at;
+    at.start((const T*)A.q + t * A.qs_row + h * A.qs_head, A.scale, lane);
+    // what may be kept: every key that there is, or those above the list's last entry
+    const int floor = floored ? __float_as_int(weight[listed - 1]) & 0x7FFFFFFF : -1;
+    int c = 0;
+    sweep([&](int, int slot, const int (&u)[16]) {
+        int count = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) count += u[i] > floor;
+        int to = count;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, at, o);
-            if (lane >= o) at += y;
+            const int y = __shfl_up_sync(0xffffffffu, to, o);
+            if (lane >= o) to += y;
         }
-        const int total = __shfl_sync(0xffffffffu, at, 31);
-        at += c - mine_count;
+        const int total = __shfl_sync(0xffffffffu, to, 31);
+        to += c - count;
+        if (to + count <= room) {
 #pragma unroll
-        for (int i = 0; i < 4 * kBatch; ++i)
-            if (flags >> i & 1u) {
-                if (at < room) mine[at] = make_uint2(word(u[i / 4], i % 4), b + 128 * (i / 4) + 4 * lane + i % 4);
-                ++at;
-            }
+            for (int i = 0; i < 16; ++i)
+                if (u[i] > floor) mine[to++] = make_uint2((uint32_t)u[i], (uint32_t)(slot + i));
+        }
         c += total;
     });
-    seen = __reduce_add_sync(0xffffffffu, seen);
-    const bool over = c > room;
+    if (lane == 0) S.cands[warp] = c;
     __syncwarp();
-    int own = seen, cands = c, most = c, step = 0;
+    int cands = c, most = c, step = 0;
     if (team > 1) {
-        if (lane == 0) { S.seen[warp] = seen; S.cands[warp] = c; }
         team_sync(bar, team * 32);
-        own = cands = most = 0;
+        cands = most = 0;
         for (int i = 0; i < team; ++i) {
-            own += S.seen[leader + i];
             cands += S.cands[leader + i];
             most = max(most, S.cands[leader + i]);
         }
     }
-    auto team_sum = [&](int x) {
-        x = __reduce_add_sync(0xffffffffu, x);
-        if (team > 1) {
-            if (lane == 0) S.part[step & 1][warp] = x;
-            team_sync(bar, team * 32);
-            x = 0;
-            for (int i = 0; i < team; ++i) x += S.part[step & 1][leader + i];
-            ++step;
-        }
-        return x;
-    };
-    const int k = (int)min((int64_t)A.w, (int64_t)listed + own);
+    const bool over = most > room;                                // (of the whole team: keys are then told apart by position, else by their place in the list)
+    // keys that the row sees: all own ones are candidates where the list may not be full
+    const int k = floored ? listed : (int)min((int64_t)A.w, (int64_t)listed + cands);
     int cut = listed;
-    unsigned long long least = 0;
-    if (k < listed + own) {
-        unsigned long long keys[kHeld];
+    unsigned long long least = 0;                                 // kept: the order keys that are not below
+    auto place = [&](int e) { return in_team * (1 << 20) + e; };
+    if (k < listed + cands) {
+        constexpr int kSorted = 256;
+        if (!over && cands <= kSorted) {
+            // The best own key is kept if the list's last entry is below it, the second if the last but one is, and so on: the own keys in descending order against the list from its end on
+            // (the k - listed best ones are kept anyway). By the team's first warp.
+            if (in_team == 0) {
+                auto match = [&](auto r_tag) {
+                    constexpr int R = decltype(r_tag)::value;
+                    uint32_t v[R], w[R];
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) keys[i] = !over && 32 * i + lane < c ? order_key(mine[32 * i + lane].x, (int)mine[32 * i + lane].y) : 0ull;
-        if (most <= 32 * kHeld && most <= room && cands <= 32 * kHeld) {
-            // Few candidates: each against all, and against as many of the last entries. One is kept if fewer than k keys come before it; of the prefix' those that are not below it, and
-            // all entries further up are at most another reason to keep it.
-            int before[kHeld];
-#pragma unroll
-            for (int i = 0; i < kHeld; ++i) before[i] = listed;
-            for (int w = leader; w < leader + team; ++w) {
-                const uint2* f = found + w * room;
-                const int count = w == warp ? c : S.cands[w];
-                for (int e = 0; e < count; ++e) {
-                    const uint2 o = f[e];
-                    const unsigned long long x = order_key(o.x, (int)o.y);
-#pragma unroll
-                    for (int i = 0; i < kHeld; ++i) before[i] += x > keys[i];
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < kHeld; ++i)
-                if (32 * i < cands) {
-                    const int end = min(32, min(cands, listed) - 32 * i);
-                    for (int e = 0; e < end; ++e) {
-                        const uint32_t x = __shfl_sync(0xffffffffu, held[i], e);
-#pragma unroll
-                        for (int y = 0; y < kHeld; ++y) before[y] -= x < (uint32_t)(keys[y] >> 32);
+                    for (int i = 0; i < R; ++i) {
+                        const int back = i * 32 + lane - (k - listed);       // in the list, from its end on
+                        w[i] = back < 0 ? 0u : back < listed ? (__float_as_uint(weight[listed - 1 - back]) & 0x7FFFFFFFu) + 1u : ~0u;
+                        v[i] = 0u;                                // (patterns plus one: 0 is none)
                     }
-                }
-            // the kept ones to the front of the warp's part
-            int kept = 0;
-            team_sync(bar, team * 32);                            // (all have read)
+                    if (team == 1) {
 #pragma unroll
-            for (int i = 0; i < kHeld; ++i) {
-                const bool keep = 32 * i + lane < c && before[i] < k;
-                const uint32_t bits = __ballot_sync(0xffffffffu, keep);
-                const uint2 o = keep ? mine[32 * i + lane] : make_uint2(0u, 0u);
-                __syncwarp();
-                if (keep) mine[kept + __popc(bits & ((1u << lane) - 1u))] = o;
-                kept += __popc(bits);
-                __syncwarp();
+                        for (int i = 0; i < R; ++i)
+                            if (i * 32 + lane < c) v[i] = mine[i * 32 + lane].x + 1u;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < R; ++i) {
+                            int e = i * 32 + lane, x = 0;
+                            while (x < team && e >= S.cands[warp + x]) e -= S.cands[warp + x++];
+                            if (x < team) v[i] = found[(warp + x) * room + e].x + 1u;
+                        }
+                    }
+                    sort_down<R>(v, lane);
+                    int kept = 0;
+#pragma unroll
+                    for (int i = 0; i < R; ++i) kept += __popc(__ballot_sync(0xffffffffu, v[i] > w[i]));       // (the first so many)
+                    cut = k - kept;
+                    uint32_t last = 0u, next = 0u;                // the weakest kept one, and the one behind it
+#pragma unroll
+                    for (int i = 0; i < R; ++i) {
+                        if ((kept - 1) >> 5 == i) last = v[i];
+                        if (kept >> 5 == i) next = v[i];
+                    }
+                    last = __shfl_sync(0xffffffffu, last, (kept - 1) & 31);
+                    next = __shfl_sync(0xffffffffu, next, kept & 31);
+                    if (kept >= 32 * R) next = 0u;
+                    least = kept == 0 ? ~0ull : (unsigned long long)(last - 1u) << 32;
+                    if (kept > 0 && next == last) {               // equal ones: the first of them
+                        int better = 0;
+#pragma unroll
+                        for (int i = 0; i < R; ++i) better += __popc(__ballot_sync(0xffffffffu, v[i] > last));
+                        int need = kept - better;
+                        for (int x = 0; x < team && need > 0; ++x)
+                            for (int e = 0; e < S.cands[warp + x] && need > 0; e += 32) {
+                                const uint32_t same = __ballot_sync(0xffffffffu, e + lane < S.cands[warp + x] && found[(warp + x) * room + e + lane].x + 1u == last);
+                                if (__popc(same) >= need) {
+                                    const int at_lane = __fns(same, 0, need);
+                                    least = order_key(last - 1u, x * (1 << 20) + e + at_lane);
+                                }
+                                need -= __popc(same);
+                            }
+                    }
+                };
+                if (cands <= 32) match(std::integral_constant<int, 1>{});
+                else if (cands <= 64) match(std::integral_constant<int, 2>{});
+                else if (cands <= 128) match(std::integral_constant<int, 4>{});
+                else match(std::integral_constant<int, 8>{});
             }
-            c = kept;
-            cut = k - team_sum(lane == 0 ? kept : 0);
+            if (team > 1) {
+                if (in_team == 0 && lane == 0) {
+                    S.least[warp] = least;
+                    S.cut[warp] = cut;
+                }
+                team_sync(bar, team * 32);
+                least = S.least[leader];
+                cut = S.cut[leader];
+            }
         } else {
             // order keys greater than entry m's weight
-            auto above = [&](int m) {
-                const int back = listed - 1 - m;
-                uint32_t u = held[0];
-#pragma unroll
-                for (int i = 1; i < kHeld; ++i) u = back >> 5 == i ? held[i] : u;
-                u = back < 32 * kHeld ? __shfl_sync(0xffffffffu, u, back & 31) : __float_as_uint(weight[m]) & 0x7FFFFFFFu;
-                return (unsigned long long)(u + 1u) << 32;
-            };
-            // Each own key takes at most one entry's place, so that the cut lies among the last `cands` entries (k >= listed): bisection of the cut, then of the weakest kept own key between
-            // a, which `need` own keys or more are not below, and b, which at most so many are not below.
+            auto above = [&](int m) { return (unsigned long long)((__float_as_uint(weight[m]) & 0x7FFFFFFFu) + 1u) << 32; };
+            // Entry m of the list has m entries before it and every own key that is greater: the first of which there are k or more is not kept. Each own key takes at most one entry's
+            // place, so that it lies among the last `cands` (k >= listed). Bisection of the cut, then of the weakest kept own key between a, which `need` own keys or more are not below, and
+            // b, which at most so many are not below.
             int lo = max(0, k - cands), hi = listed, need = 0, at_a = -1;
             unsigned long long a = 0, b = 0;
             bool cutting = true;
@@ -457,21 +668,21 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int team
                 // own keys whose order key is not below x (> 0)
                 int sum = 0;
                 if (!over) {
-#pragma unroll
-                    for (int i = 0; i < kHeld; ++i) sum += keys[i] >= x;
-                    for (int e = 32 * kHeld + lane; e < c; e += 32) sum += order_key(mine[e].x, (int)mine[e].y) >= x;
+                    for (int e = lane; e < c; e += 32) sum += order_key(mine[e].x, place(e)) >= x;
                 } else {
-                    sweep([&](int base, const int (&page)[kBatch], const uint4 (&u)[kBatch]) {
+                    sweep([&](int j, int, const int (&u)[16]) {
 #pragma unroll
-                        for (int i = 0; i < kBatch; ++i)
-#pragma unroll
-                            for (int y = 0; y < 4; ++y) {
-                                const int j = base + 128 * i + 4 * lane + y;
-                                sum += page[i] >= 0 && j < j1 && order_key(word(u[i], y), j) >= x;
-                            }
+                        for (int i = 0; i < 16; ++i) sum += u[i] > floor && order_key((uint32_t)u[i], j + i) >= x;
                     });
                 }
-                sum = team_sum(sum);
+                sum = __reduce_add_sync(0xffffffffu, sum);
+                if (team > 1) {
+                    if (lane == 0) S.part[step & 1][warp] = sum;
+                    team_sync(bar, team * 32);
+                    sum = 0;
+                    for (int i = 0; i < team; ++i) sum += S.part[step & 1][leader + i];
+                    ++step;
+                }
                 if (cutting) {
                     const int m = (lo + hi) >> 1;
                     if (m + sum >= k) hi = m; else lo = m + 1;
@@ -484,89 +695,80 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int team
             }
         }
     }
-    if (in_team == 0 && lane == 0) A.cut[item] = cut;
-    // attention over the kept ones, a stage of keys at a time: a bulk copy per key
-    At at;
-    at.start((const T*)A.q + t * A.qs_row + h * A.qs_head, A.scale, lane);
-    uint32_t phase = 0;
-    bool ok = true;
-    for (int b = 0; b < (over ? j1 - j0 : c) && ok;) {
-        // as many kept ones as there is room for, at the front of the warp's part; where its candidates did not fit, from the cache again
+    // attention over the kept ones, a stage of keys at a time
+    for (int b = over ? j0 : 0; b < (over ? j1 : c);) {
+        // as many kept ones as there is room for, at the front of the warp's part; where the candidates did not fit, from the cache again
         int kept = 0;
-        const int end = over ? j1 - j0 : c;
+        const int end = over ? j1 : c;
         for (; b < end && (!over || kept + 32 <= room); b += 32) {
-            uint32_t u = 0;
-            int j = -1, page = -1;
+            uint2 o = make_uint2(0u, 0u);
+            bool keep = false;
             if (over) {
-                j = j0 + b + lane;
-                page = page_of(j);
-                if (page >= 0) u = __float_as_uint(*delta_at(page, j)) & 0x7FFFFFFFu;
+                const int j = b + lane, page = j < j1 ? pages[j >> A.page_log] : -1;
+                if ((unsigned)page < (unsigned)A.num_pages) {
+                    const int u = __float_as_int(A.delta[(((size_t)page * A.Hq + h) << A.page_log) + (j & mask)]);
+                    o = make_uint2((uint32_t)u, (uint32_t)((page << A.page_log) + (j & mask)));
+                    keep = u > floor && order_key(o.x, j) >= least;
+                }
             } else if (b + lane < c) {
-                u = mine[b + lane].x;
-                j = (int)mine[b + lane].y;
-                page = pages[j >> A.page_log];
+                o = mine[b + lane];
+                keep = order_key(o.x, place(b + lane)) >= least;
             }
-            const bool keep = page >= 0 && order_key(u, j) >= least && (!floored || u > floor);
             const uint32_t bits = __ballot_sync(0xffffffffu, keep);            // (behind every lane's read)
-            if (keep) mine[kept + __popc(bits & ((1u << lane) - 1u))] = make_uint2(u, (page << A.page_log) + (j & mask));
+            if (keep) mine[kept + __popc(bits & ((1u << lane) - 1u))] = o;
             kept += __popc(bits);
             __syncwarp();
         }
 #pragma unroll 1
-        for (int i = 0; i < kept && ok; i += At::kStage) {
-            const int count = min(kept - i, At::kStage);
-            ptx::fence_proxy_async();                             // (the stage before has been read)
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive_expect_tx(&S.full[warp], count * 2 * D * (uint32_t)sizeof(T));
-            __syncwarp();
-            if (lane < count) {
-                const int slot = (int)mine[i + lane].y;
-                bulk_load(ptx::smem_u32(keys_at + lane * At::kPitch), kv + key_row(slot >> A.page_log, hk, slot & mask, A.Hkv, A.page_log) * (2 * D), 2 * D * sizeof(T), &S.full[warp]);
+        for (int i = 0; i < kept; i += At::kStage) {
+            const int count = min(kept - i, At::kStage), slot = lane < count ? (int)mine[i + lane].y : 0;
+            const size_t row = key_row(slot >> A.page_log, hk, slot & mask, A.Hkv, A.page_log);
+            const uint32_t to = ptx::smem_u32(keys_at);
+#pragma unroll 4
+            for (int e0 = 0; e0 < count; e0 += kTogether) {
+                const int e = e0 + (kTogether > 1 ? lane / kParts : 0);
+                const uint8_t* from = (const uint8_t*)kv + __shfl_sync(0xffffffffu, row, e) * (2 * D * sizeof(T));
+#pragma unroll
+                for (int part = lane % kParts; part < kParts; part += 32)
+                    if (kTogether == 1 || e < count) ptx::cp_async16_at(to + e * At::kPitch + part * 16, from + part * 16);
             }
-            ok = ptx::mbar_wait_warp(&S.full[warp], phase, &S.abort_flag);
-            phase ^= 1u;
-            if (ok) at.stage(keys_at, mine + i, count, lane);
+            ptx::cp_async_wait_all();
+            __syncwarp();
+            at.stage(keys_at, mine + i, count, lane);
             __syncwarp();
         }
     }
-    if (!ok) {
-        ptx::mbar_wait_warp(&S.full[warp], phase ^ 1u, &S.drain_flag);      // (copies in flight)
-        if (lane == 0) atomicExch(A.status, (int32_t)DMA_ERR_DEVICE_TIMEOUT);
-    }
-    at.end(sO[warp], lane);
+    at.end(reinterpret_cast<float*>(keys_at), lane);
     if (lane == 0) { S.m[warp] = at.m; S.l[warp] = at.l; }
     team_sync(bar, team * 32);
-    float top = -INFINITY, sum = 0.0f;
-    for (int i = 0; i < team; ++i) top = fmaxf(top, S.m[leader + i]);
-    auto factor = [&](int w) { return S.m[w] == -INFINITY ? (S.l[w] == 0.0f ? 0.0f : 1.0f) : expf(S.m[w] - top); };
-    for (int i = 0; i < team; ++i) sum += S.l[leader + i] * factor(leader + i);
-    float* out = A.piece_of(t, h, 0, D);
-    for (int x = in_team * 32 + lane; x < D; x += team * 32) {
-        float a = 0.0f;
-        for (int i = 0; i < team; ++i) {
-            const float f = factor(leader + i);
-            if (f != 0.0f) a += sO[leader + i][x] * f;
+    if (in_team == 0) {
+        float top = -INFINITY, sum = 0.0f, out[D / 32] = {};
+        for (int w = warp; w < warp + team; ++w) top = fmaxf(top, S.m[w]);
+        for (int w = warp; w < warp + team; ++w) {
+            const float f = S.m[w] == -INFINITY ? (S.l[w] == 0.0f ? 0.0f : 1.0f) : expf(S.m[w] - top);
+            if (f == 0.0f) continue;
+            sum += S.l[w] * f;
+#pragma unroll
+            for (int x = 0; x < D / 32; ++x) out[x] += reinterpret_cast<const float*>(dynamic + w * kStageBytes)[lane + 32 * x] * f;
         }
-        if (behind) out[2 + x] = a;
-        else store_as((T*)A.o + t * A.os_row + h * A.os_head + x, sum == 0.0f ? 0.0f : a / sum);
+        write_own<T, D>(A, t, h, behind, cut, top, sum, out, lane);
     }
-    if (in_team == 0 && lane == 0) {
-        if (behind) { out[0] = top; out[1] = sum; }
-        else A.lse[item] = sum == 0.0f ? -INFINITY : top + logf(sum);
+    team_sync(bar, team * 32);
     }
 }
 
-// Warps per (row, head): as many as make the chip's SMs have 16 of them, and so many that a row's own keys find room as candidates, at most 512 per warp.
+// Warps: one per head of a group, or teams of them where all make fewer than 16 per SM or where a row's own keys would not find room as candidates; eight at most.
 template <typename T, int D>
 int own(const Cache& C, const DecodeArgs& A, cudaStream_t st) {
-    const int64_t capacity = (int64_t)C.max_blocks << C.page_log, items = (int64_t)C.rows * C.Hq;
-    int team = 1;
-    while (team < kWarps && (items * team * 2 <= 16 * 148 || capacity > 1024 * team)) team *= 2;
-    const int room = (int)std::min<int64_t>((capacity + team * 128 - 1) / (team * 128) * 128, 512);
-    const size_t smem = (size_t)kWarps * (room * sizeof(uint2) + Attend<T, D>::kStage * Attend<T, D>::kPitch);
-    if (cudaFuncSetAttribute(own_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return DMA_ERR_CUDA;
-    const int64_t per = kWarps / team;
-    return launch_overlapped(own_kernel<T, D>, dim3((unsigned)((items + per - 1) / per + 1)), dim3(kThreads), smem, st, 1, A, team, room);
+    const int64_t capacity = (int64_t)C.max_blocks << C.page_log, items = (int64_t)C.rows * C.Hkv;
+    int heads = 1, team = 1;
+    while (heads < C.G && heads < kWarps) heads *= 2;
+    while (heads * team < kWarps && (items * heads * team * 2 <= 16 * 148 || capacity > 1024 * team)) team *= 2;
+    const int room = (int)std::min<int64_t>((capacity + team * 64 - 1) / (team * 64) * 64, 512), warps = heads * team;
+    const size_t smem = std::max<size_t>((size_t)warps * (room * sizeof(uint2) + Attend<T, D>::kStage * Attend<T, D>::kPitch), 32 * 1024 / kWarps * warps);
+    auto kernel = team > 1 ? own_kernel<T, D, true> : own_kernel<T, D, false>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return DMA_ERR_CUDA;
+    return launch_overlapped(kernel, dim3((unsigned)(items + 1)), dim3(32 * warps), smem, st, 1, A, team, room);
 }
 
 }  // namespace
