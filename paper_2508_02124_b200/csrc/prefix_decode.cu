@@ -22,10 +22,8 @@ __global__ void __launch_bounds__(kThreads) simt_kernel(DecodeArgs A) {
     const int tile = blockIdx.x / A.Hq, h = blockIdx.x % A.Hq, hk = h / A.G;
     if (tile >= *A.ntiles) return;
     const int4 rows = A.tiles[tile];
-    const bool active = warp < rows.z;
-    const int t = A.members[rows.y + min(warp, rows.z - 1)];
-    int n;
-    A.listed(t, n);
+    const bool active = warp < rows.y;
+    const int t = A.members[tile * kWarps + min(warp, rows.y - 1)], n = rows.z;
     const int cut = A.cut[t * A.Hq + h], nslots = A.num_pages << A.page_log;
     const int32_t* slot = A.order_slot + ((int64_t)rows.x * A.Hq + h) * A.order_ld;
     const float* weight = A.order_weight + ((int64_t)rows.x * A.Hq + h) * A.order_ld;
@@ -126,7 +124,7 @@ struct Layout {
         cut = take((size_t)C.rows * C.Hq * 4);
         piece = take((size_t)C.rows * C.Hq * pieces * (C.d + 2) * 4);
         first = take((size_t)(nprefix + 1) * 4);
-        members = take((size_t)C.rows * 4);
+        members = take((size_t)max_tiles * tile_rows * 4);
         tiles = take((size_t)max_tiles * 16);
         ntiles = take(4);
         total = x;

@@ -21,8 +21,8 @@ struct DecodeArgs {
     int* cut;                    // [rows * Hq]: entries of its prefix' order that a row's head keeps
     float* piece;                // [rows * Hq][pieces][D + 2]: maximum, sum and weighted values of a part of the keys; the first piece: own keys
     int pieces;
-    int *first, *members;        // [nprefix + 1], [rows]: the rows by prefix
-    int4* tiles;                 // (prefix, first of its members, how many, -): at most tile_rows of them
+    int *first, *members;        // [nprefix + 1]: scratch; [tiles * tile_rows]: the rows of each tile
+    int4* tiles;                 // (prefix, rows of it, listed keys, -)
     int* ntiles;
     int tile_rows;
     // keys that row t sees of its own sequence; -1: the row is left as it is

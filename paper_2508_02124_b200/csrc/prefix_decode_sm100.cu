@@ -35,7 +35,7 @@ struct Shared {
     uint32_t bad[4];                                          // rows to form again, a bit each
     uint64_t q_full, full[kStages], bias_full[kStages], empty[kStages], s_full[2], p_full[2], o_done[2];
     uint32_t tmem;
-    int top, abort_flag;
+    int abort_flag;
 };
 
 __device__ __forceinline__ void cluster_sync() {
@@ -151,31 +151,27 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_kernel(DecodeArgs A, int n
             mbar_init(&S.o_done[i], 1);
         }
         S.abort_flag = 0;
-        S.top = 0;
         fence_barrier_init();
     }
     if (tid < 4) S.bad[tid] = 0;
     pdl_enter(A.q, A.kv, A.prefix, A.order_slot, A.order_len, A.order_weight, A.o, A.lse, A.status, A.cut, A.piece, A.members, A.tiles, A.ntiles);
-    if (tile >= *A.ntiles) return;                                // (all CTAs of the cluster)
+    const int ntiles_all = *A.ntiles, member = tid < 128 ? A.members[tile * 128 + tid] : 0;
     const int4 rows = A.tiles[tile];
-    const int R = rows.z, copies = R <= 32 ? 4 : R <= 64 ? 2 : 1, lanes = 128 / copies;
+    if (tile >= ntiles_all) return;                               // (all CTAs of the cluster)
+    const int R = rows.y, listed = rows.z, copies = R <= 32 ? 4 : R <= 64 ? 2 : 1, lanes = 128 / copies;
     if (warp == kIssuer) {
         tmem_alloc(&S.tmem, 256);
         tmem_relinquish();
     }
-    __syncthreads();
-    if (tid < 128) {
-        const int r = tid % lanes, t = r < R ? A.members[rows.y + r] : -1, cut = t >= 0 ? A.cut[t * A.Hq + h] : 0;
-        S.row[tid] = t;
-        S.cut[tid] = cut;
-        const int top = __reduce_max_sync(0xffffffffu, cut);
-        if (lane == 0) atomicMax(&S.top, top);
-    }
+    if (tid < R)
+        for (int i = 0; i < copies; ++i) S.row[i * lanes + tid] = member;
+    if (tid < lanes && tid >= R)
+        for (int i = 0; i < copies; ++i) S.row[i * lanes + tid] = -1;
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = S.tmem;
-    const int ntiles = (S.top + kKeys - 1) / kKeys, i0 = (int)((int64_t)ntiles * rank / nrank), i1 = (int)((int64_t)ntiles * (rank + 1) / nrank);
+    const int ntiles = (listed + kKeys - 1) / kKeys, i0 = (int)((int64_t)ntiles * rank / nrank), i1 = (int)((int64_t)ntiles * (rank + 1) / nrank);
     const __nv_bfloat16 *q = (const __nv_bfloat16*)A.q + h * A.qs_head, *kv = (const __nv_bfloat16*)A.kv;
     const int64_t list = ((int64_t)rows.x * A.Hq + h) * A.order_ld;
     const int32_t* slots = A.order_slot + list;
@@ -183,6 +179,8 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_kernel(DecodeArgs A, int n
     const int nslots = A.num_pages << A.page_log;
     float m = -INFINITY, l = 0.0f;
     if (warp < 4) {
+        const int mine_t = S.row[tid], cut = mine_t >= 0 ? A.cut[mine_t * A.Hq + h] : 0;
+        S.cut[tid] = cut;
         if (i0 < i1) {
             // Q: lanes of D / 8 side by side take a row
             constexpr int LPR = D / 8;
@@ -193,7 +191,7 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_kernel(DecodeArgs A, int n
             cp_async_wait_all();
             fence_proxy_async();
             mbar_arrive(&S.q_full);
-            const int copy = tid / lanes, cut = S.cut[tid];
+            const int copy = tid / lanes;
             const float c1 = A.scale * kLog2e;
             const uint32_t mine = tmem + ((uint32_t)(warp * 32) << 16);
             bool ok = copies == 4   ? softmax<D, 16>(S, i0, i1, copy, cut, c1, mine, m, l)
@@ -266,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_kernel(DecodeArgs A, int n
             const int e = i * kKeys + w * kMine + lane;
             slot = -1;
             bias = -INFINITY;
-            if (lane < kMine && i < i1 && e < S.top) {            // (no list is shorter than a row's cut)
+            if (lane < kMine && i < i1 && e < listed) {
                 slot = slots[e];
                 bias = weights[e] * kLog2e;
                 if ((unsigned)slot >= (unsigned)nslots) { slot = -1; bias = -INFINITY; }
@@ -347,6 +345,7 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_kernel(DecodeArgs A, int n
             pl = ld_cluster(map_rank(smem_u32(&S.l[at]), lane / copies));
         }
         const float om = own[0], ol = own[1];
+        const float2 own0 = lane < D / 4 ? *reinterpret_cast<const float2*>(own + 2 + lane * 4) : make_float2(0.0f, 0.0f), own1 = lane < D / 4 ? *reinterpret_cast<const float2*>(own + 4 + lane * 4) : make_float2(0.0f, 0.0f);
         float top = pm;
 #pragma unroll
         for (int x = 1; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
@@ -359,15 +358,21 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_kernel(DecodeArgs A, int n
         if (of != 0.0f) sum += ol * of;
         float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         auto add = [&](const float4& v, float g) { acc.x += v.x * g; acc.y += v.y * g; acc.z += v.z * g; acc.w += v.w * g; };
-        for (int i = 0; i < parts; ++i) {
-            const float g = __shfl_sync(0xffffffffu, f, i);
-            if (g != 0.0f && lane < D / 4) add(ld_cluster4(map_rank(sO + o_part<D>(i % copies * lanes + r, lane), i / copies)), g);
+        for (int i0 = 0; i0 < parts; i0 += 8) {
+            float4 v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int at = min(i0 + i, parts - 1);
+                v[i] = ld_cluster4(map_rank(sO + o_part<D>(at % copies * lanes + r, lane % (D / 4)), at / copies));
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float g = __shfl_sync(0xffffffffu, f, min(i0 + i, parts - 1));
+                if (i0 + i < parts && g != 0.0f) add(v[i], g);    // (what a part without keys left may be anything)
+            }
         }
         if (lane < D / 4) {
-            if (of != 0.0f) {
-                const float2 u = *reinterpret_cast<const float2*>(own + 2 + lane * 4), v = *reinterpret_cast<const float2*>(own + 4 + lane * 4);
-                add(make_float4(u.x, u.y, v.x, v.y), of);
-            }
+            if (of != 0.0f) add(make_float4(own0.x, own0.y, own1.x, own1.y), of);
             const float inv = 1.0f / sum;
             uint2 w = make_uint2(0u, 0u);
             if (sum != 0.0f) w = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));

@@ -271,7 +271,7 @@ struct AttendAll {
 // The rows by prefix, in the order of rows, and tiles of them.
 __device__ void group_rows(const DecodeArgs& A, int* turn) {       // turn: kTogether per thread
     constexpr int kTogether = 4;                                  // rows of a thread requested together
-    __shared__ int part[kWarps], tile_part[kWarps];
+    __shared__ int part[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x;
     if (A.nprefix == 0) {
         if (tid == 0) *A.ntiles = 0;
@@ -305,31 +305,28 @@ __device__ void group_rows(const DecodeArgs& A, int* turn) {       // turn: kTog
             if (g[i] >= 0) atomicAdd(&A.first[g[i]], 1);
     });
     __syncthreads();
-    int row_carry = 0, tile_carry = 0;
+    int tile_carry = 0;
     for (int b = 0; b < A.nprefix; b += threads) {
         const int g = b + tid, n = g < A.nprefix ? __ldcg(&A.first[g]) : 0, nt = (n + A.tile_rows - 1) / A.tile_rows;
-        int x = n, y = nt;
+        int y = nt;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int u = __shfl_up_sync(0xffffffffu, x, o), v = __shfl_up_sync(0xffffffffu, y, o);
-            if (lane >= o) { x += u; y += v; }
+            const int v = __shfl_up_sync(0xffffffffu, y, o);
+            if (lane >= o) y += v;
         }
-        if (lane == 31) { part[warp] = x; tile_part[warp] = y; }
+        if (lane == 31) part[warp] = y;
         __syncthreads();
-        int before = 0, tiles_before = 0, all = 0, all_tiles = 0;
+        int tiles_before = 0, all_tiles = 0;
         for (int i = 0; i < threads / 32; ++i) {
-            before += i < warp ? part[i] : 0;
-            tiles_before += i < warp ? tile_part[i] : 0;
-            all += part[i];
-            all_tiles += tile_part[i];
+            tiles_before += i < warp ? part[i] : 0;
+            all_tiles += part[i];
         }
         if (g < A.nprefix) {
-            const int start = row_carry + before + x - n;
-            __stcg(&A.first[g], start);
-            for (int i = 0; i < nt; ++i)
-                A.tiles[tile_carry + tiles_before + y - nt + i] = make_int4(g, start + i * A.tile_rows, min(A.tile_rows, n - i * A.tile_rows), 0);
+            const int tile = tile_carry + tiles_before + y - nt;
+            __stcg(&A.first[g], tile * A.tile_rows);
+            const int listed = nt ? (int)min((int64_t)min(A.order_len[g], A.w), A.order_ld) : 0;
+            for (int i = 0; i < nt; ++i) A.tiles[tile + i] = make_int4(g, min(A.tile_rows, n - i * A.tile_rows), listed, 0);
         }
-        row_carry += all;
         tile_carry += all_tiles;
         __syncthreads();
     }
@@ -418,7 +415,7 @@ __device__ __forceinline__ void write_own(const DecodeArgs& A, int t, int h, boo
 // A CTA per (row, KV head); the last one groups the rows by prefix. The group's heads each have a warp or a team of them (kTeams; else up to eight heads at a time, the others
 // in turn). Where a row keeps all keys whatever their weights, the warps share its own keys, all heads together.
 template <typename T, int D, bool kTeams>
-__global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warps_per_head, int room) {
+__global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warps_per_head, int room, int heads) {       // heads: of a CTA
     using At = Attend<T, D>;
     extern __shared__ __align__(16) uint8_t dynamic[];            // of each warp [At::kStage][At::kPitch] keys, [room]: (pattern of delta, slot) of candidates by position, then of the kept ones
     __shared__ OwnShared S;
@@ -429,7 +426,7 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
         group_rows(A, reinterpret_cast<int*>(dynamic));
         return;
     }
-    const int t = blockIdx.x / A.Hkv, hk = blockIdx.x % A.Hkv;
+    const int parts = (A.G + heads - 1) / heads, t = blockIdx.x / (A.Hkv * parts), hk = blockIdx.x / parts % A.Hkv, head0 = blockIdx.x % parts * heads, head1 = min(A.G, head0 + heads);
     const int r = A.seq[t], p = A.pos[t], g = A.nprefix ? A.prefix[t] : -1;
     if ((unsigned)r >= (unsigned)A.nseq) return;
     const int n = min(max(p, -1), (A.max_blocks << A.page_log) - 1) + 1;
@@ -445,9 +442,9 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
 
     if constexpr (sizeof(T) == 2) {
         if ((int64_t)listed + n <= A.w) {
-            for (int g0 = 0; g0 < A.G; g0 += 8) {
+            for (int g0 = head0; g0 < head1; g0 += 8) {
                 const int mine = g0 + (lane >> 2), h = hk * A.G + mine;
-                const bool real = mine < A.G;
+                const bool real = mine < head1;
                 AttendAll<D> at;
                 at.start((const T*)A.q + t * A.qs_row + h * A.qs_head, real, A.scale, lane);
                 // 16 keys at a time, side by side in one page, turn by turn of the warps
@@ -480,7 +477,7 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
                     S.all_l[warp][lane >> 2] = at.l;
                 }
                 __syncthreads();
-                for (int y = warp; y < min(8, A.G - g0); y += warps) {
+                for (int y = warp; y < min(8, head1 - g0); y += warps) {
                     const int head = hk * A.G + g0 + y;
                     float top = -INFINITY, sum = 0.0f, out[D / 32] = {};
                     for (int w = 0; w < warps; ++w) top = fmaxf(top, S.all_m[w][y]);
@@ -503,7 +500,7 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
     uint2* mine = found + warp * room;
     const int seg = (n + team * 64 - 1) / (team * 64) * 64, j0 = min(n, in_team * seg), j1 = min(n, j0 + seg);
 #pragma unroll 1
-    for (int head = warp / team; head < A.G; head += warps / team) {
+    for (int head = head0 + warp / team; head < head1; head += warps / team) {
     const int h = hk * A.G + head;
     const float* weight = A.order_weight + ((int64_t)g * A.Hq + h) * A.order_ld;
     // f(position, slot, patterns) for the part's keys, 512 at a time: a lane has 16 of them, side by side in one page (pages have 16 keys and more). Patterns of places without a key: -2
@@ -757,18 +754,23 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
     }
 }
 
-// Warps: one per head of a group, or teams of them where all make fewer than 16 per SM or where a row's own keys would not find room as candidates; eight at most.
+// Warps: one per head of a group, eight at most; teams of them, and fewer heads per CTA, where all make fewer than 16 per SM or where a row's own keys would not find room as candidates.
 template <typename T, int D>
 int own(const Cache& C, const DecodeArgs& A, cudaStream_t st) {
-    const int64_t capacity = (int64_t)C.max_blocks << C.page_log, items = (int64_t)C.rows * C.Hkv;
+    const int64_t capacity = (int64_t)C.max_blocks << C.page_log;
     int heads = 1, team = 1;
     while (heads < C.G && heads < kWarps) heads *= 2;
-    while (heads * team < kWarps && (items * heads * team * 2 <= 16 * 148 || capacity > 1024 * team)) team *= 2;
+    const int most = heads;                                       // (more heads take turns)
+    auto ctas = [&](int per) { return (int64_t)C.rows * C.Hkv * (per == most ? 1 : (C.G + per - 1) / per); };
+    while (team < kWarps && (ctas(heads) * heads * team * 2 <= 16 * 148 || capacity > 1024 * team)) {
+        team *= 2;
+        if (heads * team > kWarps) heads /= 2;
+    }
     const int room = (int)std::min<int64_t>((capacity + team * 64 - 1) / (team * 64) * 64, 512), warps = heads * team;
     const size_t smem = std::max<size_t>((size_t)warps * (room * sizeof(uint2) + Attend<T, D>::kStage * Attend<T, D>::kPitch), 32 * 1024 / kWarps * warps);
     auto kernel = team > 1 ? own_kernel<T, D, true> : own_kernel<T, D, false>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return DMA_ERR_CUDA;
-    return launch_overlapped(kernel, dim3((unsigned)(items + 1)), dim3(32 * warps), smem, st, 1, A, team, room);
+    return launch_overlapped(kernel, dim3((unsigned)(ctas(heads) + 1)), dim3(32 * warps), smem, st, 1, A, team, room, heads == most ? C.G : heads);
 }
 
 }  // namespace
