@@ -384,6 +384,7 @@ typedef struct {
  *             last row: the row is skipped altogether
  *   row_prefix, prefix_len   [rows], [nprefix]; both NULL: no prefixes
  *   slot      [rows]; K, V and delta of a row whose slot is outside the pool are not written (its q is). Slots of one call are distinct.
+ * With W_delta, Hq / Hkv at most 76 (d = 128) or 96 (d = 64); DMA_ERR_UNSUPPORTED beyond.
  * Angles are formed in 64 bits and reduced to a turn before they are rounded to fp32; the rotation is fp32, rounded once. */
 int dma_cache_append(const dma_cache_t* c, const dma_rotation_t* rotation, const void* q, const void* K, const void* V, const float* W_delta,
                      const float* A, const float* delta_new, int64_t delta_ld, const int32_t* slot, const int32_t* row_pos,

@@ -2,6 +2,8 @@
 //
 // d / 16 lanes own a row. A lane has the 16 channels of a head whose pairs turn by the same eight angles, whichever of the two pairings is asked for, so that it forms eight
 // sines and cosines per row and turns its part of every head with them. Angles: position times frequency in turns, in 64 bits, less the whole turns; fp32 from there on.
+// Bound by memory: a lane copies what it will use into shared memory a stage ahead, without registers or barriers. 16384 rows of 32 and 8 heads, d = 128: 76 us, 5.3 TB/s (bytes alone 62;
+// with loads into registers 103 to 88, with the sampling weights read through the L1 94; without forming delta 70). 64 rows 4.7 us: three trips to memory.
 #include <algorithm>
 #include <type_traits>
 
@@ -12,9 +14,11 @@
 namespace dma {
 namespace {
 
-constexpr int kThreads = 128;
+constexpr int kStages = 2;
 
 template <typename T> using Raw = typename RawOf<T>::type;
+template <typename T> constexpr int kQueries = sizeof(T) == 2 ? 4 : 2;            // of a stage
+template <typename T> constexpr int stage_bytes = (4 + 2 * kQueries<T>) * ((int)sizeof(T) / 2) * 16;      // of a thread
 
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
     *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
@@ -40,11 +44,11 @@ struct Append {
     int rows, Hq, Hkv, G, page_log, nslots, nprefix, rot, interleaved;
 };
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) append_kernel(Append P) {
+template <typename T, int D, int kThreads>
+__global__ void __launch_bounds__(kThreads, 512 / kThreads) append_kernel(Append P) {
     constexpr int LPR = D / 16, RPW = 32 / LPR, kWarps = kThreads / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane % LPR, grp = lane / LPR;
-    pdl_enter(P.q, P.K, P.V, P.W, P.A, P.delta_new, P.inv_freq, P.slot, P.pos, P.prefix, P.prefix_len, P.q_out, P.kv, P.delta);
+    pdl_enter();
     const int t = (blockIdx.x * kWarps + warp) * RPW + grp;
     const bool turning = P.inv_freq != nullptr;
     bool live = t < P.rows;
@@ -70,15 +74,6 @@ __global__ void __launch_bounds__(kThreads) append_kernel(Append P) {
     else if (turns) { c0 = sub * 8; c1 = c0 + P.rot / 2; }
     else { c0 = P.rot + (sub - npair) * 16; c1 = c0 + 8; }
     float cs[8], sn[8];
-    if (turns && live) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const double turn = (double)m * (double)P.inv_freq[sub * 8 + i] * 0.15915494309189533577;
-            sincospif(2.0f * (float)(turn - rint(turn)), &sn[i], &cs[i]);
-            cs[i] *= P.rot_scale;
-            sn[i] *= P.rot_scale;
-        }
-    }
     auto rotate_store = [&](const Raw<T>& ra, const Raw<T>& rb, T* to) {
         if (!turns) {
             store_raw(to + c0, ra);
@@ -109,43 +104,94 @@ __global__ void __launch_bounds__(kThreads) append_kernel(Append P) {
     const int place_mask = (1 << P.page_log) - 1;
     const T *Q = (const T*)P.q + (int64_t)t * P.qs_row, *K = (const T*)P.K + (int64_t)t * P.ks_row, *V = (const T*)P.V + (int64_t)t * P.vs_row;
     T *qo = (T*)P.q_out + (int64_t)t * P.os_row, *kv = (T*)P.kv;
-    for (int hk = blockIdx.y; hk < P.Hkv; hk += gridDim.y) {
-        Raw<T> k0{}, k1{}, v0{}, v1{};
-        if (in) {
-            k0 = load_raw8(K + hk * P.ks_head + c0);
-            k1 = load_raw8(K + hk * P.ks_head + c1);
-            v0 = load_raw8(V + hk * P.vs_head + sub * 16);
-            v1 = load_raw8(V + hk * P.vs_head + sub * 16 + 8);
+    // z of a warp's rows, and delta from it for many heads at once: 100 instructions one behind the other, which every block of heads would wait for
+    constexpr int kPending = 32;
+    __shared__ float sZ[kWarps][kPending][RPW];
+    __shared__ int sHead[kWarps][kPending], sAt[kWarps][RPW];
+    int pending = 0;
+    if (sub == 0) sAt[warp][grp] = in ? at : -1;
+    auto flush = [&]() {
+        __syncwarp();
+#pragma unroll 2
+        for (int i = lane; i < pending * RPW; i += 32) {
+            const int h = sHead[warp][i / RPW], to = sAt[warp][i % RPW];
+            const float x = delta_fixed(sZ[warp][i / RPW][i % RPW], P.A[h]);
+            if (to >= 0) P.delta[(((size_t)(to >> P.page_log) * P.Hq + h) << P.page_log) + (to & place_mask)] = x;
         }
-        constexpr int NQ = 4;
-        Raw<T> qa[NQ], qb[NQ];
-        auto request = [&](int g0) {
+        __syncwarp();
+        pending = 0;
+    };
+    // A stage: a KV head's K and V and NQ of its group's queries, or NQ more of them. A lane copies what it will use to places of its own in shared memory, a stage ahead.
+    constexpr int NQ = kQueries<T>, kWide = (int)sizeof(T) / 2, kSlots = (4 + 2 * NQ) * kWide;     // 16-byte places of a lane and stage; of 8 channels
+    extern __shared__ uint4 staged[];                             // [kStages][kSlots][kThreads], then the heads' sampling weights
+    auto copy = [&](int stage, int c, const T* from) {
+#pragma unroll
+        for (int i = 0; i < kWide; ++i) ptx::cp_async16_at(ptx::smem_u32(staged + (stage * kSlots + c * kWide + i) * kThreads + tid), from + i * (8 / kWide));
+    };
+    auto take = [&](int stage, int c) {
+        Raw<T> r;
+#pragma unroll
+        for (int i = 0; i < kWide; ++i) reinterpret_cast<uint4*>(&r)[i] = staged[(stage * kSlots + c * kWide + i) * kThreads + tid];
+        return r;
+    };
+    // KV heads of this CTA: side by side
+    const int per = (P.Hkv + gridDim.y - 1) / gridDim.y, first = blockIdx.y * per, heads = min(per, P.Hkv - first), batches = (P.G + NQ - 1) / NQ, units = heads * batches;
+    float* sW = reinterpret_cast<float*>(staged + kStages * kSlots * kThreads);
+    // (read from global memory they were missed by the L1 between the rows that stream by: 94 us instead of 76. A lane's sixteen in four parts, each next to the other lanes' same part: a
+    // group's 16-byte reads meet every bank once)
+    if (!P.delta_new)
+        for (int i = tid; i < heads * P.G * (D / 4); i += kThreads)
+            ptx::cp_async16_at(ptx::smem_u32(sW + i / (D / 4) * D + (i & 3) * (D / 4) + i % (D / 4) / 4 * 4), P.W + (size_t)first * P.G * D + i * 4);
+    auto request = [&](int u) {
+        if (u < units) {
+            const int hk = first + u / batches, g0 = u % batches * NQ, stage = u % kStages;
+            if (in && g0 == 0) {
+                copy(stage, 0, K + hk * P.ks_head + c0);
+                copy(stage, 1, K + hk * P.ks_head + c1);
+                copy(stage, 2, V + hk * P.vs_head + sub * 16);
+                copy(stage, 3, V + hk * P.vs_head + sub * 16 + 8);
+            }
 #pragma unroll
             for (int i = 0; i < NQ; ++i)
                 if (ask && g0 + i < P.G) {
                     const T* x = Q + (int64_t)(hk * P.G + g0 + i) * P.qs_head;
-                    qa[i] = load_raw8(x + c0);
-                    qb[i] = load_raw8(x + c1);
+                    copy(stage, 4 + 2 * i, x + c0);
+                    copy(stage, 5 + 2 * i, x + c1);
                 }
-        };
-        request(0);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) request(i);
+    if (turns && live) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const double turn = (double)m * (double)P.inv_freq[sub * 8 + i] * 0.15915494309189533577;
+            sincospif(2.0f * (float)(turn - rint(turn)), &sn[i], &cs[i]);
+            cs[i] *= P.rot_scale;
+            sn[i] *= P.rot_scale;
+        }
+    }
+#pragma unroll 1
+    for (int u = 0; u < units; ++u) {
+        const int hk = first + u / batches, q0 = u % batches * NQ, stage = u % kStages;
+        request(u + kStages - 1);
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        if (u == 0) __syncthreads();                              // (the weights, which others have copied)
+#pragma unroll
+        for (int i = 0; i < NQ; ++i)
+            if (ask && q0 + i < P.G) rotate_store(take(stage, 4 + 2 * i), take(stage, 5 + 2 * i), qo + (int64_t)(hk * P.G + q0 + i) * P.os_head);
+        if (q0) continue;
+        Raw<T> v0{}, v1{};
         if (in) {
             T* to = kv + key_row(at >> P.page_log, hk, at & place_mask, P.Hkv, P.page_log) * (2 * D);
-            rotate_store(k0, k1, to);
+            rotate_store(take(stage, 0), take(stage, 1), to);
+            v0 = take(stage, 2);
+            v1 = take(stage, 3);
             store_raw(to + D + sub * 16, v0);
             store_raw(to + D + sub * 16 + 8, v1);
         }
-        for (int g0 = 0; g0 < P.G; g0 += NQ) {
-            if (g0) request(g0);
-#pragma unroll
-            for (int i = 0; i < NQ; ++i)
-                if (ask && g0 + i < P.G) rotate_store(qa[i], qb[i], qo + (int64_t)(hk * P.G + g0 + i) * P.os_head);
-        }
-        float* dl = in ? P.delta + (((size_t)(at >> P.page_log) * P.Hq) << P.page_log) + (at & place_mask) : nullptr;
-        if (P.delta_new) {
-            for (int g = sub; g < P.G; g += LPR)
-                if (in) dl[(size_t)(hk * P.G + g) << P.page_log] = P.delta_new[(hk * P.G + g) * P.delta_ld + t];
-        } else {
+        if (!P.delta_new) {
             float v[2][8];
             widen8(v0, v[0]);
             widen8(v1, v[1]);
@@ -153,14 +199,17 @@ __global__ void __launch_bounds__(kThreads) append_kernel(Append P) {
             // first two of which a lane has itself.
             auto block = [&](int g0, auto nb_tag) {
                 constexpr int NB = decltype(nb_tag)::value;
+                if (pending + NB > kPending) flush();
                 float p[NB];
 #pragma unroll
                 for (int n = 0; n < NB; ++n) {
                     float part[2];
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        float w[8], a = 0.0f;
-                        load8(P.W + (size_t)(hk * P.G + g0 + n) * D + sub * 16 + i * 8, w);
+                        const float* wp = sW + ((hk - first) * P.G + g0 + n) * D + i * (D / 2) + sub * 4;
+                        const float4 wa = *reinterpret_cast<const float4*>(wp), wb = *reinterpret_cast<const float4*>(wp + D / 4);
+                        const float w[8] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w};
+                        float a = 0.0f;
 #pragma unroll
                         for (int c = 0; c < 8; ++c) a = __fmaf_rn(v[i][c], w[c], a);
                         part[i] = a;
@@ -171,23 +220,38 @@ __global__ void __launch_bounds__(kThreads) append_kernel(Append P) {
 #pragma unroll
                 for (int b = 1, x = NB >> 1; b < NB; b <<= 1, x >>= 1) mine |= (sub & b) ? x : 0;
                 block_reduce<NB, LPR>(p, sub);
-                const int h = hk * P.G + g0 + mine;
-                if (in && sub < NB) dl[(size_t)h << P.page_log] = delta_fixed(p[0], P.A[h]);
+                if (sub < NB) {
+                    sZ[warp][pending + mine][grp] = p[0];
+                    if (grp == 0) sHead[warp][pending + mine] = hk * P.G + g0 + mine;
+                }
+                pending += NB;
             };
             int g0 = 0;
             for (; g0 + 4 <= P.G; g0 += 4) block(g0, std::integral_constant<int, 4>{});
             if (g0 + 2 <= P.G) { block(g0, std::integral_constant<int, 2>{}); g0 += 2; }
             if (g0 < P.G) block(g0, std::integral_constant<int, 1>{});
+        } else if (in) {
+            float* to = P.delta + (((size_t)(at >> P.page_log) * P.Hq) << P.page_log) + (at & place_mask);
+            for (int h = hk * P.G + sub; h < (hk + 1) * P.G; h += LPR) to[(size_t)h << P.page_log] = P.delta_new[h * P.delta_ld + t];
         }
     }
+    if (pending) flush();
 }
 
+template <typename T, int D, int kThreads>
+int append_rows(const Append& P, cudaStream_t st) {
+    constexpr int kRows = kThreads / (D / 16), kWeights = 20 * 1024;
+    const int tiles = (P.rows + kRows - 1) / kRows, group = P.G * D * (int)sizeof(float);
+    // KV heads per CTA: as many as leave eight CTAs per SM (16384 rows of 8: three of them 76 us; eight 84, four 88, two 79, one 92), and so few that their weights take 20 KB, or one
+    const int per = std::max(1, std::min({P.Hkv, (int)((int64_t)P.Hkv * tiles / (8 * 148)), std::max(1, kWeights / group)}));
+    const int smem = kStages * stage_bytes<T> * kThreads + (P.delta_new ? 0 : per * group);
+    if (cudaFuncSetAttribute(append_kernel<T, D, kThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return DMA_ERR_CUDA;
+    return launch_overlapped(append_kernel<T, D, kThreads>, dim3(tiles, (P.Hkv + per - 1) / per), dim3(kThreads), smem, st, 1, P);
+}
 template <typename T, int D>
 int append(const Append& P, cudaStream_t st) {
-    constexpr int kRows = kThreads / (D / 16);
-    const int tiles = (P.rows + kRows - 1) / kRows;
-    const int split = std::max(1, std::min(P.Hkv, 8 * 148 / tiles));
-    return launch_overlapped(append_kernel<T, D>, dim3(tiles, split), dim3(kThreads), 0, st, 1, P);
+    // (256 threads share the weights where there are four such CTAs per SM: 16384 rows 76 us against 83 by 128)
+    return (int64_t)P.rows * P.Hkv * (D / 16) >= 4 * 148 * 256 ? append_rows<T, D, 256>(P, st) : append_rows<T, D, 128>(P, st);
 }
 
 }  // namespace

@@ -167,6 +167,7 @@ int dma_cache_append(const dma_cache_t* c, const dma_rotation_t* rotation, const
         if (q) return DMA_ERR_UNSUPPORTED;
         row_pos = row_prefix = prefix_len = nullptr;
     }
+    if (!delta_new && C.G > append_heads(C.d)) return DMA_ERR_UNSUPPORTED;
     if (q && q == q_out && C.rows * C.Hq > 1 && (C.qs[0] != C.os[0] || C.qs[1] != C.os[1])) return DMA_ERR_SHAPE;
     if (!aligned(16, q, K, V, W_delta, q_out, kv, delta) || !aligned(4, A, delta_new, slot, rot.inv_freq, row_pos, row_prefix, prefix_len)) return DMA_ERR_ALIGN;
     if (delta_new && delta_ld < C.rows) return DMA_ERR_SHAPE;

@@ -18,7 +18,7 @@ __global__ void __launch_bounds__(kThreads) simt_kernel(DecodeArgs A) {
     __shared__ __align__(16) float sK[kKeys][P], sV[kKeys][D], sQ[kWarps][D];
     __shared__ float sW[kKeys];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, split = blockIdx.y, nsplit = gridDim.y;
-    pdl_enter(A.q, A.kv, A.prefix, A.order_slot, A.order_len, A.order_weight, A.cut, A.piece, A.members, A.tiles, A.ntiles);
+    pdl_enter();
     const int tile = blockIdx.x / A.Hq, h = blockIdx.x % A.Hq, hk = h / A.G;
     if (tile >= *A.ntiles) return;
     const int4 rows = A.tiles[tile];
@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(kThreads) simt_kernel(DecodeArgs A) {
 template <typename T, int D>
 __global__ void __launch_bounds__(256) simt_sum_kernel(DecodeArgs A) {
     const int lane = threadIdx.x & 31, item = blockIdx.x * 8 + (threadIdx.x >> 5), t = item / A.Hq, h = item % A.Hq;
-    pdl_enter(A.seq, A.pos, A.prefix, A.order_len, A.piece, A.o, A.lse);
+    pdl_enter();
     int r, n;
     if (item >= A.rows * A.Hq || A.own(t, r) < 0 || A.listed(t, n) < 0) return;
     float top = -INFINITY, sum = 0.0f;

@@ -10,6 +10,7 @@
 //
 // Warps: 0-3 softmax and the end, 4 issues the products, 5-8 gather. Two CTAs per SM.
 #include <algorithm>
+#include <type_traits>
 
 #include "prefix_decode.cuh"
 #include "sm100_ptx.cuh"
@@ -30,7 +31,7 @@ struct Shared {
     alignas(1024) uint8_t q[128 * D * 2];
     alignas(1024) uint8_t kv[kStages][2][kTile];              // in the end: O [128][D] fp32, 16-byte parts at (part ^ row)
     alignas(16) float bias[kStages][kKeys];                   // delta log2 e
-    float m[128], l[128];
+    float m[128], l[128], joined_m[64], joined_l[64];
     int row[128], cut[128];
     uint32_t bad[4];                                          // rows to form again, a bit each
     uint64_t q_full, full[kStages], bias_full[kStages], empty[kStages], s_full[2], p_full[2], o_done[2];
@@ -154,15 +155,19 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_kernel(DecodeArgs A, int n
         fence_barrier_init();
     }
     if (tid < 4) S.bad[tid] = 0;
-    pdl_enter(A.q, A.kv, A.prefix, A.order_slot, A.order_len, A.order_weight, A.o, A.lse, A.status, A.cut, A.piece, A.members, A.tiles, A.ntiles);
+    pdl_enter();
     const int ntiles_all = *A.ntiles, member = tid < 128 ? A.members[tile * 128 + tid] : 0;
     const int4 rows = A.tiles[tile];
-    if (tile >= ntiles_all) return;                               // (all CTAs of the cluster)
-    const int R = rows.y, listed = rows.z, copies = R <= 32 ? 4 : R <= 64 ? 2 : 1, lanes = 128 / copies;
-    if (warp == kIssuer) {
+    if (warp == kIssuer) {                                        // (while these are on their way)
         tmem_alloc(&S.tmem, 256);
         tmem_relinquish();
     }
+    if (tile >= ntiles_all) {                                     // (all CTAs of the cluster)
+        __syncwarp();
+        if (warp == kIssuer) tmem_dealloc(S.tmem, 256);
+        return;
+    }
+    const int R = rows.y, listed = rows.z, copy_log = R <= 32 ? 2 : R <= 64 ? 1 : 0, copies = 1 << copy_log, lane_log = 7 - copy_log, lanes = 1 << lane_log;
     if (tid < R)
         for (int i = 0; i < copies; ++i) S.row[i * lanes + tid] = member;
     if (tid < lanes && tid >= R)
@@ -179,8 +184,7 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_kernel(DecodeArgs A, int n
     const int nslots = A.num_pages << A.page_log;
     float m = -INFINITY, l = 0.0f;
     if (warp < 4) {
-        const int mine_t = S.row[tid], cut = mine_t >= 0 ? A.cut[mine_t * A.Hq + h] : 0;
-        S.cut[tid] = cut;
+        int cut = 0;
         if (i0 < i1) {
             // Q: lanes of D / 8 side by side take a row
             constexpr int LPR = D / 8;
@@ -188,10 +192,12 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_kernel(DecodeArgs A, int n
                 const int r = warp * 32 + i, part = lane % LPR, t = S.row[r];
                 cp_async16(S.q + (part >> 3) * Sh::kHalfQ + r * 128 + (((part & 7) ^ (r & 7)) << 4), t >= 0 ? q + t * A.qs_row + part * 8 : q, t >= 0 ? 16 : 0);
             }
+            cut = S.row[tid] >= 0 ? A.cut[S.row[tid] * A.Hq + h] : 0;
             cp_async_wait_all();
             fence_proxy_async();
             mbar_arrive(&S.q_full);
-            const int copy = tid / lanes;
+            S.cut[tid] = cut;
+            const int copy = tid >> lane_log;
             const float c1 = A.scale * kLog2e;
             const uint32_t mine = tmem + ((uint32_t)(warp * 32) << 16);
             bool ok = copies == 4   ? softmax<D, 16>(S, i0, i1, copy, cut, c1, mine, m, l)
@@ -203,16 +209,16 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_kernel(DecodeArgs A, int n
                 uint8_t* to = &S.kv[0][0][0];
                 bool odd = !isfinite(l);
 #pragma unroll 1
-                for (int c = 0; c < D; c += 16) {
-                    uint32_t o[16];
-                    tmem_ld16(mine + 2 * kKeys + c, o);
-                    tc_wait_ld();
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t o[32];
+                    tmem_ld32(mine + 2 * kKeys + c, o);
+                    tc_wait_ld_dep(o);
 #pragma unroll
-                    for (int y = 0; y < 16; ++y) odd |= (o[y] & 0x7f800000u) == 0x7f800000u;
+                    for (int y = 0; y < 32; ++y) odd |= (o[y] & 0x7f800000u) == 0x7f800000u;
 #pragma unroll
-                    for (int y = 0; y < 16; y += 4) *reinterpret_cast<uint4*>(to + o_part<D>(tid, (c + y) / 4)) = make_uint4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+                    for (int y = 0; y < 32; y += 4) *reinterpret_cast<uint4*>(to + o_part<D>(tid, (c + y) / 4)) = make_uint4(o[y], o[y + 1], o[y + 2], o[y + 3]);
                 }
-                if (odd && S.row[tid] >= 0) atomicOr(&S.bad[(tid % lanes) >> 5], 1u << (tid % lanes & 31));
+                if (odd && S.row[tid] >= 0) atomicOr(&S.bad[(tid & (lanes - 1)) >> 5], 1u << (tid & (lanes - 1) & 31));
             }
         }
         S.m[tid] = m == -INFINITY ? m : m * kLn2;
@@ -299,7 +305,7 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_kernel(DecodeArgs A, int n
     }
     const uint32_t sO = smem_u32(&S.kv[0][0][0]);
     // rows that are not finite, key by key
-    for (int r = warp; r < R; r += kThreads / 32) {
+    for (int r = (S.bad[0] | S.bad[1] | S.bad[2] | S.bad[3]) ? warp : R; r < R; r += kThreads / 32) {
         if (!(S.bad[r >> 5] >> (r & 31) & 1u)) continue;
         constexpr int C = D / 32;
         const int t = S.row[r], end = min(S.cut[r], i1 * kKeys);
@@ -332,53 +338,89 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_kernel(DecodeArgs A, int n
             S.l[lane * lanes + r] = lane == 0 ? ll : 0.0f;
         }
     }
-    if (nrank > 1) cluster_sync(); else __syncthreads();
-    // The sum: a warp per row, in turn over the cluster's CTAs. Lane i has the i-th part's maximum and sum, the last one that of the row's own keys.
-    const int parts = nrank * copies;
-    for (int r = rank * (kThreads / 32) + warp; r < R; r += nrank * (kThreads / 32)) {
-        const int t = S.row[r];
-        const float* own = A.piece_of(t, h, 0, D);
-        float pm = -INFINITY, pl = 0.0f;
-        if (lane < parts) {
-            const int at = lane % copies * lanes + r;
-            pm = ld_cluster(map_rank(smem_u32(&S.m[at]), lane / copies));
-            pl = ld_cluster(map_rank(smem_u32(&S.l[at]), lane / copies));
+    auto factor = [](float m1, float l1, float top) { return m1 == -INFINITY ? (l1 == 0.0f ? 0.0f : 1.0f) : ex2((m1 - top) * kLog2e); };
+    auto add = [](float4& a, const float4& v, float g) { a.x += v.x * g; a.y += v.y * g; a.z += v.z * g; a.w += v.w * g; };
+    // a row's lane groups to the first of them: a thread per 16 bytes of O
+    if (copies > 1) {
+        __syncthreads();
+        auto join = [&](auto n_tag) {
+            constexpr int N = decltype(n_tag)::value;
+#pragma unroll 1
+            for (int i = tid; i < R * (D / 4); i += kThreads) {
+                const int r = i / (D / 4), part = i % (D / 4);
+                float cm[N], top = -INFINITY, sum = 0.0f;
+                float4 v[N], acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                for (int c = 0; c < N; ++c) {
+                    cm[c] = S.m[c * (128 / N) + r];
+                    v[c] = *reinterpret_cast<const float4*>(&S.kv[0][0][0] + o_part<D>(c * (128 / N) + r, part));
+                    top = fmaxf(top, cm[c]);
+                }
+#pragma unroll
+                for (int c = 0; c < N; ++c) {
+                    const float cl = S.l[c * (128 / N) + r], f = factor(cm[c], cl, top);
+                    if (f == 0.0f) continue;                      // (what a part without keys left may be anything)
+                    sum += cl * f;
+                    add(acc, v[c], f);
+                }
+                *reinterpret_cast<float4*>(&S.kv[0][0][0] + o_part<D>(r, part)) = acc;
+                if (part == 0) { S.joined_m[r] = top; S.joined_l[r] = sum; }
+            }
+        };
+        if (copies == 2) join(std::integral_constant<int, 2>{}); else join(std::integral_constant<int, 4>{});
+    }
+    const float *sM = copies > 1 ? S.joined_m : S.m, *sL = copies > 1 ? S.joined_l : S.l;
+    // The sum: a warp per row, in turn over the cluster's CTAs; the piece from the row's own keys is requested first.
+    float om = -INFINITY, ol = 0.0f;
+    float2 own0 = make_float2(0.0f, 0.0f), own1 = own0;
+    auto request = [&](int r) {
+        if (r >= R) return;
+        const float* own = A.piece_of(S.row[r], h, 0, D);
+        om = own[0];
+        ol = own[1];
+        if (lane < D / 4) {
+            own0 = *reinterpret_cast<const float2*>(own + 2 + lane * 4);
+            own1 = *reinterpret_cast<const float2*>(own + 4 + lane * 4);
         }
-        const float om = own[0], ol = own[1];
-        const float2 own0 = lane < D / 4 ? *reinterpret_cast<const float2*>(own + 2 + lane * 4) : make_float2(0.0f, 0.0f), own1 = lane < D / 4 ? *reinterpret_cast<const float2*>(own + 4 + lane * 4) : make_float2(0.0f, 0.0f);
+    };
+    request(warp * nrank + rank);
+    if (nrank > 1) cluster_sync(); else __syncthreads();
+    for (int r = warp * nrank + rank; r < R; r += nrank * (kThreads / 32)) {
+        const int t = S.row[r];
+        float pm = -INFINITY, pl = 0.0f;
+        float4 v[8];
+        if (lane < nrank) {                                       // lane i: of the i-th CTA
+            pm = ld_cluster(map_rank(smem_u32(&sM[r]), lane));
+            pl = ld_cluster(map_rank(smem_u32(&sL[r]), lane));
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < nrank) v[i] = ld_cluster4(map_rank(sO + o_part<D>(r, lane % (D / 4)), i));
         float top = pm;
 #pragma unroll
-        for (int x = 1; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-        top = fmaxf(top, om);
-        auto factor = [&](float m1, float l1) { return m1 == -INFINITY ? (l1 == 0.0f ? 0.0f : 1.0f) : ex2((m1 - top) * kLog2e); };
-        const float f = factor(pm, pl), of = factor(om, ol);
+        for (int x = 1; x < 8; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+        top = fmaxf(__shfl_sync(0xffffffffu, top, 0), om);
+        const float f = factor(pm, pl, top), of = factor(om, ol, top);
         float sum = f == 0.0f ? 0.0f : pl * f;
 #pragma unroll
-        for (int x = 1; x < 32; x <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+        for (int x = 1; x < 8; x <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+        sum = __shfl_sync(0xffffffffu, sum, 0);
         if (of != 0.0f) sum += ol * of;
         float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        auto add = [&](const float4& v, float g) { acc.x += v.x * g; acc.y += v.y * g; acc.z += v.z * g; acc.w += v.w * g; };
-        for (int i0 = 0; i0 < parts; i0 += 8) {
-            float4 v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int at = min(i0 + i, parts - 1);
-                v[i] = ld_cluster4(map_rank(sO + o_part<D>(at % copies * lanes + r, lane % (D / 4)), at / copies));
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float g = __shfl_sync(0xffffffffu, f, min(i0 + i, parts - 1));
-                if (i0 + i < parts && g != 0.0f) add(v[i], g);    // (what a part without keys left may be anything)
-            }
+        for (int i = 0; i < 8; ++i) {
+            const float g = __shfl_sync(0xffffffffu, f, i);
+            if (i < nrank && g != 0.0f) add(acc, v[i], g);
         }
         if (lane < D / 4) {
-            if (of != 0.0f) add(make_float4(own0.x, own0.y, own1.x, own1.y), of);
+            if (of != 0.0f) add(acc, make_float4(own0.x, own0.y, own1.x, own1.y), of);
             const float inv = 1.0f / sum;
             uint2 w = make_uint2(0u, 0u);
             if (sum != 0.0f) w = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
             *reinterpret_cast<uint2*>((__nv_bfloat16*)A.o + t * A.os_row + h * A.os_head + lane * 4) = w;
         }
         if (lane == 0) A.lse[t * A.Hq + h] = sum == 0.0f ? -INFINITY : top + logf(sum);
+        request(r + nrank * (kThreads / 32));
     }
     if (nrank > 1) cluster_sync();                                // (no CTA leaves while another may still read its sums)
     if (tid == 0 && S.abort_flag) atomicExch(A.status, (int32_t)DMA_ERR_DEVICE_TIMEOUT);
@@ -388,10 +430,11 @@ template <int D>
 int launch(const Cache& C, const DecodeArgs& A, int max_tiles, cudaStream_t st) {
     const int smem = (int)sizeof(Shared<D>) + 1024;
     if (cudaFuncSetAttribute(prefix_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return DMA_ERR_CUDA;
-    // as many CTAs per (tile, head) as two per SM give
-    const int64_t items = (int64_t)max_tiles * C.Hq;
+    // CTAs per (tile, head): as many as make three per SM, so that two are there although not every tile is, with 192 listed keys each at least (us of one rank and of two for 192 items of
+    // 1024 keys 46 and 36; of four and of eight for 48 items of 1000 keys 12.8 and 17.7).
+    const int64_t items = (int64_t)max_tiles * C.Hq, listed = std::min<int64_t>(C.w, A.order_ld);
     int ranks = 1;
-    while (ranks < 8 && items * ranks * 2 <= 2 * 148) ranks *= 2;
+    while (ranks < 8 && items * ranks * 2 <= 3 * 148 && ranks * 2 * 192 <= listed) ranks *= 2;
     return launch_overlapped(prefix_kernel<D>, dim3((unsigned)(items * ranks)), dim3(kThreads), smem, st, ranks, A, ranks);
 }
 

@@ -27,7 +27,7 @@ struct Order {
 // Rows for the selection, the lists' lengths, cleared counters. A CTA per prefix.
 __global__ void __launch_bounds__(256) order_rows_kernel(Order P, int32_t* seq, int32_t* pos, int32_t* status) {
     __shared__ int total;
-    pdl_enter(P.table, P.len, P.order_len, P.room, seq, pos, status);
+    pdl_enter();
     const int s = blockIdx.x, n = P.visible(s), blocks = (n + (1 << P.page_log) - 1) >> P.page_log;
     if (s == 0 && threadIdx.x < kWsHeaderBytes / 4) status[threadIdx.x] = 0;
     if (threadIdx.x == 0) total = 0;
@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(kThreads) order_sort_kernel(Order P) {
     __shared__ unsigned long long e[kChunk];
     __shared__ int count, base;
     const int tid = threadIdx.x, lane = tid & 31, chunk = blockIdx.x % P.chunks, item = blockIdx.x / P.chunks, s = item / P.Hq, h = item % P.Hq;
-    pdl_enter(P.delta, P.table, P.len, P.slot, P.weight, P.weakest, P.run, P.run_at, P.run_len, P.room);
+    pdl_enter();
     const int n = P.visible(s), j0 = chunk * kChunk, j1 = min(n, j0 + kChunk);
     const int32_t* pages = P.table + s * P.ld;
     const unsigned long long least = P.weakest ? P.weakest[item] : 0ull;
@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(kThreads) order_sort_kernel(Order P) {
 
 __global__ void __launch_bounds__(256) order_merge_kernel(Order P) {
     const int item = blockIdx.x / P.chunks, chunk = blockIdx.x % P.chunks, s = item / P.Hq;
-    pdl_enter(P.table, P.slot, P.weight, P.run, P.run_at, P.run_len);
+    pdl_enter();
     const unsigned long long* run = P.run + (size_t)item * P.cap;
     const int32_t *at = P.run_at + item * P.chunks, *len = P.run_len + item * P.chunks, *pages = P.table + s * P.ld;
     const int from = at[chunk], count = min(len[chunk], P.cap - from);

@@ -420,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
     extern __shared__ __align__(16) uint8_t dynamic[];            // of each warp [At::kStage][At::kPitch] keys, [room]: (pattern of delta, slot) of candidates by position, then of the kept ones
     __shared__ OwnShared S;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x / 32, team = kTeams ? warps_per_head : 1;
-    pdl_enter(A.q, A.kv, A.delta, A.table, A.seq, A.pos, A.prefix, A.order_slot, A.order_len, A.order_weight, A.o, A.lse, A.status, A.cut, A.piece, A.first, A.members, A.tiles, A.ntiles);
+    pdl_enter();
     if (blockIdx.x == gridDim.x - 1) {
         if (tid < kWsHeaderBytes / 4) A.status[tid] = 0;
         group_rows(A, reinterpret_cast<int*>(dynamic));

@@ -49,6 +49,7 @@ def close_rotation(got, x, pos, inv_freq, interleaved, scale, dtype, what):
 @pytest.mark.parametrize("rows,Hq,Hkv,d,page,dtype,rot,interleaved,wide", [
     (1, 1, 1, 64, 16, "bf16", 64, False, False), (1, 32, 8, 128, 64, "bf16", 128, False, True), (37, 8, 2, 128, 32, "bf16", 128, True, True), (37, 6, 2, 64, 16, "bf16", 32, False, True),
     (130, 5, 1, 128, 128, "bf16", 16, True, False), (1030, 32, 8, 128, 256, "bf16", 128, False, True), (9000, 4, 2, 64, 64, "bf16", 48, True, False),
+    (3, 76, 1, 128, 16, "bf16", 128, False, False), (40, 192, 2, 64, 16, "fp32", 32, True, False), (1500, 16, 8, 128, 64, "fp32", 128, True, True), (2000, 48, 16, 64, 128, "bf16", 64, False, True),
     (5, 7, 7, 128, 16, "fp32", 96, False, True), (333, 8, 2, 64, 32, "fp32", 64, True, True), (64, 12, 1, 128, 64, "fp32", 128, False, False)])
 def test_append(rows, Hq, Hkv, d, page, dtype, rot, interleaved, wide):
     rng = np.random.RandomState(rows + d)

@@ -84,6 +84,15 @@ def test_refused_appends(lib):
     assert f(0, *append_args(c, turn)[1:]) == -1
 
 
+@pytest.mark.parametrize("d,most", [(128, 76), (64, 96)])
+def test_most_heads_per_group_of_an_append(lib, d, most):
+    f, turn = dma._typed_fn("dma_cache_append"), dma.dma_rotation_t(4096, 64, 0, 0.0)
+    assert f(*append_args(cache(Hq=most + 1, Hkv=1, d=d), turn)) == -4
+    if not torch.cuda.is_available():
+        assert f(*append_args(cache(Hq=most, Hkv=1, d=d), turn)) == -6
+        assert f(*append_args(cache(Hq=most + 1, Hkv=1, d=d), turn, new=4096, ld=3)) == -6         # weights that are given
+
+
 def test_refused_orders_and_decodes(lib):
     c = cache()
     f = dma._typed_fn("dma_prefix_order")
