@@ -45,37 +45,36 @@ __global__ void __launch_bounds__(256) order_rows_kernel(Order P, int32_t* seq, 
     }
 }
 
-// f(pattern, position, slot) for the keys of [j0, j1) (multiples of 8), eight of a thread side by side in one page (pages have 16 keys and more); keys in pages outside the pool are left out.
+// f(order keys) for the keys of [j0, j1) (j0 a multiple of 16), sixteen of a thread side by side in one page (pages have 16 keys and more); 0 for places without a key.
 template <int NT, typename F>
 __device__ __forceinline__ void sweep(const Order& P, int s, int h, int j0, int j1, F f) {
     const int32_t* pages = P.table + s * P.ld;
     const int mask = (1 << P.page_log) - 1;
-    for (int b = j0; b < j1; b += NT * 8) {
-        const int j = b + threadIdx.x * 8, page = j < j1 ? pages[j >> P.page_log] : -1;
-        uint4 u[2];
+    auto page_of = [&](int j) { return j < j1 ? pages[j >> P.page_log] : -1; };
+    int next = page_of(j0 + threadIdx.x * 16);
+#pragma unroll 1
+    for (int b = j0; b < j1; b += NT * 16) {
+        const int j = b + threadIdx.x * 16, page = next;
         const bool there = (unsigned)page < (unsigned)P.num_pages;
-        if (there) {
-            const uint4* from = reinterpret_cast<const uint4*>(P.delta + (((size_t)page * P.Hq + h) << P.page_log) + (j & mask));
-            u[0] = from[0];
-            u[1] = from[1];
-        }
-        unsigned long long key[8];
+        uint32_t u[16];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint4& x = u[i / 4];
-            key[i] = there && j + i < j1 ? order_key((i % 4 == 0 ? x.x : i % 4 == 1 ? x.y : i % 4 == 2 ? x.z : x.w) & 0x7FFFFFFFu, j + i) : 0ull;
+        for (int i = 0; i < 16; i += 4) {
+            uint4 x = make_uint4(0u, 0u, 0u, 0u);
+            if (there) x = *reinterpret_cast<const uint4*>(P.delta + (((size_t)page * P.Hq + h) << P.page_log) + (j & mask) + i);
+            u[i] = x.x; u[i + 1] = x.y; u[i + 2] = x.z; u[i + 3] = x.w;
         }
-        f(key);
+        next = page_of(j + NT * 16);
+        f(u, j, there ? min(16, j1 - j) : 0);
     }
 }
 
-// The kept ones among a thread's keys to shared memory, in no order; `count` is moved on.
-template <int NT>
-__device__ __forceinline__ void collect(const unsigned long long (&key)[8], unsigned long long least, unsigned long long* to, int room, int* count) {
+// The kept ones among a thread's `n` keys from position j on to shared memory, in no order; `count` is moved on.
+__device__ __forceinline__ void collect(const uint32_t (&u)[16], int j, int n, unsigned long long least, unsigned long long* to, int room, int* count) {
     const int lane = threadIdx.x & 31;
-    int mine = 0;
+    uint32_t flags = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) mine += key[i] != 0 && key[i] >= least;
+    for (int i = 0; i < 16; ++i) flags |= (uint32_t)(i < n && order_key(u[i] & 0x7FFFFFFFu, j + i) >= least) << i;
+    const int mine = __popc(flags);
     int at = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -86,9 +85,9 @@ __device__ __forceinline__ void collect(const unsigned long long (&key)[8], unsi
     if (lane == 31 && at) base = atomicAdd(count, at);
     at += __shfl_sync(0xffffffffu, base, 31) - mine;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (key[i] != 0 && key[i] >= least) {
-            if (at < room) to[at] = key[i];
+    for (int i = 0; i < 16; ++i)
+        if (flags >> i & 1u) {
+            if (at < room) to[at] = order_key(u[i] & 0x7FFFFFFFu, j + i);
             ++at;
         }
 }
@@ -99,31 +98,17 @@ __device__ __forceinline__ void put(const Order& P, int item, int s, int place, 
     P.weight[item * P.order_ld + place] = __uint_as_float((uint32_t)(key >> 32));
 }
 
-// Lists of up to E * 1024 entries by a CTA per (prefix, head): what is kept is collected in shared memory and sorted by a bitonic network, E entries side by side per thread. Exchanges over fewer
-// than 32 E places stay in registers and shuffles; the others, 15 of 66 for 2048, go through shared memory.
-template <int E>
-__global__ void __launch_bounds__(1024) order_held_kernel(Order P) {
-    constexpr int NT = 1024, N = E * NT;
-    extern __shared__ unsigned long long e[];                     // [2][N]
-    __shared__ int count;
-    const int tid = threadIdx.x, item = blockIdx.x, s = item / P.Hq, h = item % P.Hq;
-    pdl_enter();
-    const int n = P.visible(s);
-    const unsigned long long least = P.weakest ? P.weakest[item] : 0ull;
-    if (tid == 0) count = 0;
-    for (int i = tid; i < N; i += NT) e[i] = 0;
-    __syncthreads();
-    sweep<NT>(P, s, h, 0, n, [&](const unsigned long long (&key)[8]) { collect<NT>(key, least, e, N, &count); });
-    __syncthreads();
-    unsigned long long v[E];
-#pragma unroll
-    for (int i = 0; i < E; ++i) v[i] = e[tid * E + i];
-    int buf = 1;
+// Numbers of a CTA, E side by side per thread, in descending order by a bitonic network; buf: 2 E NT places. Exchanges over fewer than 32 E places stay in registers and shuffles.
+template <int NT, int E>
+__device__ void sort_down(unsigned long long (&v)[E], unsigned long long* buf) {
+    constexpr int N = E * NT;
+    const int tid = threadIdx.x;
+    int which = 0;
 #pragma unroll 1
     for (int k = 2; k <= N; k *= 2) {
 #pragma unroll 1
         for (int x = k / 2; x >= 32 * E; x /= 2) {                // other warps'
-            unsigned long long* to = e + buf * N;
+            unsigned long long* to = buf + which * N;
 #pragma unroll
             for (int i = 0; i < E; ++i) to[i * NT + tid] = v[i];
             __syncthreads();
@@ -133,7 +118,7 @@ __global__ void __launch_bounds__(1024) order_held_kernel(Order P) {
                 const unsigned long long o = to[i * NT + (tid ^ x / E)];
                 v[i] = (o > v[i]) == high ? o : v[i];
             }
-            buf ^= 1;
+            which ^= 1;
         }
 #pragma unroll 1
         for (int x = min(k / 2, 16 * E); x >= E; x /= 2) {        // other lanes'
@@ -158,12 +143,95 @@ __global__ void __launch_bounds__(1024) order_held_kernel(Order P) {
                     }
             }
     }
-    const int c = min(count, P.cap);
-    unsigned long long* out = e + buf * N;
-#pragma unroll
-    for (int i = 0; i < E; ++i) out[i * NT + tid] = v[i];
+}
+
+// Lists of up to E * NT entries by a CTA per (prefix, head). What is kept is collected in shared memory, dealt into as many bins between the smallest and the largest weight as the list may
+// have entries, and ranked within its bin; where a bin has many (weights that crowd), sorted by a bitonic network instead (2048 entries: 6 us more).
+template <int NT, int E>
+__global__ void __launch_bounds__(NT) order_held_kernel(Order P) {
+    constexpr int N = E * NT, kCrowd = 48;
+    extern __shared__ unsigned long long e[];                     // [2][N] entries, [N] bins
+    __shared__ int count, crowd;
+    __shared__ uint32_t lowest, highest;
+    __shared__ int part[NT / 32];
+    int* bins = reinterpret_cast<int*>(e + 2 * N);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, item = blockIdx.x, s = item / P.Hq, h = item % P.Hq;
+    pdl_enter();
+    const int n = P.visible(s);
+    const unsigned long long least = P.weakest ? P.weakest[item] : 0ull;
+    if (tid == 0) { count = 0; crowd = 0; lowest = ~0u; highest = 0u; }
+    for (int i = tid; i < N; i += NT) bins[i] = 0;
     __syncthreads();
-    for (int i = tid; i < c; i += NT) put(P, item, s, i, out[i % E * NT + i / E]);
+    sweep<NT>(P, s, h, 0, n, [&](const uint32_t (&u)[16], int j, int m) { collect(u, j, m, least, e, N, &count); });
+    __syncthreads();
+    const int c = min(count, P.cap);
+    uint32_t lo = ~0u, hi = 0u;
+    for (int i = tid; i < c; i += NT) {
+        lo = min(lo, (uint32_t)(e[i] >> 32));
+        hi = max(hi, (uint32_t)(e[i] >> 32));
+    }
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    if (lane == 0) { atomicMin(&lowest, lo); atomicMax(&highest, hi); }
+    __syncthreads();
+    lo = lowest;
+    const float scale = (float)(N - 1) / fmaxf((float)(highest - lo), 1.0f);
+    auto bin_of = [&](unsigned long long key) { return N - 1 - min(N - 1, (int)((float)((uint32_t)(key >> 32) - lo) * scale)); };     // (the largest first; never falls as the weight does)
+    int where[E];                                                 // in its bin, as they come
+    int most = 0;
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+        if (i * NT + tid < c) {
+            where[i] = atomicAdd(&bins[bin_of(e[i * NT + tid])], 1);
+            most = max(most, where[i]);
+        }
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 0) atomicMax(&crowd, most);
+    __syncthreads();
+    if (crowd >= kCrowd) {
+        unsigned long long v[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] = tid * E + i < c ? e[tid * E + i] : 0ull;
+        __syncthreads();
+        sort_down<NT, E>(v, e);
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (tid * E + i < c) put(P, item, s, tid * E + i, v[i]);
+        return;
+    }
+    // bins to places
+    int mine[E], sum = 0;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        mine[i] = sum;
+        sum += bins[tid * E + i];
+    }
+    int x = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+    }
+    if (lane == 31) part[warp] = x;
+    __syncthreads();
+    int before = x - sum;
+    for (int i = 0; i < NT / 32; ++i) before += i < warp ? part[i] : 0;
+#pragma unroll
+    for (int i = 0; i < E; ++i) bins[tid * E + i] = before + mine[i];
+    __syncthreads();
+    unsigned long long* dealt = e + N;
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+        if (i * NT + tid < c) dealt[bins[bin_of(e[i * NT + tid])] + where[i]] = e[i * NT + tid];
+    __syncthreads();
+#pragma unroll 1
+    for (int i = tid; i < c; i += NT) {
+        const unsigned long long key = dealt[i];
+        const int bin = bin_of(key), from = bins[bin], to = bin + 1 < N ? bins[bin + 1] : c;
+        int place = from;
+        for (int o = from; o < to; ++o) place += dealt[o] > key;
+        put(P, item, s, place, key);
+    }
 }
 
 // Longer lists, and few long prefixes: chunks of kChunk positions, sorted in shared memory, and each entry's place as the sum of its places in all of them.
@@ -176,7 +244,7 @@ __global__ void __launch_bounds__(kThreads) order_sort_kernel(Order P) {
     const unsigned long long least = P.weakest ? P.weakest[item] : 0ull;
     if (tid == 0) count = 0;
     __syncthreads();
-    sweep<kThreads>(P, s, h, j0, j1, [&](const unsigned long long (&key)[8]) { collect<kThreads>(key, least, e, kChunk, &count); });
+    sweep<kThreads>(P, s, h, j0, j1, [&](const uint32_t (&u)[16], int j, int m) { collect(u, j, m, least, e, kChunk, &count); });
     __syncthreads();
     const int c = count;
     int size = 2;
@@ -281,9 +349,10 @@ int launch_prefix_order(const Cache& C0, const float* delta, const int32_t* tabl
     }
     const int64_t items = (int64_t)C.nseq * C.Hq;
     auto held = [&](auto e_tag) {
-        constexpr int E = decltype(e_tag)::value, smem = 2 * E * 1024 * 8;
-        if (cudaFuncSetAttribute(order_held_kernel<E>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return (int)DMA_ERR_CUDA;
-        return launch_overlapped(order_held_kernel<E>, dim3((unsigned)items), dim3(1024), smem, st, 1, P);
+        constexpr int E = decltype(e_tag)::value, NT = 1024, smem = E * NT * 20;
+        auto kernel = order_held_kernel<NT, E>;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return (int)DMA_ERR_CUDA;
+        return launch_overlapped(kernel, dim3((unsigned)items), dim3(NT), smem, st, 1, P);
     };
     if (L.cap <= 8192 && (L.chunks <= 16 || items >= 148)) {
         if (L.cap <= 1024) return held(std::integral_constant<int, 1>{});
