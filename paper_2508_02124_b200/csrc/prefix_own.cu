@@ -33,6 +33,8 @@ __device__ __forceinline__ float warp_max(float x) {              // (NaN only w
     asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 template <bool kTrans>
 __device__ __forceinline__ void ldmatrix(uint32_t (&r)[4], uint32_t addr) {
     if constexpr (kTrans) asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -58,9 +60,10 @@ struct Attend<float, D> {
             q[x] = row[x / 4 * 32 + (lane & 7) * 4 + x % 4] * scale;
         }
     }
-    __device__ __forceinline__ void stage(uint8_t* keys, const uint2* list, int count, int lane) {
-#pragma unroll 1
-        for (int i = 0; i < count; i += 4) {
+    float s[kStage / 4];                                          // of the keys lane / 8, lane / 8 + 4
+    __device__ __forceinline__ void scores(const uint8_t* keys, const uint2* list, int count, int lane) {
+#pragma unroll
+        for (int i = 0; i < kStage; i += 4) {
             const int e = i + (lane >> 3);
             const float* row = reinterpret_cast<const float*>(keys + e * kPitch) + (lane & 7) * 4;
             float s = 0.0f;
@@ -73,7 +76,15 @@ struct Attend<float, D> {
             }
 #pragma unroll
             for (int x = 1; x < 8; x <<= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
-            s = e < count ? s + __uint_as_float(list[e].x) : -INFINITY;
+            this->s[i / 4] = e < count ? s + __uint_as_float(list[e].x) : -INFINITY;
+        }
+    }
+    __device__ __forceinline__ void values(uint8_t* keys, int count, int lane) {
+#pragma unroll
+        for (int i = 0; i < kStage; i += 4) {
+            const int e = i + (lane >> 3);
+            const float* row = reinterpret_cast<const float*>(keys + e * kPitch) + (lane & 7) * 4;
+            const float s = this->s[i / 4];
             float top = fmaxf(s, __shfl_xor_sync(0xffffffffu, s, 8));
             top = fmaxf(m, fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16)));
             // (a NaN score leaves no maximum and makes the sum NaN; so does one of +inf)
@@ -124,25 +135,28 @@ struct Attend<__nv_bfloat16, D> {
             for (int y = 0; y < 2; ++y) q[x][y] = lane < 4 ? *reinterpret_cast<const uint32_t*>(row + x * 16 + y * 8 + lane * 2) : 0u;
         }
     }
-    __device__ __forceinline__ void stage(uint8_t* keys, const uint2* list, int count, int lane) {
+    float x0, x1;                                                 // of lane 4 i: the scores of keys i and i + 8, log2 units
+    __device__ __forceinline__ void scores(const uint8_t* keys, const uint2* list, int count, int lane) {
+        const uint32_t at_k = ptx::smem_u32(keys) + ((lane & 7) + ((lane >> 3) & 1) * 8) * kPitch + (lane >> 4) * 16;
+        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, s1[4] = {0.0f, 0.0f, 0.0f, 0.0f};       // (two chains)
+#pragma unroll
+        for (int x = 0; x < D / 16; x += 2) {
+            uint32_t a[4], b[4];
+            ldmatrix<false>(a, at_k + x * 32);
+            ldmatrix<false>(b, at_k + x * 32 + 32);
+            mma_16816(s, a, q[x][0], q[x][1]);
+            mma_16816(s1, b, q[x + 1][0], q[x + 1][1]);
+        }
+        const int e = lane >> 2;
+        x0 = (lane & 3) == 0 && e < count ? fmaf(s[0] + s1[0], c1, __uint_as_float(list[e].x) * 1.4426950408889634f) : -INFINITY;
+        x1 = (lane & 3) == 0 && e + 8 < count ? fmaf(s[2] + s1[2], c1, __uint_as_float(list[e + 8].x) * 1.4426950408889634f) : -INFINITY;
+    }
+    __device__ __forceinline__ void values(uint8_t* keys, int count, int lane) {
         if (count < kStage) {                                     // (0 times what lies there must be 0)
             for (int i = count * (D / 8) + lane; i < kStage * (D / 8); i += 32) *reinterpret_cast<uint4*>(keys + i / (D / 8) * kPitch + D * 2 + i % (D / 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
             __syncwarp();
         }
-        const uint32_t base = ptx::smem_u32(keys), at_k = base + ((lane & 7) + ((lane >> 3) & 1) * 8) * kPitch + (lane >> 4) * 16;
-        const uint32_t at_v = base + ((lane & 7) + (lane >> 4) * 8) * kPitch + D * 2 + ((lane >> 3) & 1) * 16;
-        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int x = 0; x < D / 16; ++x) {
-            uint32_t a[4];
-            ldmatrix<false>(a, at_k + x * 32);
-            mma_16816(s, a, q[x][0], q[x][1]);
-        }
-        // lane 4 i has the scores of keys i and i + 8
-        const int e = lane >> 2;
-        const bool real0 = (lane & 3) == 0 && e < count, real1 = (lane & 3) == 0 && e + 8 < count;
-        const float x0 = real0 ? fmaf(s[0], c1, __uint_as_float(list[e].x) * 1.4426950408889634f) : -INFINITY;
-        const float x1 = real1 ? fmaf(s[2], c1, __uint_as_float(list[e + 8].x) * 1.4426950408889634f) : -INFINITY;
+        const uint32_t at_v = ptx::smem_u32(keys) + ((lane & 7) + (lane >> 4) * 8) * kPitch + D * 2 + ((lane >> 3) & 1) * 16;
         const float top = fmaxf(m, warp_max(fmaxf(x0, x1)));
         if (top > m) {                                            // (the same in all lanes)
             if (m != -INFINITY) {
@@ -155,7 +169,7 @@ struct Attend<__nv_bfloat16, D> {
             }
             m = top;
         }
-        const float ref = m == -INFINITY ? 0.0f : m, p0 = real0 ? ptx::ex2(x0 - ref) : 0.0f, p1 = real1 ? ptx::ex2(x1 - ref) : 0.0f;
+        const float ref = m == -INFINITY ? 0.0f : m, p0 = ptx::ex2(x0 - ref), p1 = ptx::ex2(x1 - ref);
         l += p0 + p1;
         const int from = (lane & 3) * 8;
         float w[4] = {__shfl_sync(0xffffffffu, p0, from), __shfl_sync(0xffffffffu, p0, from + 4), __shfl_sync(0xffffffffu, p1, from), __shfl_sync(0xffffffffu, p1, from + 4)};
@@ -202,30 +216,31 @@ struct AttendAll {
 #pragma unroll
             for (int y = 0; y < 2; ++y) q[x][y] = real ? *reinterpret_cast<const uint32_t*>(row + x * 16 + y * 8 + (lane & 3) * 2) : 0u;
     }
-    // bias: of the lane's head, for the keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9 with c = lane % 4
-    __device__ __forceinline__ void stage(uint8_t* keys, const float (&bias)[4], int count, int lane) {
-        if (count < kStage) {                                     // (0 times what lies there must be 0)
-            for (int i = count * (D / 8) + lane; i < kStage * (D / 8); i += 32) *reinterpret_cast<uint4*>(keys + i / (D / 8) * kPitch + D * 2 + i % (D / 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
-            __syncwarp();
-        }
-        const uint32_t base = ptx::smem_u32(keys), at_k = base + ((lane & 7) + (lane >> 4) * 8) * kPitch + ((lane >> 3) & 1) * 16;
-        const uint32_t at_v = base + ((lane & 7) + ((lane >> 3) & 1) * 8) * kPitch + D * 2 + (lane >> 4) * 16;
+    float x[4];                                                   // scores of the keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9 with c = lane % 4; bias: of the same
+    __device__ __forceinline__ void scores(const uint8_t* keys, const float (&bias)[4], int count, int lane) {
+        const uint32_t at_k = ptx::smem_u32(keys) + ((lane & 7) + (lane >> 4) * 8) * kPitch + ((lane >> 3) & 1) * 16;
         float s[2][4] = {};
 #pragma unroll
-        for (int x = 0; x < D / 16; ++x) {
+        for (int y = 0; y < D / 16; ++y) {
             uint32_t b[4];
-            ldmatrix<false>(b, at_k + x * 32);
-            const uint32_t a[4] = {q[x][0], 0u, q[x][1], 0u};
+            ldmatrix<false>(b, at_k + y * 32);
+            const uint32_t a[4] = {q[y][0], 0u, q[y][1], 0u};
             mma_16816(s[0], a, b[0], b[1]);
             mma_16816(s[1], a, b[2], b[3]);
         }
-        float x[4], top = m;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int e = (lane & 3) * 2 + (i >> 1) * 8 + (i & 1);
             x[i] = e < count ? fmaf(s[i >> 1][i & 1], c1, bias[i] * 1.4426950408889634f) : -INFINITY;
-            top = fmaxf(top, x[i]);
         }
+    }
+    __device__ __forceinline__ void values(uint8_t* keys, int count, int lane) {
+        if (count < kStage) {                                     // (0 times what lies there must be 0)
+            for (int i = count * (D / 8) + lane; i < kStage * (D / 8); i += 32) *reinterpret_cast<uint4*>(keys + i / (D / 8) * kPitch + D * 2 + i % (D / 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            __syncwarp();
+        }
+        const uint32_t at_v = ptx::smem_u32(keys) + ((lane & 7) + ((lane >> 3) & 1) * 8) * kPitch + D * 2 + (lane >> 4) * 16;
+        float top = fmaxf(fmaxf(m, fmaxf(x[0], x[1])), fmaxf(x[2], x[3]));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
         if (__any_sync(0xffffffffu, top > m)) {
@@ -412,7 +427,7 @@ __device__ __forceinline__ void write_own(const DecodeArgs& A, int t, int h, boo
     }
 }
 
-// A CTA per (row, KV head); the last one groups the rows by prefix. The group's heads each have a warp or a team of them (kTeams; else up to eight heads at a time, the others
+// A CTA per (row, KV head); the first one groups the rows by prefix. The group's heads each have a warp or a team of them (kTeams; else up to eight heads at a time, the others
 // in turn). Where a row keeps all keys whatever their weights, the warps share its own keys, all heads together.
 template <typename T, int D, bool kTeams>
 __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warps_per_head, int room, int heads) {       // heads: of a CTA
@@ -421,12 +436,12 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
     __shared__ OwnShared S;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x / 32, team = kTeams ? warps_per_head : 1;
     pdl_enter();
-    if (blockIdx.x == gridDim.x - 1) {
+    if (blockIdx.x == 0) {                                        // (first: it is done while the others are at work)
         if (tid < kWsHeaderBytes / 4) A.status[tid] = 0;
         group_rows(A, reinterpret_cast<int*>(dynamic));
         return;
     }
-    const int parts = (A.G + heads - 1) / heads, t = blockIdx.x / (A.Hkv * parts), hk = blockIdx.x / parts % A.Hkv, head0 = blockIdx.x % parts * heads, head1 = min(A.G, head0 + heads);
+    const int parts = (A.G + heads - 1) / heads, item = blockIdx.x - 1, t = item / (A.Hkv * parts), hk = item / parts % A.Hkv, head0 = item % parts * heads, head1 = min(A.G, head0 + heads);
     const int r = A.seq[t], p = A.pos[t], g = A.nprefix ? A.prefix[t] : -1;
     if ((unsigned)r >= (unsigned)A.nseq) return;
     const int n = min(max(p, -1), (A.max_blocks << A.page_log) - 1) + 1;
@@ -438,7 +453,7 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
     int listed = 0;
     if ((unsigned)g < (unsigned)A.nprefix) listed = (int)max((int64_t)0, min((int64_t)min(A.order_len[g], A.w), A.order_ld));
     const bool behind = listed > 0, floored = listed == A.w;      // (as DecodeArgs::listed)
-    constexpr int kParts = 2 * D * (int)sizeof(T) / 16, kTogether = kParts < 32 ? 32 / kParts : 1;       // 16-byte parts of a key, keys per instruction
+    constexpr int kRow = D * (int)sizeof(T);                      // bytes of K's row, and of V's
 
     if constexpr (sizeof(T) == 2) {
         if ((int64_t)listed + n <= A.w) {
@@ -455,19 +470,28 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
                     next = j + warps * 16 < n ? pages[(j + warps * 16) >> A.page_log] : -1;
                     if ((unsigned)page >= (unsigned)A.num_pages) continue;
                     const uint8_t* from = (const uint8_t*)(kv + key_row(page, hk, j & mask, A.Hkv, A.page_log) * (2 * D));
-                    const uint32_t to = ptx::smem_u32(keys_at);
+                    auto copy = [&](int which) {
 #pragma unroll
-                    for (int i = lane; i < 16 * kParts; i += 32)
-                        if (i / kParts < count) ptx::cp_async16_at(to + i / kParts * At::kPitch + i % kParts * 16, from + i * 16);
+                        for (int i = lane; i < kRow; i += 32) {   // 16 rows of kRow / 16 parts
+                            const int e = i / (kRow / 16), x = which * kRow + i % (kRow / 16) * 16;
+                            if (e < count) ptx::cp_async16_at(ptx::smem_u32(keys_at) + e * At::kPitch + x, from + e * 2 * kRow + x);
+                        }
+                        cp_async_commit();
+                    };
+                    copy(0);
+                    copy(1);
                     float bias[4] = {};
                     const float* delta = A.delta + (((size_t)page * A.Hq + h) << A.page_log) + (j & mask) + (lane & 3) * 2;
                     if (real) {
                         const float2 u = *reinterpret_cast<const float2*>(delta), v = *reinterpret_cast<const float2*>(delta + 8);
                         bias[0] = u.x; bias[1] = u.y; bias[2] = v.x; bias[3] = v.y;
                     }
-                    ptx::cp_async_wait_all();
+                    cp_async_wait<1>();
                     __syncwarp();
-                    at.stage(keys_at, bias, count, lane);
+                    at.scores(keys_at, bias, count, lane);
+                    cp_async_wait<0>();
+                    __syncwarp();
+                    at.values(keys_at, count, lane);
                     __syncwarp();
                 }
                 float* o = reinterpret_cast<float*>(keys_at);     // [8][D]
@@ -567,8 +591,38 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
     unsigned long long least = 0;                                 // kept: the order keys that are not below
     auto place = [&](int e) { return in_team * (1 << 20) + e; };
     if (k < listed + cands) {
-        constexpr int kSorted = 256;
-        if (!over && cands <= kSorted) {
+        constexpr int kSorted = 256, kDrops = 16;
+        bool done = false;
+        if (!kTeams && floored && !over && cands <= 128) {
+            // Few of a warp's candidates fail against a full list: the lowest one is dropped as long as the list's entry that it has to beat is not below it. (k = listed: the i-th best against the
+            // i-th entry from the end.)
+            unsigned long long keys[4];
+            uint32_t last[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int e = 32 * i + lane;
+                last[i] = e < cands && e < listed ? __float_as_uint(weight[listed - 1 - e]) & 0x7FFFFFFFu : ~0u;
+                keys[i] = e < c ? order_key(mine[e].x, place(e)) : ~0ull;
+            }
+            for (int kept = cands; kept >= cands - kDrops && !done; --kept) {
+                unsigned long long low = keys[0] < keys[1] ? keys[0] : keys[1];
+                const unsigned long long other = keys[2] < keys[3] ? keys[2] : keys[3];
+                low = other < low ? other : low;
+                const uint32_t hi = __reduce_min_sync(0xffffffffu, (uint32_t)(low >> 32)), lo = __reduce_min_sync(0xffffffffu, (uint32_t)(low >> 32) == hi ? (uint32_t)low : ~0u);
+                const int back = max(kept - 1, 0);
+                const uint32_t a = back & 32 ? last[1] : last[0], b = back & 32 ? last[3] : last[2], rival = __shfl_sync(0xffffffffu, back & 64 ? b : a, back & 31);
+                if (kept == 0 || rival < hi) {
+                    done = true;
+                    least = kept == 0 ? ~0ull : (unsigned long long)hi << 32 | lo;
+                    cut = k - kept;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) keys[i] = keys[i] == ((unsigned long long)hi << 32 | lo) ? ~0ull : keys[i];
+                }
+            }
+        }
+        if (done) {
+        } else if (!over && cands <= kSorted) {
             // The best own key is kept if the list's last entry is below it, the second if the last but one is, and so on: the own keys in descending order against the list from its end on
             // (the k - listed best ones are kept anyway). By the team's first warp.
             if (in_team == 0) {
@@ -716,23 +770,38 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
             kept += __popc(bits);
             __syncwarp();
         }
+        // eight lanes take 128 bytes of a key at a time; K's rows and V's are groups of their own, the next stage's K on its way while this one's V is used
+        auto copy = [&](int i, int which) {
+            const uint32_t to = ptx::smem_u32(keys_at) + which * kRow + (lane & 7) * 16;
+#pragma unroll
+            for (int e0 = 0; e0 < At::kStage; e0 += 4) {
+                const int e = i + e0 + (lane >> 3);
+                if (e < kept) {
+                    const int slot = (int)mine[e].y;
+                    const uint8_t* from = (const uint8_t*)(kv + key_row(slot >> A.page_log, hk, slot & mask, A.Hkv, A.page_log) * (2 * D)) + which * kRow + (lane & 7) * 16;
+#pragma unroll
+                    for (int x = 0; x < kRow; x += 128) ptx::cp_async16_at(to + (e0 + (lane >> 3)) * At::kPitch + x, from + x);
+                }
+            }
+            cp_async_commit();
+        };
+        if (kept) {
+            copy(0, 0);
+            copy(0, 1);
+        }
 #pragma unroll 1
         for (int i = 0; i < kept; i += At::kStage) {
-            const int count = min(kept - i, At::kStage), slot = lane < count ? (int)mine[i + lane].y : 0;
-            const size_t row = key_row(slot >> A.page_log, hk, slot & mask, A.Hkv, A.page_log);
-            const uint32_t to = ptx::smem_u32(keys_at);
-#pragma unroll 4
-            for (int e0 = 0; e0 < count; e0 += kTogether) {
-                const int e = e0 + (kTogether > 1 ? lane / kParts : 0);
-                const uint8_t* from = (const uint8_t*)kv + __shfl_sync(0xffffffffu, row, e) * (2 * D * sizeof(T));
-#pragma unroll
-                for (int part = lane % kParts; part < kParts; part += 32)
-                    if (kTogether == 1 || e < count) ptx::cp_async16_at(to + e * At::kPitch + part * 16, from + part * 16);
-            }
-            ptx::cp_async_wait_all();
+            const int count = min(kept - i, At::kStage);
+            cp_async_wait<1>();
             __syncwarp();
-            at.stage(keys_at, mine + i, count, lane);
+            at.scores(keys_at, mine + i, count, lane);
             __syncwarp();
+            copy(i + At::kStage, 0);
+            cp_async_wait<1>();
+            __syncwarp();
+            at.values(keys_at, count, lane);
+            __syncwarp();
+            copy(i + At::kStage, 1);
         }
     }
     at.end(reinterpret_cast<float*>(keys_at), lane);
