@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(256) simt_sum_kernel(DecodeArgs A) {
 }
 
 struct Layout {
-    size_t cut, least, piece, first, members, tiles, ntiles, total;
+    size_t cut, piece, first, members, tiles, ntiles, total;
     int pieces, tile_rows, max_tiles;
     bool simt;
     Layout(const Cache& C, int nprefix) {
@@ -122,7 +122,6 @@ struct Layout {
         size_t x = kWsHeaderBytes;
         auto take = [&](size_t bytes) { const size_t at = x; x += (bytes + 255) / 256 * 256; return at; };
         cut = take((size_t)C.rows * C.Hq * 4);
-        least = take((size_t)C.rows * C.Hq * 8);
         piece = take((size_t)C.rows * C.Hq * pieces * (C.d + 2) * 4);
         first = take((size_t)(nprefix + 1) * 4);
         members = take((size_t)max_tiles * tile_rows * 4);
@@ -153,10 +152,9 @@ int launch_cache_decode(const Cache& C, const void* q, const void* kv, const flo
     const Layout L(C, nprefix);
     char* p = (char*)ws;
     const DecodeArgs A = {q, kv, delta, table, row_seq, row_pos, row_prefix, order_slot, order_len, order_weight, o, lse, C.table_ld, order_ld, C.qs[0], C.qs[1], C.os[0], C.os[1],
-                          C.scale, C.rows, C.nseq, nprefix, C.Hq, C.Hkv, C.G, C.w, C.page_log, C.num_pages, C.max_blocks, (int32_t*)p, (int*)(p + L.cut), (unsigned long long*)(p + L.least), (float*)(p + L.piece),
+                          C.scale, C.rows, C.nseq, nprefix, C.Hq, C.Hkv, C.G, C.w, C.page_log, C.num_pages, C.max_blocks, (int32_t*)p, (int*)(p + L.cut), (float*)(p + L.piece),
                           L.pieces, (int*)(p + L.first), (int*)(p + L.members), (int4*)(p + L.tiles), (int*)(p + L.ntiles), L.tile_rows};
-    int rc = launch_cuts(C, A, st);
-    if (!rc) rc = launch_own_keys(C, A, st);
+    const int rc = launch_own_keys(C, A, st);
     if (rc || nprefix == 0) return rc;
     return L.simt ? launch_prefix_simt(C, A, L.max_tiles, st) : launch_prefix_tc(C, A, L.max_tiles, st);
 }

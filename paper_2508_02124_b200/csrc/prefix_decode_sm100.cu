@@ -155,8 +155,7 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_kernel(DecodeArgs A, int n
         fence_barrier_init();
     }
     if (tid < 4) S.bad[tid] = 0;
-    // This kernel may run beside the one before it, which waited for all that is read here: the cuts, the tiles, the call's inputs. Of that one's own results, the pieces, nothing is
-    // touched before the wait below.
+    pdl_enter();
     const int ntiles_all = *A.ntiles, member = tid < 128 ? A.members[tile * 128 + tid] : 0;
     const int4 rows = A.tiles[tile];
     if (warp == kIssuer) {                                        // (while these are on their way)
@@ -166,7 +165,6 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_kernel(DecodeArgs A, int n
     if (tile >= ntiles_all) {                                     // (all CTAs of the cluster)
         __syncwarp();
         if (warp == kIssuer) tmem_dealloc(S.tmem, 256);
-        pdl_enter();                                              // (this kernel does not end before the one before it has)
         return;
     }
     const int R = rows.y, listed = rows.z, copy_log = R <= 32 ? 2 : R <= 64 ? 1 : 0, copies = 1 << copy_log, lane_log = 7 - copy_log, lanes = 1 << lane_log;
@@ -385,7 +383,6 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_kernel(DecodeArgs A, int n
             own1 = *reinterpret_cast<const float2*>(own + 4 + lane * 4);
         }
     };
-    pdl_enter();
     request(warp * nrank + rank);
     if (nrank > 1) cluster_sync(); else __syncthreads();
     for (int r = warp * nrank + rank; r < R; r += nrank * (kThreads / 32)) {

@@ -1,9 +1,11 @@
-// Second step of dma_cache_decode (include/dma.h): the rows' attention over their own keys that they keep.
+// First half of dma_cache_decode (include/dma.h): what every row keeps of its prefix' order and of its own keys, and the attention over the latter.
 //
-// A warp, or a team of them, per (row, query head): its part of the keys' weights is read again, the kept ones' slots listed, their rows fetched 16 at a time and multiplied. Where a row
-// keeps all keys, whatever their weights, a group's heads share the work: every warp takes 16 keys in turn, for all of them.
-// FIG
+// The cut. A row's head keeps k = min(w, listed + own) keys of the merged order. Entry m of the prefix' order has m entries before it and every own key that is greater; so the
+// prefix' part ends with the first m for which m + #{own > weight_m} >= k, a bisection (ties: the prefix' keys come first), and the own part is the k - m best of the row's own
+// keys, a bisection over their order keys between the weights around the cut. Where the list has w entries, own keys that do not exceed its last cannot be kept and are left out
+// at once: of n own keys behind a prefix of N about n w / N remain. They lie in shared memory, where every count is a sweep by one warp.
 #include <algorithm>
+#include <type_traits>
 
 #include "cache4_decode.cuh"
 #include "delta_fixed.cuh"
@@ -13,12 +15,19 @@
 namespace dma {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32, kRoom = 640;         // kept keys of a warp: a sweep's 512 more than what waits for the next one
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 
+// A team of 1, 2, 4 or 8 warps has a (row, head), each warp a part of the own keys.
 struct OwnShared {
+    unsigned long long least[kWarps];
+    int part[2][kWarps], cands[kWarps], cut[kWarps];
     float m[kWarps], l[kWarps], all_m[kWarps][8], all_l[kWarps][8];
 };
 
+__device__ __forceinline__ void team_sync(int id, int threads) {
+    if (threads > 32) asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+    else __syncwarp();
+}
 __device__ __forceinline__ float warp_max(float x) {              // (NaN only where all are)
     float y;
     asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
@@ -274,9 +283,133 @@ struct AttendAll {
     }
 };
 
+// The rows by prefix, in the order of rows, and tiles of them.
+__device__ void group_rows(const DecodeArgs& A, int* turn) {       // turn: kTogether per thread
+    constexpr int kTogether = 4;                                  // rows of a thread requested together
+    __shared__ int part[kWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x;
+    if (A.nprefix == 0) {
+        if (tid == 0) *A.ntiles = 0;
+        return;
+    }
+    // f(row, its prefix or -1) for kTogether rows at a time, thread by thread
+    auto turns = [&](auto f) {
+        for (int b = 0; b < A.rows; b += threads * kTogether) {
+            int r[kTogether], g[kTogether], n[kTogether];
+#pragma unroll
+            for (int i = 0; i < kTogether; ++i) {
+                const int t = b + i * threads + tid;
+                r[i] = g[i] = -1;
+                if (t < A.rows) { r[i] = A.seq[t]; g[i] = A.prefix[t]; }
+            }
+#pragma unroll
+            for (int i = 0; i < kTogether; ++i) {
+                if ((unsigned)r[i] >= (unsigned)A.nseq || (unsigned)g[i] >= (unsigned)A.nprefix) g[i] = -1;
+                n[i] = g[i] >= 0 ? A.order_len[g[i]] : 0;
+            }
+#pragma unroll
+            for (int i = 0; i < kTogether; ++i) g[i] = n[i] > 0 ? g[i] : -1;
+            f(b, g);
+        }
+    };
+    for (int i = tid; i <= A.nprefix; i += threads) A.first[i] = 0;
+    __syncthreads();
+    turns([&](int, const int (&g)[kTogether]) {
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i)
+            if (g[i] >= 0) atomicAdd(&A.first[g[i]], 1);
+    });
+    __syncthreads();
+    int tile_carry = 0;
+    for (int b = 0; b < A.nprefix; b += threads) {
+        const int g = b + tid, n = g < A.nprefix ? __ldcg(&A.first[g]) : 0, nt = (n + A.tile_rows - 1) / A.tile_rows;
+        int y = nt;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, y, o);
+            if (lane >= o) y += v;
+        }
+        if (lane == 31) part[warp] = y;
+        __syncthreads();
+        int tiles_before = 0, all_tiles = 0;
+        for (int i = 0; i < threads / 32; ++i) {
+            tiles_before += i < warp ? part[i] : 0;
+            all_tiles += part[i];
+        }
+        if (g < A.nprefix) {
+            const int tile = tile_carry + tiles_before + y - nt;
+            __stcg(&A.first[g], tile * A.tile_rows);
+            const int listed = nt ? (int)min((int64_t)min(A.order_len[g], A.w), A.order_ld) : 0;
+            for (int i = 0; i < nt; ++i) A.tiles[tile + i] = make_int4(g, min(A.tile_rows, n - i * A.tile_rows), listed, 0);
+        }
+        tile_carry += all_tiles;
+        __syncthreads();
+    }
+    if (tid == 0) *A.ntiles = tile_carry;
+    // a turn's rows of the same prefix follow one another, the first of them moves the prefix' start on
+    turns([&](int b, const int (&g)[kTogether]) {
+        const int count = min(A.rows - b, threads * kTogether);
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i) turn[i * threads + tid] = g[i];
+        __syncthreads();
+        int rank[kTogether] = {}, same[kTogether] = {}, start[kTogether];
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i) start[i] = g[i] >= 0 ? __ldcg(&A.first[g[i]]) : 0;
+        for (int e = 0; e < count; ++e) {
+            const int x = turn[e];
+#pragma unroll
+            for (int i = 0; i < kTogether; ++i) {
+                same[i] += x == g[i];
+                rank[i] += x == g[i] && e < i * threads + tid;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i)
+            if (g[i] >= 0) {
+                A.members[start[i] + rank[i]] = b + i * threads + tid;
+                if (rank[i] == 0) __stcg(&A.first[g[i]], start[i] + same[i]);
+            }
+        __syncthreads();
+    });
+}
+
+// R * 32 numbers of a warp in descending order, number i * 32 + lane in v[i].
+template <int R>
+__device__ __forceinline__ void sort_down(uint32_t (&v)[R], int lane) {
+    auto lanes = [&](int k, int j) {                              // pairs that j < 32 lanes part, in runs of k
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const uint32_t o = __shfl_xor_sync(0xffffffffu, v[i], j);
+            const bool up = ((lane & j) == 0) == (((i * 32 + lane) & k) == 0);
+            v[i] = up ? max(v[i], o) : min(v[i], o);
+        }
+    };
+#pragma unroll 1
+    for (int k = 2; k <= 32; k *= 2)
+#pragma unroll 1
+        for (int j = k / 2; j > 0; j /= 2) lanes(k, j);
+#pragma unroll
+    for (int k = 64; k <= 32 * R; k *= 2) {
+#pragma unroll
+        for (int j = k / 2; j >= 32; j /= 2)
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                if (!(i & (j / 32))) {
+                    const int o = i | (j / 32);
+                    const uint32_t a = v[i], b = v[o];
+                    const bool down = ((i * 32) & k) == 0;
+                    v[i] = down ? max(a, b) : min(a, b);
+                    v[o] = down ? min(a, b) : max(a, b);
+                }
+#pragma unroll 1
+        for (int j = 16; j > 0; j /= 2) lanes(k, j);
+    }
+}
+
 // The sums of a row's own keys, D / 32 channels per lane: its piece, or its result where there is no prefix.
 template <typename T, int D>
-__device__ __forceinline__ void write_own(const DecodeArgs& A, int t, int h, bool behind, float top, float sum, const float (&o)[D / 32], int lane) {
+__device__ __forceinline__ void write_own(const DecodeArgs& A, int t, int h, bool behind, int cut, float top, float sum, const float (&o)[D / 32], int lane) {
     if (behind) {
         float* out = A.piece_of(t, h, 0, D);
 #pragma unroll
@@ -284,6 +417,7 @@ __device__ __forceinline__ void write_own(const DecodeArgs& A, int t, int h, boo
         if (lane == 0) {
             out[0] = top;
             out[1] = sum;
+            A.cut[t * A.Hq + h] = cut;
         }
     } else {
         T* out = (T*)A.o + t * A.os_row + h * A.os_head;
@@ -293,37 +427,47 @@ __device__ __forceinline__ void write_own(const DecodeArgs& A, int t, int h, boo
     }
 }
 
-// A CTA per (row, KV head) or part of its heads.
+// A CTA per (row, KV head); the first one groups the rows by prefix. The group's heads each have a warp or a team of them (kTeams; else up to eight heads at a time, the others
+// in turn). Where a row keeps all keys whatever their weights, the warps share its own keys, all heads together.
 template <typename T, int D, bool kTeams>
-__global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warps_per_head, int heads) {
+__global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warps_per_head, int room, int heads) {       // heads: of a CTA
     using At = Attend<T, D>;
-    constexpr int kStageBytes = At::kStage * At::kPitch;
-    extern __shared__ __align__(16) uint8_t dynamic[];            // of each warp [At::kStage][At::kPitch] keys, [kRoom]: (pattern of delta, slot) of kept keys
+    extern __shared__ __align__(16) uint8_t dynamic[];            // of each warp [At::kStage][At::kPitch] keys, [room]: (pattern of delta, slot) of candidates by position, then of the kept ones
     __shared__ OwnShared S;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x / 32, team = kTeams ? warps_per_head : 1;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x / 32, team = kTeams ? warps_per_head : 1;
     pdl_enter();
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // (the prefixes' attention needs nothing of this kernel before its last step)
-    OwnRow R;
-    if (!R.find(A, blockIdx.x, heads)) return;
-    const int t = R.t, hk = R.hk, n = R.n, listed = R.listed, mask = (1 << A.page_log) - 1;
+    if (blockIdx.x == 0) {                                        // (first: it is done while the others are at work)
+        if (tid < kWsHeaderBytes / 4) A.status[tid] = 0;
+        group_rows(A, reinterpret_cast<int*>(dynamic));
+        return;
+    }
+    const int parts = (A.G + heads - 1) / heads, item = blockIdx.x - 1, t = item / (A.Hkv * parts), hk = item / parts % A.Hkv, head0 = item % parts * heads, head1 = min(A.G, head0 + heads);
+    const int r = A.seq[t], p = A.pos[t], g = A.nprefix ? A.prefix[t] : -1;
+    if ((unsigned)r >= (unsigned)A.nseq) return;
+    const int n = min(max(p, -1), (A.max_blocks << A.page_log) - 1) + 1;
+    const int32_t* pages = A.table + r * A.ld;
+    const int mask = (1 << A.page_log) - 1;
     const T* kv = (const T*)A.kv;
+    constexpr int kStageBytes = At::kStage * At::kPitch;
     uint8_t* keys_at = dynamic + warp * kStageBytes;
-    const bool behind = listed > 0;
+    int listed = 0;
+    if ((unsigned)g < (unsigned)A.nprefix) listed = (int)max((int64_t)0, min((int64_t)min(A.order_len[g], A.w), A.order_ld));
+    const bool behind = listed > 0, floored = listed == A.w;      // (as DecodeArgs::listed)
     constexpr int kRow = D * (int)sizeof(T);                      // bytes of K's row, and of V's
 
     if constexpr (sizeof(T) == 2) {
-        if (R.keeps_all(A)) {
-            for (int g0 = R.head0; g0 < R.head1; g0 += 8) {
+        if ((int64_t)listed + n <= A.w) {
+            for (int g0 = head0; g0 < head1; g0 += 8) {
                 const int mine = g0 + (lane >> 2), h = hk * A.G + mine;
-                const bool real = mine < R.head1;
+                const bool real = mine < head1;
                 AttendAll<D> at;
                 at.start((const T*)A.q + t * A.qs_row + h * A.qs_head, real, A.scale, lane);
                 // 16 keys at a time, side by side in one page, turn by turn of the warps
-                int next = warp * 16 < n ? R.pages[warp * 16 >> A.page_log] : -1;
+                int next = warp * 16 < n ? pages[warp * 16 >> A.page_log] : -1;
 #pragma unroll 1
                 for (int j = warp * 16; j < n; j += warps * 16) {
                     const int page = next, count = min(n - j, 16);
-                    next = j + warps * 16 < n ? R.pages[(j + warps * 16) >> A.page_log] : -1;
+                    next = j + warps * 16 < n ? pages[(j + warps * 16) >> A.page_log] : -1;
                     if ((unsigned)page >= (unsigned)A.num_pages) continue;
                     const uint8_t* from = (const uint8_t*)(kv + key_row(page, hk, j & mask, A.Hkv, A.page_log) * (2 * D));
                     auto copy = [&](int which) {
@@ -357,7 +501,7 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
                     S.all_l[warp][lane >> 2] = at.l;
                 }
                 __syncthreads();
-                for (int y = warp; y < min(8, R.head1 - g0); y += warps) {
+                for (int y = warp; y < min(8, head1 - g0); y += warps) {
                     const int head = hk * A.G + g0 + y;
                     float top = -INFINITY, sum = 0.0f, out[D / 32] = {};
                     for (int w = 0; w < warps; ++w) top = fmaxf(top, S.all_m[w][y]);
@@ -368,24 +512,264 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
 #pragma unroll
                         for (int x = 0; x < D / 32; ++x) out[x] += reinterpret_cast<const float*>(dynamic + w * kStageBytes)[y * D + lane + 32 * x] * f;
                     }
-                    write_own<T, D>(A, t, head, behind, top, sum, out, lane);
+                    write_own<T, D>(A, t, head, behind, listed, top, sum, out, lane);
                 }
                 __syncthreads();
             }
             return;
         }
     }
-    const int in_team = kTeams ? warp % team : 0, bar = 1 + warp / team;
-    uint2* mine = reinterpret_cast<uint2*>(dynamic + warps * kStageBytes) + warp * kRoom;
+    const int in_team = kTeams ? warp % team : 0, leader = warp - in_team, bar = 1 + warp / team;
+    uint2* found = reinterpret_cast<uint2*>(dynamic + warps * kStageBytes);
+    uint2* mine = found + warp * room;
     const int seg = (n + team * 64 - 1) / (team * 64) * 64, j0 = min(n, in_team * seg), j1 = min(n, j0 + seg);
 #pragma unroll 1
-    for (int head = R.head0 + warp / team; head < R.head1; head += warps / team) {
+    for (int head = head0 + warp / team; head < head1; head += warps / team) {
     const int h = hk * A.G + head;
-    const unsigned long long least = A.least[t * A.Hq + h];
+    const float* weight = A.order_weight + ((int64_t)g * A.Hq + h) * A.order_ld;
+    // f(position, slot, patterns) for the part's keys, 512 at a time: a lane has 16 of them, side by side in one page (pages have 16 keys and more). Patterns of places without a key: -2
+    auto sweep = [&](auto f) {
+        auto page_of = [&](int j) { return j < j1 ? pages[j >> A.page_log] : -1; };
+        int next = page_of(j0 + 16 * lane);
+#pragma unroll 1
+        for (int b = j0; b < j1; b += 512) {
+            const int j = b + 16 * lane, page = next, slot = (page << A.page_log) + (j & mask);
+            const bool there = (unsigned)page < (unsigned)A.num_pages;
+            int u[16];
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                int4 x = make_int4(-2, -2, -2, -2);
+                if (there) x = *reinterpret_cast<const int4*>(A.delta + (((size_t)page * A.Hq + h) << A.page_log) + (j & mask) + i);
+                u[i] = x.x; u[i + 1] = x.y; u[i + 2] = x.z; u[i + 3] = x.w;
+            }
+            next = page_of(j + 512);
+            if (b + 512 > j1)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) u[i] = j + i < j1 ? u[i] : -2;
+            f(j, slot, u);
+        }
+    };
     At at;
     at.start((const T*)A.q + t * A.qs_row + h * A.qs_head, A.scale, lane);
-    int kept = 0;
-    auto attend = [&]() {
+    // what may be kept: every key that there is, or those above the list's last entry
+    const int floor = floored ? __float_as_int(weight[listed - 1]) & 0x7FFFFFFF : -1;
+    int c = 0;
+    sweep([&](int, int slot, const int (&u)[16]) {
+        int count = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) count += u[i] > floor;
+        int to = count;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, to, o);
+            if (lane >= o) to += y;
+        }
+        const int total = __shfl_sync(0xffffffffu, to, 31);
+        to += c - count;
+        if (to + count <= room) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (u[i] > floor) mine[to++] = make_uint2((uint32_t)u[i], (uint32_t)(slot + i));
+        }
+        c += total;
+    });
+    if (lane == 0) S.cands[warp] = c;
+    __syncwarp();
+    int cands = c, most = c, step = 0;
+    if (team > 1) {
+        team_sync(bar, team * 32);
+        cands = most = 0;
+        for (int i = 0; i < team; ++i) {
+            cands += S.cands[leader + i];
+            most = max(most, S.cands[leader + i]);
+        }
+    }
+    const bool over = most > room;                                // (of the whole team: keys are then told apart by position, else by their place in the list)
+    // keys that the row sees: all own ones are candidates where the list may not be full
+    const int k = floored ? listed : (int)min((int64_t)A.w, (int64_t)listed + cands);
+    int cut = listed;
+    unsigned long long least = 0;                                 // kept: the order keys that are not below
+    auto place = [&](int e) { return in_team * (1 << 20) + e; };
+    if (k < listed + cands) {
+        constexpr int kSorted = 256, kDrops = 16;
+        bool done = false;
+        if (!kTeams && floored && !over && cands <= 128) {
+            // Few of a warp's candidates fail against a full list: the lowest one is dropped as long as the list's entry that it has to beat is not below it. (k = listed: the i-th best against the
+            // i-th entry from the end.)
+            unsigned long long keys[4];
+            uint32_t last[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int e = 32 * i + lane;
+                last[i] = e < cands && e < listed ? __float_as_uint(weight[listed - 1 - e]) & 0x7FFFFFFFu : ~0u;
+                keys[i] = e < c ? order_key(mine[e].x, place(e)) : ~0ull;
+            }
+            for (int kept = cands; kept >= cands - kDrops && !done; --kept) {
+                unsigned long long low = keys[0] < keys[1] ? keys[0] : keys[1];
+                const unsigned long long other = keys[2] < keys[3] ? keys[2] : keys[3];
+                low = other < low ? other : low;
+                const uint32_t hi = __reduce_min_sync(0xffffffffu, (uint32_t)(low >> 32)), lo = __reduce_min_sync(0xffffffffu, (uint32_t)(low >> 32) == hi ? (uint32_t)low : ~0u);
+                const int back = max(kept - 1, 0);
+                const uint32_t a = back & 32 ? last[1] : last[0], b = back & 32 ? last[3] : last[2], rival = __shfl_sync(0xffffffffu, back & 64 ? b : a, back & 31);
+                if (kept == 0 || rival < hi) {
+                    done = true;
+                    least = kept == 0 ? ~0ull : (unsigned long long)hi << 32 | lo;
+                    cut = k - kept;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) keys[i] = keys[i] == ((unsigned long long)hi << 32 | lo) ? ~0ull : keys[i];
+                }
+            }
+        }
+        if (done) {
+        } else if (!over && cands <= kSorted) {
+            // The best own key is kept if the list's last entry is below it, the second if the last but one is, and so on: the own keys in descending order against the list from its end on
+            // (the k - listed best ones are kept anyway). By the team's first warp.
+            if (in_team == 0) {
+                auto match = [&](auto r_tag) {
+                    constexpr int R = decltype(r_tag)::value;
+                    uint32_t v[R], w[R];
+#pragma unroll
+                    for (int i = 0; i < R; ++i) {
+                        const int back = i * 32 + lane - (k - listed);       // in the list, from its end on
+                        w[i] = back < 0 ? 0u : back < listed ? (__float_as_uint(weight[listed - 1 - back]) & 0x7FFFFFFFu) + 1u : ~0u;
+                        v[i] = 0u;                                // (patterns plus one: 0 is none)
+                    }
+                    if (team == 1) {
+#pragma unroll
+                        for (int i = 0; i < R; ++i)
+                            if (i * 32 + lane < c) v[i] = mine[i * 32 + lane].x + 1u;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < R; ++i) {
+                            int e = i * 32 + lane, x = 0;
+                            while (x < team && e >= S.cands[warp + x]) e -= S.cands[warp + x++];
+                            if (x < team) v[i] = found[(warp + x) * room + e].x + 1u;
+                        }
+                    }
+                    sort_down<R>(v, lane);
+                    int kept = 0;
+#pragma unroll
+                    for (int i = 0; i < R; ++i) kept += __popc(__ballot_sync(0xffffffffu, v[i] > w[i]));       // (the first so many)
+                    cut = k - kept;
+                    uint32_t last = 0u, next = 0u;                // the weakest kept one, and the one behind it
+#pragma unroll
+                    for (int i = 0; i < R; ++i) {
+                        if ((kept - 1) >> 5 == i) last = v[i];
+                        if (kept >> 5 == i) next = v[i];
+                    }
+                    last = __shfl_sync(0xffffffffu, last, (kept - 1) & 31);
+                    next = __shfl_sync(0xffffffffu, next, kept & 31);
+                    if (kept >= 32 * R) next = 0u;
+                    least = kept == 0 ? ~0ull : (unsigned long long)(last - 1u) << 32;
+                    if (kept > 0 && next == last) {               // equal ones: the first of them
+                        int better = 0;
+#pragma unroll
+                        for (int i = 0; i < R; ++i) better += __popc(__ballot_sync(0xffffffffu, v[i] > last));
+                        int need = kept - better;
+                        for (int x = 0; x < team && need > 0; ++x)
+                            for (int e = 0; e < S.cands[warp + x] && need > 0; e += 32) {
+                                const uint32_t same = __ballot_sync(0xffffffffu, e + lane < S.cands[warp + x] && found[(warp + x) * room + e + lane].x + 1u == last);
+                                if (__popc(same) >= need) {
+                                    const int at_lane = __fns(same, 0, need);
+                                    least = order_key(last - 1u, x * (1 << 20) + e + at_lane);
+                                }
+                                need -= __popc(same);
+                            }
+                    }
+                };
+                if (cands <= 32) match(std::integral_constant<int, 1>{});
+                else if (cands <= 64) match(std::integral_constant<int, 2>{});
+                else if (cands <= 128) match(std::integral_constant<int, 4>{});
+                else match(std::integral_constant<int, 8>{});
+            }
+            if (team > 1) {
+                if (in_team == 0 && lane == 0) {
+                    S.least[warp] = least;
+                    S.cut[warp] = cut;
+                }
+                team_sync(bar, team * 32);
+                least = S.least[leader];
+                cut = S.cut[leader];
+            }
+        } else {
+            // order keys greater than entry m's weight
+            auto above = [&](int m) { return (unsigned long long)((__float_as_uint(weight[m]) & 0x7FFFFFFFu) + 1u) << 32; };
+            // Entry m of the list has m entries before it and every own key that is greater: the first of which there are k or more is not kept. Each own key takes at most one entry's
+            // place, so that it lies among the last `cands` (k >= listed). Bisection of the cut, then of the weakest kept own key between a, which `need` own keys or more are not below, and
+            // b, which at most so many are not below.
+            int lo = max(0, k - cands), hi = listed, need = 0, at_a = -1;
+            unsigned long long a = 0, b = 0;
+            bool cutting = true;
+            while (true) {
+                unsigned long long x;
+                if (cutting && lo < hi) x = above((lo + hi) >> 1);
+                else if (cutting) {
+                    cutting = false;
+                    cut = lo;
+                    need = k - cut;
+                    if (need == 0) { least = ~0ull; break; }
+                    a = cut < listed ? above(cut) : 1;
+                    b = cut > 0 ? above(cut - 1) : 1ull << 63;
+                    x = a;
+                } else {
+                    if (at_a == need || b - a <= 1) { least = a; break; }
+                    x = a + (b - a) / 2;
+                }
+                // own keys whose order key is not below x (> 0)
+                int sum = 0;
+                if (!over) {
+                    for (int e = lane; e < c; e += 32) sum += order_key(mine[e].x, place(e)) >= x;
+                } else {
+                    sweep([&](int j, int, const int (&u)[16]) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sum += u[i] > floor && order_key((uint32_t)u[i], j + i) >= x;
+                    });
+                }
+                sum = __reduce_add_sync(0xffffffffu, sum);
+                if (team > 1) {
+                    if (lane == 0) S.part[step & 1][warp] = sum;
+                    team_sync(bar, team * 32);
+                    sum = 0;
+                    for (int i = 0; i < team; ++i) sum += S.part[step & 1][leader + i];
+                    ++step;
+                }
+                if (cutting) {
+                    const int m = (lo + hi) >> 1;
+                    if (m + sum >= k) hi = m; else lo = m + 1;
+                } else if (sum >= need) {
+                    a = x;
+                    at_a = sum;
+                } else {
+                    b = x;
+                }
+            }
+        }
+    }
+    // attention over the kept ones, a stage of keys at a time
+    for (int b = over ? j0 : 0; b < (over ? j1 : c);) {
+        // as many kept ones as there is room for, at the front of the warp's part; where the candidates did not fit, from the cache again
+        int kept = 0;
+        const int end = over ? j1 : c;
+        for (; b < end && (!over || kept + 32 <= room); b += 32) {
+            uint2 o = make_uint2(0u, 0u);
+            bool keep = false;
+            if (over) {
+                const int j = b + lane, page = j < j1 ? pages[j >> A.page_log] : -1;
+                if ((unsigned)page < (unsigned)A.num_pages) {
+                    const int u = __float_as_int(A.delta[(((size_t)page * A.Hq + h) << A.page_log) + (j & mask)]);
+                    o = make_uint2((uint32_t)u, (uint32_t)((page << A.page_log) + (j & mask)));
+                    keep = u > floor && order_key(o.x, j) >= least;
+                }
+            } else if (b + lane < c) {
+                o = mine[b + lane];
+                keep = order_key(o.x, place(b + lane)) >= least;
+            }
+            const uint32_t bits = __ballot_sync(0xffffffffu, keep);            // (behind every lane's read)
+            if (keep) mine[kept + __popc(bits & ((1u << lane) - 1u))] = o;
+            kept += __popc(bits);
+            __syncwarp();
+        }
         // eight lanes take 128 bytes of a key at a time; K's rows and V's are groups of their own, the next stage's K on its way while this one's V is used
         auto copy = [&](int i, int which) {
             const uint32_t to = ptx::smem_u32(keys_at) + which * kRow + (lane & 7) * 16;
@@ -419,29 +803,7 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
             __syncwarp();
             copy(i + At::kStage, 1);
         }
-        kept = 0;
-    };
-    sweep_own(A, R, h, j0, j1, [&](int j, int slot, const int (&u)[16]) {
-        if (kept > kRoom - 512) attend();
-        uint32_t flags = 0;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) flags |= (uint32_t)(u[i] >= 0 && order_key((uint32_t)u[i], j + i) >= least) << i;
-        const int count = __popc(flags);
-        int to = count;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, to, o);
-            if (lane >= o) to += y;
-        }
-        const int total = __shfl_sync(0xffffffffu, to, 31);
-        to += kept - count;
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (flags >> i & 1u) mine[to++] = make_uint2((uint32_t)u[i], (uint32_t)(slot + i));
-        kept += total;
-        __syncwarp();
-    });
-    attend();
+    }
     at.end(reinterpret_cast<float*>(keys_at), lane);
     if (lane == 0) { S.m[warp] = at.m; S.l[warp] = at.l; }
     team_sync(bar, team * 32);
@@ -455,19 +817,29 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
 #pragma unroll
             for (int x = 0; x < D / 32; ++x) out[x] += reinterpret_cast<const float*>(dynamic + w * kStageBytes)[lane + 32 * x] * f;
         }
-        write_own<T, D>(A, t, h, behind, top, sum, out, lane);
+        write_own<T, D>(A, t, h, behind, cut, top, sum, out, lane);
     }
     team_sync(bar, team * 32);
     }
 }
 
+// Warps: one per head of a group, eight at most; teams of them, and fewer heads per CTA, where all make fewer than 16 per SM or where a row's own keys would not find room as candidates.
 template <typename T, int D>
 int own(const Cache& C, const DecodeArgs& A, cudaStream_t st) {
-    const Teams W(C, 16, 1024);
-    const size_t smem = (size_t)W.warps * (kRoom * sizeof(uint2) + Attend<T, D>::kStage * Attend<T, D>::kPitch);
-    auto kernel = W.team > 1 ? own_kernel<T, D, true> : own_kernel<T, D, false>;
+    const int64_t capacity = (int64_t)C.max_blocks << C.page_log;
+    int heads = 1, team = 1;
+    while (heads < C.G && heads < kWarps) heads *= 2;
+    const int most = heads;                                       // (more heads take turns)
+    auto ctas = [&](int per) { return (int64_t)C.rows * C.Hkv * (per == most ? 1 : (C.G + per - 1) / per); };
+    while (team < kWarps && (ctas(heads) * heads * team * 2 <= 16 * 148 || capacity > 1024 * team)) {
+        team *= 2;
+        if (heads * team > kWarps) heads /= 2;
+    }
+    const int room = (int)std::min<int64_t>((capacity + team * 64 - 1) / (team * 64) * 64, 512), warps = heads * team;
+    const size_t smem = std::max<size_t>((size_t)warps * (room * sizeof(uint2) + Attend<T, D>::kStage * Attend<T, D>::kPitch), 32 * 1024 / kWarps * warps);
+    auto kernel = team > 1 ? own_kernel<T, D, true> : own_kernel<T, D, false>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return DMA_ERR_CUDA;
-    return launch_overlapped(kernel, dim3((unsigned)W.ctas), dim3(32 * W.warps), smem, st, 1, A, W.team, W.heads);
+    return launch_overlapped(kernel, dim3((unsigned)(ctas(heads) + 1)), dim3(32 * warps), smem, st, 1, A, team, room, heads == most ? C.G : heads);
 }
 
 }  // namespace
