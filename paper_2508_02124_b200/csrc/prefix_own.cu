@@ -21,6 +21,7 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 struct OwnShared {
     unsigned long long least[kWarps];
     int part[2][kWarps], cands[kWarps], cut[kWarps];
+    uint32_t low[kWarps], high[kWarps];
     float m[kWarps], l[kWarps], all_m[kWarps][8], all_l[kWarps][8];
 };
 
@@ -586,112 +587,176 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
     }
     const bool over = most > room;                                // (of the whole team: keys are then told apart by position, else by their place in the list)
     // keys that the row sees: all own ones are candidates where the list may not be full
+    auto team_sum = [&](int x) {
+        x = __reduce_add_sync(0xffffffffu, x);
+        if (kTeams) {
+            if (lane == 0) S.part[step & 1][warp] = x;
+            team_sync(bar, team * 32);
+            x = 0;
+            for (int i = 0; i < team; ++i) x += S.part[step & 1][leader + i];
+            ++step;
+        }
+        return x;
+    };
     const int k = floored ? listed : (int)min((int64_t)A.w, (int64_t)listed + cands);
     int cut = listed;
     unsigned long long least = 0;                                 // kept: the order keys that are not below
     auto place = [&](int e) { return in_team * (1 << 20) + e; };
     if (k < listed + cands) {
-        constexpr int kSorted = 256, kDrops = 16;
-        bool done = false;
-        if (!kTeams && floored && !over && cands <= 128) {
-            // Few of a warp's candidates fail against a full list: the lowest one is dropped as long as the list's entry that it has to beat is not below it. (k = listed: the i-th best against the
-            // i-th entry from the end.)
-            unsigned long long keys[4];
-            uint32_t last[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int e = 32 * i + lane;
-                last[i] = e < cands && e < listed ? __float_as_uint(weight[listed - 1 - e]) & 0x7FFFFFFFu : ~0u;
-                keys[i] = e < c ? order_key(mine[e].x, place(e)) : ~0ull;
-            }
-            for (int kept = cands; kept >= cands - kDrops && !done; --kept) {
-                unsigned long long low = keys[0] < keys[1] ? keys[0] : keys[1];
-                const unsigned long long other = keys[2] < keys[3] ? keys[2] : keys[3];
-                low = other < low ? other : low;
-                const uint32_t hi = __reduce_min_sync(0xffffffffu, (uint32_t)(low >> 32)), lo = __reduce_min_sync(0xffffffffu, (uint32_t)(low >> 32) == hi ? (uint32_t)low : ~0u);
-                const int back = max(kept - 1, 0);
-                const uint32_t a = back & 32 ? last[1] : last[0], b = back & 32 ? last[3] : last[2], rival = __shfl_sync(0xffffffffu, back & 64 ? b : a, back & 31);
-                if (kept == 0 || rival < hi) {
-                    done = true;
-                    least = kept == 0 ? ~0ull : (unsigned long long)hi << 32 | lo;
-                    cut = k - kept;
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) keys[i] = keys[i] == ((unsigned long long)hi << 32 | lo) ? ~0ull : keys[i];
+        constexpr int kSorted = 256;
+        // the i-th best own key has to be above one of this many entries from the list's end on (the entry's pattern plus one)
+        auto rival = [&](int i) {
+            const int back = i - (k - listed);
+            return back < 0 ? 0u : back < listed ? (__float_as_uint(weight[listed - 1 - back]) & 0x7FFFFFFFu) + 1u : ~0u;
+        };
+        // of candidates that are equal the first `need` are kept: the last of these
+        auto among_equals = [&](uint32_t u, int need) {
+            for (int x = 0; x < team; ++x)
+                for (int e = 0; e < S.cands[leader + x]; e += 32) {
+                    const uint32_t same = __ballot_sync(0xffffffffu, e + lane < S.cands[leader + x] && found[(leader + x) * room + e + lane].x == u);
+                    if (__popc(same) >= need) return order_key(u, x * (1 << 20) + e + (int)__fns(same, 0, need));
+                    need -= __popc(same);
                 }
-            }
-        }
-        if (done) {
-        } else if (!over && cands <= kSorted) {
-            // The best own key is kept if the list's last entry is below it, the second if the last but one is, and so on: the own keys in descending order against the list from its end on
-            // (the k - listed best ones are kept anyway). By the team's first warp.
-            if (in_team == 0) {
-                auto match = [&](auto r_tag) {
-                    constexpr int R = decltype(r_tag)::value;
-                    uint32_t v[R], w[R];
+            return 0ull;
+        };
+        bool done = false;
+        if (floored && !over && cands <= (kTeams ? 64 : kSorted)) {
+            // Few candidates fail against a full list: the lowest one is dropped as long as it does. (By a team's first warp.)
+            auto drop = [&](auto n_tag) {
+                constexpr int N = decltype(n_tag)::value;
+                unsigned long long keys[N];
+                uint32_t last[N];
 #pragma unroll
-                    for (int i = 0; i < R; ++i) {
-                        const int back = i * 32 + lane - (k - listed);       // in the list, from its end on
-                        w[i] = back < 0 ? 0u : back < listed ? (__float_as_uint(weight[listed - 1 - back]) & 0x7FFFFFFFu) + 1u : ~0u;
-                        v[i] = 0u;                                // (patterns plus one: 0 is none)
+                for (int i = 0; i < N; ++i) {
+                    const int e = 32 * i + lane;
+                    last[i] = e < cands ? rival(e) : ~0u;
+                    int x = 0, at = e;
+                    if (kTeams)
+                        while (x < team && at >= S.cands[leader + x]) at -= S.cands[leader + x++];
+                    const uint2* of = found + (leader + x) * room;
+                    keys[i] = e < cands ? order_key(of[at].x, x * (1 << 20) + at) : ~0ull;
+                }
+#pragma unroll 1
+                for (int kept = cands; kept >= cands - 24 && !done; --kept) {
+                    unsigned long long low = keys[0];
+                    uint32_t pass = last[0];                      // what the kept-th best has to be above
+#pragma unroll
+                    for (int i = 1; i < N; ++i) {
+                        low = keys[i] < low ? keys[i] : low;
+                        pass = (kept - 1) >> 5 == i ? last[i] : pass;
                     }
-                    if (team == 1) {
-#pragma unroll
-                        for (int i = 0; i < R; ++i)
-                            if (i * 32 + lane < c) v[i] = mine[i * 32 + lane].x + 1u;
+                    const uint32_t hi = __reduce_min_sync(0xffffffffu, (uint32_t)(low >> 32)), lo = __reduce_min_sync(0xffffffffu, (uint32_t)(low >> 32) == hi ? (uint32_t)low : ~0u);
+                    pass = __shfl_sync(0xffffffffu, pass, (kept - 1) & 31);
+                    if (kept <= 0 || hi + 1u > pass) {
+                        done = true;
+                        least = kept <= 0 ? ~0ull : (unsigned long long)hi << 32 | lo;
+                        cut = k - kept;
                     } else {
 #pragma unroll
-                        for (int i = 0; i < R; ++i) {
-                            int e = i * 32 + lane, x = 0;
-                            while (x < team && e >= S.cands[warp + x]) e -= S.cands[warp + x++];
-                            if (x < team) v[i] = found[(warp + x) * room + e].x + 1u;
-                        }
+                        for (int i = 0; i < N; ++i) keys[i] = keys[i] == ((unsigned long long)hi << 32 | lo) ? ~0ull : keys[i];
                     }
-                    sort_down<R>(v, lane);
-                    int kept = 0;
-#pragma unroll
-                    for (int i = 0; i < R; ++i) kept += __popc(__ballot_sync(0xffffffffu, v[i] > w[i]));       // (the first so many)
-                    cut = k - kept;
-                    uint32_t last = 0u, next = 0u;                // the weakest kept one, and the one behind it
-#pragma unroll
-                    for (int i = 0; i < R; ++i) {
-                        if ((kept - 1) >> 5 == i) last = v[i];
-                        if (kept >> 5 == i) next = v[i];
-                    }
-                    last = __shfl_sync(0xffffffffu, last, (kept - 1) & 31);
-                    next = __shfl_sync(0xffffffffu, next, kept & 31);
-                    if (kept >= 32 * R) next = 0u;
-                    least = kept == 0 ? ~0ull : (unsigned long long)(last - 1u) << 32;
-                    if (kept > 0 && next == last) {               // equal ones: the first of them
-                        int better = 0;
-#pragma unroll
-                        for (int i = 0; i < R; ++i) better += __popc(__ballot_sync(0xffffffffu, v[i] > last));
-                        int need = kept - better;
-                        for (int x = 0; x < team && need > 0; ++x)
-                            for (int e = 0; e < S.cands[warp + x] && need > 0; e += 32) {
-                                const uint32_t same = __ballot_sync(0xffffffffu, e + lane < S.cands[warp + x] && found[(warp + x) * room + e + lane].x + 1u == last);
-                                if (__popc(same) >= need) {
-                                    const int at_lane = __fns(same, 0, need);
-                                    least = order_key(last - 1u, x * (1 << 20) + e + at_lane);
-                                }
-                                need -= __popc(same);
-                            }
-                    }
-                };
-                if (cands <= 32) match(std::integral_constant<int, 1>{});
-                else if (cands <= 64) match(std::integral_constant<int, 2>{});
-                else if (cands <= 128) match(std::integral_constant<int, 4>{});
-                else match(std::integral_constant<int, 8>{});
+                }
+            };
+            if (in_team == 0) {
+                if (kTeams || cands <= 64) drop(std::integral_constant<int, 2>{});
+                else drop(std::integral_constant<int, kTeams ? 2 : 8>{});
             }
-            if (team > 1) {
+            if (kTeams) {
                 if (in_team == 0 && lane == 0) {
                     S.least[warp] = least;
-                    S.cut[warp] = cut;
+                    S.cut[warp] = done ? cut : -1;
                 }
                 team_sync(bar, team * 32);
                 least = S.least[leader];
                 cut = S.cut[leader];
+                done = cut >= 0;
             }
+        }
+        if (kTeams && !done && most <= 64) {
+            // every warp its own candidates, sorted; one's rank is the sum of its ranks in all of them (equal ones by warp)
+            uint32_t* sorted = reinterpret_cast<uint32_t*>(keys_at);
+            uint32_t v[2];                                        // (patterns plus one: 0 is none)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) v[i] = i * 32 + lane < c ? mine[i * 32 + lane].x + 1u : 0u;
+            sort_down<2>(v, lane);
+            sorted[lane] = v[0];
+            sorted[lane + 32] = v[1];
+            team_sync(bar, team * 32);
+            int rank[2] = {lane, 32 + lane};
+#pragma unroll 1
+            for (int x = leader; x < leader + team; ++x) {
+                if (x == warp) continue;
+                const uint32_t* other = reinterpret_cast<const uint32_t*>(dynamic + x * kStageBytes);
+                const uint32_t less = x < warp ? 0u : 1u;         // in front of v: what is not below v + less
+                int lo[2] = {0, 0};
+#pragma unroll
+                for (int b = 32; b > 0; b /= 2)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        if (other[lo[i] + b - 1] >= v[i] + less) lo[i] += b;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) rank[i] += lo[i] + (lo[i] == 63 && other[63] >= v[i] + less);
+            }
+            uint32_t low = ~0u, high = 0u;                        // the weakest kept one, and the best of the others
+            int mine_kept = 0;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const bool keep = v[i] > 0u && v[i] > rival(rank[i]);
+                mine_kept += keep;
+                if (keep) low = min(low, v[i]); else high = max(high, v[i]);
+            }
+            const int kept = team_sum(mine_kept);
+            low = __reduce_min_sync(0xffffffffu, low);
+            high = __reduce_max_sync(0xffffffffu, high);
+            if (lane == 0) { S.low[warp] = low; S.high[warp] = high; }
+            team_sync(bar, team * 32);
+            for (int i = 0; i < team; ++i) {
+                low = min(low, S.low[leader + i]);
+                high = max(high, S.high[leader + i]);
+            }
+            cut = k - kept;
+            least = kept == 0 ? ~0ull : (unsigned long long)(low - 1u) << 32;
+            if (kept > 0 && high == low) least = among_equals(low - 1u, kept - team_sum((v[0] > low) + (v[1] > low)));
+            done = true;
+            team_sync(bar, team * 32);                            // (the sorted ones have been read)
+        }
+        if (done) {
+        } else if (!kTeams && !over && cands <= kSorted) {
+            // The best own key is kept if the list's last entry is below it, the second if the last but one is, and so on: the own keys in descending order against the list from its end on.
+            auto match = [&](auto r_tag) {
+                constexpr int R = decltype(r_tag)::value;
+                uint32_t v[R], w[R];                              // (patterns plus one: 0 is none)
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    w[i] = rival(i * 32 + lane);
+                    v[i] = i * 32 + lane < c ? mine[i * 32 + lane].x + 1u : 0u;
+                }
+                sort_down<R>(v, lane);
+                int kept = 0;
+#pragma unroll
+                for (int i = 0; i < R; ++i) kept += __popc(__ballot_sync(0xffffffffu, v[i] > w[i]));       // (the first so many)
+                cut = k - kept;
+                uint32_t last = 0u, next = 0u;                    // the weakest kept one, and the one behind it
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    if ((kept - 1) >> 5 == i) last = v[i];
+                    if (kept >> 5 == i) next = v[i];
+                }
+                last = __shfl_sync(0xffffffffu, last, (kept - 1) & 31);
+                next = __shfl_sync(0xffffffffu, next, kept & 31);
+                if (kept >= 32 * R) next = 0u;
+                least = kept == 0 ? ~0ull : (unsigned long long)(last - 1u) << 32;
+                if (kept > 0 && next == last) {
+                    int better = 0;
+#pragma unroll
+                    for (int i = 0; i < R; ++i) better += __popc(__ballot_sync(0xffffffffu, v[i] > last));
+                    least = among_equals(last - 1u, kept - better);
+                }
+            };
+            if (cands <= 32) match(std::integral_constant<int, 1>{});
+            else if (cands <= 64) match(std::integral_constant<int, 2>{});
+            else if (cands <= 128) match(std::integral_constant<int, 4>{});
+            else match(std::integral_constant<int, 8>{});
         } else {
             // order keys greater than entry m's weight
             auto above = [&](int m) { return (unsigned long long)((__float_as_uint(weight[m]) & 0x7FFFFFFFu) + 1u) << 32; };
@@ -726,14 +791,7 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
                         for (int i = 0; i < 16; ++i) sum += u[i] > floor && order_key((uint32_t)u[i], j + i) >= x;
                     });
                 }
-                sum = __reduce_add_sync(0xffffffffu, sum);
-                if (team > 1) {
-                    if (lane == 0) S.part[step & 1][warp] = sum;
-                    team_sync(bar, team * 32);
-                    sum = 0;
-                    for (int i = 0; i < team; ++i) sum += S.part[step & 1][leader + i];
-                    ++step;
-                }
+                sum = team_sum(sum);
                 if (cutting) {
                     const int m = (lo + hi) >> 1;
                     if (m + sum >= k) hi = m; else lo = m + 1;
