@@ -266,9 +266,9 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_kernel(DecodeArgs A, int n
             __syncwarp();
         }
     } else {
-        // a warp has 16 keys of each tile; 512 bytes, K's row and V's, per instruction
-        constexpr int KPI = 128 / D, kMine = kKeys / kGather;     // keys per instruction
-        const int w = warp - kIssuer - 1, part = lane % (D / 4), which = part / (D / 8), ch = part % (D / 8), sub = lane / (D / 4);
+        // a warp has 16 keys of each tile; eight lanes take 128 bytes of a key at a time
+        constexpr int kMine = kKeys / kGather;
+        const int w = warp - kIssuer - 1;
         int slot = -1;
         float bias = -INFINITY;
         auto fetch = [&](int i) {
@@ -290,12 +290,13 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_kernel(DecodeArgs A, int n
             if (lane < kMine) S.bias[st][w * kMine + lane] = bias;
             __syncwarp();
             if (lane == 0) mbar_arrive(&S.bias_full[st]);
-            uint8_t* to = S.kv[st][which] + (ch >> 3) * Sh::kHalf;
 #pragma unroll
-            for (int k = 0; k < kMine; k += KPI) {
-                const int at = __shfl_sync(0xffffffffu, slot, k + sub), r = w * kMine + k + sub;
-                const __nv_bfloat16* from = kv + (at >= 0 ? key_row(at >> A.page_log, hk, at & ((1 << A.page_log) - 1), A.Hkv, A.page_log) * (2 * D) + part * 8 : 0);
-                cp_async16(to + r * 128 + (((ch & 7) ^ (r & 7)) << 4), from, at >= 0 ? 16 : 0);
+            for (int k = 0; k < kMine; k += 4) {
+                const int at = __shfl_sync(0xffffffffu, slot, k + (lane >> 3)), r = w * kMine + k + (lane >> 3);
+                const __nv_bfloat16* from = kv + (at >= 0 ? key_row(at >> A.page_log, hk, at & ((1 << A.page_log) - 1), A.Hkv, A.page_log) * (2 * D) : 0) + (lane & 7) * 8;
+                uint8_t* to = S.kv[st][0] + r * 128 + (((lane & 7) ^ (r & 7)) << 4);
+#pragma unroll
+                for (int x = 0; x < 2 * D / 64; ++x) cp_async16(to + x / (D / 64) * Sh::kTile + x % (D / 64) * Sh::kHalf, from + x * 64, at >= 0 ? 16 : 0);
             }
             cp_async_arrive(&S.full[st]);
             fetch(i + 1);
