@@ -409,7 +409,9 @@ int dma_prefix_order(const dma_cache_t* c, const float* delta, const int32_t* bl
  * q and o have q_stride and o_stride; lse [rows, Hq]. order_*: of nprefix prefixes, of dma_prefix_order with the same Hq, pool and w (0 prefixes: the four
  * pointers are not read). All rows of a prefix attend to its keys together: the listed keys are read once per 128 rows and query
  * head. Rows in no order; a row that sees no key gets o = 0, lse = -inf; a row whose row_seq is outside [0, nseq) is left as it is.
- * Results depend on the call's rows and prefixes in the last bits, and are the same bits from run to run.
+ * Results depend on the call's rows and prefixes in the last bits, and are the same bits from run to run. nprefix is at most 2^30, and
+ * min(rows, nprefix + rows / 8) below 2^24. The kernels' forms, and so the time, go by rows, nprefix, w, order_ld and the table's width: give no more prefixes
+ * than the call's rows stand behind (64 rows of one prefix in a call of 64 prefixes are attended to by a quarter of the chip).
  * ws: dma_cache_decode_workspace() bytes, a size that does not fall as rows, Hq, max_blocks or nprefix grow. It serves one call at a time: calls that may
  * overlap on the GPU need one each. */
 int dma_cache_decode_workspace(const dma_cache_t* c, int32_t nprefix, size_t* bytes);

@@ -206,11 +206,12 @@ int dma_prefix_order(const dma_cache_t* c, const float* delta, const int32_t* bl
     return launch_prefix_order(C, delta, block_table, prefix_len, order_slot, order_weight, order_ld, order_len, ws, (cudaStream_t)cuda_stream);
 }
 
-// CTAs are counted in 32 bits.
+// The rows of all tiles, of which there are min(rows, nprefix + rows / 8) at most, are counted in 32 bits.
 static int resolve_decode(const dma_cache_t* c, int32_t nprefix, Cache* C) {
     const int rc = resolve_cache(c, C);
     if (rc) return rc;
-    return nprefix < 0 || nprefix > (1 << 30) ? DMA_ERR_SHAPE : DMA_OK;
+    if (nprefix < 0 || nprefix > (1 << 30) || std::min<int64_t>(C->rows, (int64_t)nprefix + C->rows / 8) >= (1 << 24)) return DMA_ERR_SHAPE;
+    return DMA_OK;
 }
 
 int dma_cache_decode_workspace(const dma_cache_t* c, int32_t nprefix, size_t* bytes) {

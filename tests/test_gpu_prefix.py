@@ -239,7 +239,8 @@ class World:
 
     def check(self, o, lse, rows=None, skip=()):
         """Score: products of d channels, added in fp32 in any order, scale, bias and reference: (d + 8) roundings of the sum of magnitudes (on the tensor cores' sums: cut, not rounded: twice).
-        Its error is the weight's relative one. Weights in bf16: half a step of each, against an unrounded sum. Sums of up to n weights and values: n roundings. One rounding at the end."""
+        Its error is the weight's relative one. On the tensor cores a weight is two bf16 numbers, the second half a step of half a step off: 2^-16. Sums of up to n weights and values: n roundings. One
+        rounding at the end."""
         o, lse, kv, q = f64(o), f64(lse), f64(self.kv), f64(self.q)
         tensor = self.dtype == "bf16" and not self.c.flags
         for t in range(self.rows) if rows is None else rows:
@@ -255,7 +256,7 @@ class World:
                     assert (o[t, h] == 0).all() and lse[t, h] == -np.inf, (t, h)
                     continue
                 es = (2 if tensor else 1) * (self.d + 8) * 2.0 ** -24 * mag
-                tol = pv * (2 * es + (n + 16) * 2.0 ** -24 * (2 if tensor else 1) + (HALF["bf16"] if tensor else 0)) + HALF[self.dtype] * np.abs(eo[h])
+                tol = pv * (2 * es + (n + 16) * 2.0 ** -24 * (2 if tensor else 1) + (HALF["bf16"] ** 2 if tensor else 0)) + HALF[self.dtype] * np.abs(eo[h])
                 assert (np.abs(o[t, h] - eo[h]) <= tol).all(), (t, h, float((np.abs(o[t, h] - eo[h]) / tol).max()))
                 assert abs(lse[t, h] - el[h]) <= es + (n + 16) * 2.0 ** -24 + 4 * 2.0 ** -24 * abs(el[h]), (t, h, lse[t, h], el[h])
 
@@ -279,6 +280,61 @@ def test_decode(lens, tails, prefix, w, Hq, Hkv, d, page, dtype, flags):
     assert (ws[-512:] == 0x5A).all()
     o2, lse2 = s.run()
     assert torch.equal(o, o2) and torch.equal(lse, lse2), "the same bits from run to run"
+
+
+LONG = [
+    # what a row keeps of many own keys: lens, tails, w, Hq, Hkv, d, page, rows per prefix
+    ([5000], [2000, 1900], 256, 4, 1, 64, 64, 2), ([5000], [700], 128, 8, 8, 64, 16, 40),           # few candidates: by a team of warps, by one
+    ([3000], [1000], 900, 2, 1, 128, 64, 80), ([600], [1000], 500, 2, 2, 64, 64, 80),               # a third and more of the own keys are candidates: dropped, sorted
+    ([50], [1500, 30], 700, 4, 2, 64, 32, 2), ([10], [4096], 3000, 2, 1, 64, 128, 3),               # a short list: all are candidates, bisected
+    ([50], [9000, 4000], 3000, 1, 1, 64, 64, 2), ([0], [6000], 1, 2, 1, 64, 256, 1), ([20], [20000], 9000, 1, 1, 64, 16, 1)]    # more candidates than there is room for
+
+
+@pytest.mark.parametrize("lens,tails,w,Hq,Hkv,d,page,rows", LONG)
+@pytest.mark.parametrize("dtype,kind", [("bf16", "random"), ("fp32", "random"), ("bf16", "crowded")])
+def test_decode_of_long_own_sequences(lens, tails, w, Hq, Hkv, d, page, rows, dtype, kind):
+    seq = np.arange(rows) % len(tails)
+    s = World(lens, tails, np.arange(rows) % len(lens), w, Hq, Hkv, d, page, dtype, kind, seed=w + rows, seq=seq, pos=np.asarray(tails)[seq] - 1 - np.arange(rows) % 7)
+    o, lse = s.run()
+    s.check(o, lse, rows=range(min(rows, 5)))
+    again = s.run()
+    assert torch.equal(o, again[0]) and torch.equal(lse, again[1])
+
+
+@pytest.mark.parametrize("rows,nprefix,Hq,Hkv,dtype", [(700, 300, 2, 1, "bf16"), (3000, 1, 2, 2, "bf16"), (1500, 7, 1, 1, "fp32"), (1100, 1100, 2, 1, "bf16"), (257, 2, 16, 1, "bf16"), (129, 1, 24, 2, "bf16"),
+                                                      (40, 2, 5, 1, "fp32")])
+def test_decode_of_many_rows_and_prefixes(rows, nprefix, Hq, Hkv, dtype):
+    """More prefixes, and more rows of a prefix, than a turn of their grouping; more heads per group than a CTA takes at a time; prefixes without rows."""
+    rng = np.random.RandomState(rows)
+    lens = rng.randint(0, 60, nprefix)
+    s = World(list(lens), [int(x) for x in rng.randint(1, 20, rows)], rng.randint(-1, nprefix, rows) // 2 * 2, 24, Hq, Hkv, 64, 16, dtype, seed=rows)
+    o, lse = s.run()
+    s.check(o, lse, rows=sorted(rng.choice(rows, min(rows, 60 if Hq < 8 else 25), replace=False)))
+    again = s.run()
+    assert torch.equal(o, again[0]) and torch.equal(lse, again[1])
+
+
+def test_pools_beyond_32_bits():
+    """A pool of more than 2^32 bytes, all that is used of it at its end."""
+    Hq, Hkv, d, page, pages = 4, 2, 128, 256, 17000                       # 4.46 GB of K and V
+    c = dma.cache(Hq, Hkv, d, w=40, rows=150, nseq=3, page_size=page, num_pages=pages, max_blocks=1)
+    kv, delta = torch.zeros(pages, Hkv, page, 2, d, dtype=torch.bfloat16, device="cuda"), torch.zeros(pages, Hq, page, device="cuda")
+    assert kv.numel() * 2 > 1 << 32
+    g = torch.Generator("cuda").manual_seed(0)
+    K, V = (torch.randn(150, Hkv, d, generator=g, device="cuda").bfloat16() for _ in range(2))
+    given = torch.rand(Hq, 150, generator=g, device="cuda") + 0.5
+    table = i32([[pages - 1], [pages - 2], [pages - 3]])
+    slot = torch.cat([(pages - 1 - i) * page + torch.arange(50) for i in range(3)]).int().cuda()
+    dma.dma_cache_append(c, K, V, slot, kv, delta, delta_new=given)
+    order = dma.dma_prefix_order(dma.cache(Hq, Hkv, d, w=40, nseq=1, page_size=page, num_pages=pages, max_blocks=1), delta, table[:1], i32([50]))
+    q = torch.randn(2, Hq, d, generator=g, device="cuda").bfloat16()
+    c = dma.cache(Hq, Hkv, d, w=40, rows=2, nseq=2, page_size=page, num_pages=pages, max_blocks=1)
+    o, lse = dma.dma_cache_decode(c, q, kv, delta, table[1:], i32([0, 1]), i32([49, 20]), i32([0, 0]), order)
+    for t, n in ((0, 50), (1, 21)):
+        rows = np.concatenate([np.arange(50), 50 * (t + 1) + np.arange(n)])
+        eo, el, parts = ref4.decode(f64(q[t]), f64(K)[rows], f64(V)[rows], given.cpu().numpy()[:, rows], 40, d ** -0.5)
+        for h in range(Hq):
+            assert (np.abs(f64(o[t, h]) - eo[h]) <= 2.0 ** -8 * np.abs(eo[h]) + parts[h][2] * 2.0 ** -8).all() and abs(float(lse[t, h]) - el[h]) < 1e-4
 
 
 @pytest.mark.parametrize("kind", ["equal", "crowded", "wide"])

@@ -50,7 +50,7 @@ def test_refused_descriptors(lib, kw, code):
 
 
 def test_refused_sizes(lib):
-    for f in (lambda: dma.dma_cache_decode_workspace(cache(), -1), lambda: dma.dma_cache_decode_workspace(cache(), (1 << 30) + 1),
+    for f in (lambda: dma.dma_cache_decode_workspace(cache(rows=1 << 24, Hq=1, Hkv=1), 1 << 24), lambda: dma.dma_cache_decode_workspace(cache(), -1), lambda: dma.dma_cache_decode_workspace(cache(), (1 << 30) + 1),
               lambda: dma.dma_prefix_order_workspace(cache(nseq=1 << 28)), lambda: dma.dma_prefix_order_workspace(cache(nseq=1 << 20, max_blocks=1 << 20))):
         with pytest.raises(dma.DmaError) as e:
             f()
