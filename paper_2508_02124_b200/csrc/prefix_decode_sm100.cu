@@ -1,15 +1,21 @@
-// Second half of dma_cache_decode (include/dma.h) on the tensor cores (bf16): up to 128 rows of a prefix together over a head's list, and the sum with the rows' own keys.
+// dma_cache_decode (include/dma.h), second kernel, on the tensor cores (bf16): up to 128 rows of a prefix together over a head's list, and the sum with the rows' own keys.
 //
 // The list is sorted, so that a row keeps its first `cut` entries: a dense product whose rows differ in length. A cluster takes a (tile of rows, head); its CTAs take parts of the
 // list, 64 keys at a time: rows of K and V gathered by 16-byte asynchronous copies into the swizzled layout, S = Q K^T into tensor memory, softmax by a thread per row, P back over
 // S as bf16, O += P V. Then the CTAs' sums meet in distributed shared memory, with each row's piece from its own keys, and o and lse are written.
 // The products have 128 rows whatever the tile has. Where it has at most 64 (32), the other lanes take the same rows and other columns: lane group i of n the i-th part of every 64 keys,
-// with zeros of P elsewhere, so that a thread walks 32 (16) columns instead of 64.
+// with zeros of P elsewhere, so that a thread walks 32 (16) columns instead of 64 (three tiles of 14 rows 21.4 us instead of 25.8, 16 rows 18.3 instead of 19.7, 64 rows the same).
 // Rounding: scores, sums and O are fp32. P goes in as two bf16 numbers, the one next to it and what that leaves (2^-16 of a weight), over the same V: with one, o is a quarter further from
 // 64 bits than its own rounding makes it (rms 2.1e-3 and 1.7e-3).
 // A value that is not finite would reach rows that do not keep its key, as 0 times infinity. A row whose O is not finite is therefore formed again, by a warp, over the keys it keeps.
 //
-// Warps: 0-3 softmax and the end, 4 issues the products, 5-8 gather. Two CTAs per SM.
+// Warps: 0-3 softmax and the end, 4 issues the products, 5-8 gather (with two gathering 64 rows 26.7 us instead of 24.1, eight rows with long lists 34 instead of 29). Two CTAs per SM: 97 KB
+// of stages, Q and O each.
+//
+// Times (32 and 8 heads, d = 128): 64 rows behind 16K keys, w = 2048: 23 us; 256 rows in four prefixes of 8K: 36; 8 rows behind 64K, w = 4096: 26.5; 1024 rows behind 16K 111. On the CUDA
+// cores, whose tiles have eight rows (prefix_decode.cu): one row 28 us instead of 17, four 34 instead of 17, 64 rows of a prefix each 520 instead of 281; so bf16 comes here however few its rows are.
+// With few rows it is the list's read, a gather of 512 bytes a key from places as the weights fall, that a CTA's 8 tiles wait for (64 rows: 34 MB asked of the L2, 30 of them of memory; tensor
+// pipe 14 % active), and start and end: rows, Q, the cluster's sum. With many rows it is the softmax' threads (1024 rows: 0.47 PFLOP/s of products, both parts of P counted).
 #include <algorithm>
 #include <type_traits>
 

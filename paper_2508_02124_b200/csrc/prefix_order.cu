@@ -1,6 +1,9 @@
 // The order of prefixes (include/dma.h, dma_prefix_order): of every prefix and query head the w keys of the largest delta, sorted.
 //
-// The weakest kept key of each (prefix, head) is found as decoding finds it (cache4_select.cu); what is not below it is collected and sorted, by a CTA per (prefix, head) or in chunks.
+// The weakest kept key of each (prefix, head) is found as decoding finds it (cache4_select.cu); what is not below it is collected and sorted, by a CTA per (prefix, head) where shared memory
+// holds the list, 8192 entries, else in chunks of it. Ordering is round trips and instructions, not memory: 32 heads of 16K keys, w = 2048: 17 us (rows 2, selection 6.4, lists 8.5; the
+// weights' bytes 0.4); five prefixes of up to 64K, w = 4096: 45 us (2, 20, 23; bytes 4.6). In chunks the first takes 33 us; 16 prefixes of 16K, w = 4096, 110 instead of 57; one of 256K 63
+// and 65, one of 1M, w = 8192, 155 and 192, which a prefix pays once. In chunks one of 256K, w = 16384, takes 91 us, one of 1M 157.
 #include <algorithm>
 #include <type_traits>
 
@@ -9,7 +12,7 @@
 namespace dma {
 namespace {
 
-constexpr int kChunk = 4096, kThreads = 512;
+constexpr int kHeld = 8192, kChunk = 4096, kSpan = 4096;
 
 struct Order {
     const float* delta;
@@ -18,9 +21,9 @@ struct Order {
     float* weight;
     int64_t ld, order_ld;
     const unsigned long long* weakest;       // NULL: all are kept
-    unsigned long long* run;                 // [nseq * Hq, cap]: the chunks' sorted entries, wherever there was room
-    int32_t *run_at, *run_len, *room;        // [nseq * Hq, chunks], [nseq * Hq]
-    int nseq, Hq, w, page_log, num_pages, max_blocks, chunks, cap;
+    unsigned long long* run;                 // [nseq * Hq, cap]: entries of lists that no CTA holds
+    int32_t* room;                           // [nseq * Hq]: how many there are
+    int Hq, w, page_log, num_pages, max_blocks, spans, chunks, cap;
     __device__ __forceinline__ int visible(int s) const { return min(max(len[s], 0), max_blocks << page_log); }
 };
 
@@ -68,7 +71,7 @@ __device__ __forceinline__ void sweep(const Order& P, int s, int h, int j0, int 
     }
 }
 
-// The kept ones among a thread's `n` keys from position j on to shared memory, in no order; `count` is moved on.
+// The kept ones among a thread's `n` keys from position j on to `to`, in no order; `count` is moved on.
 __device__ __forceinline__ void collect(const uint32_t (&u)[16], int j, int n, unsigned long long least, unsigned long long* to, int room, int* count) {
     const int lane = threadIdx.x & 31;
     uint32_t flags = 0;
@@ -234,62 +237,50 @@ __global__ void __launch_bounds__(NT) order_held_kernel(Order P) {
     }
 }
 
-// Longer lists, and few long prefixes: chunks of kChunk positions, sorted in shared memory, and each entry's place as the sum of its places in all of them.
-__global__ void __launch_bounds__(kThreads) order_sort_kernel(Order P) {
-    __shared__ unsigned long long e[kChunk];
-    __shared__ int count, base;
-    const int tid = threadIdx.x, chunk = blockIdx.x % P.chunks, item = blockIdx.x / P.chunks, s = item / P.Hq, h = item % P.Hq;
+// Longer lists. What is kept is collected as it comes, a CTA per kSpan positions, and sorted in chunks; an entry's place is the sum of its places in all of them.
+__global__ void __launch_bounds__(kSpan / 16) order_collect_kernel(Order P) {
+    const int span = blockIdx.x % P.spans, item = blockIdx.x / P.spans, s = item / P.Hq, h = item % P.Hq;
     pdl_enter();
-    const int n = P.visible(s), j0 = min(n, chunk * kChunk), j1 = min(n, j0 + kChunk);
+    const int n = P.visible(s), j0 = min(n, span * kSpan), j1 = min(n, j0 + kSpan);
     const unsigned long long least = P.weakest ? P.weakest[item] : 0ull;
-    if (tid == 0) count = 0;
-    __syncthreads();
-    sweep<kThreads>(P, s, h, j0, j1, [&](const uint32_t (&u)[16], int j, int m) { collect(u, j, m, least, e, kChunk, &count); });
-    __syncthreads();
-    const int c = count;
-    int size = 2;
-    while (size < c) size *= 2;
-    for (int i = c + tid; i < size; i += kThreads) e[i] = 0;
-    __syncthreads();
-    for (int k = 2; k <= size; k *= 2)
-        for (int x = k / 2; x > 0; x /= 2) {
-            for (int i = tid; i < size / 2; i += kThreads) {
-                const int a = 2 * i - (i & (x - 1));
-                const unsigned long long u = e[a], v = e[a + x];
-                if ((u < v) == ((a & k) == 0)) { e[a] = v; e[a + x] = u; }
-            }
-            __syncthreads();
-        }
-    if (tid == 0) {
-        base = atomicAdd(&P.room[item], c);
-        P.run_at[blockIdx.x] = base;
-        P.run_len[blockIdx.x] = c;
-    }
-    __syncthreads();
-    for (int i = tid; i < c && base + i < P.cap; i += kThreads) P.run[(size_t)item * P.cap + base + i] = e[i];
+    sweep<kSpan / 16>(P, s, h, j0, j1, [&](const uint32_t (&u)[16], int j, int m) { collect(u, j, m, least, P.run + (size_t)item * P.cap, P.cap, &P.room[item]); });
 }
 
-__global__ void __launch_bounds__(256) order_merge_kernel(Order P) {
+__global__ void __launch_bounds__(1024) order_sort_kernel(Order P) {
+    constexpr int E = kChunk / 1024;
+    extern __shared__ unsigned long long e[];                     // [2][kChunk]
+    const int chunk = blockIdx.x % P.chunks, item = blockIdx.x / P.chunks, from = chunk * kChunk + threadIdx.x * E;
+    pdl_enter();
+    const int count = min(P.room[item], P.cap);
+    if (count <= chunk * kChunk) return;
+    unsigned long long* run = P.run + (size_t)item * P.cap;
+    unsigned long long v[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] = from + i < count ? run[from + i] : 0ull;
+    sort_down<1024, E>(v, e);
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+        if (from + i < count) run[from + i] = v[i];
+}
+
+__global__ void __launch_bounds__(1024) order_merge_kernel(Order P) {
     constexpr int kTogether = 4;                                  // chunks searched side by side
-    const int item = blockIdx.x / P.chunks, chunk = blockIdx.x % P.chunks, s = item / P.Hq;
+    const int part = blockIdx.x % P.chunks, item = blockIdx.x / P.chunks, s = item / P.Hq;
     pdl_enter();
     const unsigned long long* run = P.run + (size_t)item * P.cap;
-    const int32_t *at = P.run_at + item * P.chunks, *len = P.run_len + item * P.chunks;
-    const int from = at[chunk], count = min(len[chunk], P.cap - from);
-    for (int i = threadIdx.x; i < count; i += 256) {
-        const unsigned long long key = run[from + i];
-        int place = i;
-        for (int c0 = 0; c0 < P.chunks; c0 += kTogether) {
-            int lo[kTogether], hi[kTogether], start[kTogether];
+    const int count = min(P.room[item], P.cap), end = min(count, (part + 1) * kChunk);
+    for (int i = part * kChunk + threadIdx.x; i < end; i += 1024) {
+        const unsigned long long key = run[i];
+        int place = i - part * kChunk;
+        for (int c0 = 0; c0 * kChunk < count; c0 += kTogether) {
+            int lo[kTogether], hi[kTogether];
             bool more = false;
 #pragma unroll
             for (int y = 0; y < kTogether; ++y) {
                 const int c = c0 + y;
-                const bool other = c < P.chunks && c != chunk;
-                start[y] = other ? at[c] : 0;
                 lo[y] = 0;
-                hi[y] = other ? min(len[c], P.cap - start[y]) : 0;
-                more |= lo[y] < hi[y];
+                hi[y] = c == part ? 0 : max(0, min(count - c * kChunk, kChunk));
+                more |= hi[y] > 0;
             }
             while (more) {
                 more = false;
@@ -297,33 +288,32 @@ __global__ void __launch_bounds__(256) order_merge_kernel(Order P) {
                 for (int y = 0; y < kTogether; ++y)
                     if (lo[y] < hi[y]) {
                         const int mid = (lo[y] + hi[y]) >> 1;
-                        if (run[start[y] + mid] > key) lo[y] = mid + 1; else hi[y] = mid;
+                        if (run[(c0 + y) * kChunk + mid] > key) lo[y] = mid + 1; else hi[y] = mid;
                         more |= lo[y] < hi[y];
                     }
             }
 #pragma unroll
             for (int y = 0; y < kTogether; ++y) place += lo[y];
         }
-        if (place < P.cap) put(P, item, s, place, key);
+        put(P, item, s, place, key);
     }
 }
 
 struct Layout {
-    size_t seq, pos, weakest, room, at, len, run, total;
-    int chunks, cap;
+    size_t seq, pos, weakest, room, run, total;
+    int spans, chunks, cap;
     explicit Layout(const Cache& C) {
         const int64_t capacity = (int64_t)C.max_blocks << C.page_log, items = (int64_t)C.nseq * C.Hq;
-        chunks = (int)((capacity + kChunk - 1) / kChunk);
         cap = (int)std::min<int64_t>(C.w, capacity);
+        spans = (int)((capacity + kSpan - 1) / kSpan);
+        chunks = (cap + kChunk - 1) / kChunk;
         size_t x = kWsHeaderBytes;
         auto take = [&](size_t bytes) { const size_t at = x; x += (bytes + 255) / 256 * 256; return at; };
         seq = take((size_t)C.nseq * 4);
         pos = take((size_t)C.nseq * 4);
         weakest = take((size_t)items * 8);
         room = take((size_t)items * 4);
-        at = take((size_t)items * chunks * 4);
-        len = take((size_t)items * chunks * 4);
-        run = take((size_t)items * cap * 8);
+        run = take(cap > kHeld ? (size_t)items * cap * 8 : 0);
         total = x;
     }
 };
@@ -340,7 +330,7 @@ int launch_prefix_order(const Cache& C0, const float* delta, const int32_t* tabl
     char* p = (char*)ws;
     const bool select = L.cap < ((int64_t)C.max_blocks << C.page_log);
     Order P = {delta, table, len, slot, order_len, weight, C.table_ld, order_ld, select ? (unsigned long long*)(p + L.weakest) : nullptr, (unsigned long long*)(p + L.run),
-               (int32_t*)(p + L.at), (int32_t*)(p + L.len), (int32_t*)(p + L.room), C.nseq, C.Hq, C.w, C.page_log, C.num_pages, C.max_blocks, L.chunks, L.cap};
+               (int32_t*)(p + L.room), C.Hq, C.w, C.page_log, C.num_pages, C.max_blocks, L.spans, L.chunks, L.cap};
     int rc = launch_overlapped(order_rows_kernel, dim3(C.nseq), dim3(256), 0, st, 1, P, (int32_t*)(p + L.seq), (int32_t*)(p + L.pos), (int32_t*)p);
     if (rc) return rc;
     if (select) {
@@ -354,15 +344,18 @@ int launch_prefix_order(const Cache& C0, const float* delta, const int32_t* tabl
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return (int)DMA_ERR_CUDA;
         return launch_overlapped(kernel, dim3((unsigned)items), dim3(NT), smem, st, 1, P);
     };
-    if (L.cap <= 8192 && (L.chunks <= 16 || items >= 148)) {
+    if (L.cap <= kHeld) {
         if (L.cap <= 1024) return held(std::integral_constant<int, 1>{});
         if (L.cap <= 2048) return held(std::integral_constant<int, 2>{});
         if (L.cap <= 4096) return held(std::integral_constant<int, 4>{});
         return held(std::integral_constant<int, 8>{});
     }
+    if ((rc = launch_overlapped(order_collect_kernel, dim3((unsigned)(items * L.spans)), dim3(kSpan / 16), 0, st, 1, P))) return rc;
     const unsigned grid = (unsigned)(items * L.chunks);
-    if ((rc = launch_overlapped(order_sort_kernel, dim3(grid), dim3(kThreads), 0, st, 1, P))) return rc;
-    return launch_overlapped(order_merge_kernel, dim3(grid), dim3(256), 0, st, 1, P);
+    constexpr int smem = 2 * kChunk * 8;
+    if (cudaFuncSetAttribute(order_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return DMA_ERR_CUDA;
+    if ((rc = launch_overlapped(order_sort_kernel, dim3(grid), dim3(1024), smem, st, 1, P))) return rc;
+    return launch_overlapped(order_merge_kernel, dim3(grid), dim3(1024), 0, st, 1, P);
 }
 
 }  // namespace dma

@@ -1,9 +1,22 @@
-// First half of dma_cache_decode (include/dma.h): what every row keeps of its prefix' order and of its own keys, and the attention over the latter.
+// dma_cache_decode (include/dma.h), first kernel: what every row keeps of its prefix' order and of its own keys, and the attention over the latter.
 //
 // The cut. A row's head keeps k = min(w, listed + own) keys of the merged order. Entry m of the prefix' order has m entries before it and every own key that is greater; so the
-// prefix' part ends with the first m for which m + #{own > weight_m} >= k, a bisection (ties: the prefix' keys come first), and the own part is the k - m best of the row's own
-// keys, a bisection over their order keys between the weights around the cut. Where the list has w entries, own keys that do not exceed its last cannot be kept and are left out
-// at once: of n own keys behind a prefix of N about n w / N remain. They lie in shared memory, where every count is a sweep by one warp.
+// prefix' part ends with the first m for which m + #{own > weight_m} >= k (ties: the prefix' keys come first), and the own part is the k - m best of the row's own keys. Where the list
+// has w entries, own keys that do not exceed its last cannot be kept and are left out at once: of n own keys behind a prefix of N about n w / N remain, the candidates. Each of them takes
+// at most one entry's place: the i-th best is kept if it is above the i-th entry from the list's end. So
+//   - few candidates, a full list: the lowest is dropped as long as it fails, a minimum of the warp each time (by sorting at once: 256 rows of 512 own keys 105 us instead of 101, 64 of
+//     1024 34.6 instead of 33);
+//   - else they are sorted and matched against the list's end: by a warp up to 256 of them in registers, by a team up to 64 per warp, ranks added up by searching the other warps' sorted ones;
+//   - beyond, or without room in shared memory for all of them (512 a warp): bisection of the cut, then of the weakest own key, each count a sweep of the team.
+// A row that keeps everything whatever its weights needs no cut: its warps take parts of the keys with all heads together (40 rows of up to 300 own keys: 25 -> 6.5 us).
+//
+// A CTA takes a (row, KV head), so that K and V of a key that several heads keep come from the L1 or L2. A head has a warp or a team of them: teams where few rows would leave the SMs with
+// few warps (8 rows of 4096 own keys: 36 us without them, 19 with), up to 16 warps per SM (asked to make 32 with 64 rows of 1024 own keys: 57 us instead of 33, since every team pays for
+// its barriers).
+//
+// Times (own keys ragged, 32 and 8 heads, d = 128): 64 rows of up to 1024 own keys behind 16K keys, w = 2048: 24 us; 256 rows of up to 512 behind 8K: 58; 8 rows of up to 4096 behind 64K,
+// w = 4096: 16. Bound by round trips that few warps hide: pages, weights, the cut, then rows of K and V a stage ahead (64 rows: 10 warps per SM, issue slots 17 % busy; 256 rows: 14 warps, 32 %,
+// 186 MB from memory at 39 % of the copy's rate). 128 registers and 6.5 KB of shared memory per warp allow no more of them.
 #include <algorithm>
 #include <type_traits>
 
@@ -438,7 +451,7 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x / 32, team = kTeams ? warps_per_head : 1;
     pdl_enter();
     if (blockIdx.x == 0) {                                        // (first: it is done while the others are at work)
-        if (tid < kWsHeaderBytes / 4) A.status[tid] = 0;
+        for (int i = tid; i < kWsHeaderBytes / 4; i += blockDim.x) A.status[i] = 0;      // (a CTA may be one warp)
         group_rows(A, reinterpret_cast<int*>(dynamic));
         return;
     }
@@ -881,7 +894,8 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
     }
 }
 
-// Warps: one per head of a group, eight at most; teams of them, and fewer heads per CTA, where all make fewer than 16 per SM or where a row's own keys would not find room as candidates.
+// Warps: one per head of a group, eight at most; teams of them, and fewer heads per CTA, where all make fewer than 16 per SM (both sides at the file's head) or where a row's own keys would not
+// find room as candidates (up to 1024 of a warp, of which half may be: beyond, every count reads the cache again).
 template <typename T, int D>
 int own(const Cache& C, const DecodeArgs& A, cudaStream_t st) {
     const int64_t capacity = (int64_t)C.max_blocks << C.page_log;

@@ -189,6 +189,13 @@ def test_order(lens, w, Hq, page, blocks, kind, holes):
         assert torch.equal(again[0][i, :, :k], got[0][i, :, :k])
 
 
+@pytest.mark.parametrize("lens,w,Hq,kind", [([150000, 9000], 8192, 1, "crowded"), ([300000, 70000], 6000, 2, "random"), ([131072], 8192, 1, "equal"), ([40000, 100], 8193, 2, "equal"),
+                                            ([90000], 20000, 2, "crowded")])
+def test_order_of_long_prefixes(lens, w, Hq, kind):
+    """Lists that a CTA holds, of many pages of keys, and longer ones."""
+    test_order(lens, w, Hq, 256, -(-max(lens) // 256), kind, 0.02)
+
+
 # ---- decode --------------------------------------------------------------------------------------------------------------
 
 class World:
