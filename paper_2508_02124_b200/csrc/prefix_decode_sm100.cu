@@ -12,7 +12,7 @@
 // Warps: 0-3 softmax and the end, 4 issues the products, 5-8 gather (with two gathering 64 rows 26.7 us instead of 24.1, eight rows with long lists 34 instead of 29). Two CTAs per SM: 97 KB
 // of stages, Q and O each.
 //
-// Times (32 and 8 heads, d = 128): 64 rows behind 16K keys, w = 2048: 23 us; 256 rows in four prefixes of 8K: 36; 8 rows behind 64K, w = 4096: 26.5; 1024 rows behind 16K 111. On the CUDA
+// Times (32 and 8 heads, d = 128): 64 rows behind 16K keys, w = 2048: 23 us; 256 rows in four prefixes of 8K, w = 1024: 36; 8 rows behind 64K, w = 4096: 26.5; 1024 rows behind 16K, w = 2048, 111. On the CUDA
 // cores, whose tiles have eight rows (prefix_decode.cu): one row 28 us instead of 17, four 34 instead of 17, 64 rows of a prefix each 520 instead of 281; so bf16 comes here however few its rows are.
 // With few rows it is the list's read, a gather of 512 bytes a key from places as the weights fall, that a CTA's 8 tiles wait for (64 rows: 34 MB asked of the L2, 30 of them of memory; tensor
 // pipe 14 % active), and start and end: rows, Q, the cluster's sum. With many rows it is the softmax' threads (1024 rows: 0.47 PFLOP/s of products, both parts of P counted).

@@ -1,9 +1,9 @@
 // The order of prefixes (include/dma.h, dma_prefix_order): of every prefix and query head the w keys of the largest delta, sorted.
 //
 // The weakest kept key of each (prefix, head) is found as decoding finds it (cache4_select.cu); what is not below it is collected and sorted, by a CTA per (prefix, head) where shared memory
-// holds the list, 8192 entries, else in chunks of it. Ordering is round trips and instructions, not memory: 32 heads of 16K keys, w = 2048: 17 us (rows 2, selection 6.4, lists 8.5; the
-// weights' bytes 0.4); five prefixes of up to 64K, w = 4096: 45 us (2, 20, 23; bytes 4.6). In chunks the first takes 33 us; 16 prefixes of 16K, w = 4096, 110 instead of 57; one of 256K 63
-// and 65, one of 1M, w = 8192, 155 and 192, which a prefix pays once. In chunks one of 256K, w = 16384, takes 91 us, one of 1M 157.
+// holds the list, 8192 entries, else in chunks of it. Ordering is round trips and instructions, not memory: 32 heads of 16K keys, w = 2048: 16 us (rows 2, selection 6.4, lists 7.8; the
+// weights' bytes 0.4); five prefixes of up to 64K, w = 4096: 40 us (2, 20, 18; bytes 4.6). In chunks the first takes 33 us; 16 prefixes of 16K, w = 4096, 110 instead of 49; one of 256K 63
+// instead of 54, one of 1M, w = 8192, 155 instead of 180. In chunks one of 256K, w = 16384, takes 91 us, one of 1M 157.
 #include <algorithm>
 #include <type_traits>
 
@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(256) order_rows_kernel(Order P, int32_t* seq, 
     }
 }
 
-// f(order keys) for the keys of [j0, j1) (j0 a multiple of 16), sixteen of a thread side by side in one page (pages have 16 keys and more); 0 for places without a key.
+// f(patterns, position, how many there are, where they lie) for the keys of [j0, j1) (j0 a multiple of 16), sixteen of a thread side by side in one page (pages have 16 keys and more).
 template <int NT, typename F>
 __device__ __forceinline__ void sweep(const Order& P, int s, int h, int j0, int j1, F f) {
     const int32_t* pages = P.table + s * P.ld;
@@ -59,24 +59,35 @@ __device__ __forceinline__ void sweep(const Order& P, int s, int h, int j0, int 
     for (int b = j0; b < j1; b += NT * 16) {
         const int j = b + threadIdx.x * 16, page = next;
         const bool there = (unsigned)page < (unsigned)P.num_pages;
+        const uint32_t* from = reinterpret_cast<const uint32_t*>(P.delta) + (((size_t)(there ? page : 0) * P.Hq + h) << P.page_log) + (j & mask);
         uint32_t u[16];
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
             uint4 x = make_uint4(0u, 0u, 0u, 0u);
-            if (there) x = *reinterpret_cast<const uint4*>(P.delta + (((size_t)page * P.Hq + h) << P.page_log) + (j & mask) + i);
+            if (there) x = *reinterpret_cast<const uint4*>(from + i);
             u[i] = x.x; u[i + 1] = x.y; u[i + 2] = x.z; u[i + 3] = x.w;
         }
         next = page_of(j + NT * 16);
-        f(u, j, there ? min(16, j1 - j) : 0);
+        f(u, j, there ? min(16, j1 - j) : 0, from);
     }
 }
 
-// The kept ones among a thread's `n` keys from position j on to `to`, in no order; `count` is moved on.
-__device__ __forceinline__ void collect(const uint32_t (&u)[16], int j, int n, unsigned long long least, unsigned long long* to, int room, int* count) {
+// The kept ones among a thread's `n` keys from position j on to `to`, in no order; `count` is moved on. Few are kept as a rule: a thread reads them again one by one (all sixteen
+// in turn, with keys compared in 64 bits: 160 lists of 64K keys 35 us instead of 27).
+__device__ __forceinline__ void collect(const uint32_t (&u)[16], int j, int n, const uint32_t* from, unsigned long long least, unsigned long long* to, int room, int* count) {
     const int lane = threadIdx.x & 31;
-    uint32_t flags = 0;
+    // the weakest kept key's pattern and position: keys of the same weight are kept up to there
+    const int pattern = (int)(least >> 32);
+    const uint32_t last = 0xFFFFFFFFu - (uint32_t)least;
+    auto above = [&](int than) {
+        uint32_t flags = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) flags |= (uint32_t)(i < n && order_key(u[i] & 0x7FFFFFFFu, j + i) >= least) << i;
+        for (int i = 0; i < 16; ++i) flags |= (uint32_t)((int)(u[i] & 0x7FFFFFFFu) > than) << i;
+        return flags;
+    };
+    uint32_t flags = above((uint32_t)j <= last ? pattern - 1 : pattern);
+    if ((uint32_t)j <= last && last < (uint32_t)j + 15u) flags &= above(pattern) | ((2u << (last - (uint32_t)j)) - 1u);
+    flags &= (1u << max(n, 0)) - 1u;
     const int mine = __popc(flags);
     int at = mine;
 #pragma unroll
@@ -87,12 +98,10 @@ __device__ __forceinline__ void collect(const uint32_t (&u)[16], int j, int n, u
     int base = 0;
     if (lane == 31 && at) base = atomicAdd(count, at);
     at += __shfl_sync(0xffffffffu, base, 31) - mine;
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-        if (flags >> i & 1u) {
-            if (at < room) to[at] = order_key(u[i] & 0x7FFFFFFFu, j + i);
-            ++at;
-        }
+    for (; flags; flags &= flags - 1u, ++at) {
+        const int i = __ffs(flags) - 1;
+        if (at < room) to[at] = order_key(from[i] & 0x7FFFFFFFu, j + i);
+    }
 }
 
 __device__ __forceinline__ void put(const Order& P, int item, int s, int place, unsigned long long key) {
@@ -151,7 +160,7 @@ __device__ void sort_down(unsigned long long (&v)[E], unsigned long long* buf) {
 // Lists of up to E * NT entries by a CTA per (prefix, head). What is kept is collected in shared memory, dealt into as many bins between the smallest and the largest weight as the list may
 // have entries, and ranked within its bin; where a bin has many (weights that crowd), sorted by a bitonic network instead (2048 entries: 6 us more).
 template <int NT, int E>
-__global__ void __launch_bounds__(NT) order_held_kernel(Order P) {
+__global__ void __launch_bounds__(NT, 1024 / NT) order_held_kernel(Order P) {
     constexpr int N = E * NT, kCrowd = 48;
     extern __shared__ unsigned long long e[];                     // [2][N] entries, [N] bins
     __shared__ int count, crowd;
@@ -165,7 +174,7 @@ __global__ void __launch_bounds__(NT) order_held_kernel(Order P) {
     if (tid == 0) { count = 0; crowd = 0; lowest = ~0u; highest = 0u; }
     for (int i = tid; i < N; i += NT) bins[i] = 0;
     __syncthreads();
-    sweep<NT>(P, s, h, 0, n, [&](const uint32_t (&u)[16], int j, int m) { collect(u, j, m, least, e, N, &count); });
+    sweep<NT>(P, s, h, 0, n, [&](const uint32_t (&u)[16], int j, int m, const uint32_t* from) { collect(u, j, m, from, least, e, N, &count); });
     __syncthreads();
     const int c = min(count, P.cap);
     uint32_t lo = ~0u, hi = 0u;
@@ -243,7 +252,7 @@ __global__ void __launch_bounds__(kSpan / 16) order_collect_kernel(Order P) {
     pdl_enter();
     const int n = P.visible(s), j0 = min(n, span * kSpan), j1 = min(n, j0 + kSpan);
     const unsigned long long least = P.weakest ? P.weakest[item] : 0ull;
-    sweep<kSpan / 16>(P, s, h, j0, j1, [&](const uint32_t (&u)[16], int j, int m) { collect(u, j, m, least, P.run + (size_t)item * P.cap, P.cap, &P.room[item]); });
+    sweep<kSpan / 16>(P, s, h, j0, j1, [&](const uint32_t (&u)[16], int j, int m, const uint32_t* from) { collect(u, j, m, from, least, P.run + (size_t)item * P.cap, P.cap, &P.room[item]); });
 }
 
 __global__ void __launch_bounds__(1024) order_sort_kernel(Order P) {
@@ -338,17 +347,21 @@ int launch_prefix_order(const Cache& C0, const float* delta, const int32_t* tabl
         if ((rc = launch_cache4_select(C, R, (unsigned long long*)(p + L.weakest), Plan{}, st))) return rc;
     }
     const int64_t items = (int64_t)C.nseq * C.Hq;
-    auto held = [&](auto e_tag) {
-        constexpr int E = decltype(e_tag)::value, NT = 1024, smem = E * NT * 20;
+    auto held = [&](auto n_tag, auto e_tag) {
+        constexpr int NT = decltype(n_tag)::value, E = decltype(e_tag)::value, smem = E * NT * 20;
         auto kernel = order_held_kernel<NT, E>;
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return (int)DMA_ERR_CUDA;
         return launch_overlapped(kernel, dim3((unsigned)items), dim3(NT), smem, st, 1, P);
     };
+    // More lists than SMs: smaller CTAs, several per SM (2048 lists of 1024 entries 26 us, of 1024 threads 72; 512 of 4096 30 and 37). Else all the threads that a CTA may have (32 of 4096
+    // from 256K keys 29 us, of 512 threads 36).
     if (L.cap <= kHeld) {
-        if (L.cap <= 1024) return held(std::integral_constant<int, 1>{});
-        if (L.cap <= 2048) return held(std::integral_constant<int, 2>{});
-        if (L.cap <= 4096) return held(std::integral_constant<int, 4>{});
-        return held(std::integral_constant<int, 8>{});
+        using std::integral_constant;
+        const bool many = items > 148;
+        if (L.cap <= 1024) return many ? held(integral_constant<int, 256>{}, integral_constant<int, 4>{}) : held(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
+        if (L.cap <= 2048) return many ? held(integral_constant<int, 512>{}, integral_constant<int, 4>{}) : held(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+        if (L.cap <= 4096) return many ? held(integral_constant<int, 512>{}, integral_constant<int, 8>{}) : held(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+        return held(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
     }
     if ((rc = launch_overlapped(order_collect_kernel, dim3((unsigned)(items * L.spans)), dim3(kSpan / 16), 0, st, 1, P))) return rc;
     const unsigned grid = (unsigned)(items * L.chunks);

@@ -14,7 +14,7 @@
 // few warps (8 rows of 4096 own keys: 36 us without them, 19 with), up to 16 warps per SM (asked to make 32 with 64 rows of 1024 own keys: 57 us instead of 33, since every team pays for
 // its barriers).
 //
-// Times (own keys ragged, 32 and 8 heads, d = 128): 64 rows of up to 1024 own keys behind 16K keys, w = 2048: 24 us; 256 rows of up to 512 behind 8K: 58; 8 rows of up to 4096 behind 64K,
+// Times (own keys ragged, 32 and 8 heads, d = 128): 64 rows of up to 1024 own keys behind 16K keys, w = 2048: 24 us; 256 rows of up to 512 behind 8K, w = 1024: 58; 8 rows of up to 4096 behind 64K,
 // w = 4096: 16. Bound by round trips that few warps hide: pages, weights, the cut, then rows of K and V a stage ahead (64 rows: 10 warps per SM, issue slots 17 % busy; 256 rows: 14 warps, 32 %,
 // 186 MB from memory at 39 % of the copy's rate). 128 registers and 6.5 KB of shared memory per warp allow no more of them.
 #include <algorithm>

@@ -196,6 +196,13 @@ def test_order_of_long_prefixes(lens, w, Hq, kind):
     test_order(lens, w, Hq, 256, -(-max(lens) // 256), kind, 0.02)
 
 
+@pytest.mark.parametrize("w", [1, 1000, 1024, 2048, 2500, 4096, 5000])
+@pytest.mark.parametrize("kind", ["random", "crowded", "wide"])
+def test_order_of_many_prefixes(w, kind):
+    """More lists than the GPU has SMs."""
+    test_order([6000, 0, 1, 1024, 17, 5999, 2500, 4097, 100, 333, 4096, 3000], w, 13, 16, 375, kind, 0.01)
+
+
 # ---- decode --------------------------------------------------------------------------------------------------------------
 
 class World:
