@@ -59,7 +59,7 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4],
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Attention of a warp over keys that lie in shared memory (K's row, V's, kPitch bytes apart), a stage of them at a time; `bias` by key. Maximum and sum in natural units at the end.
+// Attention of a warp over keys that lie in shared memory (K's row, V's, kPitch bytes apart), a stage of them at a time; use: a bit for each that counts; list: their biases. Maximum and sum in natural units at the end.
 template <typename T, int D> struct Attend;
 
 // fp32, on the CUDA cores: eight lanes take a key, 4 channels of every 32 each.
@@ -75,13 +75,13 @@ struct Attend<float, D> {
         }
     }
     float s[kStage / 4];                                          // of the keys lane / 8, lane / 8 + 4
-    __device__ __forceinline__ void scores(const uint8_t* keys, const uint2* list, int count, int lane) {
+    __device__ __forceinline__ void scores(const uint8_t* keys, const uint2* list, uint32_t use, int lane) {
 #pragma unroll
         for (int i = 0; i < kStage; i += 4) {
             const int e = i + (lane >> 3);
             const float* row = reinterpret_cast<const float*>(keys + e * kPitch) + (lane & 7) * 4;
             float s = 0.0f;
-            if (e < count) {
+            if (use >> e & 1u) {
 #pragma unroll
                 for (int x = 0; x < C; x += 4) {
                     const float4 k = *reinterpret_cast<const float4*>(row + x * 8);
@@ -90,10 +90,10 @@ struct Attend<float, D> {
             }
 #pragma unroll
             for (int x = 1; x < 8; x <<= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
-            this->s[i / 4] = e < count ? s + __uint_as_float(list[e].x) : -INFINITY;
+            this->s[i / 4] = use >> e & 1u ? s + __uint_as_float(list[e].x) : -INFINITY;
         }
     }
-    __device__ __forceinline__ void values(uint8_t* keys, int count, int lane) {
+    __device__ __forceinline__ void values(uint8_t* keys, uint32_t use, int lane) {
 #pragma unroll
         for (int i = 0; i < kStage; i += 4) {
             const int e = i + (lane >> 3);
@@ -107,7 +107,7 @@ struct Attend<float, D> {
             l *= fade;
 #pragma unroll
             for (int x = 0; x < C; ++x) acc[x] = fade == 0.0f ? 0.0f : acc[x] * fade;
-            if (e < count) {
+            if (use >> e & 1u) {
                 const float w = expf(s - ref);
                 l += w;
 #pragma unroll
@@ -150,7 +150,7 @@ struct Attend<__nv_bfloat16, D> {
         }
     }
     float x0, x1;                                                 // of lane 4 i: the scores of keys i and i + 8, log2 units
-    __device__ __forceinline__ void scores(const uint8_t* keys, const uint2* list, int count, int lane) {
+    __device__ __forceinline__ void scores(const uint8_t* keys, const uint2* list, uint32_t use, int lane) {
         const uint32_t at_k = ptx::smem_u32(keys) + ((lane & 7) + ((lane >> 3) & 1) * 8) * kPitch + (lane >> 4) * 16;
         float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, s1[4] = {0.0f, 0.0f, 0.0f, 0.0f};       // (two chains)
 #pragma unroll
@@ -162,12 +162,13 @@ struct Attend<__nv_bfloat16, D> {
             mma_16816(s1, b, q[x + 1][0], q[x + 1][1]);
         }
         const int e = lane >> 2;
-        x0 = (lane & 3) == 0 && e < count ? fmaf(s[0] + s1[0], c1, __uint_as_float(list[e].x) * 1.4426950408889634f) : -INFINITY;
-        x1 = (lane & 3) == 0 && e + 8 < count ? fmaf(s[2] + s1[2], c1, __uint_as_float(list[e + 8].x) * 1.4426950408889634f) : -INFINITY;
+        x0 = (lane & 3) == 0 && (use >> e & 1u) ? fmaf(s[0] + s1[0], c1, __uint_as_float(list[e].x) * 1.4426950408889634f) : -INFINITY;
+        x1 = (lane & 3) == 0 && (use >> (e + 8) & 1u) ? fmaf(s[2] + s1[2], c1, __uint_as_float(list[e + 8].x) * 1.4426950408889634f) : -INFINITY;
     }
-    __device__ __forceinline__ void values(uint8_t* keys, int count, int lane) {
-        if (count < kStage) {                                     // (0 times what lies there must be 0)
-            for (int i = count * (D / 8) + lane; i < kStage * (D / 8); i += 32) *reinterpret_cast<uint4*>(keys + i / (D / 8) * kPitch + D * 2 + i % (D / 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
+    __device__ __forceinline__ void values(uint8_t* keys, uint32_t use, int lane) {
+        if (use != 0xFFFFu) {                                     // (0 times what lies there must be 0)
+            for (int i = lane; i < kStage * (D / 8); i += 32)
+                if (!(use >> i / (D / 8) & 1u)) *reinterpret_cast<uint4*>(keys + i / (D / 8) * kPitch + D * 2 + i % (D / 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
             __syncwarp();
         }
         const uint32_t at_v = ptx::smem_u32(keys) + ((lane & 7) + (lane >> 4) * 8) * kPitch + D * 2 + ((lane >> 3) & 1) * 16;
@@ -446,7 +447,7 @@ __device__ __forceinline__ void write_own(const DecodeArgs& A, int t, int h, boo
 template <typename T, int D, bool kTeams>
 __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warps_per_head, int room, int heads) {       // heads: of a CTA
     using At = Attend<T, D>;
-    extern __shared__ __align__(16) uint8_t dynamic[];            // of each warp [At::kStage][At::kPitch] keys, [room]: (pattern of delta, slot) of candidates by position, then of the kept ones
+    extern __shared__ __align__(16) uint8_t dynamic[];            // of each warp [At::kStage][At::kPitch] keys, [room]: (pattern of delta, slot) of candidates by position, then of the kept ones; of teams [64] sorted
     __shared__ OwnShared S;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x / 32, team = kTeams ? warps_per_head : 1;
     pdl_enter();
@@ -464,6 +465,11 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
     const T* kv = (const T*)A.kv;
     constexpr int kStageBytes = At::kStage * At::kPitch;
     uint8_t* keys_at = dynamic + warp * kStageBytes;
+    // what may be asked for at once: the list's length, the first pages
+    const int in_team = kTeams ? warp % team : 0, leader = warp - in_team, bar = 1 + warp / team;
+    const int seg = (n + team * 64 - 1) / (team * 64) * 64, j0 = min(n, in_team * seg), j1 = min(n, j0 + seg);
+    auto page_of = [&](int j, int end) { return j < end ? pages[j >> A.page_log] : -1; };
+    const int page_all = sizeof(T) == 2 ? page_of(warp * 16, n) : -1, page_mine = page_of(j0 + 16 * lane, j1);
     int listed = 0;
     if ((unsigned)g < (unsigned)A.nprefix) listed = (int)max((int64_t)0, min((int64_t)min(A.order_len[g], A.w), A.order_ld));
     const bool behind = listed > 0, floored = listed == A.w;      // (as DecodeArgs::listed)
@@ -477,11 +483,11 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
                 AttendAll<D> at;
                 at.start((const T*)A.q + t * A.qs_row + h * A.qs_head, real, A.scale, lane);
                 // 16 keys at a time, side by side in one page, turn by turn of the warps
-                int next = warp * 16 < n ? pages[warp * 16 >> A.page_log] : -1;
+                int next = page_all;
 #pragma unroll 1
                 for (int j = warp * 16; j < n; j += warps * 16) {
                     const int page = next, count = min(n - j, 16);
-                    next = j + warps * 16 < n ? pages[(j + warps * 16) >> A.page_log] : -1;
+                    next = page_of(j + warps * 16, n);
                     if ((unsigned)page >= (unsigned)A.num_pages) continue;
                     const uint8_t* from = (const uint8_t*)(kv + key_row(page, hk, j & mask, A.Hkv, A.page_log) * (2 * D));
                     auto copy = [&](int which) {
@@ -533,18 +539,15 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
             return;
         }
     }
-    const int in_team = kTeams ? warp % team : 0, leader = warp - in_team, bar = 1 + warp / team;
     uint2* found = reinterpret_cast<uint2*>(dynamic + warps * kStageBytes);
     uint2* mine = found + warp * room;
-    const int seg = (n + team * 64 - 1) / (team * 64) * 64, j0 = min(n, in_team * seg), j1 = min(n, j0 + seg);
 #pragma unroll 1
     for (int head = head0 + warp / team; head < head1; head += warps / team) {
     const int h = hk * A.G + head;
     const float* weight = A.order_weight + ((int64_t)g * A.Hq + h) * A.order_ld;
     // f(position, slot, patterns) for the part's keys, 512 at a time: a lane has 16 of them, side by side in one page (pages have 16 keys and more). Patterns of places without a key: -2
     auto sweep = [&](auto f) {
-        auto page_of = [&](int j) { return j < j1 ? pages[j >> A.page_log] : -1; };
-        int next = page_of(j0 + 16 * lane);
+        int next = page_mine;
 #pragma unroll 1
         for (int b = j0; b < j1; b += 512) {
             const int j = b + 16 * lane, page = next, slot = (page << A.page_log) + (j & mask);
@@ -556,17 +559,25 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
                 if (there) x = *reinterpret_cast<const int4*>(A.delta + (((size_t)page * A.Hq + h) << A.page_log) + (j & mask) + i);
                 u[i] = x.x; u[i + 1] = x.y; u[i + 2] = x.z; u[i + 3] = x.w;
             }
-            next = page_of(j + 512);
+            next = page_of(j + 512, j1);
             if (b + 512 > j1)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) u[i] = j + i < j1 ? u[i] : -2;
             f(j, slot, u);
         }
     };
+    // what a full list's end asks of the own keys: its entries' patterns plus one, from the last on
+    uint32_t asked[2] = {0u, 0u};
+    if (floored)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int back = i * 32 + lane;
+            asked[i] = back < listed ? (__float_as_uint(weight[listed - 1 - back]) & 0x7FFFFFFFu) + 1u : ~0u;
+        }
     At at;
     at.start((const T*)A.q + t * A.qs_row + h * A.qs_head, A.scale, lane);
     // what may be kept: every key that there is, or those above the list's last entry
-    const int floor = floored ? __float_as_int(weight[listed - 1]) & 0x7FFFFFFF : -1;
+    const int floor = (int)__shfl_sync(0xffffffffu, asked[0], 0) - 1;
     int c = 0;
     sweep([&](int, int slot, const int (&u)[16]) {
         int count = 0;
@@ -589,6 +600,27 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
     });
     if (lane == 0) S.cands[warp] = c;
     __syncwarp();
+    // eight lanes take 128 bytes of a key at a time; K's rows and V's are groups of their own
+    auto copy = [&](int i, int which, int kept) {
+        const uint32_t to = ptx::smem_u32(keys_at) + which * kRow + (lane & 7) * 16;
+#pragma unroll
+        for (int e0 = 0; e0 < At::kStage; e0 += 4) {
+            const int e = i + e0 + (lane >> 3);
+            if (e < kept) {
+                const int slot = (int)mine[e].y;
+                const uint8_t* from = (const uint8_t*)(kv + key_row(slot >> A.page_log, hk, slot & mask, A.Hkv, A.page_log) * (2 * D)) + which * kRow + (lane & 7) * 16;
+#pragma unroll
+                for (int x = 0; x < kRow; x += 128) ptx::cp_async16_at(to + (e0 + (lane >> 3)) * At::kPitch + x, from + x);
+            }
+        }
+        cp_async_commit();
+    };
+    // Candidates against a full list are kept as a rule: the first of them are on their way while the cut is found, and count or not.
+    const int ahead = floored && c <= room ? min(c, At::kStage) : 0;
+    if (ahead) {
+        copy(0, 0, ahead);
+        copy(0, 1, ahead);
+    }
     int cands = c, most = c, step = 0;
     if (team > 1) {
         team_sync(bar, team * 32);
@@ -642,7 +674,7 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     const int e = 32 * i + lane;
-                    last[i] = e < cands ? rival(e) : ~0u;
+                    last[i] = e >= cands ? ~0u : i < 2 ? asked[i & 1] : rival(e);
                     int x = 0, at = e;
                     if (kTeams)
                         while (x < team && at >= S.cands[leader + x]) at -= S.cands[leader + x++];
@@ -687,7 +719,7 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
         }
         if (kTeams && !done && most <= 64) {
             // every warp its own candidates, sorted; one's rank is the sum of its ranks in all of them (equal ones by warp)
-            uint32_t* sorted = reinterpret_cast<uint32_t*>(keys_at);
+            uint32_t* sorted = reinterpret_cast<uint32_t*>(found + warps * room) + warp * 64;
             uint32_t v[2];                                        // (patterns plus one: 0 is none)
 #pragma unroll
             for (int i = 0; i < 2; ++i) v[i] = i * 32 + lane < c ? mine[i * 32 + lane].x + 1u : 0u;
@@ -699,7 +731,7 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
 #pragma unroll 1
             for (int x = leader; x < leader + team; ++x) {
                 if (x == warp) continue;
-                const uint32_t* other = reinterpret_cast<const uint32_t*>(dynamic + x * kStageBytes);
+                const uint32_t* other = reinterpret_cast<const uint32_t*>(found + warps * room) + x * 64;
                 const uint32_t less = x < warp ? 0u : 1u;         // in front of v: what is not below v + less
                 int lo[2] = {0, 0};
 #pragma unroll
@@ -818,10 +850,19 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
         }
     }
     // attention over the kept ones, a stage of keys at a time
-    for (int b = over ? j0 : 0; b < (over ? j1 : c);) {
+    int b = over ? j0 : 0, front = over ? 0 : ahead;              // (a warp whose candidates had room may be of a team whose had not: what is on its way is then not used)
+    uint32_t use = ~0u;                                           // of the first stage
+    if (front) {
+        use = __ballot_sync(0xffffffffu, lane < front && order_key(mine[lane].x, place(lane)) >= least);
+        b = front;
+    } else if (ahead) {
+        cp_async_wait<0>();
+        __syncwarp();
+    }
+    const int end = over ? j1 : c;
+    do {
         // as many kept ones as there is room for, at the front of the warp's part; where the candidates did not fit, from the cache again
-        int kept = 0;
-        const int end = over ? j1 : c;
+        int kept = front;
         for (; b < end && (!over || kept + 32 <= room); b += 32) {
             uint2 o = make_uint2(0u, 0u);
             bool keep = false;
@@ -841,40 +882,28 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
             kept += __popc(bits);
             __syncwarp();
         }
-        // eight lanes take 128 bytes of a key at a time; K's rows and V's are groups of their own, the next stage's K on its way while this one's V is used
-        auto copy = [&](int i, int which) {
-            const uint32_t to = ptx::smem_u32(keys_at) + which * kRow + (lane & 7) * 16;
-#pragma unroll
-            for (int e0 = 0; e0 < At::kStage; e0 += 4) {
-                const int e = i + e0 + (lane >> 3);
-                if (e < kept) {
-                    const int slot = (int)mine[e].y;
-                    const uint8_t* from = (const uint8_t*)(kv + key_row(slot >> A.page_log, hk, slot & mask, A.Hkv, A.page_log) * (2 * D)) + which * kRow + (lane & 7) * 16;
-#pragma unroll
-                    for (int x = 0; x < kRow; x += 128) ptx::cp_async16_at(to + (e0 + (lane >> 3)) * At::kPitch + x, from + x);
-                }
-            }
-            cp_async_commit();
-        };
-        if (kept) {
-            copy(0, 0);
-            copy(0, 1);
+        if (kept && !front) {
+            copy(0, 0, kept);
+            copy(0, 1, kept);
         }
+        // the next stage's K is on its way while this one's V is used
 #pragma unroll 1
         for (int i = 0; i < kept; i += At::kStage) {
-            const int count = min(kept - i, At::kStage);
+            use &= (1u << min(kept - i, At::kStage)) - 1u;
             cp_async_wait<1>();
             __syncwarp();
-            at.scores(keys_at, mine + i, count, lane);
+            at.scores(keys_at, mine + i, use, lane);
             __syncwarp();
-            copy(i + At::kStage, 0);
+            copy(i + At::kStage, 0, kept);
             cp_async_wait<1>();
             __syncwarp();
-            at.values(keys_at, count, lane);
+            at.values(keys_at, use, lane);
             __syncwarp();
-            copy(i + At::kStage, 1);
+            copy(i + At::kStage, 1, kept);
+            use = ~0u;
         }
-    }
+        front = 0;
+    } while (b < end);
     at.end(reinterpret_cast<float*>(keys_at), lane);
     if (lane == 0) { S.m[warp] = at.m; S.l[warp] = at.l; }
     team_sync(bar, team * 32);
@@ -908,7 +937,7 @@ int own(const Cache& C, const DecodeArgs& A, cudaStream_t st) {
         if (heads * team > kWarps) heads /= 2;
     }
     const int room = (int)std::min<int64_t>((capacity + team * 64 - 1) / (team * 64) * 64, 512), warps = heads * team;
-    const size_t smem = std::max<size_t>((size_t)warps * (room * sizeof(uint2) + Attend<T, D>::kStage * Attend<T, D>::kPitch), 32 * 1024 / kWarps * warps);
+    const size_t smem = std::max<size_t>((size_t)warps * (room * sizeof(uint2) + Attend<T, D>::kStage * Attend<T, D>::kPitch + (team > 1 ? 256 : 0)), 32 * 1024 / kWarps * warps);
     auto kernel = team > 1 ? own_kernel<T, D, true> : own_kernel<T, D, false>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return DMA_ERR_CUDA;
     return launch_overlapped(kernel, dim3((unsigned)(ctas(heads) + 1)), dim3(32 * warps), smem, st, 1, A, team, room, heads == most ? C.G : heads);
