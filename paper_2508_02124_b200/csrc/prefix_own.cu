@@ -4,21 +4,21 @@
 // prefix' part ends with the first m for which m + #{own > weight_m} >= k (ties: the prefix' keys come first), and the own part is the k - m best of the row's own keys. Where the list
 // has w entries, own keys that do not exceed its last cannot be kept and are left out at once: of n own keys behind a prefix of N about n w / N remain, the candidates. Each of them takes
 // at most one entry's place: the i-th best is kept if it is above the i-th entry from the list's end. So
-//   - few candidates, a full list: the lowest is dropped as long as it fails, a minimum of the warp each time (by sorting at once: 256 rows of 512 own keys 105 us instead of 101, 64 of
-//     1024 34.6 instead of 33);
-//   - else they are sorted and matched against the list's end: by a warp up to 256 of them in registers, by a team up to 64 per warp, ranks added up by searching the other warps' sorted ones;
-//   - beyond, or without room in shared memory for all of them (512 a warp): bisection of the cut, then of the weakest own key, each count a sweep of the team.
+//   - up to 64 candidates, a full list: the first stage's K and V are requested, the lowest candidate is dropped as long as it fails, a minimum of the warp each time (without both: 16 rows of
+//     64 own keys 10.3 us instead of 8.2, 256 of 512 55 instead of 53.5);
+//   - else: how many are kept by bisection, #{own keys that are not below entry i from the end} > i, the entries in shared memory; then the weakest between the two entries around it (256 rows
+//     of 512 own keys behind 2048, w = 1024: 140 us; by sorting up to 256 of them, and bisecting over the list where it lies beyond, 173);
+//   - without room in shared memory for all of them (512 a warp): bisection of the cut over the list where it lies, then of the weakest own key, each count a sweep of the cache by the team.
 // A row that keeps everything whatever its weights needs no cut: its warps take parts of the keys with all heads together (40 rows of up to 300 own keys: 25 -> 6.5 us).
 //
 // A CTA takes a (row, KV head), so that K and V of a key that several heads keep come from the L1 or L2. A head has a warp or a team of them: teams where few rows would leave the SMs with
 // few warps (8 rows of 4096 own keys: 36 us without them, 19 with), up to 16 warps per SM (asked to make 32 with 64 rows of 1024 own keys: 57 us instead of 33, since every team pays for
 // its barriers).
 //
-// Times (own keys ragged, 32 and 8 heads, d = 128): 64 rows of up to 1024 own keys behind 16K keys, w = 2048: 24 us; 256 rows of up to 512 behind 8K, w = 1024: 58; 8 rows of up to 4096 behind 64K,
+// Times (own keys ragged, 32 and 8 heads, d = 128): 64 rows of up to 1024 own keys behind 16K keys, w = 2048: 23 us; 256 rows of up to 512 behind 8K, w = 1024: 54; 8 rows of up to 4096 behind 64K,
 // w = 4096: 16. Bound by round trips that few warps hide: pages, weights, the cut, then rows of K and V a stage ahead (64 rows: 10 warps per SM, issue slots 17 % busy; 256 rows: 14 warps, 32 %,
-// 186 MB from memory at 39 % of the copy's rate). 128 registers and 6.5 KB of shared memory per warp allow no more of them.
+// 186 MB from memory at 39 % of the copy's rate). 128 registers and 13 KB of shared memory per warp allow no more of them.
 #include <algorithm>
-#include <type_traits>
 
 #include "cache4_decode.cuh"
 #include "delta_fixed.cuh"
@@ -34,7 +34,6 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 struct OwnShared {
     unsigned long long least[kWarps];
     int part[2][kWarps], cands[kWarps], cut[kWarps];
-    uint32_t low[kWarps], high[kWarps];
     float m[kWarps], l[kWarps], all_m[kWarps][8], all_l[kWarps][8];
 };
 
@@ -389,39 +388,6 @@ __device__ void group_rows(const DecodeArgs& A, int* turn) {       // turn: kTog
     });
 }
 
-// R * 32 numbers of a warp in descending order, number i * 32 + lane in v[i].
-template <int R>
-__device__ __forceinline__ void sort_down(uint32_t (&v)[R], int lane) {
-    auto lanes = [&](int k, int j) {                              // pairs that j < 32 lanes part, in runs of k
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const uint32_t o = __shfl_xor_sync(0xffffffffu, v[i], j);
-            const bool up = ((lane & j) == 0) == (((i * 32 + lane) & k) == 0);
-            v[i] = up ? max(v[i], o) : min(v[i], o);
-        }
-    };
-#pragma unroll 1
-    for (int k = 2; k <= 32; k *= 2)
-#pragma unroll 1
-        for (int j = k / 2; j > 0; j /= 2) lanes(k, j);
-#pragma unroll
-    for (int k = 64; k <= 32 * R; k *= 2) {
-#pragma unroll
-        for (int j = k / 2; j >= 32; j /= 2)
-#pragma unroll
-            for (int i = 0; i < R; ++i)
-                if (!(i & (j / 32))) {
-                    const int o = i | (j / 32);
-                    const uint32_t a = v[i], b = v[o];
-                    const bool down = ((i * 32) & k) == 0;
-                    v[i] = down ? max(a, b) : min(a, b);
-                    v[o] = down ? min(a, b) : max(a, b);
-                }
-#pragma unroll 1
-        for (int j = 16; j > 0; j /= 2) lanes(k, j);
-    }
-}
-
 // The sums of a row's own keys, D / 32 channels per lane: its piece, or its result where there is no prefix.
 template <typename T, int D>
 __device__ __forceinline__ void write_own(const DecodeArgs& A, int t, int h, bool behind, int cut, float top, float sum, const float (&o)[D / 32], int lane) {
@@ -447,7 +413,7 @@ __device__ __forceinline__ void write_own(const DecodeArgs& A, int t, int h, boo
 template <typename T, int D, bool kTeams>
 __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warps_per_head, int room, int heads) {       // heads: of a CTA
     using At = Attend<T, D>;
-    extern __shared__ __align__(16) uint8_t dynamic[];            // of each warp [At::kStage][At::kPitch] keys, [room]: (pattern of delta, slot) of candidates by position, then of the kept ones; of teams [64] sorted
+    extern __shared__ __align__(16) uint8_t dynamic[];            // of each warp [At::kStage][At::kPitch] keys, [room]: (pattern of delta, slot) of candidates by position, then of the kept ones
     __shared__ OwnShared S;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x / 32, team = kTeams ? warps_per_head : 1;
     pdl_enter();
@@ -615,12 +581,6 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
         }
         cp_async_commit();
     };
-    // Candidates against a full list are kept as a rule: the first of them are on their way while the cut is found, and count or not.
-    const int ahead = floored && c <= room ? min(c, At::kStage) : 0;
-    if (ahead) {
-        copy(0, 0, ahead);
-        copy(0, 1, ahead);
-    }
     int cands = c, most = c, step = 0;
     if (team > 1) {
         team_sync(bar, team * 32);
@@ -631,6 +591,13 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
         }
     }
     const bool over = most > room;                                // (of the whole team: keys are then told apart by position, else by their place in the list)
+    // Few candidates against a full list are kept as a rule: the first of them are on their way while the cut is found, and count or not.
+    const bool few = floored && !over && cands <= 64;
+    int ahead = few ? min(c, At::kStage) : 0;
+    if (ahead) {
+        copy(0, 0, ahead);
+        copy(0, 1, ahead);
+    }
     // keys that the row sees: all own ones are candidates where the list may not be full
     auto team_sum = [&](int x) {
         x = __reduce_add_sync(0xffffffffu, x);
@@ -648,7 +615,6 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
     unsigned long long least = 0;                                 // kept: the order keys that are not below
     auto place = [&](int e) { return in_team * (1 << 20) + e; };
     if (k < listed + cands) {
-        constexpr int kSorted = 256;
         // the i-th best own key has to be above one of this many entries from the list's end on (the entry's pattern plus one)
         auto rival = [&](int i) {
             const int back = i - (k - listed);
@@ -665,16 +631,15 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
             return 0ull;
         };
         bool done = false;
-        if (floored && !over && cands <= (kTeams ? 64 : kSorted)) {
-            // Few candidates fail against a full list: the lowest one is dropped as long as it does. (By a team's first warp.)
-            auto drop = [&](auto n_tag) {
-                constexpr int N = decltype(n_tag)::value;
-                unsigned long long keys[N];
-                uint32_t last[N];
+        if (few) {
+            // The lowest one is dropped as long as it fails. (By a team's first warp.)
+            if (in_team == 0) {
+                unsigned long long keys[2];
+                uint32_t last[2];
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
+                for (int i = 0; i < 2; ++i) {
                     const int e = 32 * i + lane;
-                    last[i] = e >= cands ? ~0u : i < 2 ? asked[i & 1] : rival(e);
+                    last[i] = e < cands ? asked[i] : ~0u;
                     int x = 0, at = e;
                     if (kTeams)
                         while (x < team && at >= S.cands[leader + x]) at -= S.cands[leader + x++];
@@ -683,28 +648,18 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
                 }
 #pragma unroll 1
                 for (int kept = cands; kept >= cands - 24 && !done; --kept) {
-                    unsigned long long low = keys[0];
-                    uint32_t pass = last[0];                      // what the kept-th best has to be above
-#pragma unroll
-                    for (int i = 1; i < N; ++i) {
-                        low = keys[i] < low ? keys[i] : low;
-                        pass = (kept - 1) >> 5 == i ? last[i] : pass;
-                    }
+                    const unsigned long long low = keys[0] < keys[1] ? keys[0] : keys[1];
                     const uint32_t hi = __reduce_min_sync(0xffffffffu, (uint32_t)(low >> 32)), lo = __reduce_min_sync(0xffffffffu, (uint32_t)(low >> 32) == hi ? (uint32_t)low : ~0u);
-                    pass = __shfl_sync(0xffffffffu, pass, (kept - 1) & 31);
+                    const uint32_t pass = __shfl_sync(0xffffffffu, (kept - 1) >> 5 == 1 ? last[1] : last[0], (kept - 1) & 31);       // what the kept-th best has to be above
                     if (kept <= 0 || hi + 1u > pass) {
                         done = true;
                         least = kept <= 0 ? ~0ull : (unsigned long long)hi << 32 | lo;
                         cut = k - kept;
                     } else {
 #pragma unroll
-                        for (int i = 0; i < N; ++i) keys[i] = keys[i] == ((unsigned long long)hi << 32 | lo) ? ~0ull : keys[i];
+                        for (int i = 0; i < 2; ++i) keys[i] = keys[i] == ((unsigned long long)hi << 32 | lo) ? ~0ull : keys[i];
                     }
                 }
-            };
-            if (in_team == 0) {
-                if (kTeams || cands <= 64) drop(std::integral_constant<int, 2>{});
-                else drop(std::integral_constant<int, kTeams ? 2 : 8>{});
             }
             if (kTeams) {
                 if (in_team == 0 && lane == 0) {
@@ -717,92 +672,42 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
                 done = cut >= 0;
             }
         }
-        if (kTeams && !done && most <= 64) {
-            // every warp its own candidates, sorted; one's rank is the sum of its ranks in all of them (equal ones by warp)
-            uint32_t* sorted = reinterpret_cast<uint32_t*>(found + warps * room) + warp * 64;
-            uint32_t v[2];                                        // (patterns plus one: 0 is none)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) v[i] = i * 32 + lane < c ? mine[i * 32 + lane].x + 1u : 0u;
-            sort_down<2>(v, lane);
-            sorted[lane] = v[0];
-            sorted[lane + 32] = v[1];
+        if (!done && !over) {
+            // The best own key is kept if the list's last entry is below it, the second if the last but one is, and so on: how many are, by bisection, i + 1 own keys or more being above
+            // the i-th entry from the end; then the weakest of them, between the entries on both sides.
+            uint32_t* ask = reinterpret_cast<uint32_t*>(dynamic + leader * kStageBytes);
+            if (ahead) cp_async_wait<0>();
+            ahead = 0;
             team_sync(bar, team * 32);
-            int rank[2] = {lane, 32 + lane};
-#pragma unroll 1
-            for (int x = leader; x < leader + team; ++x) {
-                if (x == warp) continue;
-                const uint32_t* other = reinterpret_cast<const uint32_t*>(found + warps * room) + x * 64;
-                const uint32_t less = x < warp ? 0u : 1u;         // in front of v: what is not below v + less
-                int lo[2] = {0, 0};
-#pragma unroll
-                for (int b = 32; b > 0; b /= 2)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        if (other[lo[i] + b - 1] >= v[i] + less) lo[i] += b;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) rank[i] += lo[i] + (lo[i] == 63 && other[63] >= v[i] + less);
-            }
-            uint32_t low = ~0u, high = 0u;                        // the weakest kept one, and the best of the others
-            int mine_kept = 0;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const bool keep = v[i] > 0u && v[i] > rival(rank[i]);
-                mine_kept += keep;
-                if (keep) low = min(low, v[i]); else high = max(high, v[i]);
-            }
-            const int kept = team_sum(mine_kept);
-            low = __reduce_min_sync(0xffffffffu, low);
-            high = __reduce_max_sync(0xffffffffu, high);
-            if (lane == 0) { S.low[warp] = low; S.high[warp] = high; }
+            for (int e = in_team * 32 + lane; e < cands; e += team * 32) ask[e] = rival(e);
             team_sync(bar, team * 32);
-            for (int i = 0; i < team; ++i) {
-                low = min(low, S.low[leader + i]);
-                high = max(high, S.high[leader + i]);
+            auto not_below = [&](uint32_t u) {
+                int sum = 0;
+#pragma unroll 4
+                for (int e = lane; e < c; e += 32) sum += mine[e].x >= u;
+                return team_sum(sum);
+            };
+            int kept = 0, end = cands;
+            while (kept < end) {
+                const int i = (kept + end) >> 1;
+                if (not_below(ask[i]) > i) kept = i + 1; else end = i;
             }
             cut = k - kept;
-            least = kept == 0 ? ~0ull : (unsigned long long)(low - 1u) << 32;
-            if (kept > 0 && high == low) least = among_equals(low - 1u, kept - team_sum((v[0] > low) + (v[1] > low)));
-            done = true;
-            team_sync(bar, team * 32);                            // (the sorted ones have been read)
-        }
-        if (done) {
-        } else if (!kTeams && !over && cands <= kSorted) {
-            // The best own key is kept if the list's last entry is below it, the second if the last but one is, and so on: the own keys in descending order against the list from its end on.
-            auto match = [&](auto r_tag) {
-                constexpr int R = decltype(r_tag)::value;
-                uint32_t v[R], w[R];                              // (patterns plus one: 0 is none)
-#pragma unroll
-                for (int i = 0; i < R; ++i) {
-                    w[i] = rival(i * 32 + lane);
-                    v[i] = i * 32 + lane < c ? mine[i * 32 + lane].x + 1u : 0u;
+            least = ~0ull;
+            if (kept) {
+                uint32_t a = ask[kept - 1], b = kept < cands ? ask[kept] : 1u << 31;     // `kept` or more are not below a, at most so many not below b
+                int at_a = not_below(a);
+                while (at_a != kept && b - a > 1u) {
+                    const uint32_t x = a + (b - a) / 2;
+                    const int n_x = not_below(x);
+                    if (n_x >= kept) { a = x; at_a = n_x; } else b = x;
                 }
-                sort_down<R>(v, lane);
-                int kept = 0;
-#pragma unroll
-                for (int i = 0; i < R; ++i) kept += __popc(__ballot_sync(0xffffffffu, v[i] > w[i]));       // (the first so many)
-                cut = k - kept;
-                uint32_t last = 0u, next = 0u;                    // the weakest kept one, and the one behind it
-#pragma unroll
-                for (int i = 0; i < R; ++i) {
-                    if ((kept - 1) >> 5 == i) last = v[i];
-                    if (kept >> 5 == i) next = v[i];
-                }
-                last = __shfl_sync(0xffffffffu, last, (kept - 1) & 31);
-                next = __shfl_sync(0xffffffffu, next, kept & 31);
-                if (kept >= 32 * R) next = 0u;
-                least = kept == 0 ? ~0ull : (unsigned long long)(last - 1u) << 32;
-                if (kept > 0 && next == last) {
-                    int better = 0;
-#pragma unroll
-                    for (int i = 0; i < R; ++i) better += __popc(__ballot_sync(0xffffffffu, v[i] > last));
-                    least = among_equals(last - 1u, kept - better);
-                }
-            };
-            if (cands <= 32) match(std::integral_constant<int, 1>{});
-            else if (cands <= 64) match(std::integral_constant<int, 2>{});
-            else if (cands <= 128) match(std::integral_constant<int, 4>{});
-            else match(std::integral_constant<int, 8>{});
-        } else {
+                const int need = at_a == kept ? kept : kept - not_below(b);
+                if (at_a == kept || need == 0) least = (unsigned long long)(at_a == kept ? a : b) << 32;
+                else least = among_equals(a, need);
+            }
+            team_sync(bar, team * 32);                            // (the entries have been read)
+        } else if (!done) {
             // order keys greater than entry m's weight
             auto above = [&](int m) { return (unsigned long long)((__float_as_uint(weight[m]) & 0x7FFFFFFFu) + 1u) << 32; };
             // Entry m of the list has m entries before it and every own key that is greater: the first of which there are k or more is not kept. Each own key takes at most one entry's
@@ -828,14 +733,10 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
                 }
                 // own keys whose order key is not below x (> 0)
                 int sum = 0;
-                if (!over) {
-                    for (int e = lane; e < c; e += 32) sum += order_key(mine[e].x, place(e)) >= x;
-                } else {
-                    sweep([&](int j, int, const int (&u)[16]) {
+                sweep([&](int j, int, const int (&u)[16]) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) sum += u[i] > floor && order_key((uint32_t)u[i], j + i) >= x;
-                    });
-                }
+                    for (int i = 0; i < 16; ++i) sum += u[i] > floor && order_key((uint32_t)u[i], j + i) >= x;
+                });
                 sum = team_sum(sum);
                 if (cutting) {
                     const int m = (lo + hi) >> 1;
@@ -937,7 +838,7 @@ int own(const Cache& C, const DecodeArgs& A, cudaStream_t st) {
         if (heads * team > kWarps) heads /= 2;
     }
     const int room = (int)std::min<int64_t>((capacity + team * 64 - 1) / (team * 64) * 64, 512), warps = heads * team;
-    const size_t smem = std::max<size_t>((size_t)warps * (room * sizeof(uint2) + Attend<T, D>::kStage * Attend<T, D>::kPitch + (team > 1 ? 256 : 0)), 32 * 1024 / kWarps * warps);
+    const size_t smem = std::max<size_t>((size_t)warps * (room * sizeof(uint2) + Attend<T, D>::kStage * Attend<T, D>::kPitch), 32 * 1024 / kWarps * warps);
     auto kernel = team > 1 ? own_kernel<T, D, true> : own_kernel<T, D, false>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return DMA_ERR_CUDA;
     return launch_overlapped(kernel, dim3((unsigned)(ctas(heads) + 1)), dim3(32 * warps), smem, st, 1, A, team, room, heads == most ? C.G : heads);
