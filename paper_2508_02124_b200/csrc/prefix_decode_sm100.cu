@@ -12,10 +12,10 @@
 // Warps: 0-3 softmax and the end, 4 issues the products, 5-8 gather (with two gathering 64 rows 26.7 us instead of 24.1, eight rows with long lists 34 instead of 29). Two CTAs per SM: 97 KB
 // of stages, Q and O each.
 //
-// Times (32 and 8 heads, d = 128): 64 rows behind 16K keys, w = 2048: 23 us; 256 rows in four prefixes of 8K, w = 1024: 36; 8 rows behind 64K, w = 4096: 26.5; 1024 rows behind 16K, w = 2048, 111. On the CUDA
+// Times (32 and 8 heads, d = 128): 64 rows behind 16K keys, w = 2048: 23 us; 256 rows in four prefixes of 8K, w = 1024: 32; 8 rows behind 64K, w = 4096: 26.5; 1024 rows behind 16K, w = 2048, 94. On the CUDA
 // cores, whose tiles have eight rows (prefix_decode.cu): one row 28 us instead of 17, four 34 instead of 17, 64 rows of a prefix each 520 instead of 281; so bf16 comes here however few its rows are.
 // With few rows it is the list's read, a gather of 512 bytes a key from places as the weights fall, that a CTA's 8 tiles wait for (64 rows: 34 MB asked of the L2, 30 of them of memory; tensor
-// pipe 14 % active), and start and end: rows, Q, the cluster's sum. With many rows it is the softmax' threads (1024 rows: 0.47 PFLOP/s of products, both parts of P counted).
+// pipe 14 % active), and start and end: rows, Q, the cluster's sum. With many rows it is the softmax' threads (1024 rows: 0.55 PFLOP/s of products, both parts of P counted).
 #include <algorithm>
 #include <type_traits>
 
@@ -39,6 +39,7 @@ struct Shared {
     alignas(1024) uint8_t kv[kStages][2][kTile];              // in the end: O [128][D] fp32, 16-byte parts at (part ^ row)
     alignas(16) float bias[kStages][kKeys];                   // delta log2 e
     float m[128], l[128], joined_m[64], joined_l[64];
+    float share[128], own_share[128], over_sum[128];          // of the sum: factors by (row of this CTA, rank), of the rows' own keys, one by the sum
     int row[128], cut[128];
     uint32_t bad[4];                                          // rows to form again, a bit each
     uint64_t q_full, full[kStages], bias_full[kStages], empty[kStages], s_full[2], p_full[2], o_done[2];
@@ -382,58 +383,77 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_kernel(DecodeArgs A, int n
         if (copies == 2) join(std::integral_constant<int, 2>{}); else join(std::integral_constant<int, 4>{});
     }
     const float *sM = copies > 1 ? S.joined_m : S.m, *sL = copies > 1 ? S.joined_l : S.l;
-    // The sum: a warp per row, in turn over the cluster's CTAs; the piece from the row's own keys is requested first.
+    // The sum: every CTA of the cluster has every nrank-th row. A thread per row for the factors, then one per 16 bytes of O, several of
+    // which it has under way at once (a warp per row after row, factors by shuffles: 256 rows 36 us instead of 32, 1024 110 instead of 94).
+    const int mine = (R - rank + nrank - 1) / nrank;
     float om = -INFINITY, ol = 0.0f;
-    float2 own0 = make_float2(0.0f, 0.0f), own1 = own0;
-    auto request = [&](int r) {
-        if (r >= R) return;
-        const float* own = A.piece_of(S.row[r], h, 0, D);
+    if (tid < mine) {
+        const float* own = A.piece_of(S.row[tid * nrank + rank], h, 0, D);
         om = own[0];
         ol = own[1];
-        if (lane < D / 4) {
-            own0 = *reinterpret_cast<const float2*>(own + 2 + lane * 4);
-            own1 = *reinterpret_cast<const float2*>(own + 4 + lane * 4);
+    }
+    if (nrank > 1) cluster_sync(); else __syncthreads();
+    auto sum_up = [&](auto n_tag) {
+        constexpr int N = decltype(n_tag)::value, U = N == 1 ? 4 : 8 / N;
+        if (tid < mine) {
+            const int r = tid * N + rank;
+            float pm[N], pl[N], top = om, sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                pm[i] = ld_cluster(map_rank(smem_u32(&sM[r]), i));
+                pl[i] = ld_cluster(map_rank(smem_u32(&sL[r]), i));
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) top = fmaxf(top, pm[i]);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float f = factor(pm[i], pl[i], top);
+                if (f != 0.0f) sum += pl[i] * f;
+                S.share[tid * N + i] = f;
+            }
+            const float of = factor(om, ol, top);
+            if (of != 0.0f) sum += ol * of;
+            S.own_share[tid] = of;
+            S.over_sum[tid] = sum == 0.0f ? 0.0f : 1.0f / sum;
+            A.lse[S.row[r] * A.Hq + h] = sum == 0.0f ? -INFINITY : top + logf(sum);
+        }
+        __syncthreads();
+#pragma unroll 1
+        for (int i0 = tid; i0 < mine * (D / 4); i0 += kThreads * U) {
+            float4 v[U][N];
+            float2 own[U][2];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * kThreads, r = i / (D / 4) * N + rank, part = i % (D / 4);
+                if (i >= mine * (D / 4)) continue;
+#pragma unroll
+                for (int x = 0; x < N; ++x) v[u][x] = ld_cluster4(map_rank(sO + o_part<D>(r, part), x));
+                const float* piece = A.piece_of(S.row[r], h, 0, D) + 2 + part * 4;
+                own[u][0] = *reinterpret_cast<const float2*>(piece);
+                own[u][1] = *reinterpret_cast<const float2*>(piece + 2);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * kThreads, k = i / (D / 4), part = i % (D / 4);
+                if (i >= mine * (D / 4)) continue;
+                float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                for (int x = 0; x < N; ++x) {
+                    const float f = S.share[k * N + x];
+                    if (f != 0.0f) add(acc, v[u][x], f);          // (what a part without keys left may be anything)
+                }
+                const float of = S.own_share[k], inv = S.over_sum[k];
+                if (of != 0.0f) add(acc, make_float4(own[u][0].x, own[u][0].y, own[u][1].x, own[u][1].y), of);
+                uint2 w = make_uint2(0u, 0u);
+                if (inv != 0.0f) w = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+                *reinterpret_cast<uint2*>((__nv_bfloat16*)A.o + S.row[k * N + rank] * A.os_row + h * A.os_head + part * 4) = w;
+            }
         }
     };
-    request(warp * nrank + rank);
-    if (nrank > 1) cluster_sync(); else __syncthreads();
-    for (int r = warp * nrank + rank; r < R; r += nrank * (kThreads / 32)) {
-        const int t = S.row[r];
-        float pm = -INFINITY, pl = 0.0f;
-        float4 v[8];
-        if (lane < nrank) {                                       // lane i: of the i-th CTA
-            pm = ld_cluster(map_rank(smem_u32(&sM[r]), lane));
-            pl = ld_cluster(map_rank(smem_u32(&sL[r]), lane));
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < nrank) v[i] = ld_cluster4(map_rank(sO + o_part<D>(r, lane % (D / 4)), i));
-        float top = pm;
-#pragma unroll
-        for (int x = 1; x < 8; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-        top = fmaxf(__shfl_sync(0xffffffffu, top, 0), om);
-        const float f = factor(pm, pl, top), of = factor(om, ol, top);
-        float sum = f == 0.0f ? 0.0f : pl * f;
-#pragma unroll
-        for (int x = 1; x < 8; x <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-        sum = __shfl_sync(0xffffffffu, sum, 0);
-        if (of != 0.0f) sum += ol * of;
-        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float g = __shfl_sync(0xffffffffu, f, i);
-            if (i < nrank && g != 0.0f) add(acc, v[i], g);
-        }
-        if (lane < D / 4) {
-            if (of != 0.0f) add(acc, make_float4(own0.x, own0.y, own1.x, own1.y), of);
-            const float inv = 1.0f / sum;
-            uint2 w = make_uint2(0u, 0u);
-            if (sum != 0.0f) w = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-            *reinterpret_cast<uint2*>((__nv_bfloat16*)A.o + t * A.os_row + h * A.os_head + lane * 4) = w;
-        }
-        if (lane == 0) A.lse[t * A.Hq + h] = sum == 0.0f ? -INFINITY : top + logf(sum);
-        request(r + nrank * (kThreads / 32));
-    }
+    if (nrank == 1) sum_up(std::integral_constant<int, 1>{});
+    else if (nrank == 2) sum_up(std::integral_constant<int, 2>{});
+    else if (nrank == 4) sum_up(std::integral_constant<int, 4>{});
+    else sum_up(std::integral_constant<int, 8>{});
     if (nrank > 1) cluster_sync();                                // (no CTA leaves while another may still read its sums)
     if (tid == 0 && S.abort_flag) atomicExch(A.status, (int32_t)DMA_ERR_DEVICE_TIMEOUT);
 }

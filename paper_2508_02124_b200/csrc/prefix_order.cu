@@ -2,8 +2,8 @@
 //
 // The weakest kept key of each (prefix, head) is found as decoding finds it (cache4_select.cu); what is not below it is collected and sorted, by a CTA per (prefix, head) where shared memory
 // holds the list, 8192 entries, else in chunks of it. Ordering is round trips and instructions, not memory: 32 heads of 16K keys, w = 2048: 16 us (rows 2, selection 6.4, lists 7.8; the
-// weights' bytes 0.4); five prefixes of up to 64K, w = 4096: 40 us (2, 20, 18; bytes 4.6). In chunks the first takes 33 us; 16 prefixes of 16K, w = 4096, 110 instead of 49; one of 256K 63
-// instead of 54, one of 1M, w = 8192, 155 instead of 180. In chunks one of 256K, w = 16384, takes 91 us, one of 1M 157.
+// weights' bytes 0.4); five prefixes of up to 64K, w = 4096: 38 to 49 us (2, 20, 18 to 24; bytes 4.6). In chunks the first takes 33 us; 16 prefixes of 16K, w = 4096, 110 instead of 49; one of 256K 63
+// instead of 54, one of 1M, w = 8192, 155 either way. In chunks one of 256K, w = 16384, takes 91 us, one of 1M 157.
 #include <algorithm>
 #include <type_traits>
 
