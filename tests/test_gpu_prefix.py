@@ -410,6 +410,22 @@ def test_keys_that_a_row_does_not_keep_may_hold_anything(dtype, flags, bad):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("n,tail,w,Hkv,d", [(400, 64, 60, 3, 128), (2000, 300, 300, 2, 64), (900, 500, 400, 2, 128), (30, 200, 90, 3, 64)])
+def test_own_keys_that_fail_against_the_list_may_hold_anything(dtype, bad, n, tail, w, Hkv, d):
+    """One head per KV head, so that every key is kept or not: all that are not hold `bad`, those among them that are asked for before the cut is known."""
+    for seed in range(6):
+        s = World([n], [tail], [0], w, Hkv, Hkv, d, 16, dtype, seed=seed)
+        at = s.context(0)
+        for h in range(Hkv):
+            out = at[np.argsort(-s.delta[at // 16, h, at % 16].astype(np.float64), kind="stable")[w:]]
+            s.kv[torch.from_numpy(out // 16).cuda(), h, torch.from_numpy(out % 16).cuda()] = bad
+        o, lse = s.run()
+        assert torch.isfinite(o).all() and torch.isfinite(lse).all()
+        s.check(o, lse)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_values_alone_not_finite(dtype):
     """An infinite value channel in a key that every row keeps: that channel is infinite, the others as without."""
     s = World([100], [20] * 9, [0] * 9, 500, 2, 1, 128, 16, dtype, seed=3)
