@@ -28,7 +28,7 @@
 namespace dma {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32, kRoom = 512;      // kRoom: candidates of a warp at most
 
 // A team of 1, 2, 4 or 8 warps has a (row, head), each warp a part of the own keys.
 struct OwnShared {
@@ -837,11 +837,12 @@ int own(const Cache& C, const DecodeArgs& A, cudaStream_t st) {
         team *= 2;
         if (heads * team > kWarps) heads /= 2;
     }
-    const int room = (int)std::min<int64_t>((capacity + team * 64 - 1) / (team * 64) * 64, 512), warps = heads * team;
-    const size_t smem = std::max<size_t>((size_t)warps * (room * sizeof(uint2) + Attend<T, D>::kStage * Attend<T, D>::kPitch), 32 * 1024 / kWarps * warps);
+    const int room = (int)std::min<int64_t>((capacity + team * 64 - 1) / (team * 64) * 64, kRoom), warps = heads * team;
+    auto bytes = [](int warps, int room) { return std::max<size_t>((size_t)warps * (room * sizeof(uint2) + Attend<T, D>::kStage * Attend<T, D>::kPitch), 32 * 1024 / kWarps * warps); };
     auto kernel = team > 1 ? own_kernel<T, D, true> : own_kernel<T, D, false>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return DMA_ERR_CUDA;
-    return launch_overlapped(kernel, dim3((unsigned)(ctas(heads) + 1)), dim3(32 * warps), smem, st, 1, A, team, room, heads == most ? C.G : heads);
+    // (state of the function, which other threads' calls share: always the limit)
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes(kWarps, kRoom)) != cudaSuccess) return DMA_ERR_CUDA;
+    return launch_overlapped(kernel, dim3((unsigned)(ctas(heads) + 1)), dim3(32 * warps), bytes(warps, room), st, 1, A, team, room, heads == most ? C.G : heads);
 }
 
 }  // namespace

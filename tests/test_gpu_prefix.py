@@ -560,3 +560,53 @@ def test_a_server_run():
                     es = 2.0 ** -9 * parts[h][1]
                     assert (np.abs(got[h] - eo[h]) <= parts[h][2] * (2 * es + 2.0 ** -8) + 2.0 ** -8 * np.abs(eo[h])).all(), (step, t, h)
         want = np.concatenate([want[:nprefix], want[nprefix:] + rng.randint(0, 25, nseq)])
+
+
+@pytest.mark.parametrize("which", ["append", "decode"])
+def test_shared_memory_sizes_from_several_threads(which, monkeypatch):
+    """Threads whose calls of one kernel take different amounts of shared memory, each on a stream of its own: the limit is state of the kernel that all of them share, so a call may not lower it to its
+    own size."""
+    import threading
+    g = torch.Generator("cuda").manual_seed(0)
+
+    def append(rows, Hq, Hkv, given):
+        c = dma.cache(Hq, Hkv, 128, rows=rows, page_size=16, num_pages=2)
+        K, V, W, A, new = (torch.randn(*x, generator=g, device="cuda") for x in ((rows, Hkv, 128), (rows, Hkv, 128), (Hq, 128), (Hq,), (Hq, rows)))
+        K, V, W, slot = K.bfloat16(), V.bfloat16(), W / 11, i32(np.arange(rows))
+        pool = dma.cache_kv(c, "cuda")
+        return lambda: dma.dma_cache_append(c, K, V, slot, *pool, **(dict(delta_new=new) if given else dict(W_delta=W, A=A))), pool
+
+    def decode(rows, n):
+        s = World([], [n] * rows, [-1] * rows, 8, 1, 1, 128, 16, seed=n)
+        delta, table, seq, pos = torch.from_numpy(s.delta).cuda(), i32(s.table), i32(s.seq), i32(s.pos)
+        out, ws = (torch.empty(rows, 1, 128, dtype=torch.bfloat16, device="cuda"), torch.empty(rows, 1, device="cuda")), torch.empty(dma.dma_cache_decode_workspace(s.c), dtype=torch.uint8, device="cuda")
+        return lambda: dma.dma_cache_decode(s.c, s.q, s.kv, delta, table, seq, pos, None, None, *out, ws=ws), out
+
+    make = {"append": [lambda: append(3, 76, 1, False), lambda: append(5, 4, 2, True)], "decode": [lambda: decode(2, 4000), lambda: decode(3, 16)]}[which]
+    jobs, bad, through = [], [], dma._call
+    for i in range(4):
+        call, out = make[i % 2]()
+        call()
+        # the arguments of the call on a stream of its own: threads that only make the library's calls meet each other in them
+        made, stream = [], torch.cuda.Stream()
+        monkeypatch.setattr(dma, "_call", lambda name, *args: made.append((dma._typed_fn(name), args)))
+        with torch.cuda.stream(stream):
+            call()
+        monkeypatch.setattr(dma, "_call", through)
+        jobs.append((made[0], stream, out, [x.clone() for x in out], call))
+    torch.cuda.synchronize()
+
+    def worker(f, args):
+        for _ in range(20000):
+            rc = f(*args)
+            if rc:
+                bad.append(rc)
+
+    threads = [threading.Thread(target=worker, args=job[0]) for job in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not bad, bad[:5]
+    assert all(torch.equal(a, b) for _, _, out, exp, _ in jobs for a, b in zip(out, exp))
