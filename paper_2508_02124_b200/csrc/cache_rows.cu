@@ -241,11 +241,12 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) append_kernel(Append
 template <typename T, int D, int kThreads>
 int append_rows(const Append& P, cudaStream_t st) {
     constexpr int kRows = kThreads / (D / 16), kWeights = 20 * 1024;
-    const int tiles = (P.rows + kRows - 1) / kRows, group = P.G * D * (int)sizeof(float);
+    const int tiles = (P.rows + kRows - 1) / kRows;
+    const int64_t group = (int64_t)P.G * D * sizeof(float);       // (weights that are given come for groups of any size)
     // KV heads per CTA: as many as leave eight CTAs per SM (16384 rows of 8: three of them 76 us; eight 84, four 88, two 79, one 92), and so few that their weights take 20 KB, or one
-    const int per = std::max(1, std::min({P.Hkv, (int)((int64_t)P.Hkv * tiles / (8 * 148)), std::max(1, kWeights / group)}));
+    const int per = std::max(1, std::min({P.Hkv, (int)((int64_t)P.Hkv * tiles / (8 * 148)), (int)std::max<int64_t>(1, kWeights / group)}));
     constexpr int stages = kStages * stage_bytes<T> * kThreads, limit = stages + std::max(kWeights, append_heads(D) * D * (int)sizeof(float));
-    const int smem = stages + (P.delta_new ? 0 : per * group);
+    const int smem = stages + (P.delta_new ? 0 : per * (int)group);
     // (state of the function, which other threads' calls share: always the limit)
     if (cudaFuncSetAttribute(append_kernel<T, D, kThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize, limit) != cudaSuccess) return DMA_ERR_CUDA;
     return launch_overlapped(append_kernel<T, D, kThreads>, dim3(tiles, (P.Hkv + per - 1) / per), dim3(kThreads), smem, st, 1, P);

@@ -610,3 +610,15 @@ def test_shared_memory_sizes_from_several_threads(which, monkeypatch):
     torch.cuda.synchronize()
     assert not bad, bad[:5]
     assert all(torch.equal(a, b) for _, _, out, exp, _ in jobs for a, b in zip(out, exp))
+
+
+@pytest.mark.parametrize("d,heads", [(128, 1 << 23), (64, 1 << 24)])
+def test_append_of_given_weights_for_a_group_of_any_size(d, heads):
+    """Heads whose sampling weights would take 2^32 bytes, if they were asked for."""
+    c = dma.cache(heads, 1, d, rows=2, page_size=16, num_pages=1)
+    kv, delta = dma.cache_kv(c, "cuda")
+    K, V, given, slot = torch.randn(2, 1, d, device="cuda").bfloat16(), torch.randn(2, 1, d, device="cuda").bfloat16(), torch.rand(heads, 2, device="cuda"), [11, 3]
+    dma.dma_cache_append(c, K, V, i32(slot), kv, delta, delta_new=given)
+    assert torch.equal(delta[0, :, slot], given) and torch.equal(kv[0, 0, slot, 0], K[:, 0]) and torch.equal(kv[0, 0, slot, 1], V[:, 0])
+    delta[0, :, slot] = 0
+    assert not delta.any()
