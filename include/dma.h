@@ -382,7 +382,7 @@ typedef struct {
  *   q         NULL: only K is rotated. q_out has o_stride; it may be q, with the same strides
  *   row_pos   [rows]; row t is rotated by row_pos[t] + prefix_len[row_prefix[t]] (a length below 0 counts as 0). row_pos[t] < 0, as behind a plan's
  *             last row: the row is skipped altogether
- *   row_prefix, prefix_len   [rows], [nprefix]; both NULL: no prefixes
+ *   row_prefix, prefix_len   [rows], [nprefix]; both NULL: no prefixes; nprefix = 0: none either, the two are not read
  *   slot      [rows]; K, V and delta of a row whose slot is outside the pool are not written (its q is). Slots of one call are distinct.
  * With W_delta, Hq / Hkv at most 76 (d = 128) or 96 (d = 64); DMA_ERR_UNSUPPORTED beyond.
  * Angles are formed in 64 bits and reduced to a turn before they are rounded to fp32; the rotation is fp32, rounded once. */

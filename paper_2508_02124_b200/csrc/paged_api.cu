@@ -158,6 +158,7 @@ int dma_cache_append(const dma_cache_t* c, const dma_rotation_t* rotation, const
     if (rc) return rc;
     if (!K || !V || !slot || !kv || !delta || (!delta_new && (!W_delta || !A)) || (q == nullptr) != (q_out == nullptr)) return DMA_ERR_NULL;
     Rotation rot = {};
+    if (nprefix == 0) row_prefix = prefix_len = nullptr;           // (an empty array may have no address)
     if (rotation) {
         if (!rotation->inv_freq || !row_pos || (row_prefix == nullptr) != (prefix_len == nullptr)) return DMA_ERR_NULL;
         if (rotation->rot < 16 || rotation->rot > C.d || nprefix < 0 || !std::isfinite(rotation->scale)) return DMA_ERR_SHAPE;

@@ -622,3 +622,20 @@ def test_append_of_given_weights_for_a_group_of_any_size(d, heads):
     assert torch.equal(delta[0, :, slot], given) and torch.equal(kv[0, 0, slot, 0], K[:, 0]) and torch.equal(kv[0, 0, slot, 1], V[:, 0])
     delta[0, :, slot] = 0
     assert not delta.any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_a_step_of_a_server_that_has_no_prefixes(dtype):
+    """Empty arrays of prefixes: the bits of a call without them."""
+    rows, Hq, Hkv, d = 5, 4, 2, 64
+    c = dma.cache(Hq, Hkv, d, w=4, dtype=DT[dtype], rows=rows, nseq=1, page_size=16, num_pages=1, max_blocks=1)
+    K, V, q = (torch.randn(rows, h, d, device="cuda").to(DT[dtype]) for h in (Hkv, Hkv, Hq))
+    W, A, freq, none = torch.randn(Hq, d, device="cuda") / 8, torch.rand(Hq, device="cuda"), torch.from_numpy(frequencies(d)).cuda(), i32([])
+    at, seq, behind, table = i32(np.arange(rows)), i32([0] * rows), i32([0, -1, 5, 0, -1]), i32([[0]])
+    got = []
+    for prefix in (dict(), dict(row_prefix=behind, prefix_len=none)):
+        kv, delta = dma.cache_kv(c, "cuda")
+        turned = dma.dma_cache_append(c, K, V, at, kv, delta, W, A, q=q, row_pos=at + 7, inv_freq=freq, **prefix)
+        lists = (torch.empty(0, Hq, 4, dtype=torch.int32, device="cuda"), torch.empty(0, Hq, 4, device="cuda"), none) if prefix else None
+        got.append([kv, delta, turned, *dma.dma_cache_decode(c, turned, kv, delta, table, seq, at, behind if prefix else None, lists)])
+    assert all(torch.equal(a, b) for a, b in zip(*got))

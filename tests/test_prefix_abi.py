@@ -187,3 +187,23 @@ def test_the_plain_implementation():
     delta = np.zeros((4, 1, 4), np.float32)
     delta[2, 0], delta[1, 0] = [5, 1, 5, 2], [9, 5, 0.5, 7]
     assert ref.order(delta, [2, 9, 1], 11, 4, 4).tolist() == [[4, 8, 10, 5]]
+
+
+def test_no_prefixes_at_the_moment(lib, monkeypatch):
+    """A server without prefixes: arrays of none may have no address, and are not read."""
+    f, turn = dma._typed_fn("dma_cache_append"), dma.dma_rotation_t(4096, 128, 0, 0.0)
+    if not torch.cuda.is_available():
+        for kw in (dict(length=0), dict(prefix=0), dict(prefix=0, length=0), dict(prefix=4098, length=4098), {}):
+            assert f(*append_args(cache(), turn, n=0, **kw)) == -6, kw         # all arguments taken: there is no device here
+    seen = []
+    monkeypatch.setattr(dma, "_raw_device", lambda: -1)
+    monkeypatch.setattr(dma, "_stream", lambda: 0)
+    monkeypatch.setattr(dma, "_call", lambda name, c, *a: seen.append(a))
+    c, i32 = cache(), torch.zeros(3, dtype=torch.int32)
+    kv, delta = dma.cache_kv(c, "cpu")
+    K, q = torch.zeros(3, 2, 128, dtype=torch.bfloat16), torch.zeros(3, 4, 128, dtype=torch.bfloat16)
+    dma.dma_cache_append(c, K, K, i32, kv, delta, torch.zeros(4, 128), torch.zeros(4), q=q, row_pos=i32, row_prefix=i32 - 1, prefix_len=i32[:0], inv_freq=torch.zeros(64))
+    assert seen[-1][11] == 0                                                     # nprefix
+    order = torch.zeros(0, 4, 16, dtype=torch.int32), torch.zeros(0, 4, 16), i32[:0]
+    dma.dma_cache_decode(c, q, kv, delta, torch.zeros(2, 5, dtype=torch.int32), i32, i32, i32 - 1, order, ws=torch.empty(1, dtype=torch.uint8))
+    assert seen[-1][7] == 0
