@@ -7,7 +7,8 @@
 // with zeros of P elsewhere, so that a thread walks 32 (16) columns instead of 64 (three tiles of 14 rows 21.4 us instead of 25.8, 16 rows 18.3 instead of 19.7, 64 rows the same).
 // Rounding: scores, sums and O are fp32. P goes in as two bf16 numbers, the one next to it and what that leaves (2^-16 of a weight), over the same V: with one, o is a quarter further from
 // 64 bits than its own rounding makes it (rms 2.1e-3 and 1.7e-3).
-// A value that is not finite would reach rows that do not keep its key, as 0 times infinity. A row whose O is not finite is therefore formed again, by a warp, over the keys it keeps.
+// A value that is not finite would reach rows that do not keep its key, as 0 times infinity. A row whose O is not finite is therefore formed again, by a warp, over the keys it keeps, and in
+// natural units: so is one whose weights pass 2^128 / log2 e, which have no value in units of log 2.
 //
 // Warps: 0-3 softmax and the end, 4 issues the products, 5-8 gather (with two gathering 64 rows 26.7 us instead of 24.1, eight rows with long lists 34 instead of 29). Two CTAs per SM: 97 KB
 // of stages, Q and O each.

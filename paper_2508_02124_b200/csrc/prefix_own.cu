@@ -29,6 +29,7 @@ namespace dma {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32, kRoom = 512;      // kRoom: candidates of a warp at most
+constexpr float kLog2e = 1.4426950408889634f;     // of differences of scores: a weight as large as fp32 holds has no value in units of log 2
 
 // A team of 1, 2, 4 or 8 warps has a (row, head), each warp a part of the own keys.
 struct OwnShared {
@@ -58,7 +59,7 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4],
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Attention of a warp over keys that lie in shared memory (K's row, V's, kPitch bytes apart), a stage of them at a time; use: a bit for each that counts; list: their biases. Maximum and sum in natural units at the end.
+// Attention of a warp over keys that lie in shared memory (K's row, V's, kPitch bytes apart), a stage of them at a time; use: a bit for each that counts; list: their biases.
 template <typename T, int D> struct Attend;
 
 // fp32, on the CUDA cores: eight lanes take a key, 4 channels of every 32 each.
@@ -137,9 +138,9 @@ template <int D>
 struct Attend<__nv_bfloat16, D> {
     static constexpr int kStage = 16, kPitch = 2 * D * 2 + 16;     // (rows 16 bytes off: the eight rows of a matrix lie in different banks)
     uint32_t q[D / 16][2];
-    float acc[D / 16][4], m = -INFINITY, l = 0.0f, c1;             // m in log2 units
-    __device__ __forceinline__ void start(const __nv_bfloat16* row, float scale, int lane) {
-        c1 = scale * 1.4426950408889634f;
+    float acc[D / 16][4], m = -INFINITY, l = 0.0f, scale;
+    __device__ __forceinline__ void start(const __nv_bfloat16* row, float by, int lane) {
+        scale = by;
 #pragma unroll
         for (int x = 0; x < D / 16; ++x) {
 #pragma unroll
@@ -148,7 +149,7 @@ struct Attend<__nv_bfloat16, D> {
             for (int y = 0; y < 2; ++y) q[x][y] = lane < 4 ? *reinterpret_cast<const uint32_t*>(row + x * 16 + y * 8 + lane * 2) : 0u;
         }
     }
-    float x0, x1;                                                 // of lane 4 i: the scores of keys i and i + 8, log2 units
+    float x0, x1;                                                 // of lane 4 i: the scores of keys i and i + 8
     __device__ __forceinline__ void scores(const uint8_t* keys, const uint2* list, uint32_t use, int lane) {
         const uint32_t at_k = ptx::smem_u32(keys) + ((lane & 7) + ((lane >> 3) & 1) * 8) * kPitch + (lane >> 4) * 16;
         float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, s1[4] = {0.0f, 0.0f, 0.0f, 0.0f};       // (two chains)
@@ -161,8 +162,8 @@ struct Attend<__nv_bfloat16, D> {
             mma_16816(s1, b, q[x + 1][0], q[x + 1][1]);
         }
         const int e = lane >> 2;
-        x0 = (lane & 3) == 0 && (use >> e & 1u) ? fmaf(s[0] + s1[0], c1, __uint_as_float(list[e].x) * 1.4426950408889634f) : -INFINITY;
-        x1 = (lane & 3) == 0 && (use >> (e + 8) & 1u) ? fmaf(s[2] + s1[2], c1, __uint_as_float(list[e + 8].x) * 1.4426950408889634f) : -INFINITY;
+        x0 = (lane & 3) == 0 && (use >> e & 1u) ? fmaf(s[0] + s1[0], scale, __uint_as_float(list[e].x)) : -INFINITY;
+        x1 = (lane & 3) == 0 && (use >> (e + 8) & 1u) ? fmaf(s[2] + s1[2], scale, __uint_as_float(list[e + 8].x)) : -INFINITY;
     }
     __device__ __forceinline__ void values(uint8_t* keys, uint32_t use, int lane) {
         if (use != 0xFFFFu) {                                     // (0 times what lies there must be 0)
@@ -174,7 +175,7 @@ struct Attend<__nv_bfloat16, D> {
         const float top = fmaxf(m, warp_max(fmaxf(x0, x1)));
         if (top > m) {                                            // (the same in all lanes)
             if (m != -INFINITY) {
-                const float fade = ptx::ex2(m - top);
+                const float fade = ptx::ex2((m - top) * kLog2e);
                 l *= fade;
 #pragma unroll
                 for (int x = 0; x < D / 16; ++x)
@@ -183,7 +184,7 @@ struct Attend<__nv_bfloat16, D> {
             }
             m = top;
         }
-        const float ref = m == -INFINITY ? 0.0f : m, p0 = ptx::ex2(x0 - ref), p1 = ptx::ex2(x1 - ref);
+        const float ref = m == -INFINITY ? 0.0f : m, p0 = ptx::ex2((x0 - ref) * kLog2e), p1 = ptx::ex2((x1 - ref) * kLog2e);
         l += p0 + p1;
         const int from = (lane & 3) * 8;
         float w[4] = {__shfl_sync(0xffffffffu, p0, from), __shfl_sync(0xffffffffu, p0, from + 4), __shfl_sync(0xffffffffu, p1, from), __shfl_sync(0xffffffffu, p1, from + 4)};
@@ -204,7 +205,6 @@ struct Attend<__nv_bfloat16, D> {
 #pragma unroll
         for (int x = 4; x < 32; x <<= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
         l = __shfl_sync(0xffffffffu, l, 0);
-        m = m == -INFINITY ? m : m * 0.6931471805599453f;
         if ((lane & 3) == 0)
 #pragma unroll
             for (int x = 0; x < D / 16; ++x)                      // (an infinite value's second part is not a number)
@@ -218,9 +218,9 @@ template <int D>
 struct AttendAll {
     static constexpr int kStage = 16, kPitch = 2 * D * 2 + 16;
     uint32_t q[D / 16][2];
-    float acc[D / 8][4], m = -INFINITY, l = 0.0f, c1;              // of row lane / 4; m in log2 units
-    __device__ __forceinline__ void start(const __nv_bfloat16* row, bool real, float scale, int lane) {
-        c1 = scale * 1.4426950408889634f;
+    float acc[D / 8][4], m = -INFINITY, l = 0.0f, scale;           // of row lane / 4
+    __device__ __forceinline__ void start(const __nv_bfloat16* row, bool real, float by, int lane) {
+        scale = by;
 #pragma unroll
         for (int x = 0; x < D / 8; ++x)
 #pragma unroll
@@ -245,7 +245,7 @@ struct AttendAll {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int e = (lane & 3) * 2 + (i >> 1) * 8 + (i & 1);
-            x[i] = e < count ? fmaf(s[i >> 1][i & 1], c1, bias[i] * 1.4426950408889634f) : -INFINITY;
+            x[i] = e < count ? fmaf(s[i >> 1][i & 1], scale, bias[i]) : -INFINITY;
         }
     }
     __device__ __forceinline__ void values(uint8_t* keys, int count, int lane) {
@@ -258,7 +258,7 @@ struct AttendAll {
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
         if (__any_sync(0xffffffffu, top > m)) {
-            const float fade = m == -INFINITY ? 1.0f : ptx::ex2(m - top);
+            const float fade = m == -INFINITY ? 1.0f : ptx::ex2((m - top) * kLog2e);
             l *= fade;
 #pragma unroll
             for (int y = 0; y < D / 8; ++y)
@@ -270,7 +270,7 @@ struct AttendAll {
         float p[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            p[i] = ptx::ex2(x[i] - ref);
+            p[i] = ptx::ex2((x[i] - ref) * kLog2e);
             l += p[i];
         }
         const uint32_t h0 = ptx::pack_bf16(p[0], p[1]), h1 = ptx::pack_bf16(p[2], p[3]);
@@ -284,11 +284,10 @@ struct AttendAll {
             mma_16816(acc[2 * y + 1], a, b[2], b[3]);
         }
     }
-    // o [8][D] to shared memory; (m, l) of the lane's head, natural units
+    // o [8][D] to shared memory; (m, l) of the lane's head
     __device__ __forceinline__ void end(float* o, int lane) {
         l += __shfl_xor_sync(0xffffffffu, l, 1);
         l += __shfl_xor_sync(0xffffffffu, l, 2);
-        m = m == -INFINITY ? m : m * 0.6931471805599453f;
 #pragma unroll
         for (int y = 0; y < D / 8; ++y)
 #pragma unroll

@@ -639,3 +639,23 @@ def test_a_step_of_a_server_that_has_no_prefixes(dtype):
         lists = (torch.empty(0, Hq, 4, dtype=torch.int32, device="cuda"), torch.empty(0, Hq, 4, device="cuda"), none) if prefix else None
         got.append([kv, delta, turned, *dma.dma_cache_decode(c, turned, kv, delta, table, seq, at, behind if prefix else None, lists)])
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("dtype,flags", [("bf16", 0), ("bf16", dma.DMA_FLAG_SIMT), ("fp32", 0)])
+@pytest.mark.parametrize("lens,w", [([], 500), ([], 20), ([90], 500), ([90], 40)])
+@pytest.mark.parametrize("where", ["own", "prefix"])
+def test_weights_up_to_the_largest_number(lens, w, where, dtype, flags):
+    """Weights above 2^128 / log2(e), which have no fp32 value in units of log 2: the key of the largest is all that counts, also next to others that are as large but for a quarter."""
+    if where == "prefix" and not lens:
+        return
+    for tail in (30, 700):
+        s = World(lens, [tail] * 3, [0 if lens else -1] * 3, w, 4, 2, 128, 16, dtype, seed=w, flags=flags)
+        at = np.stack([ref.visible_slots(s.table0[0], lens[0], 16, s.pages) if where == "prefix" else ref.visible_slots(s.table[t], tail, 16, s.pages) for t in range(3)])[:, [17, 3, 25]]
+        for t in range(3):
+            s.delta[at[t] // 16, :, at[t] % 16] = np.array([3.0e38, 2.4e38, 2.5e38], np.float32)[:, None]
+        o, lse = s.run()
+        for t in range(3):
+            V = s.kv[int(at[t, 0]) // 16, :, int(at[t, 0]) % 16, 1].repeat_interleave(2, 0)
+            assert torch.equal(o[t], V), (tail, t)
+            # the weight, rounded, in and out of units of log 2: four roundings
+            assert (lse[t].double() / 3.0e38 - 1).abs().max() <= 4 * 2.0 ** -24
