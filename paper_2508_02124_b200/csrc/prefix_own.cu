@@ -4,7 +4,7 @@
 // prefix' part ends with the first m for which m + #{own > weight_m} >= k (ties: the prefix' keys come first), and the own part is the k - m best of the row's own keys. Where the list
 // has w entries, own keys that do not exceed its last cannot be kept and are left out at once: of n own keys behind a prefix of N about n w / N remain, the candidates. Each of them takes
 // at most one entry's place: the i-th best is kept if it is above the i-th entry from the list's end. So
-//   - up to 64 candidates, a full list: the first stage's K and V are requested, the lowest candidate is dropped as long as it fails, a minimum of the warp each time (without both: 16 rows of
+//   - up to 64 candidates, a full list: the first stage's K and V are requested, the lowest candidate is dropped as long as it fails, a minimum of the warp each time, 25 times at most (without both: 16 rows of
 //     64 own keys 10.3 us instead of 8.2, 256 of 512 55 instead of 53.5);
 //   - else: how many are kept by bisection, #{own keys that are not below entry i from the end} > i, the entries in shared memory; then the weakest between the two entries around it (256 rows
 //     of 512 own keys behind 2048, w = 1024: 140 us; by sorting up to 256 of them, and bisecting over the list where it lies beyond, 173);
@@ -631,7 +631,8 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
         };
         bool done = false;
         if (few) {
-            // The lowest one is dropped as long as it fails. (By a team's first warp.)
+            // The lowest one is dropped as long as it fails. (By a team's first warp. 25 of them at most, else the bisection's twelve counts are fewer steps; 256 rows of 60 own keys behind 512,
+            // w = 400: 37.4 us, 39.4 with 9 at most, 37.4 with 64; the same within 1 % where a tenth of the own keys are candidates.)
             if (in_team == 0) {
                 unsigned long long keys[2];
                 uint32_t last[2];
@@ -750,14 +751,11 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
         }
     }
     // attention over the kept ones, a stage of keys at a time
-    int b = over ? j0 : 0, front = over ? 0 : ahead;              // (a warp whose candidates had room may be of a team whose had not: what is on its way is then not used)
+    int b = over ? j0 : 0, front = ahead;
     uint32_t use = ~0u;                                           // of the first stage
     if (front) {
         use = __ballot_sync(0xffffffffu, lane < front && order_key(mine[lane].x, place(lane)) >= least);
         b = front;
-    } else if (ahead) {
-        cp_async_wait<0>();
-        __syncwarp();
     }
     const int end = over ? j1 : c;
     do {
