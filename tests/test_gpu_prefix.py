@@ -298,6 +298,7 @@ def test_decode(lens, tails, prefix, w, Hq, Hkv, d, page, dtype, flags):
 
 LONG = [
     # what a row keeps of many own keys: lens, tails, w, Hq, Hkv, d, page, rows per prefix
+    # ("dropped, sorted": one by one, up to 25 of them, else by bisection against the list's end; "bisected": the same in shared memory, or by sweeps where there is no room)
     ([5000], [2000, 1900], 256, 4, 1, 64, 64, 2), ([5000], [700], 128, 8, 8, 64, 16, 40),           # few candidates: by a team of warps, by one
     ([3000], [1000], 900, 2, 1, 128, 64, 80), ([600], [1000], 500, 2, 2, 64, 64, 80),               # a third and more of the own keys are candidates: dropped, sorted
     ([50], [1500, 30], 700, 4, 2, 64, 32, 2), ([10], [4096], 3000, 2, 1, 64, 128, 3),               # a short list: all are candidates, bisected
@@ -659,3 +660,141 @@ def test_weights_up_to_the_largest_number(lens, w, where, dtype, flags):
             assert torch.equal(o[t], V), (tail, t)
             # the weight, rounded, in and out of units of log 2: four roundings
             assert (lse[t].double() / 3.0e38 - 1).abs().max() <= 4 * 2.0 ** -24
+
+
+# ---- the forms that large batches take -----------------------------------------------------------------------------------
+
+def own_form(rows, Hq, Hkv, blocks, page):
+    """(heads that a CTA takes at once, warps of a head, candidates that a warp has room for) of the own keys' kernel, by the host's rule."""
+    G, keys, heads, team = Hq // Hkv, blocks * page, 1, 1
+    while heads < G and heads < 8:
+        heads *= 2
+    most = heads
+    while team < 8 and (rows * Hkv * (1 if heads == most else -(-G // heads)) * heads * team * 2 <= 16 * 148 or keys > 1024 * team):
+        team *= 2
+        if heads * team > 8:
+            heads //= 2
+    return heads, team, min(-(-keys // (team * 64)) * 64, 512)
+
+
+FORMS = [
+    # heads at once, warps of a head; rows, Hq, Hkv, d, page
+    (2, 1, 300, 8, 4, 128, 16), (4, 1, 160, 16, 4, 128, 32), (1, 1, 600, 4, 4, 128, 16), (8, 1, 90, 32, 4, 64, 64), (4, 1, 250, 9, 3, 64, 16), (2, 2, 100, 8, 4, 128, 16), (4, 2, 60, 16, 4, 64, 16),
+    (4, 2, 90, 6, 2, 128, 32), (2, 4, 40, 6, 2, 128, 32), (1, 2, 150, 4, 4, 64, 16), (2, 4, 40, 8, 4, 128, 16), (1, 4, 80, 4, 4, 128, 64)]
+
+
+@pytest.mark.parametrize("heads,team,rows,Hq,Hkv,d,page", FORMS)
+@pytest.mark.parametrize("lens,w,kind", [([3000], 900, "random"), ([3000], 900, "crowded"), ([40], 700, "random"), ([40], 300, "crowded"), ([2500, 0], 60, "random"), ([50], 4000, "random")])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_decode_of_every_form_of_the_own_keys(heads, team, rows, Hq, Hkv, d, page, lens, w, kind, dtype):
+    """A warp or a team per head, alone or several in a CTA: behind a full list few candidates and many (of which many fail, equal ones among them), without one every own key is a candidate, more of
+    them than there is room for too; and windows that keep everything."""
+    rng = np.random.RandomState(rows + w)
+    longest = 1000 * team if team < 8 else 4000
+    tails = [longest, longest - 1, 1, 90, longest // 2, 40] + [int(x) for x in rng.randint(1, 80, rows - 6)]
+    s = World(lens, tails, [0, 0, 0, 0, 0, 0] + [int(x) for x in rng.randint(-1, len(lens), rows - 6)], w, Hq, Hkv, d, page, dtype, kind, seed=rows)
+    assert own_form(rows, Hq, Hkv, s.table.shape[1], page)[:2] == (heads, team)
+    o, lse = s.run()
+    assert torch.isfinite(o).all() and torch.isfinite(lse).all()
+    s.check(o, lse, rows=[0, 1, 2, 3, 4, 5, rows - 1])
+    again = s.run()
+    assert torch.equal(o, again[0]) and torch.equal(lse, again[1])
+
+
+@pytest.mark.parametrize("team,rows,Hkv,tail,few,many", [(1, 600, 4, 1000, 40, 300), (2, 150, 4, 2000, 40, 600), (4, 80, 4, 3500, 60, 900), (8, 4, 1, 4000, 30, 1000)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_decode_by_the_number_of_candidates(team, rows, Hkv, tail, few, many, dtype):
+    """Behind a full list: as many of a row's own keys as given are above its last entry, of which none, some or all but one fail; the first 64 are dropped one by one, up to 25 of them. Then every form of
+    the bisection between entries, with ties at the end."""
+    for candidates, above, ties in ((few, few, 1), (few, 3, 1), (few, few - 8, 7), (few, 1, few), (64, 64, 1), (65, 5, 1), (many, 2, 1), (many, many // 2, 9), (many, many, 1), (many, 1, many)):
+        n, w = 1500, 1100
+        s = World([n], [tail] * 4 + [9] * (rows - 4), [0] * rows, w, Hkv, Hkv, 64, 16, dtype, seed=candidates)
+        assert own_form(rows, Hkv, Hkv, s.table.shape[1], 16)[:2] == (1, team)
+        # the list: weights 2000 - place / 4 down to its last entry; own keys: `above` of them at the top of it, the rest of the candidates just above its end (so that each but the first fails against
+        # the entries that the better ones displace), all others below
+        at = ref.visible_slots(s.table0[0], n, 16, s.pages)
+        for h in range(Hkv):
+            s.delta[at // 16, h, at % 16] = (20.0 - np.argsort(s.rng.permutation(n)) / 100).astype(np.float32)
+        end = np.float32(20.0 - (w - 1) / 100)
+        for t in range(4):
+            own = ref.visible_slots(s.table[t], tail, 16, s.pages)
+            for h in range(Hkv):
+                x = np.full(tail, 1e-3, np.float32)
+                x[:above] = 21.0 + (np.arange(above) // ties).astype(np.float32) / 64
+                x[above:candidates] = end + np.float32(0.001) * (1 + np.arange(candidates - above) // ties).astype(np.float32)
+                s.delta[own // 16, h, own % 16] = x[s.rng.permutation(tail)]
+        o, lse = s.run()
+        s.check(o, lse, rows=range(4))
+
+
+@pytest.mark.parametrize("rows,d,tail", [(3, 64, 20), (31, 128, 9), (40, 64, 30), (64, 128, 5), (65, 64, 12), (130, 128, 7)])
+@pytest.mark.parametrize("bad", [None, float("nan")])
+def test_prefixes_on_clusters_of_eight(rows, d, tail, bad):
+    """Eight CTAs per tile and head, with every number of lane groups; keys that only some of the rows keep hold anything."""
+    n, w, Hq, Hkv = 5000, 1700, 8, 4
+    tiles = min(rows, 1 + rows // 128)
+    assert tiles * Hq * 8 <= 3 * 148 and 8 * 192 <= w
+    s = World([n], [tail + i % 3 for i in range(rows)], [0] * rows, w, Hq, Hkv, d, 64, seed=rows)
+    order, skip = s.order(), []
+    picked = sorted(set([0, 1, 2, rows // 2, rows - 1]))
+    if bad is not None:
+        for e in (w - 1, w - 3, w - 6):
+            last = int(order[0][0, 0, e])                          # of head 0's list; K and V are head 0's and its neighbour's
+            s.kv[last // 64, 0, last % 64, :, 3] = bad
+            for t in picked:
+                at = s.context(t)
+                skip += [(t, h) for h in range(Hq // Hkv) if last in at[ref.best(s.delta[at // 64, h, at % 64], w)]]
+    o, lse = s.run(order)
+    s.check(o, lse, rows=picked, skip=skip)
+    if bad is not None:
+        assert all(not torch.isfinite(o[t, h, 3]) for t, h in skip)
+
+
+@pytest.mark.parametrize("rows,Hq,Hkv,d,page,dtype,rot,interleaved,per", [
+    (12000, 14, 7, 128, 64, "bf16", 128, False, 2), (16384, 8, 8, 128, 64, "bf16", 64, True, 3), (26000, 10, 10, 64, 32, "bf16", 64, False, 3), (12000, 14, 7, 128, 64, "fp32", 128, True, 2),
+    (40000, 3, 1, 64, 16, "fp32", 16, False, 1), (4800, 12, 4, 128, 256, "fp32", 96, False, 1)])
+def test_append_of_prompts(rows, Hq, Hkv, d, page, dtype, rot, interleaved, per):
+    """256 threads per CTA, several KV heads of each, the last CTA's fewer."""
+    assert rows * Hkv * (d // 16) >= 4 * 148 * 256
+    tiles = -(-rows // (256 // (d // 16)))
+    assert max(1, min(Hkv, Hkv * tiles // (8 * 148), max(1, 20 * 1024 // (Hq // Hkv * d * 4)))) == per
+    test_append(rows, Hq, Hkv, d, page, dtype, rot, interleaved, rows % 3 == 0)
+
+
+@pytest.mark.parametrize("dtype,flags", [("bf16", 0), ("bf16", dma.DMA_FLAG_SIMT), ("fp32", 0)])
+def test_a_server_run_over_what_lies_in_the_cache(dtype, flags):
+    """Plan, append, order and decode, step by step: o and lse against the plain implementation over the rotated rows as the cache holds them, which are compared with the rows that came."""
+    rng = np.random.RandomState(11)
+    Hq, Hkv, d, page, w, pages, nseq, nprefix, blocks, rows = 6, 2, 128, 16, 70, 150, 5, 2, 12, 200
+    g = torch.Generator("cuda").manual_seed(2)
+    W, A = torch.randn(Hq, d, generator=g, device="cuda") / 16, torch.rand(Hq, generator=g, device="cuda") + 0.3
+    freq = frequencies(64)
+    inv = torch.from_numpy(freq).cuda()
+    lens, pool = i32([0] * (nprefix + nseq)), i32([0, pages, 0, 0])
+    ring, table = i32(rng.permutation(pages)), i32(np.full((nprefix + nseq, blocks), -1))
+    c = dma.cache(Hq, Hkv, d, w=w, dtype=DT[dtype], rows=rows, nseq=nprefix + nseq, page_size=page, num_pages=pages, max_blocks=blocks, flags=flags)
+    kv, delta = dma.cache_kv(c, "cuda")
+    want, prefix_of, order = np.array([120, 45] + [0] * nseq), np.array([-1, -1, 0, 0, 1, 1, -1]), None
+    for step in range(4):
+        lens, pool, cu, seq, pos, slot = dma.dma_page_plan(c, lens, i32(want), table, ring, pool)
+        n, plen = int(cu[-1]), lens[:nprefix].tolist()
+        sq, ps, at = (x.cpu().numpy()[:n] for x in (seq, pos, slot))
+        qkv = torch.randn(rows, Hq + 2 * Hkv, d, generator=g, device="cuda").to(DT[dtype])
+        prefix = np.full(rows, -1)
+        prefix[:n] = prefix_of[sq]
+        q = dma.dma_cache_append(c, qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:], slot, kv, delta, W, A, q=qkv[:, :Hq], row_pos=pos, row_prefix=i32(prefix), prefix_len=lens[:nprefix], inv_freq=inv)
+        place = ps + np.where(prefix[:n] >= 0, np.array(plen)[prefix[:n].clip(0)], 0)
+        flat = kv.transpose(1, 2).reshape(-1, Hkv, 2, d)
+        close_rotation(flat[at][:, :, 0], f64(qkv[:n, Hq:Hq + Hkv]), place, freq, False, 1.0, dtype, "K")
+        close_rotation(q[:n], f64(qkv[:n, :Hq]), place, freq, False, 1.0, dtype, "q")
+        assert torch.equal(flat[at][:, :, 1], qkv[:n, Hq + Hkv:])
+        if step == 0:
+            order = dma.dma_prefix_order(dma.cache(Hq, Hkv, d, w=w, nseq=nprefix, page_size=page, num_pages=pages, max_blocks=blocks), delta, table[:nprefix], lens[:nprefix])
+        else:
+            s = World.__new__(World)
+            s.w, s.dtype, s.page, s.c, s.scale, s.rows, s.Hq, s.Hkv, s.d, s.pages, s.tails = w, dtype, page, c, d ** -0.5, n, Hq, Hkv, d, pages, [0] * (nprefix + nseq)
+            s.seq, s.pos, s.prefix, s.lens, s.q, s.kv, s.delta = sq, ps, prefix[:n], np.array(plen), q[:n], kv, delta.cpu().numpy()
+            s.table0, s.table = table.cpu().numpy()[:nprefix], table.cpu().numpy()
+            o, lse = dma.dma_cache_decode(c, q, kv, delta, table, seq, pos, i32(prefix), order)
+            s.check(o, lse)
+        want = np.concatenate([want[:nprefix], want[nprefix:] + rng.randint(0, 30, nseq)])
