@@ -408,7 +408,10 @@ def _written(name, t, dtype, rows, heads, d, dev):
     row, head, one = t.stride()
     if one != 1:
         raise ValueError(f"{name}: strides {t.stride()}, the channels of a head lie side by side")
-    return t.data_ptr(), row if shape[0] > 1 else heads * d, head if heads > 1 else d
+    row, head = row if shape[0] > 1 else heads * d, head if heads > 1 else d
+    if row == 0 and head == 0:                 # (which the library would take for the contiguous strides; one of them it refuses itself)
+        raise DmaError(-3, f"{name}: strides {t.stride()}, rows and heads on top of each other")
+    return t.data_ptr(), row, head
 
 
 def _table(c, t, dev):

@@ -274,3 +274,23 @@ def test_values_between_the_largest_numbers_of_bf16_and_of_fp32():
     with np.errstate(over="ignore"):
         back = v[2].astype(np.float32)
     assert not np.isnan(back).any() and np.isfinite(back[4]) and (np.isfinite(back) | (n[2] == 15)).all()
+
+
+def test_rows_on_top_of_each_other_are_not_written(monkeypatch):
+    """A tensor that is expanded in rows and heads has strides of zero, which stand for the contiguous ones in the descriptor: the rows would be written past its storage."""
+    monkeypatch.setattr(dma, "_raw_device", lambda: -1)
+    monkeypatch.setattr(dma, "_stream", lambda: 0)
+    seen = []
+    monkeypatch.setattr(dma, "_call", lambda name, c, *a: seen.append((tuple(c._obj.k_stride), tuple(c._obj.v_stride))))
+    c = dma.cache(Hq=4, Hkv=2, d=64, w=16, rows=3, nseq=2, page_size=32, num_pages=10, max_blocks=5)
+    pool, slot, rows = dma.cache4(c, "cpu"), torch.zeros(3, dtype=torch.int32), torch.zeros(3, 2, 64, dtype=torch.bfloat16)
+    for kw in (dict(K=rows[:1, :1].expand(3, 2, 64), V=rows), dict(K=rows, V=rows[:1, :1].expand(3, 2, 64))):
+        with pytest.raises(dma.DmaError, match="on top of each other") as e:
+            dma.dma_cache4_read(c, *pool, slot, **kw)
+        assert e.value.status == -3
+    assert not seen
+    wide = torch.zeros(3, 6, 64, dtype=torch.bfloat16)
+    dma.dma_cache4_read(c, *pool, slot, K=wide[:, :2], V=wide[:, 2:4])
+    one = dma.cache(Hq=2, Hkv=1, d=64, w=16, rows=3, nseq=2, page_size=32, num_pages=10, max_blocks=5)
+    dma.dma_cache4_read(one, *dma.cache4(one, "cpu"), slot, K=wide[:, :1], V=wide[:, 1:2])
+    assert seen == [((384, 64), (384, 64)), ((384, 64), (384, 64))]
