@@ -11,12 +11,12 @@
 // natural units: so is one whose weights pass 2^128 / log2 e, which have no value in units of log 2.
 //
 // Warps: 0-3 softmax and the end, 4 issues the products, 5-8 gather (with two gathering 64 rows 26.7 us instead of 24.1, eight rows with long lists 34 instead of 29). Two CTAs per SM: 97 KB
-// of stages, Q and O each.
+// of stages, Q and O each. Nine warps twice leave a thread 96 registers, of which softmax and sum want more (132 bytes spilled for 128 channels, 184 for 64).
 //
 // Times (32 and 8 heads, d = 128): 64 rows behind 16K keys, w = 2048: 23 us; 256 rows in four prefixes of 8K, w = 1024: 32; 8 rows behind 64K, w = 4096: 26.5; 1024 rows behind 16K, w = 2048, 94. On the CUDA
 // cores, whose tiles have eight rows (prefix_decode.cu): one row 28 us instead of 17, four 34 instead of 17, 64 rows of a prefix each 520 instead of 281; so bf16 comes here however few its rows are.
-// With few rows it is the list's read, a gather of 512 bytes a key from places as the weights fall, that a CTA's 8 tiles wait for (64 rows: 34 MB asked of the L2, 30 of them of memory; tensor
-// pipe 14 % active), and start and end: rows, Q, the cluster's sum. With many rows it is the softmax' threads (1024 rows: 0.55 PFLOP/s of products, both parts of P counted).
+// With few rows it is the list's read, a gather of 512 bytes a key from places as the weights fall, that a CTA's tiles wait for (64 rows: four of them, 34 MB asked of the L2, 30 of them of memory; tensor
+// pipe 14 % active), and start and end: rows, Q, the cluster's sum (eight rows of a list of 4096 have eight tiles per CTA, twice as many, and take 26.5 us). With many rows it is the softmax' threads (1024 rows: 0.55 PFLOP/s of products, both parts of P counted).
 #include <algorithm>
 #include <type_traits>
 

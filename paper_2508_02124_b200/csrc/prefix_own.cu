@@ -8,7 +8,8 @@
 //     64 own keys 10.3 us instead of 8.2, 256 of 512 55 instead of 53.5);
 //   - else: how many are kept by bisection, #{own keys that are not below entry i from the end} > i, the entries in shared memory; then the weakest between the two entries around it (256 rows
 //     of 512 own keys behind 2048, w = 1024: 140 us; by sorting up to 256 of them, and bisecting over the list where it lies beyond, 173);
-//   - without room in shared memory for all of them (512 a warp): bisection of the cut over the list where it lies, then of the weakest own key, each count a sweep of the cache by the team.
+//   - without room in shared memory for all of them (512 a warp): bisection of the cut over the list where it lies, then of the weakest own key, each count a sweep of the cache by the team. That is
+//     slow, and only rows without a full list come to it: 2048 of 16K own keys and no prefix 115 us, of 64K 312 (615 with ten weights only), of 256K 1214; 32 such rows of 64K 1815.
 // A row that keeps everything whatever its weights needs no cut: its warps take parts of the keys with all heads together (40 rows of up to 300 own keys: 25 -> 6.5 us).
 //
 // A CTA takes a (row, KV head), so that K and V of a key that several heads keep come from the L1 or L2. A head has a warp or a team of them: teams where few rows would leave the SMs with
@@ -16,8 +17,8 @@
 // its barriers).
 //
 // Times (own keys ragged, 32 and 8 heads, d = 128): 64 rows of up to 1024 own keys behind 16K keys, w = 2048: 23 us; 256 rows of up to 512 behind 8K, w = 1024: 54; 8 rows of up to 4096 behind 64K,
-// w = 4096: 16. Bound by round trips that few warps hide: pages, weights, the cut, then rows of K and V a stage ahead (64 rows: 10 warps per SM, issue slots 17 % busy; 256 rows: 14 warps, 32 %,
-// 186 MB from memory at 39 % of the copy's rate). 128 registers and 13 KB of shared memory per warp allow no more of them.
+// w = 4096: 16. Bound by round trips that few warps hide: pages, weights, the cut, then rows of K and V a stage ahead (64 rows: 10 warps per SM, issue slots 34 % busy; 256 rows: 14 warps, 43 %,
+// 186 MB from memory at half the copy's rate). 128 registers (bf16, d = 128: 56 bytes of them spilled, 80 with teams) and 13 KB of shared memory per warp allow no more of them.
 #include <algorithm>
 
 #include "cache4_decode.cuh"
@@ -296,7 +297,8 @@ struct AttendAll {
     }
 };
 
-// The rows by prefix, in the order of rows, and tiles of them.
+// The rows by prefix, in the order of rows, and tiles of them, by one CTA beside the others. It has the others' width: where thousands of rows have groups of one head, a single warp, whose grouping is
+// what the call then waits for (this kernel, 16 own keys behind a prefix and without any: 4096 rows of one head 107 and 19 us, 16384 rows of one 453 and 64, of four 581 and 268).
 __device__ void group_rows(const DecodeArgs& A, int* turn) {       // turn: kTogether per thread
     constexpr int kTogether = 4;                                  // rows of a thread requested together
     __shared__ int part[kWarps];
@@ -416,7 +418,7 @@ __global__ void __launch_bounds__(kThreads, 2) own_kernel(DecodeArgs A, int warp
     __shared__ OwnShared S;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x / 32, team = kTeams ? warps_per_head : 1;
     pdl_enter();
-    if (blockIdx.x == 0) {                                        // (first: it is done while the others are at work)
+    if (blockIdx.x == 0) {                                        // (first: while the others are at work)
         for (int i = tid; i < kWsHeaderBytes / 4; i += blockDim.x) A.status[i] = 0;      // (a CTA may be one warp)
         group_rows(A, reinterpret_cast<int*>(dynamic));
         return;
